@@ -1,0 +1,455 @@
+// tas_step_abi.hip - host side of the C ABI declared in include/tas_step.h.
+//
+// tas_step_create validates a batch on the host (every block number that a
+// kernel will follow is checked here), cuts its attention into items of work
+// and copies the plan into the caller's workspace once. tas_step_append and
+// tas_step_attention only enqueue kernels.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "tas_step.h"
+#include "tas_step_internal.h"
+
+using namespace tas_step_impl;
+
+struct tas_step {
+    PlanHead head{};
+    int32_t heads = 0, kv_heads = 0, head_dim = 0, blk_shift = 0;
+    int64_t max_pos = 0;  // largest position of a new token + 1
+    bool appendable = false;
+    char *ws = nullptr;
+    float *part_o = nullptr, *part_lse = nullptr;
+};
+
+namespace {
+
+constexpr int64_t kMaxTokens = int64_t(1) << 24;     // of a batch
+constexpr int64_t kMaxPartRows = int64_t(1) << 28;
+constexpr int64_t kMaxStride = int64_t(1) << 24;     // of a token or head, elements
+constexpr int32_t kSlots = 512;                      // wide items that run at once
+constexpr int32_t kThinItems = 2048;                 // thin items wanted
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+struct Plan {
+    PlanHead head{};
+    std::vector<Req> reqs;
+    std::vector<Seg> segs;
+    std::vector<Item> thin, wide;
+    std::vector<int32_t> tables, tok_req, merge;
+    int64_t max_pos = 0;
+    bool appendable = true;
+};
+
+bool valid_shape(const tas_batch *b) {
+    if (!b || b->kv_heads < 1 || b->heads < 1 || b->heads > 1024 || b->heads % b->kv_heads)
+        return false;
+    if (b->head_dim != 64 && b->head_dim != 128) return false;
+    if (b->block_tokens < 16 || b->block_tokens > 4096 ||
+        (b->block_tokens & (b->block_tokens - 1)))
+        return false;
+    if (b->n_req < 1 || b->n_blocks < 1 || b->n_prefix < 0) return false;
+    if (b->causal != 0 && b->causal != 1) return false;
+    if (!b->n_new || !b->kv_len || b->blocks_stride < 0) return false;
+    if (b->n_prefix && (!b->prefix_first || !b->prefix_len || b->prefix_stride < 0)) return false;
+    return true;
+}
+
+// Appends the pages of `len` keys to the tables; the table's offset, or -1.
+int64_t add_table(const tas_batch *b, const int32_t *pages, int64_t stride, int64_t len, Plan &p) {
+    const int64_t n = ceil_div(len, b->block_tokens);
+    if (n > stride || (n && !pages)) return -1;
+    const int64_t at = (int64_t)p.tables.size();
+    if (at + n > INT32_MAX) return -1;
+    for (int64_t i = 0; i < n; i++)
+        if (pages[i] < 0 || pages[i] >= b->n_blocks) return -1;
+    p.tables.insert(p.tables.end(), pages, pages + n);
+    return at;
+}
+
+// Two new tokens in one slot would race: the blocks that new tokens go to are
+// distinct, over all requests and within one.
+bool distinct_slots(const tas_batch *b, const Plan &p) {
+    std::vector<int32_t> written;
+    for (const Req &r : p.reqs) {
+        if (!r.n_new || r.n_new > r.kv_len) continue;
+        const int32_t first = (r.kv_len - r.n_new) / b->block_tokens;
+        const int32_t last = (r.kv_len - 1) / b->block_tokens;
+        for (int32_t i = first; i <= last; i++) written.push_back(p.tables[r.table + i]);
+    }
+    std::sort(written.begin(), written.end());
+    return std::adjacent_find(written.begin(), written.end()) == written.end();
+}
+
+// Cuts the keys of the segments into items. A segment's keys are split into
+// nsplit pieces of `piece` keys (the last shorter); every tile of its rows has
+// an item for each piece, an empty one where causality leaves nothing, so that
+// the merge finds nsplit partial results for every row.
+int make_items(const tas_batch *b, Plan &p) {
+    const int32_t G = b->heads / b->kv_heads, Hk = b->kv_heads;
+    int64_t thin_keys = 0, wide_tiles = 0, wide_keys = 0;
+    for (const Seg &s : p.segs) {
+        if (s.rows <= kThinRows) {
+            thin_keys += (int64_t)s.kv_len * Hk;
+        } else {
+            const int64_t tiles = ceil_div(s.rows, kWideRows) * Hk;
+            wide_tiles += tiles;
+            wide_keys += tiles * s.kv_len;
+        }
+    }
+    const int64_t step = 4 * kThinKeys;
+    const int64_t thin_piece =
+        std::max<int64_t>(ceil_div(ceil_div(thin_keys, kThinItems), step) * step, 2 * step);
+    int64_t wide_piece = INT32_MAX;
+    if (wide_tiles && wide_tiles < kSlots)
+        wide_piece = std::max<int64_t>(ceil_div(ceil_div(wide_keys, kSlots), kWideKeys) * kWideKeys,
+                                       4 * kWideKeys);
+    for (Seg &s : p.segs) {
+        const int64_t piece = s.rows <= kThinRows ? thin_piece : wide_piece;
+        s.nsplit = (int32_t)std::max<int64_t>(1, ceil_div(s.kv_len, piece));
+    }
+    // a token's result goes straight to the output where it has one part only
+    int64_t part_rows = 0;
+    for (const Req &r : p.reqs) {
+        if (!r.n_new) continue;
+        const bool split = r.pre_seg >= 0 || (r.own_seg >= 0 && p.segs[r.own_seg].nsplit > 1);
+        if (r.own_seg >= 0) {
+            Seg &s = p.segs[r.own_seg];
+            s.part = -1;
+            if (split) {
+                s.part = (int32_t)part_rows;
+                part_rows += (int64_t)Hk * s.nsplit * s.rows;
+            }
+        }
+        if (part_rows > kMaxPartRows) return TAS_EINVAL;
+        if (split)
+            for (int32_t j = 0; j < r.n_new; j++) p.merge.push_back(r.t0 + j);
+    }
+    int32_t seen = -1;
+    for (const Req &r : p.reqs)
+        if (r.pre_seg >= 0 && r.pre_seg != seen) {
+            seen = r.pre_seg;
+            Seg &s = p.segs[seen];
+            s.part = (int32_t)part_rows;
+            part_rows += (int64_t)Hk * s.nsplit * s.rows;
+            if (part_rows > kMaxPartRows) return TAS_EINVAL;
+        }
+    for (size_t i = 0; i < p.segs.size(); i++) {
+        const Seg &s = p.segs[i];
+        const bool thin = s.rows <= kThinRows;
+        const int64_t tile = thin ? kThinRows : kWideRows;
+        const int64_t unit = thin ? step : kWideKeys;
+        const int64_t piece = ceil_div(ceil_div(s.kv_len, s.nsplit), unit) * unit;
+        std::vector<Item> &to = thin ? p.thin : p.wide;
+        for (int32_t hk = 0; hk < Hk; hk++)
+            for (int64_t row0 = 0; row0 < s.rows; row0 += tile) {
+                const int64_t last = std::min<int64_t>(row0 + tile, s.rows) - 1;
+                const int64_t lim =
+                    std::max<int64_t>(0, std::min<int64_t>(s.kv_len, s.lim0 + last / G));
+                for (int32_t n = 0; n < s.nsplit; n++) {
+                    Item it;
+                    it.seg = (int32_t)i;
+                    it.hk = hk;
+                    it.row0 = (int32_t)row0;
+                    it.k0 = (int32_t)std::min<int64_t>(n * piece, lim);
+                    it.k1 = (int32_t)std::min<int64_t>((n + 1) * piece, lim);
+                    it.part = s.part < 0 ? -1
+                                         : (int32_t)(s.part +
+                                                     ((int64_t)hk * s.nsplit + n) * s.rows + row0);
+                    to.push_back(it);
+                    if (to.size() > (size_t)INT32_MAX / 2) return TAS_EINVAL;
+                }
+            }
+    }
+    // the longest first: the items that start last are short ones
+    auto longer = [](const Item &x, const Item &y) { return x.k1 - x.k0 > y.k1 - y.k0; };
+    std::stable_sort(p.thin.begin(), p.thin.end(), longer);
+    std::stable_sort(p.wide.begin(), p.wide.end(), longer);
+    p.head.part_rows = part_rows;
+    return TAS_OK;
+}
+
+int make_plan(const tas_batch *b, Plan &p) {
+    if (!valid_shape(b)) return TAS_EINVAL;
+    const int32_t G = b->heads / b->kv_heads;
+    std::vector<int64_t> prefix_table(b->n_prefix);
+    for (int32_t g = 0; g < b->n_prefix; g++) {
+        const int32_t lo = b->prefix_first[g], hi = b->prefix_first[g + 1];
+        if (lo < 0 || hi < lo || hi > b->n_req || (g == 0 && lo != 0)) return TAS_EINVAL;
+        if (g == b->n_prefix - 1 && hi != b->n_req) return TAS_EINVAL;
+        if (b->prefix_len[g] < 0) return TAS_EINVAL;
+    }
+    for (int32_t g = 0; g < b->n_prefix; g++) {
+        prefix_table[g] =
+            add_table(b, b->prefix_blocks ? b->prefix_blocks + g * b->prefix_stride : nullptr,
+                      b->prefix_stride, b->prefix_len[g], p);
+        if (prefix_table[g] < 0) return TAS_EINVAL;
+    }
+    int64_t t = 0;
+    int32_t g = 0, group_seg = -1;
+    p.reqs.reserve(b->n_req);
+    for (int32_t i = 0; i < b->n_req; i++) {
+        while (g < b->n_prefix && i >= b->prefix_first[g + 1]) g++, group_seg = -1;
+        const int64_t n = b->n_new[i], kv = b->kv_len[i];
+        const int64_t pre = b->n_prefix ? b->prefix_len[g] : 0;
+        if (n < 0 || kv < 0 || pre + kv > INT32_MAX / 2 || t + n > kMaxTokens) return TAS_EINVAL;
+        Req r{};
+        r.t0 = (int32_t)t;
+        r.n_new = (int32_t)n;
+        r.kv_len = (int32_t)kv;
+        r.prefix_len = (int32_t)pre;
+        r.own_seg = r.pre_seg = -1;
+        const int64_t at = add_table(b, b->blocks ? b->blocks + i * b->blocks_stride : nullptr,
+                                     b->blocks_stride, kv, p);
+        if (at < 0) return TAS_EINVAL;
+        r.table = (int32_t)at;
+        if (n) {
+            if (kv < n) p.appendable = false;
+            p.max_pos = std::max(p.max_pos, pre + kv);
+            if (kv || !pre) {  // without any key an empty item writes the zeros
+                Seg s{};
+                s.t0 = r.t0;
+                s.n_tok = r.n_new;
+                s.kv_len = r.kv_len;
+                s.lim0 = b->causal ? (int32_t)(kv - n + 1) : r.kv_len;
+                s.table = r.table;
+                s.rows = (int32_t)(n * G);
+                r.own_seg = (int32_t)p.segs.size();
+                p.segs.push_back(s);
+            }
+            if (pre) {
+                if (group_seg < 0) {
+                    Seg s{};
+                    s.t0 = r.t0;
+                    s.kv_len = s.lim0 = (int32_t)pre;
+                    s.table = (int32_t)prefix_table[g];
+                    group_seg = (int32_t)p.segs.size();
+                    p.segs.push_back(s);
+                }
+                // the group's tokens follow one another: requests without new
+                // ones in between add none
+                p.segs[group_seg].n_tok += (int32_t)n;
+                p.segs[group_seg].rows += (int32_t)(n * G);
+                r.pre_seg = group_seg;
+            }
+        }
+        p.tok_req.insert(p.tok_req.end(), (size_t)n, i);
+        p.reqs.push_back(r);
+        t += n;
+    }
+    if (t * G > INT32_MAX / 2) return TAS_EINVAL;
+    if (p.appendable && !distinct_slots(b, p)) return TAS_EINVAL;
+    const int rc = make_items(b, p);
+    if (rc != TAS_OK) return rc;
+    PlanHead &h = p.head;
+    size_t at = align256(sizeof(PlanHead));
+    auto place = [&](int64_t &off, size_t bytes) { off = (int64_t)at, at += align256(bytes); };
+    h.n_req = b->n_req;
+    h.n_tok = (int32_t)t;
+    h.n_seg = (int32_t)p.segs.size();
+    h.n_thin = (int32_t)p.thin.size();
+    h.n_wide = (int32_t)p.wide.size();
+    h.n_merge = (int32_t)p.merge.size();
+    h.n_table = (int32_t)p.tables.size();
+    place(h.req, p.reqs.size() * sizeof(Req));
+    place(h.seg, p.segs.size() * sizeof(Seg));
+    place(h.thin, p.thin.size() * sizeof(Item));
+    place(h.wide, p.wide.size() * sizeof(Item));
+    place(h.tables, p.tables.size() * 4);
+    place(h.tok_req, p.tok_req.size() * 4);
+    place(h.merge, p.merge.size() * 4);
+    h.bytes = (int64_t)at;
+    return TAS_OK;
+}
+
+void write_blob(const Plan &p, char *to) {
+    const PlanHead &h = p.head;
+    memcpy(to, &h, sizeof(h));
+    auto put = [&](int64_t off, const void *from, size_t bytes) {
+        if (bytes) memcpy(to + off, from, bytes);
+    };
+    put(h.req, p.reqs.data(), p.reqs.size() * sizeof(Req));
+    put(h.seg, p.segs.data(), p.segs.size() * sizeof(Seg));
+    put(h.thin, p.thin.data(), p.thin.size() * sizeof(Item));
+    put(h.wide, p.wide.data(), p.wide.size() * sizeof(Item));
+    put(h.tables, p.tables.data(), p.tables.size() * 4);
+    put(h.tok_req, p.tok_req.data(), p.tok_req.size() * 4);
+    put(h.merge, p.merge.data(), p.merge.size() * 4);
+}
+
+size_t workspace_bytes(const tas_batch *b, const Plan &p) {
+    return (size_t)p.head.bytes + align256((size_t)p.head.part_rows * b->head_dim * 4) +
+           align256((size_t)p.head.part_rows * 4);
+}
+
+bool aligned16(const void *p) { return p && ((uintptr_t)p & 15) == 0; }
+
+bool valid_cache(const tas_cache &c) {
+    if (!aligned16(c.k) || !aligned16(c.v)) return false;
+    const int64_t s[6] = {c.k_block, c.v_block, c.k_head, c.v_head, c.k_token, c.v_token};
+    for (int i = 0; i < 6; i++) {
+        if (s[i] < 0 || s[i] % 8) return false;
+        if (i >= 4 && s[i] > kMaxStride) return false;
+    }
+    return true;
+}
+
+bool valid_rows(const void *p, int64_t stride, int64_t row) {
+    return aligned16(p) && stride >= row && stride % 8 == 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t tas_step_bytes(const tas_batch *b) try {
+    Plan p;
+    if (make_plan(b, p) != TAS_OK) return 0;
+    return workspace_bytes(b, p);
+} catch (...) {
+    return 0;
+}
+
+int tas_step_plan(const tas_batch *b, void *buf, size_t buf_bytes, size_t *bytes) try {
+    if (!bytes) return TAS_EINVAL;
+    Plan p;
+    const int rc = make_plan(b, p);
+    if (rc != TAS_OK) return rc;
+    *bytes = (size_t)p.head.bytes;
+    if (!buf) return TAS_OK;
+    if (buf_bytes < *bytes) return TAS_ENOMEM;
+    memset(buf, 0, *bytes);
+    write_blob(p, (char *)buf);
+    return TAS_OK;
+} catch (...) {
+    return TAS_ENOMEM;
+}
+
+int tas_step_create(const tas_batch *b, void *d_ws, size_t ws_bytes, tas_step **out) try {
+    if (!out) return TAS_EINVAL;
+    *out = nullptr;
+    Plan p;
+    const int rc = make_plan(b, p);
+    if (rc != TAS_OK) return rc;
+    if (!d_ws || ((uintptr_t)d_ws & 255)) return TAS_EINVAL;
+    if (ws_bytes < workspace_bytes(b, p)) return TAS_ENOMEM;
+    std::vector<char> blob((size_t)p.head.bytes);
+    write_blob(p, blob.data());
+    tas_step *s = new tas_step;
+    s->head = p.head;
+    s->heads = b->heads;
+    s->kv_heads = b->kv_heads;
+    s->head_dim = b->head_dim;
+    while ((1 << s->blk_shift) < b->block_tokens) s->blk_shift++;
+    s->max_pos = p.max_pos;
+    s->appendable = p.appendable;
+    s->ws = (char *)d_ws;
+    s->part_o = (float *)(s->ws + p.head.bytes);
+    s->part_lse = (float *)(s->ws + p.head.bytes +
+                            align256((size_t)p.head.part_rows * b->head_dim * 4));
+    if (hipMemcpy(d_ws, blob.data(), blob.size(), hipMemcpyHostToDevice) != hipSuccess) {
+        delete s;
+        return TAS_EHIP;
+    }
+    *out = s;
+    return TAS_OK;
+} catch (...) {
+    return TAS_ENOMEM;
+}
+
+void tas_step_destroy(tas_step *s) { delete s; }
+
+int64_t tas_step_tokens(const tas_step *s) { return s ? s->head.n_tok : -1; }
+
+int tas_step_append(tas_step *s, const tas_append *a, void *stream) {
+    if (!s || !a || !s->appendable) return TAS_EINVAL;
+    const int64_t D = s->head_dim;
+    if (a->dtype != TAS_F16 && a->dtype != TAS_BF16) return TAS_EINVAL;
+    if (a->rot_dim < 0 || a->rot_dim > D || a->rot_dim % 16) return TAS_EINVAL;
+    if (a->interleaved != 0 && a->interleaved != 1) return TAS_EINVAL;
+    if (!(a->eps >= 0) || std::isinf(a->eps)) return TAS_EINVAL;
+    if (!a->q_weight != !a->k_weight) return TAS_EINVAL;
+    if (a->q_weight && (!aligned16(a->q_weight) || !aligned16(a->k_weight))) return TAS_EINVAL;
+    if (a->rot_dim &&
+        (!aligned16(a->cos) || !aligned16(a->sin) || a->positions < s->max_pos))
+        return TAS_EINVAL;
+    if (!valid_cache(a->cache)) return TAS_EINVAL;
+    if (s->head.n_tok == 0) return TAS_OK;
+    if (!valid_rows(a->qkv, a->qkv_stride, (s->heads + 2 * s->kv_heads) * D) ||
+        !valid_rows(a->q_out, a->q_out_stride, s->heads * D))
+        return TAS_EINVAL;
+    AppendArgs k{};
+    k.reqs = (const Req *)(s->ws + s->head.req);
+    k.tok_req = (const int32_t *)(s->ws + s->head.tok_req);
+    k.tables = (const int32_t *)(s->ws + s->head.tables);
+    k.qkv = a->qkv;
+    k.q_out = a->q_out;
+    k.q_weight = a->q_weight;
+    k.k_weight = a->k_weight;
+    k.cos = a->cos;
+    k.sin = a->sin;
+    k.qkv_stride = a->qkv_stride;
+    k.q_out_stride = a->q_out_stride;
+    k.c = a->cache;
+    k.n_tok = s->head.n_tok;
+    k.heads = s->heads;
+    k.kv_heads = s->kv_heads;
+    k.rot = a->rot_dim;
+    k.interleaved = a->interleaved;
+    k.blk_shift = s->blk_shift;
+    k.eps = a->eps;
+    return launch_append(k, a->dtype, s->head_dim, (hipStream_t)stream) == hipSuccess ? TAS_OK
+                                                                                     : TAS_EHIP;
+}
+
+int tas_step_attention(tas_step *s, const tas_attention *a, void *stream) {
+    if (!s || !a) return TAS_EINVAL;
+    if (a->dtype != TAS_F16 && a->dtype != TAS_BF16) return TAS_EINVAL;
+    if (!(a->scale > 0) || std::isinf(a->scale)) return TAS_EINVAL;
+    if (!valid_cache(a->cache)) return TAS_EINVAL;
+    if (s->head.n_tok == 0) return TAS_OK;
+    const int64_t row = (int64_t)s->heads * s->head_dim;
+    if (!valid_rows(a->q, a->q_stride, row) || !valid_rows(a->out, a->out_stride, row))
+        return TAS_EINVAL;
+    AttnArgs k{};
+    k.segs = (const Seg *)(s->ws + s->head.seg);
+    k.tables = (const int32_t *)(s->ws + s->head.tables);
+    k.reqs = (const Req *)(s->ws + s->head.req);
+    k.tok_req = (const int32_t *)(s->ws + s->head.tok_req);
+    k.merge = (const int32_t *)(s->ws + s->head.merge);
+    k.q = a->q;
+    k.out = a->out;
+    k.lse = a->lse;
+    k.part_o = s->part_o;
+    k.part_lse = s->part_lse;
+    k.q_stride = a->q_stride;
+    k.out_stride = a->out_stride;
+    k.c = a->cache;
+    k.group = s->heads / s->kv_heads;
+    k.heads = s->heads;
+    k.sub_shift = s->blk_shift - 4;
+    k.scale2 = a->scale * 1.4426950408889634f;
+    const hipStream_t st = (hipStream_t)stream;
+    if (s->head.n_wide) {
+        k.items = (const Item *)(s->ws + s->head.wide);
+        if (launch_wide(k, s->head.n_wide, a->dtype, s->head_dim, st) != hipSuccess)
+            return TAS_EHIP;
+    }
+    if (s->head.n_thin) {
+        k.items = (const Item *)(s->ws + s->head.thin);
+        if (launch_thin(k, s->head.n_thin, a->dtype, s->head_dim, st) != hipSuccess)
+            return TAS_EHIP;
+    }
+    if (s->head.n_merge &&
+        launch_merge(k, s->head.n_merge, s->kv_heads, a->dtype, s->head_dim, st) != hipSuccess)
+        return TAS_EHIP;
+    return TAS_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,448 @@
+// tas_step_attn.hip - attention of a step's new tokens over the paged cache.
+//
+// One pass over a row's keys with the running maximum m and sum l of the softmax:
+//     m' = max(m, max s),  l <- l 2^(m-m') + sum 2^(s-m'),  o <- o 2^(m-m') + 2^(s-m') V
+// with s = scale log2(e) q.k. Scores are computed transposed, S^T = K Q^T, so that
+// the matrix unit leaves a query's scores in the lane that holds the query's column:
+// the sums over keys stay in lanes, and the weights P^T are in place as the right
+// operand of O^T = V^T P^T (which keys its k-slots stand for is free, as long as both
+// operands agree). The left operand V^T is read from the rows of V in LDS by the
+// transposing LDS read. Scores, statistics and sums are held in 32 bits; the weights
+// are rounded to the inputs' type for the second product, as its operands have to be.
+#include <hip/hip_runtime.h>
+
+#include "tas_step_internal.h"
+
+namespace tas_step_impl {
+namespace {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f16x __attribute__((ext_vector_type(16)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef short s8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+template <typename T>
+using vec8 = T __attribute__((ext_vector_type(8)));
+template <typename T>
+using vec2 = T __attribute__((ext_vector_type(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+
+__device__ f4 mfma16(vec8<__bf16> a, vec8<__bf16> b, f4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ f4 mfma16(vec8<_Float16> a, vec8<_Float16> b, f4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ f16x mfma32(vec8<__bf16> a, vec8<__bf16> b, f16x c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ f16x mfma32(vec8<_Float16> a, vec8<_Float16> b, f16x c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+__device__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Maximum and sum over the lanes that hold one column: lane ^ 32, and lane ^ 16.
+__device__ float max32(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ float max16(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ float sum32(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+__device__ float sum16(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+
+// The place in LDS (in 16-byte chunks) of chunk c of a V row: the four rows that
+// one transposing read takes lie in different quarters of the banks.
+template <int D>
+__device__ int v_chunk(int row, int c) {
+    if (D == 128) return row * 16 + (c ^ (((row & 3) << 2) | ((row >> 1) & 2)));
+    return row * 8 + (c ^ ((row & 3) << 1));
+}
+
+__device__ s4 read_tr(const char *p) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)p);
+}
+
+// Elements d of result rows, in the output or as a partial result.
+template <typename T, int D>
+__device__ void store_row(const AttnArgs &a, const Seg &s, const Item &it, int r, int d,
+                          const float *o, float l, float m) {
+    const float f = l > 0 ? 1.0f / l : (l == l ? 0.0f : l);  // NaN stays
+    if (it.part >= 0) {
+        float *to = a.part_o + (int64_t)(it.part + r) * D + d;
+        f4 x = {o[0] * f, o[1] * f, o[2] * f, o[3] * f};
+        f4 y = {o[4] * f, o[5] * f, o[6] * f, o[7] * f};
+        *(f4 *)to = x, *(f4 *)(to + 4) = y;
+        if (d == 0) a.part_lse[it.part + r] = l > 0 ? m + log2f(l) : (l == l ? -INFINITY : l);
+        return;
+    }
+    const int row = it.row0 + r, j = row / a.group, head = it.hk * a.group + row - j * a.group;
+    vec8<T> x;
+    for (int e = 0; e < 8; e++) x[e] = (T)(o[e] * f);
+    const int64_t tok = s.t0 + j;
+    *(vec8<T> *)((T *)a.out + tok * a.out_stride + (int64_t)head * D + d) = x;
+    if (d == 0 && a.lse)
+        a.lse[tok * a.heads + head] =
+            l > 0 ? (m + log2f(l)) * 0.6931471805599453f : (l == l ? -INFINITY : l);
+}
+
+// Up to 16 rows against a run of keys: each of the four waves takes every fourth
+// 32 keys, K straight into registers as the left operand, V through its own LDS;
+// the waves' results are joined at the end. Memory bound: 16 rows make use of at
+// most 16 products a byte and a half.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void thin_kernel(AttnArgs a) {
+    using V = vec8<T>;
+    constexpr int QS = D / 32;          // steps of 32 over d
+    constexpr int VL = D / 16;          // 16-byte loads of a lane for 32 rows of V
+    constexpr int LPR = D / 8;          // lanes of a V row
+    constexpr int VB = kThinKeys * D * 2;  // bytes of a wave's V
+    __shared__ __attribute__((aligned(16))) char lds[4 * VB];
+    __shared__ float stat[4][kThinRows][2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int col = lane & 15, g = lane >> 4;
+    const Item it = a.items[blockIdx.x];
+    const Seg s = a.segs[it.seg];
+    const int *tab = a.tables + s.table;
+
+    const int row = min(col, s.rows - 1), j = row / a.group;
+    const int lim = min(min(s.kv_len, s.lim0 + j), it.k1);
+    V q[QS];
+    {
+        const T *src = (const T *)a.q + (int64_t)(s.t0 + j) * a.q_stride +
+                       (int64_t)(it.hk * a.group + row - j * a.group) * D + g * 8;
+        for (int i = 0; i < QS; i++) q[i] = *(const V *)(src + i * 32);
+    }
+    const int full = min(min(s.kv_len, s.lim0), it.k1);  // keys that the first row sees
+    const int sub_mask = (1 << a.sub_shift) - 1;
+    const T *kbase = (const T *)a.c.k + it.hk * a.c.k_head;
+    const T *vbase = (const T *)a.c.v + it.hk * a.c.v_head;
+    const int klane = col * (int)a.c.k_token + g * 8;
+    const int vrow = lane / LPR, vch = lane % LPR;
+    const int vlane = vrow * (int)a.c.v_token + vch * 8;
+    char *vl = lds + wave * VB;
+
+    f4 o[D / 16];
+    for (int i = 0; i < D / 16; i++) o[i] = f4{0, 0, 0, 0};
+    float m = -INFINITY, l = 0;
+    V k[2][QS];
+    u4 v[VL];
+    const int last_sub = it.k1 > 0 ? (it.k1 - 1) >> 4 : 0;
+
+    auto load = [&](int base) {
+        for (int n = 0; n < 2; n++) {
+            const int sub = min((base >> 4) + n, last_sub);
+            const int64_t page = tab[sub >> a.sub_shift];
+            const int off = (sub & sub_mask) * 16;
+            const T *kp = kbase + page * a.c.k_block + off * a.c.k_token;
+            const T *vp = vbase + page * a.c.v_block + off * a.c.v_token;
+            for (int i = 0; i < QS; i++) k[n][i] = *(const V *)(kp + klane + i * 32);
+            for (int i = 0; i < VL / 2; i++)
+                v[n * VL / 2 + i] =
+                    *(const u4 *)(vp + vlane + (int64_t)(i * (64 / LPR)) * a.c.v_token);
+        }
+    };
+    int base = it.k0 + wave * kThinKeys;
+    if (base < it.k1) load(base);
+    for (; base < it.k1; base += 4 * kThinKeys) {
+        f4 sc[2];
+        for (int n = 0; n < 2; n++) {
+            sc[n] = f4{0, 0, 0, 0};
+            for (int i = 0; i < QS; i++) sc[n] = mfma16(k[n][i], q[i], sc[n]);
+        }
+        if (base + kThinKeys > it.k1)  // slots past the keys hold anything: weight 0 times it
+            for (int i = 0; i < VL; i++)
+                if (base + i * (64 / LPR) + vrow >= it.k1) v[i] = u4{0, 0, 0, 0};
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (int i = 0; i < VL; i++)
+            *(u4 *)(vl + v_chunk<D>(i * (64 / LPR) + vrow, vch) * 16) = v[i];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (base + 4 * kThinKeys < it.k1) load(base + 4 * kThinKeys);
+
+        const bool mask = base + kThinKeys > full;
+        float x[8], mt = -INFINITY;
+        for (int n = 0; n < 2; n++)
+            for (int i = 0; i < 4; i++) {
+                float y = sc[n][i] * a.scale2;
+                if (mask && base + n * 16 + g * 4 + i >= lim) y = -INFINITY;
+                x[n * 4 + i] = y;
+                mt = fmaxf(mt, y);
+            }
+        mt = max32(max16(mt));
+        const float mn = fmaxf(m, mt), mu = mn == -INFINITY ? 0.0f : mn;
+        const float f = exp2_(m - mu);
+        m = mn;
+        V p;
+        float sum = 0;
+        for (int i = 0; i < 8; i++) {
+            const float y = exp2_(x[i] - mu);
+            sum += y;
+            p[i] = (T)y;
+        }
+        l = l * f + sum;
+        for (int i = 0; i < D / 16; i++) {
+            o[i] *= f;
+            // lane c of group g: column d = 16 i + c of the rows 4 g .. 4 g + 3 and 16 on
+            const int r0 = 4 * g + (col >> 2), c = 2 * i + ((col >> 1) & 1);
+            const s4 lo = read_tr(vl + v_chunk<D>(r0, c) * 16 + (col & 1) * 8);
+            const s4 hi = read_tr(vl + v_chunk<D>(16 + r0, c) * 16 + (col & 1) * 8);
+            const s8 t = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            o[i] = mfma16(__builtin_bit_cast(V, t), p, o[i]);
+        }
+    }
+
+    // Join the four waves' results.
+    l = sum32(sum16(l));
+    __syncthreads();
+    if (g == 0) stat[wave][col][0] = m, stat[wave][col][1] = l;
+    float *ex = (float *)lds;  // [wave][row][D], 4-float groups swizzled by the row
+    for (int i = 0; i < D / 16; i++)
+        *(f4 *)(ex + (wave * kThinRows + col) * D + (((i * 4 + g) ^ col) * 4)) = o[i];
+    __syncthreads();
+    const int r = tid / (D / 8), d = tid % (D / 8) * 8;  // D 64: the upper half has no row
+    if (r >= kThinRows || r >= s.rows) return;
+    float mm = -INFINITY, ll = 0, y[8] = {};
+    for (int w = 0; w < 4; w++) mm = fmaxf(mm, stat[w][r][0]);
+    const float mu = mm == -INFINITY ? 0.0f : mm;
+    for (int w = 0; w < 4; w++) {
+        const float f = exp2_(stat[w][r][0] - mu);
+        ll += stat[w][r][1] * f;
+        const float *from = ex + (w * kThinRows + r) * D;
+        const f4 lo = *(const f4 *)(from + ((d / 4) ^ r) * 4);
+        const f4 hi = *(const f4 *)(from + ((d / 4 + 1) ^ r) * 4);
+        for (int e = 0; e < 4; e++) y[e] += lo[e] * f, y[4 + e] += hi[e] * f;
+    }
+    store_row<T, D>(a, s, it, r, d, y, ll, mm);
+}
+
+// 128 rows against a run of keys, 64 keys a step: 32 rows to a wave, K and V of a
+// step in LDS for all four. Two buffers: the loads of the next step are under way in
+// registers while the matrix unit works on this one, and one barrier ends a step.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a) {
+    using V = vec8<T>;
+    constexpr int QS = D / 16;              // steps of 16 over d
+    constexpr int LPR = D / 8;              // lanes of a row
+    constexpr int RPL = 256 / LPR;          // rows that one load of the workgroup takes
+    constexpr int NL = kWideKeys / RPL;     // loads
+    constexpr int TB = kWideKeys * D * 2;   // bytes of a tile
+    __shared__ __attribute__((aligned(16))) char lds[2][2 * TB];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int col = lane & 31, half = lane >> 5;
+    const Item it = a.items[blockIdx.x];
+    const Seg s = a.segs[it.seg];
+    const int *tab = a.tables + s.table;
+
+    const int r = wave * 32 + col;  // row of the item
+    const int row = min(it.row0 + r, s.rows - 1), j = row / a.group;
+    const int lim = min(min(s.kv_len, s.lim0 + j), it.k1);
+    V q[QS];
+    {
+        const T *src = (const T *)a.q + (int64_t)(s.t0 + j) * a.q_stride +
+                       (int64_t)(it.hk * a.group + row - j * a.group) * D + half * 8;
+        for (int i = 0; i < QS; i++) q[i] = *(const V *)(src + i * 16);
+    }
+    const int full = min(min(s.kv_len, s.lim0 + it.row0 / a.group), it.k1);
+    const int sub_mask = (1 << a.sub_shift) - 1;
+    const T *kbase = (const T *)a.c.k + it.hk * a.c.k_head;
+    const T *vbase = (const T *)a.c.v + it.hk * a.c.v_head;
+    const int lrow = tid / LPR, lch = tid % LPR;
+
+    f16x o[D / 32];
+    for (int i = 0; i < D / 32; i++)
+        for (int e = 0; e < 16; e++) o[i][e] = 0;
+    float m = -INFINITY, l = 0;
+    u4 kr[NL], vr[NL];
+    const int last_sub = it.k1 > 0 ? (it.k1 - 1) >> 4 : 0;
+
+    auto load = [&](int base) {
+        for (int i = 0; i < NL; i++) {
+            const int y = i * RPL + lrow;
+            const int sub = min((base + y) >> 4, last_sub);
+            const int64_t page = tab[sub >> a.sub_shift];
+            const int off = (sub & sub_mask) * 16 + (y & 15);
+            kr[i] = *(const u4 *)(kbase + page * a.c.k_block + off * a.c.k_token + lch * 8);
+            vr[i] = *(const u4 *)(vbase + page * a.c.v_block + off * a.c.v_token + lch * 8);
+        }
+    };
+    // chunk c of K row y: eight rows' chunks of one column lie in different banks
+    auto k_chunk = [](int y, int c) { return y * LPR + (c ^ (y & (LPR - 1))); };
+    auto put = [&](int buf, int base) {
+        if (base + kWideKeys > it.k1)
+            for (int i = 0; i < NL; i++)
+                if (base + i * RPL + lrow >= it.k1) vr[i] = u4{0, 0, 0, 0};
+        for (int i = 0; i < NL; i++) {
+            const int y = i * RPL + lrow;
+            *(u4 *)(lds[buf] + k_chunk(y, lch) * 16) = kr[i];
+            *(u4 *)(lds[buf] + TB + v_chunk<D>(y, lch) * 16) = vr[i];
+        }
+    };
+    if (it.k0 < it.k1) {
+        load(it.k0);
+        put(0, it.k0);
+    }
+    __syncthreads();
+    int buf = 0;
+    for (int base = it.k0; base < it.k1; base += kWideKeys, buf ^= 1) {
+        const bool more = base + kWideKeys < it.k1;
+        if (more) load(base + kWideKeys);
+        const char *kl = lds[buf], *vl = lds[buf] + TB;
+        f16x sc[2];
+        for (int n = 0; n < 2; n++) {
+            for (int e = 0; e < 16; e++) sc[n][e] = 0;
+            for (int i = 0; i < QS; i++) {
+                const V k = *(const V *)(kl + k_chunk(n * 32 + col, i * 2 + half) * 16);
+                sc[n] = mfma32(k, q[i], sc[n]);
+            }
+        }
+        const bool mask = base + kWideKeys > full;
+        float mt = -INFINITY;
+        for (int n = 0; n < 2; n++)
+            for (int e = 0; e < 16; e++) {
+                float y = sc[n][e] * a.scale2;
+                if (mask && base + n * 32 + (e >> 2) * 8 + half * 4 + (e & 3) >= lim)
+                    y = -INFINITY;
+                sc[n][e] = y;
+                mt = fmaxf(mt, y);
+            }
+        mt = max32(mt);
+        const float mn = fmaxf(m, mt), mu = mn == -INFINITY ? 0.0f : mn;
+        const float f = exp2_(m - mu);
+        m = mn;
+        V p[4];
+        float sum = 0;
+        for (int n = 0; n < 2; n++)
+            for (int e = 0; e < 16; e++) {
+                const float y = exp2_(sc[n][e] - mu);
+                sum += y;
+                p[n * 2 + (e >> 3)][e & 7] = (T)y;
+            }
+        l = l * f + sum;
+        for (int i = 0; i < D / 32; i++) o[i] *= f;
+        // k-slots of step n: keys 16 n + 4 half + 0..3 and 8 on, as sc holds them
+        const int tr = (lane & 15) >> 2, tc = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
+        for (int n = 0; n < 4; n++) {
+            const int r0 = n * 16 + half * 4 + tr;
+            for (int i = 0; i < D / 32; i++) {
+                const s4 lo = read_tr(vl + v_chunk<D>(r0, i * 4 + tc) * 16 + (lane & 1) * 8);
+                const s4 hi = read_tr(vl + v_chunk<D>(r0 + 8, i * 4 + tc) * 16 + (lane & 1) * 8);
+                const s8 t = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                o[i] = mfma32(__builtin_bit_cast(V, t), p[n], o[i]);
+            }
+        }
+        if (more) put(buf ^ 1, base + kWideKeys);
+        __syncthreads();
+    }
+    l = sum32(l);
+    // A lane holds d = 32 i + 8 e + 4 half + 0..3 of its row: the halves exchange so
+    // that each has 8 adjacent ones.
+    for (int i = 0; i < D / 32; i++)
+        for (int e = 0; e < 4; e += 2) {
+            float y[8];
+            for (int c = 0; c < 4; c++) {
+                const float ue = o[i][e * 4 + c], we = o[i][e * 4 + 4 + c];
+                const uint32_t u = __builtin_bit_cast(uint32_t, ue);
+                const uint32_t w = __builtin_bit_cast(uint32_t, we);
+                // half 0: {own e, other's e}; half 1: {other's e + 1, own e + 1}
+                auto x = __builtin_amdgcn_permlane32_swap(u, w, false, false);
+                y[c] = __builtin_bit_cast(float, (uint32_t)x[0]);
+                y[4 + c] = __builtin_bit_cast(float, (uint32_t)x[1]);
+            }
+            if (it.row0 + r < s.rows) store_row<T, D>(a, s, it, r, i * 32 + e * 8 + half * 8, y, l, m);
+        }
+}
+
+// Joins the partial results of a token's head: weights 2^(lse_n - max).
+template <typename T, int D>
+__global__ __launch_bounds__(256) void merge_kernel(AttnArgs a) {
+    constexpr int E = D / 64;
+    const int lane = threadIdx.x & 63;
+    const int head = blockIdx.y * 4 + (threadIdx.x >> 6);
+    if (head >= a.heads) return;
+    const int tok = a.merge[blockIdx.x];
+    const Req r = a.reqs[a.tok_req[tok]];
+    const int hk = head / a.group, g = head - hk * a.group;
+    float m = -INFINITY;
+    bool bad = false;  // a NaN among the parts stays
+    for (int p = 0; p < 2; p++) {
+        const int seg = p ? r.pre_seg : r.own_seg;
+        if (seg < 0) continue;
+        const Seg s = a.segs[seg];
+        int64_t at = s.part + (int64_t)hk * s.nsplit * s.rows + (tok - s.t0) * a.group + g;
+        for (int n = 0; n < s.nsplit; n++, at += s.rows) {
+            const float x = a.part_lse[at];
+            bad |= x != x;
+            m = fmaxf(m, x);
+        }
+    }
+    const float mu = m == -INFINITY ? 0.0f : m;
+    float sum = 0, y[E] = {};
+    for (int p = 0; p < 2; p++) {
+        const int seg = p ? r.pre_seg : r.own_seg;
+        if (seg < 0) continue;
+        const Seg s = a.segs[seg];
+        int64_t at = s.part + (int64_t)hk * s.nsplit * s.rows + (tok - s.t0) * a.group + g;
+        for (int n = 0; n < s.nsplit; n++, at += s.rows) {
+            const float w = exp2_(a.part_lse[at] - mu);
+            sum += w;
+            for (int e = 0; e < E; e++) y[e] += w * a.part_o[at * D + lane * E + e];
+        }
+    }
+    const float f = sum > 0 ? 1.0f / sum : 0.0f;
+    T *to = (T *)a.out + (int64_t)tok * a.out_stride + (int64_t)head * D + lane * E;
+    for (int e = 0; e < E; e++) to[e] = (T)(bad ? NAN : y[e] * f);
+    if (lane == 0 && a.lse)
+        a.lse[(int64_t)tok * a.heads + head] =
+            bad ? NAN : sum > 0 ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+}
+
+enum { THIN, WIDE, MERGE };
+
+template <typename T, int D>
+hipError_t launch(int which, const AttnArgs &a, int n, hipStream_t s) {
+    if (which == THIN)
+        thin_kernel<T, D><<<dim3(n), 256, 0, s>>>(a);
+    else if (which == WIDE)
+        wide_kernel<T, D><<<dim3(n), 256, 0, s>>>(a);
+    else
+        merge_kernel<T, D><<<dim3(n, (a.heads + 3) / 4), 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t choose(int which, const AttnArgs &a, int n, int dtype, int head_dim, hipStream_t s) {
+    if (dtype == TAS_F16)
+        return head_dim == 64 ? launch<_Float16, 64>(which, a, n, s)
+                              : launch<_Float16, 128>(which, a, n, s);
+    return head_dim == 64 ? launch<__bf16, 64>(which, a, n, s)
+                          : launch<__bf16, 128>(which, a, n, s);
+}
+
+}  // namespace
+
+hipError_t launch_thin(const AttnArgs &a, int n, int dtype, int head_dim, hipStream_t s) {
+    return choose(THIN, a, n, dtype, head_dim, s);
+}
+hipError_t launch_wide(const AttnArgs &a, int n, int dtype, int head_dim, hipStream_t s) {
+    return choose(WIDE, a, n, dtype, head_dim, s);
+}
+hipError_t launch_merge(const AttnArgs &a, int n, int kv_heads, int dtype, int head_dim,
+                        hipStream_t s) {
+    (void)kv_heads;
+    return choose(MERGE, a, n, dtype, head_dim, s);
+}
+
+}  // namespace tas_step_impl

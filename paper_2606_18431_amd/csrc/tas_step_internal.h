@@ -1,0 +1,84 @@
+// tas_step_internal.h - the plan of a step as the host writes it and the
+// kernels read it, and the launchers of the kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "tas_step.h"
+
+namespace tas_step_impl {
+
+// Rows of a key head are (token, query head of its group), token-major. A
+// segment is a run of tokens with one list of keys: a request with its own
+// context, or a prefix group's tokens with the prefix.
+constexpr int kThinRows = 16;   // rows of a thin item (all rows of its segment)
+constexpr int kThinKeys = 32;   // keys of one wave's step
+constexpr int kWideRows = 128;  // rows of a wide item
+constexpr int kWideKeys = 64;   // keys of one step of a wide item
+
+struct Req {
+    int32_t t0, n_new, kv_len, table;   // first token; pages at tables[table]
+    int32_t prefix_len, own_seg, pre_seg, pad;  // segments, -1: none
+};
+struct Seg {
+    int32_t t0, n_tok;    // tokens
+    int32_t kv_len;       // keys
+    int32_t lim0;         // token j sees the keys below min(kv_len, lim0 + j)
+    int32_t table;        // pages at tables[table]
+    int32_t nsplit;       // pieces of the keys, each with a partial result
+    int32_t part;         // partial row of (key head 0, piece 0, row 0), -1: none,
+                          // results go to the output
+    int32_t rows;         // n_tok * heads / kv_heads
+};
+// Rows row0.. of one key head of a segment against its keys k0 .. k1 - 1.
+struct Item {
+    int32_t seg, hk, row0, k0, k1;
+    int32_t part;  // partial row of row0, -1: output
+};
+struct PlanHead {
+    int64_t bytes;                 // of the blob
+    int64_t part_rows;             // partial rows
+    int32_t n_req, n_tok, n_seg, n_thin, n_wide, n_merge, n_table, all_own;
+    int64_t req, seg, thin, wide, tables, tok_req, merge;  // byte offsets in the blob
+};
+
+struct AppendArgs {
+    const Req *reqs;
+    const int32_t *tok_req, *tables;
+    const void *qkv;
+    void *q_out;
+    const void *q_weight, *k_weight;
+    const float *cos, *sin;
+    int64_t qkv_stride, q_out_stride;
+    tas_cache c;
+    int32_t n_tok, heads, kv_heads, rot, interleaved;
+    int32_t blk_shift;  // log2(block_tokens)
+    float eps;
+};
+
+struct AttnArgs {
+    const Seg *segs;
+    const Item *items;
+    const int32_t *tables;
+    const Req *reqs;
+    const int32_t *tok_req, *merge;
+    const void *q;
+    void *out;
+    float *lse;
+    float *part_o;    // [part_rows][head_dim], normalised
+    float *part_lse;  // [part_rows], base 2
+    int64_t q_stride, out_stride;
+    tas_cache c;
+    int32_t group, heads;
+    int32_t sub_shift;  // log2(block_tokens / 16)
+    float scale2;       // scale * log2(e)
+};
+
+// Return hipSuccess or the launch's error.
+hipError_t launch_append(const AppendArgs &a, int dtype, int head_dim, hipStream_t s);
+hipError_t launch_thin(const AttnArgs &a, int n_items, int dtype, int head_dim, hipStream_t s);
+hipError_t launch_wide(const AttnArgs &a, int n_items, int dtype, int head_dim, hipStream_t s);
+hipError_t launch_merge(const AttnArgs &a, int n_merge, int kv_heads, int dtype, int head_dim,
+                        hipStream_t s);
+
+}  // namespace tas_step_impl

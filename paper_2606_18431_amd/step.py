@@ -1,0 +1,312 @@
+"""ctypes binding of the C ABI in include/tas_step.h: the attention part of one
+serving iteration (append to the paged KV cache, attention over it).
+
+Every operator runs in the HIP kernels of ``libtas_step.so``; this module checks
+tensors and converts arguments. It raises if the library is missing: there is no
+fallback. The functions keep the C names; ``Step`` bundles them for one batch,
+allocating the workspace and outputs as PyTorch tensors.
+
+    step = Step(n_new, kv_len, blocks, heads=32, kv_heads=8, head_dim=128,
+                block_tokens=16, n_blocks=8192)
+    for layer in layers:
+        q = step.append(layer.qkv(x), k_cache, v_cache, cos, sin)
+        o = step.attention(q, k_cache, v_cache)
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+import os
+
+import numpy as np
+import torch
+
+from .tas import TAS_EINVAL, TAS_OK, TasError
+
+PKG = os.path.dirname(os.path.abspath(__file__))
+LIB_PATH = os.path.join(PKG, "libtas_step.so")
+TAS_F16, TAS_BF16 = 0, 1
+DTYPES = {torch.float16: TAS_F16, torch.bfloat16: TAS_BF16}
+
+_P, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+
+
+class tas_batch(ctypes.Structure):
+    _fields_ = [("heads", _i32), ("kv_heads", _i32), ("head_dim", _i32), ("block_tokens", _i32),
+                ("n_req", _i32), ("n_blocks", _i32), ("causal", _i32), ("n_prefix", _i32),
+                ("n_new", _P), ("kv_len", _P), ("blocks", _P), ("blocks_stride", _i64),
+                ("prefix_first", _P), ("prefix_len", _P), ("prefix_blocks", _P),
+                ("prefix_stride", _i64)]
+
+
+class tas_cache(ctypes.Structure):
+    _fields_ = [("k", _P), ("v", _P), ("k_block", _i64), ("k_head", _i64), ("k_token", _i64),
+                ("v_block", _i64), ("v_head", _i64), ("v_token", _i64)]
+
+
+class tas_append(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("rot_dim", _i32), ("interleaved", _i32),
+                ("eps", ctypes.c_float), ("qkv", _P), ("qkv_stride", _i64), ("q_out", _P),
+                ("q_out_stride", _i64), ("q_weight", _P), ("k_weight", _P), ("cos", _P),
+                ("sin", _P), ("positions", _i64), ("cache", tas_cache)]
+
+
+class tas_attention(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("scale", ctypes.c_float), ("q", _P), ("q_stride", _i64),
+                ("out", _P), ("out_stride", _i64), ("lse", _P), ("cache", tas_cache)]
+
+
+EXPORTS = ["tas_step_bytes", "tas_step_create", "tas_step_destroy", "tas_step_tokens",
+           "tas_step_append", "tas_step_attention", "tas_step_plan"]
+
+_lib = None
+
+
+def lib():
+    """Load libtas_step.so (raises if it has not been built)."""
+    global _lib
+    if _lib is None:
+        if not os.path.exists(LIB_PATH):
+            raise ImportError(f"{LIB_PATH} is missing: run __graft_entry__.build() "
+                              "or python -m paper_2606_18431_amd.build")
+        L = ctypes.CDLL(LIB_PATH)
+        L.tas_step_bytes.argtypes = [_P]
+        L.tas_step_bytes.restype = ctypes.c_size_t
+        L.tas_step_create.argtypes = [_P, _P, ctypes.c_size_t, ctypes.POINTER(_P)]
+        L.tas_step_destroy.argtypes = [_P]
+        L.tas_step_destroy.restype = None
+        L.tas_step_tokens.argtypes = [_P]
+        L.tas_step_tokens.restype = _i64
+        L.tas_step_append.argtypes = [_P, _P, _P]
+        L.tas_step_attention.argtypes = [_P, _P, _P]
+        L.tas_step_plan.argtypes = [_P, _P, ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)]
+        _lib = L
+    return _lib
+
+
+def _check(rc: int, what: str):
+    if rc != TAS_OK:
+        raise TasError(rc, what)
+
+
+def make_batch(n_new, kv_len, blocks, *, heads, kv_heads, head_dim, block_tokens, n_blocks,
+               prefix_first=None, prefix_len=None, prefix_blocks=None, causal=True):
+    """tas_batch over host arrays; returns (struct, keepalive). ``blocks`` is
+    [n_req, pages] and ``prefix_blocks`` [groups, pages], rows as long as the
+    longest context needs."""
+    n = np.ascontiguousarray(n_new, np.int32)
+    kv = np.ascontiguousarray(kv_len, np.int32)
+    bl = np.ascontiguousarray(blocks, np.int32)
+    if n.ndim != 1 or kv.shape != n.shape:
+        raise ValueError(f"n_new has shape {n.shape}, kv_len {kv.shape}")
+    if bl.ndim != 2 or bl.shape[0] != len(n):
+        raise ValueError(f"blocks has shape {bl.shape} for {len(n)} requests")
+    keep = [n, kv, bl]
+    b = tas_batch(heads, kv_heads, head_dim, block_tokens, len(n), n_blocks, int(bool(causal)), 0,
+                  n.ctypes.data, kv.ctypes.data, bl.ctypes.data, bl.shape[1])
+    if prefix_first is not None:
+        pf = np.ascontiguousarray(prefix_first, np.int32)
+        pl = np.ascontiguousarray(prefix_len, np.int32)
+        pb = np.ascontiguousarray(prefix_blocks, np.int32)
+        if pf.ndim != 1 or len(pf) < 2 or pl.shape != (len(pf) - 1,):
+            raise ValueError(f"prefix_first has shape {pf.shape}, prefix_len {pl.shape}")
+        if pb.ndim != 2 or pb.shape[0] != len(pl):
+            raise ValueError(f"prefix_blocks has shape {pb.shape} for {len(pl)} groups")
+        keep += [pf, pl, pb]
+        b.n_prefix, b.prefix_stride = len(pl), pb.shape[1]
+        b.prefix_first, b.prefix_len = pf.ctypes.data, pl.ctypes.data
+        b.prefix_blocks = pb.ctypes.data
+    return b, keep
+
+
+def tas_step_bytes(batch: tas_batch) -> int:
+    return int(lib().tas_step_bytes(ctypes.byref(batch)))
+
+
+def tas_step_create(batch: tas_batch, ws: int, ws_bytes: int) -> int:
+    """Returns a step handle (int). ``ws`` is a device address."""
+    ctx = _P()
+    _check(lib().tas_step_create(ctypes.byref(batch), ws, ws_bytes, ctypes.byref(ctx)),
+           "tas_step_create")
+    return ctx.value
+
+
+def tas_step_plan(batch: tas_batch) -> bytes:
+    """The plan that tas_step_create copies to the device."""
+    n = ctypes.c_size_t()
+    _check(lib().tas_step_plan(ctypes.byref(batch), None, 0, ctypes.byref(n)), "tas_step_plan")
+    buf = ctypes.create_string_buffer(n.value)
+    _check(lib().tas_step_plan(ctypes.byref(batch), buf, n.value, ctypes.byref(n)),
+           "tas_step_plan")
+    return buf.raw
+
+
+class Step:
+    """The plan of one batch on one GPU: made once when the scheduler has
+    formed the batch, used for every layer.
+
+    Caches are tensors [n_blocks, kv_heads, block_tokens, head_dim], any strides
+    (a permuted view serves other orders) whose last is 1. Calls are enqueued on
+    ``stream`` (a torch stream; default: the current one); outputs are allocated
+    on that stream unless given. Attention calls of one step share its
+    workspace: keep them on one stream, or order them."""
+
+    def __init__(self, n_new, kv_len, blocks, *, heads, kv_heads, head_dim, block_tokens,
+                 n_blocks, prefix_first=None, prefix_len=None, prefix_blocks=None, causal=True,
+                 device="cuda"):
+        self.ctx = None
+        b, keep = make_batch(n_new, kv_len, blocks, heads=heads, kv_heads=kv_heads,
+                             head_dim=head_dim, block_tokens=block_tokens, n_blocks=n_blocks,
+                             prefix_first=prefix_first, prefix_len=prefix_len,
+                             prefix_blocks=prefix_blocks, causal=causal)
+        self.ws_bytes = tas_step_bytes(b)
+        if self.ws_bytes == 0:
+            raise TasError(TAS_EINVAL, "tas_step_bytes")
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.heads, self.kv_heads, self.head_dim = heads, kv_heads, head_dim
+        self.cache_shape = (n_blocks, kv_heads, block_tokens, head_dim)
+        with torch.cuda.device(self.device):
+            self.ws = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=self.device)
+            self._home = torch.cuda.current_stream().cuda_stream
+            # the memory may have been freed by work that is still under way
+            torch.cuda.current_stream().synchronize()
+            self.ctx = tas_step_create(b, self.ws.data_ptr() + (-self.ws.data_ptr()) % 256,
+                                       self.ws_bytes)
+        self.tokens = int(lib().tas_step_tokens(self.ctx))
+
+    # ------------------------------------------------------------ argument checks
+
+    def _rows(self, t, heads, dtype, what):
+        """Address and token stride of a [tokens, heads, head_dim] tensor."""
+        if t.dtype != dtype or t.device != self.device:
+            raise ValueError(f"{what} is {t.dtype} on {t.device}, expected {dtype} on "
+                             f"{self.device}")
+        if t.shape != (self.tokens, heads, self.head_dim):
+            raise ValueError(f"{what} has shape {tuple(t.shape)}, expected "
+                             f"{(self.tokens, heads, self.head_dim)}")
+        s = t.stride()
+        if s[2] != 1 or s[1] != self.head_dim:
+            raise ValueError(f"{what}: the heads of a token have to be adjacent, strides {s}")
+        # one token: its stride says nothing
+        return t.data_ptr(), s[0] if self.tokens > 1 else heads * self.head_dim
+
+    def _cache(self, k, v):
+        for t, what in ((k, "k_cache"), (v, "v_cache")):
+            if t.dtype != k.dtype or t.device != self.device:
+                raise ValueError(f"{what} is {t.dtype} on {t.device}")
+            if t.shape != self.cache_shape:
+                raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {self.cache_shape}")
+            if t.stride(3) != 1:
+                raise ValueError(f"{what}: head_dim is not the fastest, strides {t.stride()}")
+        ks, vs = k.stride(), v.stride()
+        return tas_cache(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2])
+
+    def _dtype(self, t, what):
+        code = DTYPES.get(t.dtype)
+        if code is None:
+            raise ValueError(f"{what} is {t.dtype}: float16 or bfloat16")
+        return code
+
+    def _out(self, out, like, heads, stream):
+        if out is not None:
+            return out
+        shape = (self.tokens, heads, self.head_dim)
+        if stream is None:
+            return torch.empty(shape, dtype=like.dtype, device=self.device)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=like.dtype, device=self.device)
+
+    def _enqueue(self, fn, args, stream):
+        if self.ctx is None:
+            raise ValueError("the step is closed")
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device)
+        if stream.cuda_stream != self._home:  # the workspace outlives the work there
+            self.ws.record_stream(stream)
+        if torch.cuda.current_device() == self.device.index:
+            rc = fn(self.ctx, ctypes.byref(args), stream.cuda_stream)
+        else:
+            with torch.cuda.device(self.device):
+                rc = fn(self.ctx, ctypes.byref(args), stream.cuda_stream)
+        _check(rc, fn.__name__)
+
+    # ------------------------------------------------------------ the operators
+
+    def append(self, qkv, k_cache, v_cache, cos=None, sin=None, *, q_weight=None, k_weight=None,
+               eps=1e-6, interleaved=False, out=None, stream=None):
+        """Norm (with weights), rotate (with angles) and append the new tokens.
+
+        ``qkv``: [tokens, heads + 2 kv_heads, head_dim], queries, keys, values.
+        ``cos``, ``sin``: float32 [positions, rot_dim / 2], rot_dim a multiple of
+        16; None: no rotation. ``q_weight``, ``k_weight``: [head_dim], or both
+        None. Keys and values go to the caches; returns the queries."""
+        dtype = self._dtype(qkv, "qkv")
+        qkv_p, qkv_s = self._rows(qkv, self.heads + 2 * self.kv_heads, qkv.dtype, "qkv")
+        cache = self._cache(k_cache, v_cache)
+        if k_cache.dtype != qkv.dtype:
+            raise ValueError(f"the caches are {k_cache.dtype}, qkv {qkv.dtype}")
+        rot = positions = 0
+        cos_p = sin_p = None
+        if (cos is None) != (sin is None):
+            raise ValueError("cos and sin: both or neither")
+        if cos is not None:
+            for t in (cos, sin):
+                if t.dtype != torch.float32 or t.device != self.device or t.dim() != 2 \
+                        or t.shape != cos.shape or not t.is_contiguous():
+                    raise ValueError("cos and sin: contiguous float32 [positions, rot_dim / 2] "
+                                     f"on {self.device}")
+            positions, rot = cos.shape[0], 2 * cos.shape[1]
+            cos_p, sin_p = cos.data_ptr(), sin.data_ptr()
+        if (q_weight is None) != (k_weight is None):
+            raise ValueError("q_weight and k_weight: both or neither")
+        if q_weight is not None:
+            for t in (q_weight, k_weight):
+                if t.dtype != qkv.dtype or t.device != self.device \
+                        or t.shape != (self.head_dim,) or not t.is_contiguous():
+                    raise ValueError(f"weights: contiguous {qkv.dtype} [{self.head_dim}] on "
+                                     f"{self.device}")
+            q_weight, k_weight = q_weight.data_ptr(), k_weight.data_ptr()
+        out = self._out(out, qkv, self.heads, stream)
+        out_p, out_s = self._rows(out, self.heads, qkv.dtype, "out")
+        self._enqueue(lib().tas_step_append,
+                      tas_append(dtype, rot, int(bool(interleaved)), eps, qkv_p, qkv_s, out_p,
+                                 out_s, q_weight, k_weight, cos_p, sin_p, positions, cache),
+                      stream)
+        return out
+
+    def attention(self, q, k_cache, v_cache, *, scale=None, out=None, lse=None, stream=None):
+        """softmax(scale q K^T) V of every new token and head over its request's
+        prefix and context. ``scale``: default 1 / sqrt(head_dim). ``lse``: a
+        float32 [tokens, heads] to receive the log of the sum of the exponentials.
+        ``out`` may be ``q``. Returns [tokens, heads, head_dim]."""
+        dtype = self._dtype(q, "q")
+        q_p, q_s = self._rows(q, self.heads, q.dtype, "q")
+        cache = self._cache(k_cache, v_cache)
+        if k_cache.dtype != q.dtype:
+            raise ValueError(f"the caches are {k_cache.dtype}, q {q.dtype}")
+        out = self._out(out, q, self.heads, stream)
+        out_p, out_s = self._rows(out, self.heads, q.dtype, "out")
+        if lse is not None:
+            if lse.dtype != torch.float32 or lse.device != self.device \
+                    or lse.shape != (self.tokens, self.heads) or not lse.is_contiguous():
+                raise ValueError(f"lse: contiguous float32 {(self.tokens, self.heads)} on "
+                                 f"{self.device}")
+            lse = lse.data_ptr()
+        if scale is None:
+            scale = 1.0 / math.sqrt(self.head_dim)
+        self._enqueue(lib().tas_step_attention,
+                      tas_attention(dtype, scale, q_p, q_s, out_p, out_s, lse, cache), stream)
+        return out
+
+    def close(self):
+        if getattr(self, "ctx", None):
+            lib().tas_step_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

@@ -1,0 +1,252 @@
+"""The plan of a step on the host (no GPU): what tas_step_create would copy to
+the device covers every visible key of every row once, follows the right pages,
+gives partial results disjoint places, and invalid batches are refused."""
+import ctypes
+import os
+import re
+import subprocess
+
+import numpy as np
+import pytest
+
+from paper_2606_18431_amd import step, tas
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+REQ = np.dtype([(f, np.int32) for f in ("t0", "n_new", "kv_len", "table", "prefix_len", "own_seg",
+                                        "pre_seg", "pad")])
+SEG = np.dtype([(f, np.int32) for f in ("t0", "n_tok", "kv_len", "lim0", "table", "nsplit", "part",
+                                        "rows")])
+ITEM = np.dtype([(f, np.int32) for f in ("seg", "hk", "row0", "k0", "k1", "part")])
+HEAD = np.dtype([("bytes", np.int64), ("part_rows", np.int64)]
+                + [(f, np.int32) for f in ("n_req", "n_tok", "n_seg", "n_thin", "n_wide",
+                                           "n_merge", "n_table", "all_own")]
+                + [(f, np.int64) for f in ("req", "seg", "thin", "wide", "tables", "tok_req",
+                                           "merge")])
+THIN_ROWS, WIDE_ROWS = 16, 128
+
+
+def parse(blob):
+    h = np.frombuffer(blob, HEAD, 1)[0]
+    assert h["bytes"] == len(blob)
+
+    def at(off, dtype, n):
+        return np.frombuffer(blob, dtype, int(n), int(off))
+
+    return dict(head=h, reqs=at(h["req"], REQ, h["n_req"]), segs=at(h["seg"], SEG, h["n_seg"]),
+                thin=at(h["thin"], ITEM, h["n_thin"]), wide=at(h["wide"], ITEM, h["n_wide"]),
+                tables=at(h["tables"], np.int32, h["n_table"]),
+                tok_req=at(h["tok_req"], np.int32, h["n_tok"]),
+                merge=at(h["merge"], np.int32, h["n_merge"]))
+
+
+def batch(seed, n_req, max_new, max_ctx, heads, kv_heads, block, groups=0, causal=True,
+          some_empty=False):
+    rng = np.random.default_rng(seed)
+    n = rng.integers(0 if some_empty else 1, max_new + 1, n_req)
+    kv = np.maximum(n, rng.integers(1, max_ctx + 1, n_req)) * (1 if not some_empty
+                                                             else rng.integers(0, 2, n_req))
+    if causal:
+        kv = np.maximum(kv, n)
+    width = int(max(1, (-(-kv // block)).max()))
+    pre = rng.integers(0, 3 * block, groups)
+    pwidth = int(max(1, (-(-pre // block)).max())) if groups else 0
+    n_blocks = n_req * width + groups * pwidth + 3
+    ids = rng.permutation(n_blocks).astype(np.int32)
+    blocks = ids[:n_req * width].reshape(n_req, width)
+    kw = dict(heads=heads, kv_heads=kv_heads, head_dim=64, block_tokens=block, n_blocks=n_blocks,
+              causal=causal)
+    if groups:
+        cuts = np.sort(rng.integers(0, n_req + 1, groups - 1))
+        kw.update(prefix_first=np.concatenate([[0], cuts, [n_req]]), prefix_len=pre,
+                  prefix_blocks=ids[n_req * width:n_req * width + groups * pwidth]
+                  .reshape(groups, pwidth))
+    return n, kv, blocks, kw
+
+
+CASES = [dict(seed=1, n_req=1, max_new=1, max_ctx=1, heads=8, kv_heads=8, block=16),
+         dict(seed=2, n_req=70, max_new=1, max_ctx=9000, heads=32, kv_heads=8, block=16),
+         dict(seed=3, n_req=5, max_new=300, max_ctx=700, heads=7, kv_heads=1, block=32),
+         dict(seed=4, n_req=9, max_new=6, max_ctx=40, heads=12, kv_heads=4, block=16, groups=3),
+         dict(seed=5, n_req=40, max_new=2, max_ctx=500, heads=64, kv_heads=2, block=64, groups=2,
+              some_empty=True),
+         dict(seed=6, n_req=12, max_new=40, max_ctx=100, heads=4, kv_heads=2, block=16,
+              causal=False, some_empty=True),
+         dict(seed=7, n_req=3, max_new=1000, max_ctx=9000, heads=16, kv_heads=2, block=16,
+              groups=1)]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: str(c["seed"]))
+def test_plan_covers_every_visible_key_once(case):
+    n, kv, blocks, kw = batch(**case)
+    b, keep = step.make_batch(n, kv, blocks, **kw)
+    p = parse(step.tas_step_plan(b))
+    Hk, G, bt = kw["kv_heads"], kw["heads"] // kw["kv_heads"], kw["block_tokens"]
+    T = int(n.sum())
+    assert p["head"]["n_tok"] == T and p["head"]["n_req"] == len(n)
+    assert np.array_equal(p["tok_req"], np.repeat(np.arange(len(n)), n))
+    first = kw.get("prefix_first")
+    used = np.zeros(int(p["head"]["part_rows"]), np.int32)
+    covered = {}  # (seg, hk) -> per row, the pieces that saw it
+    for kind, tile in (("thin", THIN_ROWS), ("wide", WIDE_ROWS)):
+        for it in p[kind]:
+            s = p["segs"][it["seg"]]
+            assert (s["rows"] <= THIN_ROWS) == (kind == "thin")
+            assert 0 <= it["hk"] < Hk and it["row0"] % tile == 0 and it["row0"] < s["rows"]
+            rows = min(tile, s["rows"] - it["row0"])
+            assert 0 <= it["k0"] <= it["k1"] <= s["kv_len"]
+            assert it["k0"] % 32 == 0 or it["k0"] == it["k1"]
+            assert (it["part"] >= 0) == (s["part"] >= 0)
+            if it["part"] >= 0:
+                used[it["part"]:it["part"] + rows] += 1
+            for r in range(it["row0"], it["row0"] + rows):
+                covered.setdefault((int(it["seg"]), int(it["hk"]), r), []).append(it)
+    assert (used == 1).all()  # every partial row is written, by one item
+    for i, s in enumerate(p["segs"]):
+        assert s["rows"] == s["n_tok"] * G
+        for hk in range(Hk):
+            for r in range(0, s["rows"], max(1, s["rows"] // 50)):
+                its = sorted(covered[i, hk, r], key=lambda x: (x["k0"], x["k1"]))
+                assert len(its) == s["nsplit"] and (s["part"] >= 0 or len(its) == 1)
+                lim = max(0, min(s["kv_len"], s["lim0"] + r // G))
+                at = 0
+                for it in its:
+                    assert it["k0"] == at or it["k0"] == it["k1"]
+                    at = max(at, int(it["k1"]))
+                assert at >= lim
+                if s["part"] >= 0:
+                    assert sorted(x["part"] + r - x["row0"] for x in its) == \
+                        [s["part"] + (hk * s["nsplit"] + m) * s["rows"] + r
+                         for m in range(s["nsplit"])]
+    merged = set(p["merge"].tolist())
+    t = 0
+    for i, r in enumerate(p["reqs"]):
+        assert (r["t0"], r["n_new"], r["kv_len"]) == (t, n[i], kv[i])
+        pages = -(-int(kv[i]) // bt)
+        assert np.array_equal(p["tables"][r["table"]:r["table"] + pages], blocks[i, :pages])
+        g = None if first is None else int(np.searchsorted(first, i, side="right") - 1)
+        pre = 0 if g is None else int(kw["prefix_len"][g])
+        assert r["prefix_len"] == pre
+        if n[i]:
+            own, shared = r["own_seg"], r["pre_seg"]
+            assert (shared >= 0) == (pre > 0) and (own >= 0 or pre > 0)
+            if own >= 0:
+                s = p["segs"][own]
+                assert (s["t0"], s["n_tok"], s["kv_len"], s["table"]) == (t, n[i], kv[i],
+                                                                        r["table"])
+                assert s["lim0"] == (kv[i] - n[i] + 1 if kw["causal"] else kv[i])
+            if shared >= 0:
+                s = p["segs"][shared]
+                assert s["t0"] <= t and t + n[i] <= s["t0"] + s["n_tok"]
+                assert s["kv_len"] == s["lim0"] == pre and s["part"] >= 0
+                q = -(-pre // bt)
+                assert np.array_equal(p["tables"][s["table"]:s["table"] + q],
+                                      np.asarray(kw["prefix_blocks"])[g, :q])
+            parts = shared >= 0 or p["segs"][own]["part"] >= 0
+            for j in range(t, t + n[i]):
+                assert (j in merged) == parts
+        t += int(n[i])
+
+
+def refused(n, kv, blocks, **kw):
+    base = dict(heads=8, kv_heads=2, head_dim=64, block_tokens=16, n_blocks=8)
+    b, keep = step.make_batch(n, kv, blocks, **{**base, **kw})
+    n_bytes = step.tas_step_bytes(b)
+    size = ctypes.c_size_t()
+    rc = step.lib().tas_step_plan(ctypes.byref(b), None, 0, ctypes.byref(size))
+    assert (n_bytes == 0) == (rc != 0)
+    ctx = ctypes.c_void_p()
+    if rc:  # refused before anything is copied: the address is never used
+        assert step.lib().tas_step_create(ctypes.byref(b), 1 << 40, 1 << 40,
+                                          ctypes.byref(ctx)) == rc
+    else:
+        assert step.lib().tas_step_create(ctypes.byref(b), 1 << 40, n_bytes - 1,
+                                          ctypes.byref(ctx)) == tas.TAS_ENOMEM
+        assert step.lib().tas_step_create(ctypes.byref(b), (1 << 40) + 16, n_bytes,
+                                          ctypes.byref(ctx)) == tas.TAS_EINVAL
+    assert not ctx.value
+    return rc == tas.TAS_EINVAL
+
+
+def test_refused_batches():
+    pages = [[0, 1], [2, 3]]
+    assert not refused([1, 2], [20, 32], pages)
+    assert not refused([0, 0], [0, 0], pages)
+    for bad in (dict(heads=0), dict(heads=7), dict(kv_heads=0), dict(heads=2048, kv_heads=2),
+                dict(head_dim=96), dict(head_dim=0), dict(block_tokens=8),
+                dict(block_tokens=48), dict(block_tokens=8192), dict(n_blocks=0),
+                dict(n_blocks=3)):
+        assert refused([1, 2], [20, 32], pages, **bad), bad
+    assert refused([-1, 2], [20, 32], pages)
+    assert refused([1, 2], [-1, 32], pages)
+    assert refused([1, 2], [33, 32], pages)          # three blocks of a table of two
+    assert refused([1, 2], [20, 32], [[0, 8], [2, 3]])
+    assert refused([1, 2], [20, 32], [[-1, 1], [2, 3]])
+    assert not refused([1, 2], [16, 32], [[0, -1], [2, 3]])   # not reached
+    assert refused([1, 1], [20, 32], [[0, 1], [2, 1]])        # one slot's block twice
+    assert not refused([1, 1], [20, 32], [[0, 1], [0, 3]])    # read by both, written by neither
+    assert refused([20, 1], [20, 1], [[5, 5], [2, 3]])
+    assert refused([1 << 25, 1], [1 << 25, 1], pages)
+
+
+def test_refused_prefixes():
+    pages = [[0, 1], [2, 3]]
+    good = dict(prefix_first=[0, 1, 2], prefix_len=[20, 0], prefix_blocks=[[4, 5], [6, 7]])
+    assert not refused([1, 2], [20, 32], pages, **good)
+    for bad in (dict(prefix_first=[0, 1, 1]), dict(prefix_first=[1, 1, 2]),
+                dict(prefix_first=[0, 2, 1]), dict(prefix_first=[0, 3, 2]),
+                dict(prefix_len=[-1, 0]), dict(prefix_len=[33, 0]),
+                dict(prefix_blocks=[[4, 8], [6, 7]]), dict(prefix_blocks=[[4, -1], [6, 7]])):
+        assert refused([1, 2], [20, 32], pages, **{**good, **bad}), bad
+    with pytest.raises(ValueError):
+        step.make_batch([1], [1], [[0]], heads=1, kv_heads=1, head_dim=64, block_tokens=16,
+                        n_blocks=1, prefix_first=[0, 1], prefix_len=[1, 2], prefix_blocks=[[0]])
+    with pytest.raises(ValueError):
+        step.make_batch([1, 2], [1], [[0]], heads=1, kv_heads=1, head_dim=64, block_tokens=16,
+                        n_blocks=1)
+
+
+def test_null_arguments():
+    L = step.lib()
+    assert L.tas_step_bytes(None) == 0
+    assert L.tas_step_create(None, None, 0, None) == tas.TAS_EINVAL
+    assert L.tas_step_append(None, None, None) == tas.TAS_EINVAL
+    assert L.tas_step_attention(None, None, None) == tas.TAS_EINVAL
+    assert L.tas_step_tokens(None) == -1
+    L.tas_step_destroy(None)
+    b, keep = step.make_batch([1, 1], [0, 1], [[0], [1]], heads=1, kv_heads=1, head_dim=64,
+                              block_tokens=16, n_blocks=2)
+    assert L.tas_step_bytes(ctypes.byref(b)) > 0
+    b.blocks = None
+    assert L.tas_step_bytes(ctypes.byref(b)) == 0
+
+
+def test_library_exports_every_declared_symbol():
+    src = open(os.path.join(ROOT, "include", "tas_step.h")).read()
+    src = re.sub(r"/\*.*?\*/", "", src, flags=re.S)
+    names = sorted(set(re.findall(r"\b(tas_step_[a-z_]+)\s*\(", src)))
+    assert names == sorted(step.EXPORTS)
+    for n in names:
+        assert hasattr(step.lib(), n), n
+
+
+def test_struct_layouts_match_header(tmp_path):
+    structs = [step.tas_batch, step.tas_cache, step.tas_append, step.tas_attention]
+    lines = ['#include <stddef.h>', '#include <stdio.h>', '#include "tas_step.h"',
+             'int main(void) {']
+    for st in structs:
+        n = st.__name__
+        lines.append(f'printf("{n} %zu\\n", sizeof({n}));')
+        for f, _ in st._fields_:
+            lines.append(f'printf("{n}.{f} %zu\\n", offsetof({n}, {f}));')
+    lines.append('return 0; }')
+    src = tmp_path / "layout.c"
+    src.write_text("\n".join(lines))
+    exe = tmp_path / "layout"
+    subprocess.check_call(["gcc", "-std=c11", "-I", os.path.join(ROOT, "include"), "-o", str(exe),
+                           str(src)])
+    got = dict(x.split() for x in subprocess.check_output([str(exe)], text=True).splitlines())
+    for st in structs:
+        assert int(got[st.__name__]) == ctypes.sizeof(st)
+        for f, _ in st._fields_:
+            assert int(got[f"{st.__name__}.{f}"]) == getattr(st, f).offset, f
