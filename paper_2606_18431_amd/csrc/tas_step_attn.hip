@@ -41,6 +41,10 @@ __device__ f16x mfma32(vec8<_Float16> a, vec8<_Float16> b, f16x c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
+// The running maximum is raised only where it falls behind by more than this (a
+// weight is at most 2^8 then): the rescaling of o, as long as it is, is rare.
+constexpr float kLazy = 8.0f;
+
 __device__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Maximum and sum over the lanes that hold one column: lane ^ 32, and lane ^ 16.
@@ -92,6 +96,7 @@ __device__ void store_row(const AttnArgs &a, const Seg &s, const Item &it, int r
     }
     const int row = it.row0 + r, j = row / a.group, head = it.hk * a.group + row - j * a.group;
     vec8<T> x;
+#pragma unroll
     for (int e = 0; e < 8; e++) x[e] = (T)(o[e] * f);
     const int64_t tok = s.t0 + j;
     *(vec8<T> *)((T *)a.out + tok * a.out_stride + (int64_t)head * D + d) = x;
@@ -125,77 +130,104 @@ __global__ __launch_bounds__(256) void thin_kernel(AttnArgs a) {
     {
         const T *src = (const T *)a.q + (int64_t)(s.t0 + j) * a.q_stride +
                        (int64_t)(it.hk * a.group + row - j * a.group) * D + g * 8;
+#pragma unroll
         for (int i = 0; i < QS; i++) q[i] = *(const V *)(src + i * 32);
     }
     const int full = min(min(s.kv_len, s.lim0), it.k1);  // keys that the first row sees
     const int sub_mask = (1 << a.sub_shift) - 1;
     const T *kbase = (const T *)a.c.k + it.hk * a.c.k_head;
     const T *vbase = (const T *)a.c.v + it.hk * a.c.v_head;
-    const int klane = col * (int)a.c.k_token + g * 8;
+    const uint32_t klane = (col * (uint32_t)a.c.k_token + g * 8) * 2;
     const int vrow = lane / LPR, vch = lane % LPR;
-    const int vlane = vrow * (int)a.c.v_token + vch * 8;
+    const uint32_t vlane = (vrow * (uint32_t)a.c.v_token + vch * 8) * 2;
     char *vl = lds + wave * VB;
 
     f4 o[D / 16];
+#pragma unroll
     for (int i = 0; i < D / 16; i++) o[i] = f4{0, 0, 0, 0};
     float m = -INFINITY, l = 0;
     V k[2][QS];
     u4 v[VL];
+    int page[2];
     const int last_sub = it.k1 > 0 ? (it.k1 - 1) >> 4 : 0;
 
+    auto look_up = [&](int base) {
+#pragma unroll
+        for (int n = 0; n < 2; n++)
+            page[n] = tab[min((base >> 4) + n, last_sub) >> a.sub_shift];
+    };
     auto load = [&](int base) {
+#pragma unroll
         for (int n = 0; n < 2; n++) {
-            const int sub = min((base >> 4) + n, last_sub);
-            const int64_t page = tab[sub >> a.sub_shift];
-            const int off = (sub & sub_mask) * 16;
-            const T *kp = kbase + page * a.c.k_block + off * a.c.k_token;
-            const T *vp = vbase + page * a.c.v_block + off * a.c.v_token;
-            for (int i = 0; i < QS; i++) k[n][i] = *(const V *)(kp + klane + i * 32);
+            const int64_t off = (min((base >> 4) + n, last_sub) & sub_mask) * 16;
+            const char *kp = (const char *)(kbase + page[n] * a.c.k_block + off * a.c.k_token);
+            const char *vp = (const char *)(vbase + page[n] * a.c.v_block + off * a.c.v_token);
+#pragma unroll
+            for (int i = 0; i < QS; i++) k[n][i] = *(const V *)(kp + klane + i * 64);
+#pragma unroll
             for (int i = 0; i < VL / 2; i++)
                 v[n * VL / 2 + i] =
-                    *(const u4 *)(vp + vlane + (int64_t)(i * (64 / LPR)) * a.c.v_token);
+                    *(const u4 *)(vp + (int64_t)(i * (64 / LPR)) * a.c.v_token * 2 + vlane);
         }
     };
-    int base = it.k0 + wave * kThinKeys;
-    if (base < it.k1) load(base);
-    for (; base < it.k1; base += 4 * kThinKeys) {
+    int base = __builtin_amdgcn_readfirstlane(it.k0 + wave * kThinKeys);
+    const int stride = 4 * kThinKeys;
+    if (base < it.k1) {
+        look_up(base);
+        load(base);
+        look_up(base + stride);
+    }
+    for (; base < it.k1; base += stride) {
         f4 sc[2];
+#pragma unroll
         for (int n = 0; n < 2; n++) {
             sc[n] = f4{0, 0, 0, 0};
+#pragma unroll
             for (int i = 0; i < QS; i++) sc[n] = mfma16(k[n][i], q[i], sc[n]);
         }
         if (base + kThinKeys > it.k1)  // slots past the keys hold anything: weight 0 times it
+#pragma unroll
             for (int i = 0; i < VL; i++)
                 if (base + i * (64 / LPR) + vrow >= it.k1) v[i] = u4{0, 0, 0, 0};
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
         for (int i = 0; i < VL; i++)
             *(u4 *)(vl + v_chunk<D>(i * (64 / LPR) + vrow, vch) * 16) = v[i];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (base + 4 * kThinKeys < it.k1) load(base + 4 * kThinKeys);
+        if (base + stride < it.k1) {
+            load(base + stride);
+            look_up(base + 2 * stride);
+        }
 
-        const bool mask = base + kThinKeys > full;
-        float x[8], mt = -INFINITY;
+        if (base + kThinKeys > full)
+#pragma unroll
+            for (int n = 0; n < 2; n++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    if (base + n * 16 + g * 4 + i >= lim) sc[n][i] = -INFINITY;
+        float mt = -INFINITY;
+#pragma unroll
         for (int n = 0; n < 2; n++)
-            for (int i = 0; i < 4; i++) {
-                float y = sc[n][i] * a.scale2;
-                if (mask && base + n * 16 + g * 4 + i >= lim) y = -INFINITY;
-                x[n * 4 + i] = y;
-                mt = fmaxf(mt, y);
-            }
-        mt = max32(max16(mt));
-        const float mn = fmaxf(m, mt), mu = mn == -INFINITY ? 0.0f : mn;
-        const float f = exp2_(m - mu);
-        m = mn;
+#pragma unroll
+            for (int i = 0; i < 4; i++) mt = fmaxf(mt, sc[n][i]);
+        mt = max32(max16(mt)) * a.scale2;
+        if (__any(mt > m + kLazy)) {
+            const float mn = mt > m + kLazy ? mt : m, f = mn == m ? 1.0f : exp2_(m - mn);
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < D / 16; i++) o[i] *= f;
+        }
+        const float mu = m == -INFINITY ? 0.0f : m;
         V p;
-        float sum = 0;
+#pragma unroll
         for (int i = 0; i < 8; i++) {
-            const float y = exp2_(x[i] - mu);
-            sum += y;
+            const float y = exp2_(sc[i >> 2][i & 3] * a.scale2 - mu);
+            l += y;
             p[i] = (T)y;
         }
-        l = l * f + sum;
+#pragma unroll
         for (int i = 0; i < D / 16; i++) {
-            o[i] *= f;
             // lane c of group g: column d = 16 i + c of the rows 4 g .. 4 g + 3 and 16 on
             const int r0 = 4 * g + (col >> 2), c = 2 * i + ((col >> 1) & 1);
             const s4 lo = read_tr(vl + v_chunk<D>(r0, c) * 16 + (col & 1) * 8);
@@ -210,20 +242,24 @@ __global__ __launch_bounds__(256) void thin_kernel(AttnArgs a) {
     __syncthreads();
     if (g == 0) stat[wave][col][0] = m, stat[wave][col][1] = l;
     float *ex = (float *)lds;  // [wave][row][D], 4-float groups swizzled by the row
+#pragma unroll
     for (int i = 0; i < D / 16; i++)
         *(f4 *)(ex + (wave * kThinRows + col) * D + (((i * 4 + g) ^ col) * 4)) = o[i];
     __syncthreads();
     const int r = tid / (D / 8), d = tid % (D / 8) * 8;  // D 64: the upper half has no row
     if (r >= kThinRows || r >= s.rows) return;
     float mm = -INFINITY, ll = 0, y[8] = {};
+#pragma unroll
     for (int w = 0; w < 4; w++) mm = fmaxf(mm, stat[w][r][0]);
     const float mu = mm == -INFINITY ? 0.0f : mm;
+#pragma unroll
     for (int w = 0; w < 4; w++) {
         const float f = exp2_(stat[w][r][0] - mu);
         ll += stat[w][r][1] * f;
         const float *from = ex + (w * kThinRows + r) * D;
         const f4 lo = *(const f4 *)(from + ((d / 4) ^ r) * 4);
         const f4 hi = *(const f4 *)(from + ((d / 4 + 1) ^ r) * 4);
+#pragma unroll
         for (int e = 0; e < 4; e++) y[e] += lo[e] * f, y[4 + e] += hi[e] * f;
     }
     store_row<T, D>(a, s, it, r, d, y, ll, mm);
@@ -254,6 +290,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a) {
     {
         const T *src = (const T *)a.q + (int64_t)(s.t0 + j) * a.q_stride +
                        (int64_t)(it.hk * a.group + row - j * a.group) * D + half * 8;
+#pragma unroll
         for (int i = 0; i < QS; i++) q[i] = *(const V *)(src + i * 16);
     }
     const int full = min(min(s.kv_len, s.lim0 + it.row0 / a.group), it.k1);
@@ -261,30 +298,46 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a) {
     const T *kbase = (const T *)a.c.k + it.hk * a.c.k_head;
     const T *vbase = (const T *)a.c.v + it.hk * a.c.v_head;
     const int lrow = tid / LPR, lch = tid % LPR;
+    // A load takes RPL rows: one run of 16 keys (D 128), or two, each by two waves.
+    const int wsub = RPL == 16 ? 0 : __builtin_amdgcn_readfirstlane(wave >> 1);
+    const uint32_t klane = ((lrow & 15) * (uint32_t)a.c.k_token + lch * 8) * 2;
+    const uint32_t vlane = ((lrow & 15) * (uint32_t)a.c.v_token + lch * 8) * 2;
 
     f16x o[D / 32];
+#pragma unroll
     for (int i = 0; i < D / 32; i++)
+#pragma unroll
         for (int e = 0; e < 16; e++) o[i][e] = 0;
     float m = -INFINITY, l = 0;
     u4 kr[NL], vr[NL];
+    int page[NL];
     const int last_sub = it.k1 > 0 ? (it.k1 - 1) >> 4 : 0;
 
+    auto sub_of = [&](int base, int i) {
+        return min((base >> 4) + i * (RPL / 16) + wsub, last_sub);
+    };
+    auto look_up = [&](int base) {
+#pragma unroll
+        for (int i = 0; i < NL; i++) page[i] = tab[sub_of(base, i) >> a.sub_shift];
+    };
     auto load = [&](int base) {
+#pragma unroll
         for (int i = 0; i < NL; i++) {
-            const int y = i * RPL + lrow;
-            const int sub = min((base + y) >> 4, last_sub);
-            const int64_t page = tab[sub >> a.sub_shift];
-            const int off = (sub & sub_mask) * 16 + (y & 15);
-            kr[i] = *(const u4 *)(kbase + page * a.c.k_block + off * a.c.k_token + lch * 8);
-            vr[i] = *(const u4 *)(vbase + page * a.c.v_block + off * a.c.v_token + lch * 8);
+            const int64_t off = (sub_of(base, i) & sub_mask) * 16;
+            const char *kp = (const char *)(kbase + page[i] * a.c.k_block + off * a.c.k_token);
+            const char *vp = (const char *)(vbase + page[i] * a.c.v_block + off * a.c.v_token);
+            kr[i] = *(const u4 *)(kp + klane);
+            vr[i] = *(const u4 *)(vp + vlane);
         }
     };
     // chunk c of K row y: eight rows' chunks of one column lie in different banks
     auto k_chunk = [](int y, int c) { return y * LPR + (c ^ (y & (LPR - 1))); };
     auto put = [&](int buf, int base) {
         if (base + kWideKeys > it.k1)
+#pragma unroll
             for (int i = 0; i < NL; i++)
                 if (base + i * RPL + lrow >= it.k1) vr[i] = u4{0, 0, 0, 0};
+#pragma unroll
         for (int i = 0; i < NL; i++) {
             const int y = i * RPL + lrow;
             *(u4 *)(lds[buf] + k_chunk(y, lch) * 16) = kr[i];
@@ -292,51 +345,67 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a) {
         }
     };
     if (it.k0 < it.k1) {
+        look_up(it.k0);
         load(it.k0);
+        look_up(it.k0 + kWideKeys);
         put(0, it.k0);
     }
     __syncthreads();
     int buf = 0;
     for (int base = it.k0; base < it.k1; base += kWideKeys, buf ^= 1) {
         const bool more = base + kWideKeys < it.k1;
-        if (more) load(base + kWideKeys);
+        if (more) {
+            load(base + kWideKeys);
+            look_up(base + 2 * kWideKeys);
+        }
         const char *kl = lds[buf], *vl = lds[buf] + TB;
         f16x sc[2];
+#pragma unroll
         for (int n = 0; n < 2; n++) {
+#pragma unroll
             for (int e = 0; e < 16; e++) sc[n][e] = 0;
+#pragma unroll
             for (int i = 0; i < QS; i++) {
                 const V k = *(const V *)(kl + k_chunk(n * 32 + col, i * 2 + half) * 16);
                 sc[n] = mfma32(k, q[i], sc[n]);
             }
         }
-        const bool mask = base + kWideKeys > full;
+        if (base + kWideKeys > full)
+#pragma unroll
+            for (int n = 0; n < 2; n++)
+#pragma unroll
+                for (int e = 0; e < 16; e++)
+                    if (base + n * 32 + (e >> 2) * 8 + half * 4 + (e & 3) >= lim)
+                        sc[n][e] = -INFINITY;
         float mt = -INFINITY;
+#pragma unroll
         for (int n = 0; n < 2; n++)
-            for (int e = 0; e < 16; e++) {
-                float y = sc[n][e] * a.scale2;
-                if (mask && base + n * 32 + (e >> 2) * 8 + half * 4 + (e & 3) >= lim)
-                    y = -INFINITY;
-                sc[n][e] = y;
-                mt = fmaxf(mt, y);
-            }
-        mt = max32(mt);
-        const float mn = fmaxf(m, mt), mu = mn == -INFINITY ? 0.0f : mn;
-        const float f = exp2_(m - mu);
-        m = mn;
+#pragma unroll
+            for (int e = 0; e < 16; e++) mt = fmaxf(mt, sc[n][e]);
+        mt = max32(mt) * a.scale2;
+        if (__any(mt > m + kLazy)) {
+            const float mn = mt > m + kLazy ? mt : m, f = mn == m ? 1.0f : exp2_(m - mn);
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < D / 32; i++) o[i] *= f;
+        }
+        const float mu = m == -INFINITY ? 0.0f : m;
         V p[4];
-        float sum = 0;
+#pragma unroll
         for (int n = 0; n < 2; n++)
+#pragma unroll
             for (int e = 0; e < 16; e++) {
-                const float y = exp2_(sc[n][e] - mu);
-                sum += y;
+                const float y = exp2_(sc[n][e] * a.scale2 - mu);
+                l += y;
                 p[n * 2 + (e >> 3)][e & 7] = (T)y;
             }
-        l = l * f + sum;
-        for (int i = 0; i < D / 32; i++) o[i] *= f;
         // k-slots of step n: keys 16 n + 4 half + 0..3 and 8 on, as sc holds them
         const int tr = (lane & 15) >> 2, tc = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
+#pragma unroll
         for (int n = 0; n < 4; n++) {
             const int r0 = n * 16 + half * 4 + tr;
+#pragma unroll
             for (int i = 0; i < D / 32; i++) {
                 const s4 lo = read_tr(vl + v_chunk<D>(r0, i * 4 + tc) * 16 + (lane & 1) * 8);
                 const s4 hi = read_tr(vl + v_chunk<D>(r0 + 8, i * 4 + tc) * 16 + (lane & 1) * 8);
@@ -350,9 +419,12 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a) {
     l = sum32(l);
     // A lane holds d = 32 i + 8 e + 4 half + 0..3 of its row: the halves exchange so
     // that each has 8 adjacent ones.
+#pragma unroll
     for (int i = 0; i < D / 32; i++)
+#pragma unroll
         for (int e = 0; e < 4; e += 2) {
             float y[8];
+#pragma unroll
             for (int c = 0; c < 4; c++) {
                 const float ue = o[i][e * 4 + c], we = o[i][e * 4 + 4 + c];
                 const uint32_t u = __builtin_bit_cast(uint32_t, ue);
@@ -378,6 +450,7 @@ __global__ __launch_bounds__(256) void merge_kernel(AttnArgs a) {
     const int hk = head / a.group, g = head - hk * a.group;
     float m = -INFINITY;
     bool bad = false;  // a NaN among the parts stays
+#pragma unroll
     for (int p = 0; p < 2; p++) {
         const int seg = p ? r.pre_seg : r.own_seg;
         if (seg < 0) continue;
@@ -391,6 +464,7 @@ __global__ __launch_bounds__(256) void merge_kernel(AttnArgs a) {
     }
     const float mu = m == -INFINITY ? 0.0f : m;
     float sum = 0, y[E] = {};
+#pragma unroll
     for (int p = 0; p < 2; p++) {
         const int seg = p ? r.pre_seg : r.own_seg;
         if (seg < 0) continue;
@@ -399,11 +473,13 @@ __global__ __launch_bounds__(256) void merge_kernel(AttnArgs a) {
         for (int n = 0; n < s.nsplit; n++, at += s.rows) {
             const float w = exp2_(a.part_lse[at] - mu);
             sum += w;
+#pragma unroll
             for (int e = 0; e < E; e++) y[e] += w * a.part_o[at * D + lane * E + e];
         }
     }
     const float f = sum > 0 ? 1.0f / sum : 0.0f;
     T *to = (T *)a.out + (int64_t)tok * a.out_stride + (int64_t)head * D + lane * E;
+#pragma unroll
     for (int e = 0; e < E; e++) to[e] = (T)(bad ? NAN : y[e] * f);
     if (lane == 0 && a.lse)
         a.lse[(int64_t)tok * a.heads + head] =
