@@ -61,7 +61,8 @@ typedef struct tas_batch {
 
 /* One layer's cache: element (block, head, token of the block, d) of K lies at
  * k + block * k_block + head * k_head + token * k_token + d (elements); V
- * likewise. Pointers 16-byte aligned, strides multiples of 8. */
+ * likewise. Pointers 16-byte aligned, strides multiples of 8, below 2^31, of a
+ * token at most 2^24. */
 typedef struct tas_cache {
     void *k, *v;
     int64_t k_block, k_head, k_token;

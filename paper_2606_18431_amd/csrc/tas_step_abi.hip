@@ -30,7 +30,8 @@ namespace {
 
 constexpr int64_t kMaxTokens = int64_t(1) << 24;     // of a batch
 constexpr int64_t kMaxPartRows = int64_t(1) << 28;
-constexpr int64_t kMaxStride = int64_t(1) << 24;     // of a token or head, elements
+constexpr int64_t kMaxStride = (int64_t(1) << 31) - 8;      // of a block or head, elements
+constexpr int64_t kMaxTokenStride = int64_t(1) << 24;       // of a token in a block
 constexpr int32_t kSlots = 512;                      // wide items that run at once
 constexpr int32_t kThinItems = 2048;                 // thin items wanted
 
@@ -295,7 +296,7 @@ bool valid_cache(const tas_cache &c) {
     const int64_t s[6] = {c.k_block, c.v_block, c.k_head, c.v_head, c.k_token, c.v_token};
     for (int i = 0; i < 6; i++) {
         if (s[i] < 0 || s[i] % 8) return false;
-        if (i >= 4 && s[i] > kMaxStride) return false;
+        if (s[i] > (i >= 4 ? kMaxTokenStride : kMaxStride)) return false;
     }
     return true;
 }

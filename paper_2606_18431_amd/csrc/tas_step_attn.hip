@@ -28,6 +28,9 @@ template <typename T>
 using vec2 = T __attribute__((ext_vector_type(2)));
 typedef float f2 __attribute__((ext_vector_type(2)));
 
+// Block numbers: constant while a kernel runs, read by scalar loads.
+typedef const __attribute__((address_space(4))) int *Table;
+
 __device__ f4 mfma16(vec8<__bf16> a, vec8<__bf16> b, f4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -122,7 +125,7 @@ __global__ __launch_bounds__(256) void thin_kernel(AttnArgs a) {
     const int col = lane & 15, g = lane >> 4;
     const Item it = a.items[blockIdx.x];
     const Seg s = a.segs[it.seg];
-    const int *tab = a.tables + s.table;
+    const Table tab = (Table)(a.tables + s.table);
 
     const int row = min(col, s.rows - 1), j = row / a.group;
     const int lim = min(min(s.kv_len, s.lim0 + j), it.k1);
@@ -141,6 +144,8 @@ __global__ __launch_bounds__(256) void thin_kernel(AttnArgs a) {
     const int vrow = lane / LPR, vch = lane % LPR;
     const uint32_t vlane = (vrow * (uint32_t)a.c.v_token + vch * 8) * 2;
     char *vl = lds + wave * VB;
+    // (another chunk is an exclusive or, a row 16 on an addition)
+    const uint32_t v_at = v_chunk<D>(4 * g + (col >> 2), (col >> 1) & 1) * 16 + (col & 1) * 8;
 
     f4 o[D / 16];
 #pragma unroll
@@ -229,9 +234,8 @@ __global__ __launch_bounds__(256) void thin_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < D / 16; i++) {
             // lane c of group g: column d = 16 i + c of the rows 4 g .. 4 g + 3 and 16 on
-            const int r0 = 4 * g + (col >> 2), c = 2 * i + ((col >> 1) & 1);
-            const s4 lo = read_tr(vl + v_chunk<D>(r0, c) * 16 + (col & 1) * 8);
-            const s4 hi = read_tr(vl + v_chunk<D>(16 + r0, c) * 16 + (col & 1) * 8);
+            const char *at = vl + (v_at ^ (i * 32));
+            const s4 lo = read_tr(at), hi = read_tr(at + 256 * LPR);
             const s8 t = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
             o[i] = mfma16(__builtin_bit_cast(V, t), p, o[i]);
         }
@@ -265,23 +269,55 @@ __global__ __launch_bounds__(256) void thin_kernel(AttnArgs a) {
     store_row<T, D>(a, s, it, r, d, y, ll, mm);
 }
 
+// The bytes from the start of a cache to 16 keys of a block.
+__device__ int64_t run_offset(int page, int run, int64_t block_stride, int64_t token_stride) {
+    return (int64_t)((uint64_t)(uint32_t)page * (uint32_t)(block_stride * 2) +
+                     (uint64_t)(uint32_t)run * (uint32_t)(token_stride * 32));
+}
+
+__device__ void load_to_lds(const char *from, char *to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                     (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+template <int N>
+struct Const {
+    static constexpr int value = N;
+};
+// The order of a stretch: N times a matrix product, vector work that does not wait for
+// it, and LDS reads for the next stretch.
+template <int N, int VECTOR, int READS>
+__device__ __forceinline__ void mix() {
+    if constexpr (N > 0) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, VECTOR, 0);
+        if (READS) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+        mix<N - 1, VECTOR, READS>();
+    }
+}
+constexpr int kWaitLoads = 0x0F70;  // s_waitcnt: no load outstanding
+
 // 128 rows against a run of keys, 64 keys a step: 32 rows to a wave, K and V of a
-// step in LDS for all four. Two buffers: the loads of the next step are under way in
-// registers while the matrix unit works on this one, and one barrier ends a step.
+// step in LDS for all four waves, loaded there directly and double buffered. A step
+// is two stretches in which the matrix unit and the vector unit have independent
+// work: S of the next keys beside the exponentials of these, then P V of these beside
+// the maximum of the next. One barrier ends a step; the loads it waits for had the
+// whole step to arrive.
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a) {
     using V = vec8<T>;
-    constexpr int QS = D / 16;              // steps of 16 over d
-    constexpr int LPR = D / 8;              // lanes of a row
-    constexpr int RPL = 256 / LPR;          // rows that one load of the workgroup takes
-    constexpr int NL = kWideKeys / RPL;     // loads
-    constexpr int TB = kWideKeys * D * 2;   // bytes of a tile
-    __shared__ __attribute__((aligned(16))) char lds[2][2 * TB];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    constexpr int QS = D / 16;             // steps of 16 over d
+    constexpr int LPR = D / 8;             // chunks of 16 bytes of a row
+    constexpr int TB = kWideKeys * D * 2;  // bytes of a tile
+    constexpr int NL = TB / 4096;          // loads of a wave for a tile
+    constexpr int RPL = 64 / LPR;          // rows of one wave's load
+    // four objects, so that the compiler sees which loads a read has to wait for
+    __shared__ __attribute__((aligned(16))) char k0_lds[TB], k1_lds[TB], v0_lds[TB], v1_lds[TB];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
     const Item it = a.items[blockIdx.x];
     const Seg s = a.segs[it.seg];
-    const int *tab = a.tables + s.table;
+    const Table tab = (Table)(a.tables + s.table);
 
     const int r = wave * 32 + col;  // row of the item
     const int row = min(it.row0 + r, s.rows - 1), j = row / a.group;
@@ -295,13 +331,57 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a) {
     }
     const int full = min(min(s.kv_len, s.lim0 + it.row0 / a.group), it.k1);
     const int sub_mask = (1 << a.sub_shift) - 1;
-    const T *kbase = (const T *)a.c.k + it.hk * a.c.k_head;
-    const T *vbase = (const T *)a.c.v + it.hk * a.c.v_head;
-    const int lrow = tid / LPR, lch = tid % LPR;
-    // A load takes RPL rows: one run of 16 keys (D 128), or two, each by two waves.
-    const int wsub = RPL == 16 ? 0 : __builtin_amdgcn_readfirstlane(wave >> 1);
-    const uint32_t klane = ((lrow & 15) * (uint32_t)a.c.k_token + lch * 8) * 2;
-    const uint32_t vlane = ((lrow & 15) * (uint32_t)a.c.v_token + lch * 8) * 2;
+    const int last_sub = it.k1 > 0 ? (it.k1 - 1) >> 4 : 0;
+    const char *kbase = (const char *)((const T *)a.c.k + it.hk * a.c.k_head);
+    const char *vbase = (const char *)((const T *)a.c.v + it.hk * a.c.v_head);
+
+    // Load i of a wave fills 1 KB, RPL rows from row y0(i) on; a lane's place is fixed,
+    // so it fetches the chunk that belongs there: chunk c of row y of K lies at
+    // c ^ (y mod LPR), which spreads the rows of a column over the banks.
+    auto y0 = [&](int i) { return (i * 4 + wave) * RPL; };
+    const int lrow = lane / LPR, lch = lane % LPR;
+    // (y mod 16, and so the place in the row, is the same for all i)
+    const int yl = (y0(0) + lrow) & 15;
+    const uint32_t klane = yl * (uint32_t)(a.c.k_token * 2) + (lch ^ (yl & (LPR - 1))) * 16;
+    const uint32_t vlane = yl * (uint32_t)(a.c.v_token * 2) + (v_chunk<D>(yl, lch) - yl * LPR) * 16;
+    // Lanes 0 .. 3 (mod 8) work out where the next four runs of 16 keys of K lie,
+    // lanes 4 .. 7 those of V; the block numbers are read a step before that.
+    const int which_run = lane & 3;
+    const bool of_v = lane & 4;
+    const uint32_t block_bytes = (uint32_t)((of_v ? a.c.v_block : a.c.k_block) * 2);
+    const uint32_t run_bytes = (uint32_t)((of_v ? a.c.v_token : a.c.k_token) * 32);
+    int page = 0, run = 0;
+    auto look_up = [&](int v_base, int k_base) {
+        const int sub = min(((of_v ? v_base : k_base) >> 4) + which_run, last_sub);
+        page = tab[sub >> a.sub_shift];
+        run = sub & sub_mask;
+    };
+    uint64_t off = 0;
+    auto place = [&]() {
+        off = (uint64_t)(uint32_t)page * block_bytes + (uint64_t)(uint32_t)run * run_bytes;
+    };
+    auto load = [&](char *to, const char *from, int first) {
+#pragma unroll
+        for (int i = 0; i < NL; i++) {
+            const int n = first + (y0(i) >> 4);
+            const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)off, n);
+            const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(off >> 32), n);
+            load_to_lds(from + (((uint64_t)hi << 32) | lo), to + (i * 4 + wave) * 1024);
+        }
+    };
+    auto load_k = [&](char *to) { load(to, kbase + klane, 0); };
+    auto load_v = [&](char *to) { load(to, vbase + vlane, 4); };
+    // Waits for the loads; slots past the keys hold anything, and weight 0 times it
+    // has to be 0: a wave clears what it loaded of them.
+    auto arrive = [&](char *v, int base) {
+        __builtin_amdgcn_s_waitcnt(kWaitLoads);
+        if (base + kWideKeys > it.k1)
+#pragma unroll
+            for (int i = 0; i < NL; i++)
+                if (base + y0(i) + lrow >= it.k1)
+                    *(u4 *)(v + (i * 4 + wave) * 1024 + lane * 16) = u4{0, 0, 0, 0};
+        __syncthreads();
+    };
 
     f16x o[D / 32];
 #pragma unroll
@@ -309,80 +389,48 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; e++) o[i][e] = 0;
     float m = -INFINITY, l = 0;
-    u4 kr[NL], vr[NL];
-    int page[NL];
-    const int last_sub = it.k1 > 0 ? (it.k1 - 1) >> 4 : 0;
 
-    auto sub_of = [&](int base, int i) {
-        return min((base >> 4) + i * (RPL / 16) + wsub, last_sub);
+    // The chunk's number is in bits 4 and up of an address, so another chunk is an
+    // exclusive or, another row (of the same swizzle) an addition.
+    const uint32_t k_at = (col * LPR + (half ^ (col & (LPR - 1)))) * 16;
+    const int tr = (lane & 15) >> 2, tc = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
+    const uint32_t v_at = v_chunk<D>(half * 4 + tr, tc) * 16 + (lane & 1) * 8;
+    // The left operands for 32 keys: of the scores, and of the products, whose k-slots
+    // of step n are the keys 16 n + 4 half + 0..3 and 8 on, as the scores hold them.
+    V kf[QS], vf[2][D / 32];
+    auto read_k = [&](const char *kl) {
+#pragma unroll
+        for (int i = 0; i < QS; i++) kf[i] = *(const V *)(kl + (k_at ^ (i * 32)));
     };
-    auto look_up = [&](int base) {
-#pragma unroll
-        for (int i = 0; i < NL; i++) page[i] = tab[sub_of(base, i) >> a.sub_shift];
-    };
-    auto load = [&](int base) {
-#pragma unroll
-        for (int i = 0; i < NL; i++) {
-            const int64_t off = (sub_of(base, i) & sub_mask) * 16;
-            const char *kp = (const char *)(kbase + page[i] * a.c.k_block + off * a.c.k_token);
-            const char *vp = (const char *)(vbase + page[i] * a.c.v_block + off * a.c.v_token);
-            kr[i] = *(const u4 *)(kp + klane);
-            vr[i] = *(const u4 *)(vp + vlane);
-        }
-    };
-    // chunk c of K row y: eight rows' chunks of one column lie in different banks
-    auto k_chunk = [](int y, int c) { return y * LPR + (c ^ (y & (LPR - 1))); };
-    auto put = [&](int buf, int base) {
-        if (base + kWideKeys > it.k1)
-#pragma unroll
-            for (int i = 0; i < NL; i++)
-                if (base + i * RPL + lrow >= it.k1) vr[i] = u4{0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < NL; i++) {
-            const int y = i * RPL + lrow;
-            *(u4 *)(lds[buf] + k_chunk(y, lch) * 16) = kr[i];
-            *(u4 *)(lds[buf] + TB + v_chunk<D>(y, lch) * 16) = vr[i];
-        }
-    };
-    if (it.k0 < it.k1) {
-        look_up(it.k0);
-        load(it.k0);
-        look_up(it.k0 + kWideKeys);
-        put(0, it.k0);
-    }
-    __syncthreads();
-    int buf = 0;
-    for (int base = it.k0; base < it.k1; base += kWideKeys, buf ^= 1) {
-        const bool more = base + kWideKeys < it.k1;
-        if (more) {
-            load(base + kWideKeys);
-            look_up(base + 2 * kWideKeys);
-        }
-        const char *kl = lds[buf], *vl = lds[buf] + TB;
-        f16x sc[2];
-#pragma unroll
-        for (int n = 0; n < 2; n++) {
-#pragma unroll
-            for (int e = 0; e < 16; e++) sc[n][e] = 0;
-#pragma unroll
-            for (int i = 0; i < QS; i++) {
-                const V k = *(const V *)(kl + k_chunk(n * 32 + col, i * 2 + half) * 16);
-                sc[n] = mfma32(k, q[i], sc[n]);
-            }
-        }
-        if (base + kWideKeys > full)
-#pragma unroll
-            for (int n = 0; n < 2; n++)
-#pragma unroll
-                for (int e = 0; e < 16; e++)
-                    if (base + n * 32 + (e >> 2) * 8 + half * 4 + (e & 3) >= lim)
-                        sc[n][e] = -INFINITY;
-        float mt = -INFINITY;
+    auto read_v = [&](const char *vl) {
 #pragma unroll
         for (int n = 0; n < 2; n++)
 #pragma unroll
-            for (int e = 0; e < 16; e++) mt = fmaxf(mt, sc[n][e]);
-        mt = max32(mt) * a.scale2;
+            for (int i = 0; i < D / 32; i++) {
+                const char *at = vl + (v_at ^ (i * 64)) + n * 256 * LPR;
+                const s4 lo = read_tr(at), hi = read_tr(at + 128 * LPR);
+                const s8 t = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                vf[n][i] = __builtin_bit_cast(V, t);
+            }
+    };
+    auto scores = [&](f16x &sc) {
+#pragma unroll
+        for (int e = 0; e < 16; e++) sc[e] = 0;
+#pragma unroll
+        for (int i = 0; i < QS; i++) sc = mfma32(kf[i], q[i], sc);
+    };
+    auto hide = [&](f16x &sc, int base) {
+#pragma unroll
+        for (int e = 0; e < 16; e++)
+            if (base + (e >> 2) * 8 + half * 4 + (e & 3) >= lim) sc[e] = -INFINITY;
+    };
+    auto largest = [&](const f16x &sc) {
+        float mt = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 16; e++) mt = fmaxf(mt, sc[e]);
+        return max32(mt) * a.scale2;
+    };
+    auto raise = [&](float mt) {
         if (__any(mt > m + kLazy)) {
             const float mn = mt > m + kLazy ? mt : m, f = mn == m ? 1.0f : exp2_(m - mn);
             m = mn;
@@ -390,31 +438,109 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a) {
 #pragma unroll
             for (int i = 0; i < D / 32; i++) o[i] *= f;
         }
+    };
+    auto weights = [&](V (&p)[2], const f16x &sc) {
         const float mu = m == -INFINITY ? 0.0f : m;
-        V p[4];
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+            const float y = exp2_(sc[e] * a.scale2 - mu);
+            l += y;
+            p[e >> 3][e & 7] = (T)y;
+        }
+        // computed here, beside the scores, and not where they are used
+#pragma unroll
+        for (int n = 0; n < 2; n++) {
+            u4 x = __builtin_bit_cast(u4, p[n]);
+            asm volatile("" : "+v"(x));
+            p[n] = __builtin_bit_cast(V, x);
+        }
+    };
+    auto products = [&](const V (&p)[2]) {
 #pragma unroll
         for (int n = 0; n < 2; n++)
 #pragma unroll
-            for (int e = 0; e < 16; e++) {
-                const float y = exp2_(sc[n][e] * a.scale2 - mu);
-                l += y;
-                p[n * 2 + (e >> 3)][e & 7] = (T)y;
-            }
-        // k-slots of step n: keys 16 n + 4 half + 0..3 and 8 on, as sc holds them
-        const int tr = (lane & 15) >> 2, tc = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
-#pragma unroll
-        for (int n = 0; n < 4; n++) {
-            const int r0 = n * 16 + half * 4 + tr;
-#pragma unroll
-            for (int i = 0; i < D / 32; i++) {
-                const s4 lo = read_tr(vl + v_chunk<D>(r0, i * 4 + tc) * 16 + (lane & 1) * 8);
-                const s4 hi = read_tr(vl + v_chunk<D>(r0 + 8, i * 4 + tc) * 16 + (lane & 1) * 8);
-                const s8 t = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                o[i] = mfma32(__builtin_bit_cast(V, t), p[n], o[i]);
-            }
+            for (int i = 0; i < D / 32; i++) o[i] = mfma32(vf[n][i], p[n], o[i]);
+    };
+
+    // The K of a buffer is 32 keys ahead of its V: on entry of a step sa are the scores
+    // of the keys base .. + 31, m covers them, buffer B holds the V from base on and
+    // the K from base + 32 on.
+    constexpr int HB = TB / 2;  // bytes of 32 rows
+    f16x sa, sb;
+    V p[2];
+    auto step = [&](auto which, int base) {
+        constexpr int B = decltype(which)::value;
+        const char *kl = B ? k1_lds : k0_lds, *vl = B ? v1_lds : v0_lds;
+        const int next = base + kWideKeys;
+        read_k(kl);
+        place();
+        load_v(B ? v0_lds : v1_lds);
+        load_k(B ? k0_lds : k1_lds);
+        look_up(next + kWideKeys, next + kWideKeys + 32);
+        __builtin_amdgcn_sched_barrier(0);
+        scores(sb);
+        weights(p, sa);
+        read_v(vl);
+        mix<QS, 56 / QS, D / 8 / QS>();
+        __builtin_amdgcn_sched_barrier(0);
+        if (next > full) hide(sb, base + 32);
+        products(p);
+        read_k(kl + HB);
+        const float mb = largest(sb);
+        mix<D / 16, 4, QS / (D / 16)>();
+        raise(mb);
+        __builtin_amdgcn_sched_barrier(0);
+        scores(sa);
+        weights(p, sb);
+        read_v(vl + HB);
+        mix<QS, 56 / QS, D / 8 / QS>();
+        __builtin_amdgcn_sched_barrier(0);
+        if (next + 32 > full) hide(sa, next);
+        products(p);
+        const float ma = largest(sa);
+        mix<D / 16, 4, 0>();
+        raise(ma);
+        arrive(B ? v0_lds : v1_lds, next);
+    };
+    if (it.k0 < it.k1) {
+        int base = it.k0;
+        look_up(base, base);
+        place();
+        load_k(k1_lds);
+        load_v(v0_lds);
+        look_up(base, base + 32);
+        place();
+        load_k(k0_lds);
+        look_up(base + kWideKeys, base + kWideKeys + 32);
+        arrive(v0_lds, base);
+        read_k(k1_lds);
+        scores(sa);
+        hide(sa, base);
+        raise(largest(sa));
+        __syncthreads();  // the first step loads K where these were
+        int steps = (it.k1 - base - 1) / kWideKeys;
+        for (; steps >= 2; steps -= 2) {
+            step(Const<0>{}, base);
+            step(Const<1>{}, base + kWideKeys);
+            base += 2 * kWideKeys;
         }
-        if (more) put(buf ^ 1, base + kWideKeys);
-        __syncthreads();
+        if (steps) {
+            step(Const<0>{}, base);
+            base += kWideKeys;
+        }
+        const char *kl = steps ? k1_lds : k0_lds, *vl = steps ? v1_lds : v0_lds;
+        weights(p, sa);
+        read_v(vl);
+        products(p);
+        if (base + 32 < it.k1) {
+            read_k(kl);
+            scores(sa);
+            hide(sa, base + 32);
+            raise(largest(sa));
+            weights(p, sa);
+            read_v(vl + HB);
+            products(p);
+        }
     }
     l = sum32(l);
     // A lane holds d = 32 i + 8 e + 4 half + 0..3 of its row: the halves exchange so
