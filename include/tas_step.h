@@ -18,8 +18,9 @@
  * new tokens are numbered request by request; token j of request i has position
  *     prefix_len[g] + kv_len[i] - n_new[i] + j.
  *
- * A STEP context is the plan of one batch: made once by tas_step_create when
- * the scheduler has formed the batch, used for every layer of the model.
+ * A STEP context is the plan of one batch: made by tas_step_create when the
+ * scheduler has formed the batch, bound to device memory by tas_step_bind, used
+ * for every layer of the model.
  *
  * Conventions as in tas.h: negative return codes (TAS_E*), no exceptions;
  * batch arrays are host memory, read only during the call; d_* and the tensor
@@ -102,16 +103,16 @@ typedef struct tas_attention {
 
 typedef struct tas_step tas_step;
 
-/* Device workspace of a batch's step (plan and partial results); 0 if the
- * batch is invalid. */
-size_t tas_step_bytes(const tas_batch *batch);
-
-/* Validate the batch, plan it and copy the plan to d_ws (256-byte aligned, at
- * least tas_step_bytes). The copy is complete when the call returns. TAS_EINVAL:
- * a field out of range, a block number outside the pool, two new tokens that
- * would be written to one slot; TAS_ENOMEM: ws_bytes too small, or no host
- * memory. d_ws must outlive the step and stay untouched by others. */
-int tas_step_create(const tas_batch *batch, void *d_ws, size_t ws_bytes, tas_step **out);
+/* Validate and plan a batch (host only). TAS_EINVAL: a field out of range, a
+ * block number outside the pool, two new tokens that would be written to one
+ * slot; TAS_ENOMEM: no host memory. */
+int tas_step_create(const tas_batch *batch, tas_step **out);
+/* Bytes of device workspace that the step needs (plan and partial results). */
+size_t tas_step_bytes(const tas_step *step);
+/* Copy the plan to d_ws (256-byte aligned, at least tas_step_bytes) on the
+ * stream, and wait for that. d_ws must outlive the step's last call and stay
+ * untouched by others. TAS_EINVAL, TAS_ENOMEM (ws_bytes too small), TAS_EHIP. */
+int tas_step_bind(tas_step *step, void *d_ws, size_t ws_bytes, void *stream);
 void tas_step_destroy(tas_step *step);
 /* New tokens of the batch (T). */
 int64_t tas_step_tokens(const tas_step *step);
@@ -121,7 +122,8 @@ int64_t tas_step_tokens(const tas_step *step);
  *     (a, b) <- (a cos - b sin, b cos + a sin)      (each rotated pair)
  * queries go to q_out, keys and the unchanged values to the token's slot of the
  * cache. In 32 bits, rounded once. TAS_EINVAL: an argument out of range or
- * unaligned, a batch with kv_len[i] < n_new[i], positions too small. */
+ * unaligned, a batch with kv_len[i] < n_new[i], positions too small;
+ * TAS_ESTATE: not bound (also below). */
 int tas_step_append(tas_step *step, const tas_append *a, void *stream);
 
 /* out = softmax(scale * q K^T) V of every new token and head, over the group's
@@ -131,10 +133,10 @@ int tas_step_append(tas_step *step, const tas_append *a, void *stream);
  * are not used, whatever they hold. */
 int tas_step_attention(tas_step *step, const tas_attention *a, void *stream);
 
-/* The plan that tas_step_create copies to the device, for inspection: writes
- * the blob to host memory `buf` and its size to *bytes (with buf NULL, the size
- * only). Host only. TAS_EINVAL, TAS_ENOMEM (buf_bytes too small). */
-int tas_step_plan(const tas_batch *batch, void *buf, size_t buf_bytes, size_t *bytes);
+/* The plan that tas_step_bind copies to the device, for inspection: writes it to
+ * host memory `buf` and its size to *bytes (with buf NULL, the size only). Host
+ * only. TAS_EINVAL, TAS_ENOMEM (buf_bytes too small). */
+int tas_step_plan(const tas_step *step, void *buf, size_t buf_bytes, size_t *bytes);
 
 #ifdef __cplusplus
 }

@@ -1,9 +1,9 @@
 // tas_step_abi.hip - host side of the C ABI declared in include/tas_step.h.
 //
 // tas_step_create validates a batch on the host (every block number that a
-// kernel will follow is checked here), cuts its attention into items of work
-// and copies the plan into the caller's workspace once. tas_step_append and
-// tas_step_attention only enqueue kernels.
+// kernel will follow is checked here) and cuts its attention into items of work;
+// tas_step_bind copies that plan into the caller's workspace. tas_step_append
+// and tas_step_attention only enqueue kernels.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -16,15 +16,6 @@
 #include "tas_step_internal.h"
 
 using namespace tas_step_impl;
-
-struct tas_step {
-    PlanHead head{};
-    int32_t heads = 0, kv_heads = 0, head_dim = 0, blk_shift = 0;
-    int64_t max_pos = 0;  // largest position of a new token + 1
-    bool appendable = false;
-    char *ws = nullptr;
-    float *part_o = nullptr, *part_lse = nullptr;
-};
 
 namespace {
 
@@ -43,10 +34,31 @@ struct Plan {
     std::vector<Req> reqs;
     std::vector<Seg> segs;
     std::vector<Item> thin, wide;
-    std::vector<int32_t> tables, tok_req, merge;
-    int64_t max_pos = 0;
+    std::vector<Unit> join, merge;
+    std::vector<int32_t> tables, tok_req, tok_seg;
+    int64_t max_pos = 0;  // largest position of a new token + 1
     bool appendable = true;
 };
+
+bool is_thin(const Seg &s) { return s.rows <= kThinRows; }
+int32_t tile_rows(const Seg &s) { return is_thin(s) ? kThinRows : kWideRows; }
+int32_t tiles_of(const Seg &s) { return (s.rows + tile_rows(s) - 1) / tile_rows(s); }
+
+// The longest items first: those that start last are short ones. (Items of one
+// length keep their order, which has the key heads innermost: workgroups go round
+// the chip's 8 dies, so with 8 key heads or a divisor of it the items that share
+// keys share a die's cache.)
+void longest_first(std::vector<Item> &items, int32_t unit) {
+    int32_t most = 0;
+    for (const Item &it : items) most = std::max(most, (it.k1 - it.k0 + unit - 1) / unit);
+    std::vector<size_t> at(most + 2, 0);
+    auto slot = [&](const Item &it) { return most - (it.k1 - it.k0 + unit - 1) / unit; };
+    for (const Item &it : items) at[slot(it) + 1]++;
+    for (int32_t i = 0; i <= most; i++) at[i + 1] += at[i];
+    std::vector<Item> to(items.size());
+    for (const Item &it : items) to[at[slot(it)]++] = it;
+    items.swap(to);
+}
 
 bool valid_shape(const tas_batch *b) {
     if (!b || b->kv_heads < 1 || b->heads < 1 || b->heads > 1024 || b->heads % b->kv_heads)
@@ -89,19 +101,18 @@ bool distinct_slots(const tas_batch *b, const Plan &p) {
 }
 
 // Cuts the keys of the segments into items. A segment's keys are split into
-// nsplit pieces of `piece` keys (the last shorter); every tile of its rows has
-// an item for each piece, an empty one where causality leaves nothing, so that
-// the merge finds nsplit partial results for every row.
+// nsplit pieces (the last ones shorter, or empty); every tile of its rows has an
+// item for each piece, an empty one where causality leaves nothing, so that a join
+// finds nsplit partial results for every row.
 int make_items(const tas_batch *b, Plan &p) {
     const int32_t G = b->heads / b->kv_heads, Hk = b->kv_heads;
     int64_t thin_keys = 0, wide_tiles = 0, wide_keys = 0;
     for (const Seg &s : p.segs) {
-        if (s.rows <= kThinRows) {
+        if (is_thin(s)) {
             thin_keys += (int64_t)s.kv_len * Hk;
         } else {
-            const int64_t tiles = ceil_div(s.rows, kWideRows) * Hk;
-            wide_tiles += tiles;
-            wide_keys += tiles * s.kv_len;
+            wide_tiles += (int64_t)tiles_of(s) * Hk;
+            wide_keys += (int64_t)tiles_of(s) * Hk * s.kv_len;
         }
     }
     const int64_t step = 4 * kThinKeys;
@@ -112,66 +123,77 @@ int make_items(const tas_batch *b, Plan &p) {
         wide_piece = std::max<int64_t>(ceil_div(ceil_div(wide_keys, kSlots), kWideKeys) * kWideKeys,
                                        4 * kWideKeys);
     for (Seg &s : p.segs) {
-        const int64_t piece = s.rows <= kThinRows ? thin_piece : wide_piece;
-        s.nsplit = (int32_t)std::max<int64_t>(1, ceil_div(s.kv_len, piece));
+        s.nsplit = (int32_t)std::max<int64_t>(
+            1, ceil_div(s.kv_len, is_thin(s) ? thin_piece : wide_piece));
+        s.part = -1;
     }
-    // a token's result goes straight to the output where it has one part only
+    // a result goes straight to the output where it has one part only
     int64_t part_rows = 0;
-    for (const Req &r : p.reqs) {
-        if (!r.n_new) continue;
-        const bool split = r.pre_seg >= 0 || (r.own_seg >= 0 && p.segs[r.own_seg].nsplit > 1);
-        if (r.own_seg >= 0) {
-            Seg &s = p.segs[r.own_seg];
-            s.part = -1;
-            if (split) {
-                s.part = (int32_t)part_rows;
-                part_rows += (int64_t)Hk * s.nsplit * s.rows;
-            }
-        }
-        if (part_rows > kMaxPartRows) return TAS_EINVAL;
-        if (split)
-            for (int32_t j = 0; j < r.n_new; j++) p.merge.push_back(r.t0 + j);
-    }
-    int32_t seen = -1;
+    std::vector<int32_t> unit0(p.segs.size(), -1);  // join of a thin segment's key head 0
+    std::vector<int32_t> is_prefix(p.segs.size(), 0);
     for (const Req &r : p.reqs)
-        if (r.pre_seg >= 0 && r.pre_seg != seen) {
-            seen = r.pre_seg;
-            Seg &s = p.segs[seen];
-            s.part = (int32_t)part_rows;
-            part_rows += (int64_t)Hk * s.nsplit * s.rows;
-            if (part_rows > kMaxPartRows) return TAS_EINVAL;
-        }
+        if (r.pre_seg >= 0) is_prefix[r.pre_seg] = 1;
+    auto partial = [&](int32_t seg, bool joins) {
+        Seg &s = p.segs[seg];
+        s.part = (int32_t)part_rows;
+        part_rows += (int64_t)Hk * s.nsplit * s.rows;
+        if (part_rows > kMaxPartRows) return false;
+        if (!joins) return true;
+        if (is_thin(s)) unit0[seg] = (int32_t)p.join.size();
+        for (int32_t hk = 0; hk < Hk; hk++)
+            for (int32_t row0 = 0; row0 < s.rows; row0 += kJoinRows)
+                (is_thin(s) ? p.join : p.merge)
+                    .push_back({seg, hk, row0, std::min(kJoinRows, s.rows - row0), 0,
+                                is_prefix[seg]});
+        return true;
+    };
+    std::vector<int32_t> shared(p.segs.size(), -1);  // the prefix that an own segment joins
+    for (const Req &r : p.reqs) {
+        if (r.pre_seg >= 0 && p.segs[r.pre_seg].part < 0 && !partial(r.pre_seg, true))
+            return TAS_EINVAL;
+        if (r.own_seg < 0) continue;
+        shared[r.own_seg] = r.pre_seg;
+        if ((r.pre_seg >= 0 || p.segs[r.own_seg].nsplit > 1) &&
+            !partial(r.own_seg, r.pre_seg < 0))
+            return TAS_EINVAL;
+    }
+    int64_t n_items = 0;
+    for (const Seg &s : p.segs) n_items += (int64_t)Hk * tiles_of(s) * s.nsplit;
+    if (n_items > INT32_MAX / 2) return TAS_EINVAL;
     for (size_t i = 0; i < p.segs.size(); i++) {
         const Seg &s = p.segs[i];
-        const bool thin = s.rows <= kThinRows;
-        const int64_t tile = thin ? kThinRows : kWideRows;
-        const int64_t unit = thin ? step : kWideKeys;
+        const int32_t tile = tile_rows(s);
+        const int64_t unit = is_thin(s) ? step : kWideKeys;
         const int64_t piece = ceil_div(ceil_div(s.kv_len, s.nsplit), unit) * unit;
-        std::vector<Item> &to = thin ? p.thin : p.wide;
-        for (int32_t hk = 0; hk < Hk; hk++)
-            for (int64_t row0 = 0; row0 < s.rows; row0 += tile) {
-                const int64_t last = std::min<int64_t>(row0 + tile, s.rows) - 1;
-                const int64_t lim =
-                    std::max<int64_t>(0, std::min<int64_t>(s.kv_len, s.lim0 + last / G));
-                for (int32_t n = 0; n < s.nsplit; n++) {
-                    Item it;
+        std::vector<Item> &to = is_thin(s) ? p.thin : p.wide;
+        const int32_t unit_of = unit0[shared[i] >= 0 ? shared[i] : (int32_t)i];
+        for (int32_t row0 = 0; row0 < s.rows; row0 += tile) {
+            const int32_t rows = std::min(tile, s.rows - row0);
+            const int64_t lim = std::max<int64_t>(
+                0, std::min<int64_t>(s.kv_len, (int64_t)s.lim0 + (row0 + rows - 1) / G));
+            for (int32_t n = 0; n < s.nsplit; n++)
+                for (int32_t hk = 0; hk < Hk; hk++) {
+                    Item it{};
                     it.seg = (int32_t)i;
                     it.hk = hk;
-                    it.row0 = (int32_t)row0;
+                    it.row0 = row0;
                     it.k0 = (int32_t)std::min<int64_t>(n * piece, lim);
                     it.k1 = (int32_t)std::min<int64_t>((n + 1) * piece, lim);
-                    it.part = s.part < 0 ? -1
-                                         : (int32_t)(s.part +
-                                                     ((int64_t)hk * s.nsplit + n) * s.rows + row0);
+                    it.part = it.unit = -1;
+                    if (s.part >= 0) {
+                        it.part =
+                            (int32_t)(s.part + ((int64_t)hk * s.nsplit + n) * s.rows + row0);
+                        if (unit_of >= 0) {
+                            it.unit = unit_of + hk;
+                            p.join[it.unit].items++;
+                        }
+                    }
                     to.push_back(it);
-                    if (to.size() > (size_t)INT32_MAX / 2) return TAS_EINVAL;
                 }
-            }
+        }
     }
-    // the longest first: the items that start last are short ones
-    auto longer = [](const Item &x, const Item &y) { return x.k1 - x.k0 > y.k1 - y.k0; };
-    std::stable_sort(p.thin.begin(), p.thin.end(), longer);
-    std::stable_sort(p.wide.begin(), p.wide.end(), longer);
+    longest_first(p.thin, (int32_t)step);
+    longest_first(p.wide, kWideKeys);
     p.head.part_rows = part_rows;
     return TAS_OK;
 }
@@ -241,6 +263,7 @@ int make_plan(const tas_batch *b, Plan &p) {
             }
         }
         p.tok_req.insert(p.tok_req.end(), (size_t)n, i);
+        p.tok_seg.insert(p.tok_seg.end(), (size_t)n, r.own_seg);
         p.reqs.push_back(r);
         t += n;
     }
@@ -256,15 +279,17 @@ int make_plan(const tas_batch *b, Plan &p) {
     h.n_seg = (int32_t)p.segs.size();
     h.n_thin = (int32_t)p.thin.size();
     h.n_wide = (int32_t)p.wide.size();
+    h.n_join = (int32_t)p.join.size();
     h.n_merge = (int32_t)p.merge.size();
     h.n_table = (int32_t)p.tables.size();
     place(h.req, p.reqs.size() * sizeof(Req));
     place(h.seg, p.segs.size() * sizeof(Seg));
-    place(h.thin, p.thin.size() * sizeof(Item));
-    place(h.wide, p.wide.size() * sizeof(Item));
+    place(h.items, (p.wide.size() + p.thin.size()) * sizeof(Item));
+    place(h.units, (p.join.size() + p.merge.size()) * sizeof(Unit));
     place(h.tables, p.tables.size() * 4);
     place(h.tok_req, p.tok_req.size() * 4);
-    place(h.merge, p.merge.size() * 4);
+    place(h.tok_seg, p.tok_seg.size() * 4);
+    place(h.done, p.join.size() * 4);
     h.bytes = (int64_t)at;
     return TAS_OK;
 }
@@ -277,17 +302,15 @@ void write_blob(const Plan &p, char *to) {
     };
     put(h.req, p.reqs.data(), p.reqs.size() * sizeof(Req));
     put(h.seg, p.segs.data(), p.segs.size() * sizeof(Seg));
-    put(h.thin, p.thin.data(), p.thin.size() * sizeof(Item));
-    put(h.wide, p.wide.data(), p.wide.size() * sizeof(Item));
+    put(h.items, p.wide.data(), p.wide.size() * sizeof(Item));
+    put(h.items + p.wide.size() * sizeof(Item), p.thin.data(), p.thin.size() * sizeof(Item));
+    put(h.units, p.join.data(), p.join.size() * sizeof(Unit));
+    put(h.units + p.join.size() * sizeof(Unit), p.merge.data(), p.merge.size() * sizeof(Unit));
     put(h.tables, p.tables.data(), p.tables.size() * 4);
     put(h.tok_req, p.tok_req.data(), p.tok_req.size() * 4);
-    put(h.merge, p.merge.data(), p.merge.size() * 4);
+    put(h.tok_seg, p.tok_seg.data(), p.tok_seg.size() * 4);
 }
 
-size_t workspace_bytes(const tas_batch *b, const Plan &p) {
-    return (size_t)p.head.bytes + align256((size_t)p.head.part_rows * b->head_dim * 4) +
-           align256((size_t)p.head.part_rows * 4);
-}
 
 bool aligned16(const void *p) { return p && ((uintptr_t)p & 15) == 0; }
 
@@ -307,42 +330,32 @@ bool valid_rows(const void *p, int64_t stride, int64_t row) {
 
 }  // namespace
 
+struct tas_step {
+    std::vector<char> blob;  // the plan
+    PlanHead head{};
+    int32_t heads = 0, kv_heads = 0, head_dim = 0, blk_shift = 0;
+    int64_t max_pos = 0;
+    bool appendable = false;
+    char *ws = nullptr;  // null: not bound
+    size_t part_o() const { return blob.size(); }
+    size_t part_lse() const {
+        return part_o() + align256((size_t)head.part_rows * head_dim * 4);
+    }
+    size_t bytes() const { return part_lse() + align256((size_t)head.part_rows * 4); }
+};
+
 extern "C" {
 
-size_t tas_step_bytes(const tas_batch *b) try {
-    Plan p;
-    if (make_plan(b, p) != TAS_OK) return 0;
-    return workspace_bytes(b, p);
-} catch (...) {
-    return 0;
-}
-
-int tas_step_plan(const tas_batch *b, void *buf, size_t buf_bytes, size_t *bytes) try {
-    if (!bytes) return TAS_EINVAL;
-    Plan p;
-    const int rc = make_plan(b, p);
-    if (rc != TAS_OK) return rc;
-    *bytes = (size_t)p.head.bytes;
-    if (!buf) return TAS_OK;
-    if (buf_bytes < *bytes) return TAS_ENOMEM;
-    memset(buf, 0, *bytes);
-    write_blob(p, (char *)buf);
-    return TAS_OK;
-} catch (...) {
-    return TAS_ENOMEM;
-}
-
-int tas_step_create(const tas_batch *b, void *d_ws, size_t ws_bytes, tas_step **out) try {
+int tas_step_create(const tas_batch *b, tas_step **out) try {
     if (!out) return TAS_EINVAL;
     *out = nullptr;
     Plan p;
     const int rc = make_plan(b, p);
     if (rc != TAS_OK) return rc;
-    if (!d_ws || ((uintptr_t)d_ws & 255)) return TAS_EINVAL;
-    if (ws_bytes < workspace_bytes(b, p)) return TAS_ENOMEM;
     std::vector<char> blob((size_t)p.head.bytes);
     write_blob(p, blob.data());
     tas_step *s = new tas_step;
+    s->blob.swap(blob);
     s->head = p.head;
     s->heads = b->heads;
     s->kv_heads = b->kv_heads;
@@ -350,26 +363,42 @@ int tas_step_create(const tas_batch *b, void *d_ws, size_t ws_bytes, tas_step **
     while ((1 << s->blk_shift) < b->block_tokens) s->blk_shift++;
     s->max_pos = p.max_pos;
     s->appendable = p.appendable;
-    s->ws = (char *)d_ws;
-    s->part_o = (float *)(s->ws + p.head.bytes);
-    s->part_lse = (float *)(s->ws + p.head.bytes +
-                            align256((size_t)p.head.part_rows * b->head_dim * 4));
-    if (hipMemcpy(d_ws, blob.data(), blob.size(), hipMemcpyHostToDevice) != hipSuccess) {
-        delete s;
-        return TAS_EHIP;
-    }
     *out = s;
     return TAS_OK;
 } catch (...) {
     return TAS_ENOMEM;
 }
 
+size_t tas_step_bytes(const tas_step *s) { return s ? s->bytes() : 0; }
+
+int tas_step_bind(tas_step *s, void *d_ws, size_t ws_bytes, void *stream) {
+    if (!s || !d_ws || ((uintptr_t)d_ws & 255)) return TAS_EINVAL;
+    if (ws_bytes < s->bytes()) return TAS_ENOMEM;
+    const hipStream_t st = (hipStream_t)stream;
+    if (hipMemcpyAsync(d_ws, s->blob.data(), s->blob.size(), hipMemcpyHostToDevice, st) !=
+            hipSuccess ||
+        hipStreamSynchronize(st) != hipSuccess)
+        return TAS_EHIP;
+    s->ws = (char *)d_ws;
+    return TAS_OK;
+}
+
 void tas_step_destroy(tas_step *s) { delete s; }
 
 int64_t tas_step_tokens(const tas_step *s) { return s ? s->head.n_tok : -1; }
 
+int tas_step_plan(const tas_step *s, void *buf, size_t buf_bytes, size_t *bytes) {
+    if (!s || !bytes) return TAS_EINVAL;
+    *bytes = s->blob.size();
+    if (!buf) return TAS_OK;
+    if (buf_bytes < s->blob.size()) return TAS_ENOMEM;
+    memcpy(buf, s->blob.data(), s->blob.size());
+    return TAS_OK;
+}
+
 int tas_step_append(tas_step *s, const tas_append *a, void *stream) {
     if (!s || !a || !s->appendable) return TAS_EINVAL;
+    if (!s->ws) return TAS_ESTATE;
     const int64_t D = s->head_dim;
     if (a->dtype != TAS_F16 && a->dtype != TAS_BF16) return TAS_EINVAL;
     if (a->rot_dim < 0 || a->rot_dim > D || a->rot_dim % 16) return TAS_EINVAL;
@@ -411,6 +440,7 @@ int tas_step_append(tas_step *s, const tas_append *a, void *stream) {
 
 int tas_step_attention(tas_step *s, const tas_attention *a, void *stream) {
     if (!s || !a) return TAS_EINVAL;
+    if (!s->ws) return TAS_ESTATE;
     if (a->dtype != TAS_F16 && a->dtype != TAS_BF16) return TAS_EINVAL;
     if (!(a->scale > 0) || std::isinf(a->scale)) return TAS_EINVAL;
     if (!valid_cache(a->cache)) return TAS_EINVAL;
@@ -421,14 +451,16 @@ int tas_step_attention(tas_step *s, const tas_attention *a, void *stream) {
     AttnArgs k{};
     k.segs = (const Seg *)(s->ws + s->head.seg);
     k.tables = (const int32_t *)(s->ws + s->head.tables);
-    k.reqs = (const Req *)(s->ws + s->head.req);
-    k.tok_req = (const int32_t *)(s->ws + s->head.tok_req);
-    k.merge = (const int32_t *)(s->ws + s->head.merge);
+    k.tok_seg = (const int32_t *)(s->ws + s->head.tok_seg);
+    k.items = (const Item *)(s->ws + s->head.items);
+    k.units = (const Unit *)(s->ws + s->head.units);
+    k.merge = k.units + s->head.n_join;
+    k.done = (uint32_t *)(s->ws + s->head.done);
     k.q = a->q;
     k.out = a->out;
     k.lse = a->lse;
-    k.part_o = s->part_o;
-    k.part_lse = s->part_lse;
+    k.part_o = (float *)(s->ws + s->part_o());
+    k.part_lse = (float *)(s->ws + s->part_lse());
     k.q_stride = a->q_stride;
     k.out_stride = a->out_stride;
     k.c = a->cache;
@@ -436,21 +468,11 @@ int tas_step_attention(tas_step *s, const tas_attention *a, void *stream) {
     k.heads = s->heads;
     k.sub_shift = s->blk_shift - 4;
     k.scale2 = a->scale * 1.4426950408889634f;
-    const hipStream_t st = (hipStream_t)stream;
-    if (s->head.n_wide) {
-        k.items = (const Item *)(s->ws + s->head.wide);
-        if (launch_wide(k, s->head.n_wide, a->dtype, s->head_dim, st) != hipSuccess)
-            return TAS_EHIP;
-    }
-    if (s->head.n_thin) {
-        k.items = (const Item *)(s->ws + s->head.thin);
-        if (launch_thin(k, s->head.n_thin, a->dtype, s->head_dim, st) != hipSuccess)
-            return TAS_EHIP;
-    }
-    if (s->head.n_merge &&
-        launch_merge(k, s->head.n_merge, s->kv_heads, a->dtype, s->head_dim, st) != hipSuccess)
-        return TAS_EHIP;
-    return TAS_OK;
+    k.n_wide = s->head.n_wide;
+    return launch_attention(k, s->head.n_wide + s->head.n_thin, s->head.n_merge, a->dtype,
+                            s->head_dim, (hipStream_t)stream) == hipSuccess
+               ? TAS_OK
+               : TAS_EHIP;
 }
 
 }  // extern "C"

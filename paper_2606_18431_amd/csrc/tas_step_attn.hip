@@ -26,7 +26,7 @@ template <typename T>
 using vec8 = T __attribute__((ext_vector_type(8)));
 template <typename T>
 using vec2 = T __attribute__((ext_vector_type(2)));
-typedef float f2 __attribute__((ext_vector_type(2)));
+typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
 
 // Block numbers: constant while a kernel runs, read by scalar loads.
 typedef const __attribute__((address_space(4))) int *Table;
@@ -84,28 +84,69 @@ __device__ s4 read_tr(const char *p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)p);
 }
 
-// Elements d of result rows, in the output or as a partial result.
+// Partial results. Those that a workgroup of the same launch joins cross dies, whose
+// caches do not see each other's writes: they are written through to where the whole
+// device reads them, and read from there (DEVICE). That costs their few bytes a trip to
+// memory; a release fence would cost every workgroup a write-back of its die's cache
+// (decode of 64 requests, 32/8 heads of 128: 181 us with fences, 79 us so). Those that
+// the merge kernel joins are ordinary ones.
+__device__ void put_part(float *to, float x, bool device) {
+    if (device)
+        __hip_atomic_store(to, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    else
+        *to = x;
+}
+__device__ void put_part(float *to, f4 x, bool device) {
+    if (device) {
+        const u64x2 u = __builtin_bit_cast(u64x2, x);
+        __hip_atomic_store((uint64_t *)to, u[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store((uint64_t *)to + 1, u[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    } else {
+        *(f4 *)to = x;
+    }
+}
+template <bool DEVICE>
+__device__ float get_part(const float *from) {
+    if (!DEVICE) return *from;
+    return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <bool DEVICE>
+__device__ f4 get_part4(const float *from) {
+    if (!DEVICE) return *(const f4 *)from;
+    u64x2 u;
+    u[0] = __hip_atomic_load((const uint64_t *)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    u[1] = __hip_atomic_load((const uint64_t *)from + 1, __ATOMIC_RELAXED,
+                             __HIP_MEMORY_SCOPE_AGENT);
+    return __builtin_bit_cast(f4, u);
+}
+
+// Where elements d .. d + 3 of a row lie among the partial results of a key head's piece.
+// Stores should fill whole lines: a wide item's lanes hold rows, so the fours of all its
+// rows are adjacent; a thin segment's few rows are whole.
+template <int D>
+__device__ int64_t part_at(const Seg &s, int64_t first_row, int row, int d) {
+    if (s.rows <= kThinRows) return (first_row + row) * D + d;
+    const int tile = row & ~(kWideRows - 1);
+    return (first_row + tile) * D + d * min(kWideRows, s.rows - tile) + (row - tile) * 4;
+}
+__device__ float lse2(float l, float m) {
+    return l > 0 ? m + log2f(l) : (l == l ? -INFINITY : l);  // NaN stays
+}
+__device__ float reciprocal(float l) { return l > 0 ? 1.0f / l : (l == l ? 0.0f : l); }
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Elements d .. d + 7 of row r of an item, in the output.
 template <typename T, int D>
 __device__ void store_row(const AttnArgs &a, const Seg &s, const Item &it, int r, int d,
                           const float *o, float l, float m) {
-    const float f = l > 0 ? 1.0f / l : (l == l ? 0.0f : l);  // NaN stays
-    if (it.part >= 0) {
-        float *to = a.part_o + (int64_t)(it.part + r) * D + d;
-        f4 x = {o[0] * f, o[1] * f, o[2] * f, o[3] * f};
-        f4 y = {o[4] * f, o[5] * f, o[6] * f, o[7] * f};
-        *(f4 *)to = x, *(f4 *)(to + 4) = y;
-        if (d == 0) a.part_lse[it.part + r] = l > 0 ? m + log2f(l) : (l == l ? -INFINITY : l);
-        return;
-    }
+    const float f = reciprocal(l);
     const int row = it.row0 + r, j = row / a.group, head = it.hk * a.group + row - j * a.group;
     vec8<T> x;
 #pragma unroll
     for (int e = 0; e < 8; e++) x[e] = (T)(o[e] * f);
     const int64_t tok = s.t0 + j;
     *(vec8<T> *)((T *)a.out + tok * a.out_stride + (int64_t)head * D + d) = x;
-    if (d == 0 && a.lse)
-        a.lse[tok * a.heads + head] =
-            l > 0 ? (m + log2f(l)) * 0.6931471805599453f : (l == l ? -INFINITY : l);
+    if (d == 0 && a.lse) a.lse[tok * a.heads + head] = lse2(l, m) * kLn2;
 }
 
 // Up to 16 rows against a run of keys: each of the four waves takes every fourth
@@ -113,17 +154,15 @@ __device__ void store_row(const AttnArgs &a, const Seg &s, const Item &it, int r
 // the waves' results are joined at the end. Memory bound: 16 rows make use of at
 // most 16 products a byte and a half.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void thin_kernel(AttnArgs a) {
+__device__ __forceinline__ void thin_item(const AttnArgs &a, const Item &it, char *lds01,
+                                          char *lds23, float (*stat)[kThinRows][2]) {
     using V = vec8<T>;
     constexpr int QS = D / 32;          // steps of 32 over d
     constexpr int VL = D / 16;          // 16-byte loads of a lane for 32 rows of V
     constexpr int LPR = D / 8;          // lanes of a V row
     constexpr int VB = kThinKeys * D * 2;  // bytes of a wave's V
-    __shared__ __attribute__((aligned(16))) char lds[4 * VB];
-    __shared__ float stat[4][kThinRows][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int col = lane & 15, g = lane >> 4;
-    const Item it = a.items[blockIdx.x];
     const Seg s = a.segs[it.seg];
     const Table tab = (Table)(a.tables + s.table);
 
@@ -143,7 +182,9 @@ __global__ __launch_bounds__(256) void thin_kernel(AttnArgs a) {
     const uint32_t klane = (col * (uint32_t)a.c.k_token + g * 8) * 2;
     const int vrow = lane / LPR, vch = lane % LPR;
     const uint32_t vlane = (vrow * (uint32_t)a.c.v_token + vch * 8) * 2;
-    char *vl = lds + wave * VB;
+    // a wave's 32 rows of V, and in the end its sums (16 rows of floats, as many bytes)
+    auto mine = [&](int w) { return (w < 2 ? lds01 : lds23) + (w & 1) * VB; };
+    char *vl = mine(wave);
     // (another chunk is an exclusive or, a row 16 on an addition)
     const uint32_t v_at = v_chunk<D>(4 * g + (col >> 2), (col >> 1) & 1) * 16 + (col & 1) * 8;
 
@@ -245,13 +286,33 @@ __global__ __launch_bounds__(256) void thin_kernel(AttnArgs a) {
     l = sum32(sum16(l));
     __syncthreads();
     if (g == 0) stat[wave][col][0] = m, stat[wave][col][1] = l;
-    float *ex = (float *)lds;  // [wave][row][D], 4-float groups swizzled by the row
+    // [row][D], groups of 4 floats swizzled by the row
 #pragma unroll
     for (int i = 0; i < D / 16; i++)
-        *(f4 *)(ex + (wave * kThinRows + col) * D + (((i * 4 + g) ^ col) * 4)) = o[i];
+        *(f4 *)((float *)vl + col * D + (((i * 4 + g) ^ col) * 4)) = o[i];
     __syncthreads();
-    const int r = tid / (D / 8), d = tid % (D / 8) * 8;  // D 64: the upper half has no row
-    if (r >= kThinRows || r >= s.rows) return;
+    if (it.part >= 0) {
+        for (int i = tid; i < s.rows * (D / 4); i += 256) {
+            const int r = i / (D / 4), d4 = i % (D / 4);
+            float mm = -INFINITY, ll = 0;
+            f4 y = {0, 0, 0, 0};
+#pragma unroll
+            for (int w = 0; w < 4; w++) mm = fmaxf(mm, stat[w][r][0]);
+            const float mu = mm == -INFINITY ? 0.0f : mm;
+#pragma unroll
+            for (int w = 0; w < 4; w++) {
+                const float f = exp2_(stat[w][r][0] - mu);
+                ll += stat[w][r][1] * f;
+                y += *(const f4 *)((const float *)mine(w) + r * D + (d4 ^ r) * 4) * f;
+            }
+            put_part(a.part_o + part_at<D>(s, it.part, r, d4 * 4), y * reciprocal(ll),
+                     it.unit >= 0);
+            if (d4 == 0) put_part(a.part_lse + it.part + r, lse2(ll, mm), it.unit >= 0);
+        }
+        return;
+    }
+    const int r = tid / (D / 8), d = tid % (D / 8) * 8;
+    if (r >= s.rows) return;  // (at most 16 rows)
     float mm = -INFINITY, ll = 0, y[8] = {};
 #pragma unroll
     for (int w = 0; w < 4; w++) mm = fmaxf(mm, stat[w][r][0]);
@@ -260,7 +321,7 @@ __global__ __launch_bounds__(256) void thin_kernel(AttnArgs a) {
     for (int w = 0; w < 4; w++) {
         const float f = exp2_(stat[w][r][0] - mu);
         ll += stat[w][r][1] * f;
-        const float *from = ex + (w * kThinRows + r) * D;
+        const float *from = (const float *)mine(w) + r * D;
         const f4 lo = *(const f4 *)(from + ((d / 4) ^ r) * 4);
         const f4 hi = *(const f4 *)(from + ((d / 4 + 1) ^ r) * 4);
 #pragma unroll
@@ -294,7 +355,7 @@ __device__ __forceinline__ void mix() {
         mix<N - 1, VECTOR, READS>();
     }
 }
-constexpr int kWaitLoads = 0x0F70;  // s_waitcnt: no load outstanding
+constexpr int kWaitLoads = 0x0F70;  // s_waitcnt: no load or store outstanding
 
 // 128 rows against a run of keys, 64 keys a step: 32 rows to a wave, K and V of a
 // step in LDS for all four waves, loaded there directly and double buffered. A step
@@ -303,19 +364,17 @@ constexpr int kWaitLoads = 0x0F70;  // s_waitcnt: no load outstanding
 // the maximum of the next. One barrier ends a step; the loads it waits for had the
 // whole step to arrive.
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a) {
+__device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, char *k0_lds,
+                                          char *k1_lds, char *v0_lds, char *v1_lds) {
     using V = vec8<T>;
     constexpr int QS = D / 16;             // steps of 16 over d
     constexpr int LPR = D / 8;             // chunks of 16 bytes of a row
     constexpr int TB = kWideKeys * D * 2;  // bytes of a tile
     constexpr int NL = TB / 4096;          // loads of a wave for a tile
     constexpr int RPL = 64 / LPR;          // rows of one wave's load
-    // four objects, so that the compiler sees which loads a read has to wait for
-    __shared__ __attribute__((aligned(16))) char k0_lds[TB], k1_lds[TB], v0_lds[TB], v1_lds[TB];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
-    const Item it = a.items[blockIdx.x];
     const Seg s = a.segs[it.seg];
     const Table tab = (Table)(a.tables + s.table);
 
@@ -543,8 +602,23 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a) {
         }
     }
     l = sum32(l);
-    // A lane holds d = 32 i + 8 e + 4 half + 0..3 of its row: the halves exchange so
-    // that each has 8 adjacent ones.
+    // A lane holds d = 32 i + 8 e + 4 half + 0..3 of its row.
+    if (it.part >= 0) {
+        if (it.row0 + r >= s.rows) return;
+        const float f = reciprocal(l);
+        const int64_t first = it.part - it.row0;
+#pragma unroll
+        for (int i = 0; i < D / 32; i++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const f4 x = {o[i][e * 4], o[i][e * 4 + 1], o[i][e * 4 + 2], o[i][e * 4 + 3]};
+                put_part(a.part_o + part_at<D>(s, first, it.row0 + r, i * 32 + e * 8 + half * 4),
+                         x * f, false);
+            }
+        if (half == 0) put_part(a.part_lse + it.part + r, lse2(l, m), false);
+        return;
+    }
+    // The halves exchange so that each has 8 adjacent ones.
 #pragma unroll
     for (int i = 0; i < D / 32; i++)
 #pragma unroll
@@ -564,87 +638,137 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a) {
         }
 }
 
-// Joins the partial results of a token's head: weights 2^(lse_n - max).
-template <typename T, int D>
-__global__ __launch_bounds__(256) void merge_kernel(AttnArgs a) {
-    constexpr int E = D / 64;
-    const int lane = threadIdx.x & 63;
-    const int head = blockIdx.y * 4 + (threadIdx.x >> 6);
-    if (head >= a.heads) return;
-    const int tok = a.merge[blockIdx.x];
-    const Req r = a.reqs[a.tok_req[tok]];
-    const int hk = head / a.group, g = head - hk * a.group;
-    float m = -INFINITY;
-    bool bad = false;  // a NaN among the parts stays
-#pragma unroll
-    for (int p = 0; p < 2; p++) {
-        const int seg = p ? r.pre_seg : r.own_seg;
-        if (seg < 0) continue;
-        const Seg s = a.segs[seg];
-        int64_t at = s.part + (int64_t)hk * s.nsplit * s.rows + (tok - s.t0) * a.group + g;
-        for (int n = 0; n < s.nsplit; n++, at += s.rows) {
-            const float x = a.part_lse[at];
-            bad |= x != x;
-            m = fmaxf(m, x);
-        }
+// Joins the partial results of a unit's rows, weights 2^(lse_n - max), in a fixed order
+// whoever is last. D / 8 threads to a row, adjacent threads to adjacent rows. What it
+// takes is the latency of the loads, so those of eight parts are under way at once.
+template <typename T, int D, bool DEVICE>
+__device__ __forceinline__ void join(const AttnArgs &a, const Unit &u) {
+    constexpr int P = 8;
+    const int d = threadIdx.x / kJoinRows * 8, r = threadIdx.x % kJoinRows;
+    if (r >= u.rows || d >= D) return;
+    const Seg us = a.segs[u.seg];
+    const int row = u.row0 + r, j = row / a.group, g = row - j * a.group;
+    const int tok = us.t0 + j, head = u.hk * a.group + g;
+    const int n0 = us.nsplit;
+    int all = n0;
+    Seg os = us;
+    const int own = u.prefix ? a.tok_seg[tok] : -1;
+    if (own >= 0) {
+        os = a.segs[own];
+        all += os.nsplit;
     }
-    const float mu = m == -INFINITY ? 0.0f : m;
-    float sum = 0, y[E] = {};
+    const int64_t first0 = us.part + (int64_t)u.hk * us.nsplit * us.rows;
+    const int64_t first1 = os.part + (int64_t)u.hk * os.nsplit * os.rows;
+    const int own_row = (tok - os.t0) * a.group + g;
+    float m = -INFINITY, sum = 0, y[8] = {};
+    bool bad = false;  // a NaN among the parts stays
+    for (int n = 0; n < all; n += P) {
+        float lse[P];
+        f4 o[P][2];
 #pragma unroll
-    for (int p = 0; p < 2; p++) {
-        const int seg = p ? r.pre_seg : r.own_seg;
-        if (seg < 0) continue;
-        const Seg s = a.segs[seg];
-        int64_t at = s.part + (int64_t)hk * s.nsplit * s.rows + (tok - s.t0) * a.group + g;
-        for (int n = 0; n < s.nsplit; n++, at += s.rows) {
-            const float w = exp2_(a.part_lse[at] - mu);
+        for (int i = 0; i < P; i++) {
+            const int k = min(n + i, all - 1);
+            const bool mine = k < n0;
+            const Seg &s = mine ? us : os;
+            const int64_t first =
+                mine ? first0 + (int64_t)k * us.rows : first1 + (int64_t)(k - n0) * os.rows;
+            const int at = mine ? row : own_row;
+            lse[i] = get_part<DEVICE>(a.part_lse + first + at);
+#pragma unroll
+            for (int e = 0; e < 2; e++)
+                o[i][e] = get_part4<DEVICE>(a.part_o + part_at<D>(s, first, at, d + e * 4));
+        }
+        float mn = m;
+#pragma unroll
+        for (int i = 0; i < P; i++) {
+            bad |= lse[i] != lse[i];
+            mn = fmaxf(mn, lse[i]);
+        }
+        const float mu = mn == -INFINITY ? 0.0f : mn, f = exp2_(m - mu);
+        m = mn;
+        sum *= f;
+#pragma unroll
+        for (int e = 0; e < 8; e++) y[e] *= f;
+#pragma unroll
+        for (int i = 0; i < P; i++) {
+            const float w = n + i < all ? exp2_(lse[i] - mu) : 0.0f;
             sum += w;
 #pragma unroll
-            for (int e = 0; e < E; e++) y[e] += w * a.part_o[at * D + lane * E + e];
+            for (int e = 0; e < 8; e++) y[e] += o[i][e >> 2][e & 3] * w;
         }
     }
     const float f = sum > 0 ? 1.0f / sum : 0.0f;
-    T *to = (T *)a.out + (int64_t)tok * a.out_stride + (int64_t)head * D + lane * E;
+    vec8<T> x;
 #pragma unroll
-    for (int e = 0; e < E; e++) to[e] = (T)(bad ? NAN : y[e] * f);
-    if (lane == 0 && a.lse)
+    for (int e = 0; e < 8; e++) x[e] = (T)(bad ? NAN : y[e] * f);
+    *(vec8<T> *)((T *)a.out + (int64_t)tok * a.out_stride + (int64_t)head * D + d) = x;
+    if (d == 0 && a.lse)
         a.lse[(int64_t)tok * a.heads + head] =
-            bad ? NAN : sum > 0 ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+            bad ? NAN : lse2(sum, m) * kLn2;
 }
 
-enum { THIN, WIDE, MERGE };
+// One item a workgroup, the wide ones first: they are the long ones. A thin item whose
+// partial results have reached the device is counted for its unit, and the workgroup
+// that counts the last one joins the unit; the count is left at zero for the next
+// launch. (The rows of wide segments are left to the merge kernel: the workgroup that
+// came last would join 128 rows one after another. Decode of 64 requests with a shared
+// prefix of 2048, 32/8 heads of 128: 71 us so, 25 us with the merge kernel.)
+template <typename T, int D, bool WIDE>
+__global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
+    constexpr int TB = kWideKeys * D * 2;
+    // four objects, so that the compiler sees which loads a read has to wait for
+    __shared__ __attribute__((aligned(16))) char k0_lds[TB], k1_lds[TB];
+    __shared__ __attribute__((aligned(16))) char v0_lds[WIDE ? TB : 16], v1_lds[WIDE ? TB : 16];
+    __shared__ float stat[WIDE ? 1 : 4][kThinRows][2];
+    const Item it = a.items[blockIdx.x];
+    if (WIDE && blockIdx.x < (uint32_t)a.n_wide)
+        wide_item<T, D>(a, it, k0_lds, k1_lds, v0_lds, v1_lds);
+    else
+        thin_item<T, D>(a, it, k0_lds, k1_lds,
+                        WIDE ? (float (*)[kThinRows][2])(void *)v0_lds : stat);
+    if (it.unit < 0) return;
+    // this wave's results have arrived; then the others' have
+    __builtin_amdgcn_s_waitcnt(kWaitLoads);
+    __syncthreads();
+    const Unit u = a.units[it.unit];
+    int *last = (int *)k0_lds;
+    if (threadIdx.x == 0) {
+        uint32_t *done = a.done + it.unit;
+        const uint32_t before =
+            __hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *last = before == (uint32_t)u.items - 1;
+        if (*last) __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (*last) join<T, D, true>(a, u);
+}
 
 template <typename T, int D>
-hipError_t launch(int which, const AttnArgs &a, int n, hipStream_t s) {
-    if (which == THIN)
-        thin_kernel<T, D><<<dim3(n), 256, 0, s>>>(a);
-    else if (which == WIDE)
-        wide_kernel<T, D><<<dim3(n), 256, 0, s>>>(a);
-    else
-        merge_kernel<T, D><<<dim3(n, (a.heads + 3) / 4), 256, 0, s>>>(a);
-    return hipGetLastError();
+__global__ __launch_bounds__(256) void merge_kernel(AttnArgs a) {
+    join<T, D, false>(a, a.merge[blockIdx.x]);
 }
 
-hipError_t choose(int which, const AttnArgs &a, int n, int dtype, int head_dim, hipStream_t s) {
-    if (dtype == TAS_F16)
-        return head_dim == 64 ? launch<_Float16, 64>(which, a, n, s)
-                              : launch<_Float16, 128>(which, a, n, s);
-    return head_dim == 64 ? launch<__bf16, 64>(which, a, n, s)
-                          : launch<__bf16, 128>(which, a, n, s);
+template <typename T, int D>
+hipError_t launch(const AttnArgs &a, int n, int n_merge, hipStream_t s) {
+    if (a.n_wide)
+        attn_kernel<T, D, true><<<dim3(n), 256, 0, s>>>(a);
+    else
+        attn_kernel<T, D, false><<<dim3(n), 256, 0, s>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !n_merge) return e;
+    merge_kernel<T, D><<<dim3(n_merge), 256, 0, s>>>(a);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_thin(const AttnArgs &a, int n, int dtype, int head_dim, hipStream_t s) {
-    return choose(THIN, a, n, dtype, head_dim, s);
-}
-hipError_t launch_wide(const AttnArgs &a, int n, int dtype, int head_dim, hipStream_t s) {
-    return choose(WIDE, a, n, dtype, head_dim, s);
-}
-hipError_t launch_merge(const AttnArgs &a, int n, int kv_heads, int dtype, int head_dim,
-                        hipStream_t s) {
-    (void)kv_heads;
-    return choose(MERGE, a, n, dtype, head_dim, s);
+hipError_t launch_attention(const AttnArgs &a, int n, int n_merge, int dtype, int head_dim,
+                            hipStream_t s) {
+    if (dtype == TAS_F16)
+        return head_dim == 64 ? launch<_Float16, 64>(a, n, n_merge, s)
+                              : launch<_Float16, 128>(a, n, n_merge, s);
+    return head_dim == 64 ? launch<__bf16, 64>(a, n, n_merge, s)
+                          : launch<__bf16, 128>(a, n, n_merge, s);
 }
 
 }  // namespace tas_step_impl

@@ -15,6 +15,7 @@ constexpr int kThinRows = 16;   // rows of a thin item (all rows of its segment)
 constexpr int kThinKeys = 32;   // keys of one wave's step
 constexpr int kWideRows = 128;  // rows of a wide item
 constexpr int kWideKeys = 64;   // keys of one step of a wide item
+constexpr int kJoinRows = 16;   // rows of a join
 
 struct Req {
     int32_t t0, n_new, kv_len, table;   // first token; pages at tables[table]
@@ -34,12 +35,23 @@ struct Seg {
 struct Item {
     int32_t seg, hk, row0, k0, k1;
     int32_t part;  // partial row of row0, -1: output
+    int32_t unit;  // the join that waits for this item, -1: none
+};
+// Rows row0 .. row0 + rows - 1 of one key head of a segment, the results of which are
+// partial ones; of a prefix's rows, the parts of the tokens' own segments too. Rows of
+// a thin segment are joined by the last of the `items` items that have a part of them,
+// those of a wide one by a second kernel.
+struct Unit {
+    int32_t seg, hk, row0, rows, items, prefix;
 };
 struct PlanHead {
-    int64_t bytes;                 // of the blob
-    int64_t part_rows;             // partial rows
-    int32_t n_req, n_tok, n_seg, n_thin, n_wide, n_merge, n_table, all_own;
-    int64_t req, seg, thin, wide, tables, tok_req, merge;  // byte offsets in the blob
+    int64_t bytes;      // of the blob
+    int64_t part_rows;  // partial rows
+    int32_t n_req, n_tok, n_seg, n_thin, n_wide, n_join, n_merge, n_table;
+    // byte offsets in the blob; the items are the wide ones, then the thin ones; the
+    // units those of thin segments (join), then the others (merge); done holds a
+    // counter for each of the first, zero between launches
+    int64_t req, seg, items, units, tables, tok_req, tok_seg, done;
 };
 
 struct AppendArgs {
@@ -60,8 +72,9 @@ struct AttnArgs {
     const Seg *segs;
     const Item *items;
     const int32_t *tables;
-    const Req *reqs;
-    const int32_t *tok_req, *merge;
+    const Unit *units, *merge;
+    const int32_t *tok_seg;  // own segments
+    uint32_t *done;
     const void *q;
     void *out;
     float *lse;
@@ -69,6 +82,7 @@ struct AttnArgs {
     float *part_lse;  // [part_rows], base 2
     int64_t q_stride, out_stride;
     tas_cache c;
+    int32_t n_wide;  // items
     int32_t group, heads;
     int32_t sub_shift;  // log2(block_tokens / 16)
     float scale2;       // scale * log2(e)
@@ -76,9 +90,7 @@ struct AttnArgs {
 
 // Return hipSuccess or the launch's error.
 hipError_t launch_append(const AppendArgs &a, int dtype, int head_dim, hipStream_t s);
-hipError_t launch_thin(const AttnArgs &a, int n_items, int dtype, int head_dim, hipStream_t s);
-hipError_t launch_wide(const AttnArgs &a, int n_items, int dtype, int head_dim, hipStream_t s);
-hipError_t launch_merge(const AttnArgs &a, int n_merge, int kv_heads, int dtype, int head_dim,
-                        hipStream_t s);
+hipError_t launch_attention(const AttnArgs &a, int n_items, int n_merge, int dtype, int head_dim,
+                            hipStream_t s);
 
 }  // namespace tas_step_impl

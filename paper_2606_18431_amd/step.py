@@ -21,7 +21,7 @@ import os
 import numpy as np
 import torch
 
-from .tas import TAS_EINVAL, TAS_OK, TasError
+from .tas import TAS_OK, TasError, _stream
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libtas_step.so")
@@ -56,8 +56,8 @@ class tas_attention(ctypes.Structure):
                 ("out", _P), ("out_stride", _i64), ("lse", _P), ("cache", tas_cache)]
 
 
-EXPORTS = ["tas_step_bytes", "tas_step_create", "tas_step_destroy", "tas_step_tokens",
-           "tas_step_append", "tas_step_attention", "tas_step_plan"]
+EXPORTS = ["tas_step_create", "tas_step_bytes", "tas_step_bind", "tas_step_destroy",
+           "tas_step_tokens", "tas_step_append", "tas_step_attention", "tas_step_plan"]
 
 _lib = None
 
@@ -72,7 +72,8 @@ def lib():
         L = ctypes.CDLL(LIB_PATH)
         L.tas_step_bytes.argtypes = [_P]
         L.tas_step_bytes.restype = ctypes.c_size_t
-        L.tas_step_create.argtypes = [_P, _P, ctypes.c_size_t, ctypes.POINTER(_P)]
+        L.tas_step_create.argtypes = [_P, ctypes.POINTER(_P)]
+        L.tas_step_bind.argtypes = [_P, _P, ctypes.c_size_t, _P]
         L.tas_step_destroy.argtypes = [_P]
         L.tas_step_destroy.restype = None
         L.tas_step_tokens.argtypes = [_P]
@@ -119,26 +120,47 @@ def make_batch(n_new, kv_len, blocks, *, heads, kv_heads, head_dim, block_tokens
     return b, keep
 
 
-def tas_step_bytes(batch: tas_batch) -> int:
-    return int(lib().tas_step_bytes(ctypes.byref(batch)))
-
-
-def tas_step_create(batch: tas_batch, ws: int, ws_bytes: int) -> int:
-    """Returns a step handle (int). ``ws`` is a device address."""
+def tas_step_create(batch: tas_batch) -> int:
+    """Returns a step handle (int)."""
     ctx = _P()
-    _check(lib().tas_step_create(ctypes.byref(batch), ws, ws_bytes, ctypes.byref(ctx)),
-           "tas_step_create")
+    _check(lib().tas_step_create(ctypes.byref(batch), ctypes.byref(ctx)), "tas_step_create")
     return ctx.value
 
 
-def tas_step_plan(batch: tas_batch) -> bytes:
-    """The plan that tas_step_create copies to the device."""
+def tas_step_bytes(ctx) -> int:
+    return int(lib().tas_step_bytes(ctx))
+
+
+def tas_step_bind(ctx, ws: int, ws_bytes: int, stream=None):
+    """``ws``: a device address."""
+    _check(lib().tas_step_bind(ctx, ws, ws_bytes, _stream(stream)), "tas_step_bind")
+
+
+def tas_step_tokens(ctx) -> int:
+    return int(lib().tas_step_tokens(ctx))
+
+
+def tas_step_plan(ctx) -> bytes:
+    """The plan that tas_step_bind copies to the device."""
     n = ctypes.c_size_t()
-    _check(lib().tas_step_plan(ctypes.byref(batch), None, 0, ctypes.byref(n)), "tas_step_plan")
+    _check(lib().tas_step_plan(ctx, None, 0, ctypes.byref(n)), "tas_step_plan")
     buf = ctypes.create_string_buffer(n.value)
-    _check(lib().tas_step_plan(ctypes.byref(batch), buf, n.value, ctypes.byref(n)),
-           "tas_step_plan")
+    _check(lib().tas_step_plan(ctx, buf, n.value, ctypes.byref(n)), "tas_step_plan")
     return buf.raw
+
+
+def tas_step_append(ctx, args: tas_append, stream=None):
+    _check(lib().tas_step_append(ctx, ctypes.byref(args), _stream(stream)), "tas_step_append")
+
+
+def tas_step_attention(ctx, args: tas_attention, stream=None):
+    _check(lib().tas_step_attention(ctx, ctypes.byref(args), _stream(stream)),
+           "tas_step_attention")
+
+
+def tas_step_destroy(ctx):
+    if ctx:
+        lib().tas_step_destroy(ctx)
 
 
 class Step:
@@ -159,22 +181,20 @@ class Step:
                              head_dim=head_dim, block_tokens=block_tokens, n_blocks=n_blocks,
                              prefix_first=prefix_first, prefix_len=prefix_len,
                              prefix_blocks=prefix_blocks, causal=causal)
-        self.ws_bytes = tas_step_bytes(b)
-        if self.ws_bytes == 0:
-            raise TasError(TAS_EINVAL, "tas_step_bytes")
+        self.ctx = tas_step_create(b)
+        self.tokens = tas_step_tokens(self.ctx)
+        self.ws_bytes = tas_step_bytes(self.ctx)
         self.device = torch.device(device)
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.heads, self.kv_heads, self.head_dim = heads, kv_heads, head_dim
         self.cache_shape = (n_blocks, kv_heads, block_tokens, head_dim)
         with torch.cuda.device(self.device):
-            self.ws = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=self.device)
+            # the stream whose allocator pool the workspace comes from
             self._home = torch.cuda.current_stream().cuda_stream
-            # the memory may have been freed by work that is still under way
-            torch.cuda.current_stream().synchronize()
-            self.ctx = tas_step_create(b, self.ws.data_ptr() + (-self.ws.data_ptr()) % 256,
-                                       self.ws_bytes)
-        self.tokens = int(lib().tas_step_tokens(self.ctx))
+            self.ws = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=self.device)
+            tas_step_bind(self.ctx, self.ws.data_ptr() + (-self.ws.data_ptr()) % 256,
+                          self.ws_bytes, self._home)
 
     # ------------------------------------------------------------ argument checks
 
@@ -187,21 +207,22 @@ class Step:
             raise ValueError(f"{what} has shape {tuple(t.shape)}, expected "
                              f"{(self.tokens, heads, self.head_dim)}")
         s = t.stride()
-        if s[2] != 1 or s[1] != self.head_dim:
+        if s[2] != 1 or (s[1] != self.head_dim and heads > 1):
             raise ValueError(f"{what}: the heads of a token have to be adjacent, strides {s}")
         # one token: its stride says nothing
         return t.data_ptr(), s[0] if self.tokens > 1 else heads * self.head_dim
 
-    def _cache(self, k, v):
+    def _cache(self, k, v, dtype):
         for t, what in ((k, "k_cache"), (v, "v_cache")):
-            if t.dtype != k.dtype or t.device != self.device:
-                raise ValueError(f"{what} is {t.dtype} on {t.device}")
+            if t.dtype != dtype or t.device != self.device:
+                raise ValueError(f"{what} is {t.dtype} on {t.device}, expected {dtype} on "
+                                 f"{self.device}")
             if t.shape != self.cache_shape:
                 raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {self.cache_shape}")
-            if t.stride(3) != 1:
-                raise ValueError(f"{what}: head_dim is not the fastest, strides {t.stride()}")
         ks, vs = k.stride(), v.stride()
-        return tas_cache(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2])
+        if ks[3] != 1 or vs[3] != 1:
+            raise ValueError(f"caches: head_dim is not the fastest, strides {ks} and {vs}")
+        return k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2]
 
     def _dtype(self, t, what):
         code = DTYPES.get(t.dtype)
@@ -209,28 +230,30 @@ class Step:
             raise ValueError(f"{what} is {t.dtype}: float16 or bfloat16")
         return code
 
-    def _out(self, out, like, heads, stream):
+    def _out(self, out, like, stream):
         if out is not None:
             return out
-        shape = (self.tokens, heads, self.head_dim)
+        shape = (self.tokens, self.heads, self.head_dim)
         if stream is None:
-            return torch.empty(shape, dtype=like.dtype, device=self.device)
+            return like.new_empty(shape)
         with torch.cuda.stream(stream):
-            return torch.empty(shape, dtype=like.dtype, device=self.device)
+            return like.new_empty(shape)
 
-    def _enqueue(self, fn, args, stream):
+    def _enqueue(self, call, args, stream):
         if self.ctx is None:
             raise ValueError("the step is closed")
+        index = self.device.index
         if stream is None:
-            stream = torch.cuda.current_stream(self.device)
-        if stream.cuda_stream != self._home:  # the workspace outlives the work there
-            self.ws.record_stream(stream)
-        if torch.cuda.current_device() == self.device.index:
-            rc = fn(self.ctx, ctypes.byref(args), stream.cuda_stream)
+            raw = torch._C._cuda_getCurrentRawStream(index)
+        else:
+            raw = stream.cuda_stream
+        if raw != self._home:  # the workspace outlives the work there
+            self.ws.record_stream(torch.cuda.ExternalStream(raw) if stream is None else stream)
+        if torch.cuda.current_device() == index:
+            call(self.ctx, args, raw)
         else:
             with torch.cuda.device(self.device):
-                rc = fn(self.ctx, ctypes.byref(args), stream.cuda_stream)
-        _check(rc, fn.__name__)
+                call(self.ctx, args, raw)
 
     # ------------------------------------------------------------ the operators
 
@@ -244,9 +267,7 @@ class Step:
         None. Keys and values go to the caches; returns the queries."""
         dtype = self._dtype(qkv, "qkv")
         qkv_p, qkv_s = self._rows(qkv, self.heads + 2 * self.kv_heads, qkv.dtype, "qkv")
-        cache = self._cache(k_cache, v_cache)
-        if k_cache.dtype != qkv.dtype:
-            raise ValueError(f"the caches are {k_cache.dtype}, qkv {qkv.dtype}")
+        cache = self._cache(k_cache, v_cache, qkv.dtype)
         rot = positions = 0
         cos_p = sin_p = None
         if (cos is None) != (sin is None):
@@ -268,12 +289,11 @@ class Step:
                     raise ValueError(f"weights: contiguous {qkv.dtype} [{self.head_dim}] on "
                                      f"{self.device}")
             q_weight, k_weight = q_weight.data_ptr(), k_weight.data_ptr()
-        out = self._out(out, qkv, self.heads, stream)
+        out = self._out(out, qkv, stream)
         out_p, out_s = self._rows(out, self.heads, qkv.dtype, "out")
-        self._enqueue(lib().tas_step_append,
-                      tas_append(dtype, rot, int(bool(interleaved)), eps, qkv_p, qkv_s, out_p,
-                                 out_s, q_weight, k_weight, cos_p, sin_p, positions, cache),
-                      stream)
+        self._enqueue(tas_step_append,
+                      tas_append(dtype, rot, bool(interleaved), eps, qkv_p, qkv_s, out_p, out_s,
+                                 q_weight, k_weight, cos_p, sin_p, positions, cache), stream)
         return out
 
     def attention(self, q, k_cache, v_cache, *, scale=None, out=None, lse=None, stream=None):
@@ -283,10 +303,8 @@ class Step:
         ``out`` may be ``q``. Returns [tokens, heads, head_dim]."""
         dtype = self._dtype(q, "q")
         q_p, q_s = self._rows(q, self.heads, q.dtype, "q")
-        cache = self._cache(k_cache, v_cache)
-        if k_cache.dtype != q.dtype:
-            raise ValueError(f"the caches are {k_cache.dtype}, q {q.dtype}")
-        out = self._out(out, q, self.heads, stream)
+        cache = self._cache(k_cache, v_cache, q.dtype)
+        out = self._out(out, q, stream)
         out_p, out_s = self._rows(out, self.heads, q.dtype, "out")
         if lse is not None:
             if lse.dtype != torch.float32 or lse.device != self.device \
@@ -296,13 +314,13 @@ class Step:
             lse = lse.data_ptr()
         if scale is None:
             scale = 1.0 / math.sqrt(self.head_dim)
-        self._enqueue(lib().tas_step_attention,
+        self._enqueue(tas_step_attention,
                       tas_attention(dtype, scale, q_p, q_s, out_p, out_s, lse, cache), stream)
         return out
 
     def close(self):
         if getattr(self, "ctx", None):
-            lib().tas_step_destroy(self.ctx)
+            tas_step_destroy(self.ctx)
             self.ctx = None
 
     def __del__(self):

@@ -17,27 +17,38 @@ REQ = np.dtype([(f, np.int32) for f in ("t0", "n_new", "kv_len", "table", "prefi
                                         "pre_seg", "pad")])
 SEG = np.dtype([(f, np.int32) for f in ("t0", "n_tok", "kv_len", "lim0", "table", "nsplit", "part",
                                         "rows")])
-ITEM = np.dtype([(f, np.int32) for f in ("seg", "hk", "row0", "k0", "k1", "part")])
+ITEM = np.dtype([(f, np.int32) for f in ("seg", "hk", "row0", "k0", "k1", "part", "unit")])
+UNIT = np.dtype([(f, np.int32) for f in ("seg", "hk", "row0", "rows", "items", "prefix")])
 HEAD = np.dtype([("bytes", np.int64), ("part_rows", np.int64)]
                 + [(f, np.int32) for f in ("n_req", "n_tok", "n_seg", "n_thin", "n_wide",
-                                           "n_merge", "n_table", "all_own")]
-                + [(f, np.int64) for f in ("req", "seg", "thin", "wide", "tables", "tok_req",
-                                           "merge")])
-THIN_ROWS, WIDE_ROWS = 16, 128
+                                           "n_join", "n_merge", "n_table")]
+                + [(f, np.int64) for f in ("req", "seg", "items", "units", "tables", "tok_req",
+                                           "tok_seg", "done")])
+THIN_ROWS, WIDE_ROWS, JOIN_ROWS = 16, 128, 16
 
 
-def parse(blob):
-    h = np.frombuffer(blob, HEAD, 1)[0]
-    assert h["bytes"] == len(blob)
+def plan(b):
+    """The parsed plan of a tas_batch."""
+    ctx = step.tas_step_create(b)
+    try:
+        blob = step.tas_step_plan(ctx)
+        h = np.frombuffer(blob, HEAD, 1)[0]
+        assert h["bytes"] == len(blob) and step.tas_step_tokens(ctx) == h["n_tok"]
+        assert step.tas_step_bytes(ctx) >= len(blob) + h["part_rows"] * (b.head_dim + 1) * 4
+    finally:
+        step.tas_step_destroy(ctx)
 
     def at(off, dtype, n):
         return np.frombuffer(blob, dtype, int(n), int(off))
 
+    items = at(h["items"], ITEM, h["n_wide"] + h["n_thin"])
     return dict(head=h, reqs=at(h["req"], REQ, h["n_req"]), segs=at(h["seg"], SEG, h["n_seg"]),
-                thin=at(h["thin"], ITEM, h["n_thin"]), wide=at(h["wide"], ITEM, h["n_wide"]),
+                wide=items[:h["n_wide"]], thin=items[h["n_wide"]:],
+                units=at(h["units"], UNIT, h["n_join"] + h["n_merge"]),
                 tables=at(h["tables"], np.int32, h["n_table"]),
                 tok_req=at(h["tok_req"], np.int32, h["n_tok"]),
-                merge=at(h["merge"], np.int32, h["n_merge"]))
+                tok_seg=at(h["tok_seg"], np.int32, h["n_tok"]),
+                done=at(h["done"], np.int32, h["n_join"]))
 
 
 def batch(seed, n_req, max_new, max_ctx, heads, kv_heads, block, groups=0, causal=True,
@@ -80,13 +91,15 @@ CASES = [dict(seed=1, n_req=1, max_new=1, max_ctx=1, heads=8, kv_heads=8, block=
 def test_plan_covers_every_visible_key_once(case):
     n, kv, blocks, kw = batch(**case)
     b, keep = step.make_batch(n, kv, blocks, **kw)
-    p = parse(step.tas_step_plan(b))
+    p = plan(b)
     Hk, G, bt = kw["kv_heads"], kw["heads"] // kw["kv_heads"], kw["block_tokens"]
     T = int(n.sum())
     assert p["head"]["n_tok"] == T and p["head"]["n_req"] == len(n)
     assert np.array_equal(p["tok_req"], np.repeat(np.arange(len(n)), n))
     first = kw.get("prefix_first")
     used = np.zeros(int(p["head"]["part_rows"]), np.int32)
+    n_join = int(p["head"]["n_join"])
+    counted = np.zeros(n_join, np.int64)
     covered = {}  # (seg, hk) -> per row, the pieces that saw it
     for kind, tile in (("thin", THIN_ROWS), ("wide", WIDE_ROWS)):
         for it in p[kind]:
@@ -99,9 +112,36 @@ def test_plan_covers_every_visible_key_once(case):
             assert (it["part"] >= 0) == (s["part"] >= 0)
             if it["part"] >= 0:
                 used[it["part"]:it["part"] + rows] += 1
+            if it["unit"] >= 0:  # a thin item of the unit's rows
+                assert kind == "thin" and it["part"] >= 0
+                counted[it["unit"]] += 1
+                un = p["units"][it["unit"]]
+                shift = (int(s["t0"]) - int(p["segs"][un["seg"]]["t0"])) * G + it["row0"]
+                assert un["hk"] == it["hk"] and un["row0"] <= shift
+                assert shift + rows <= un["row0"] + un["rows"]
             for r in range(it["row0"], it["row0"] + rows):
                 covered.setdefault((int(it["seg"]), int(it["hk"]), r), []).append(it)
     assert (used == 1).all()  # every partial row is written, by one item
+    # a join waits for its items, which are all that have parts of its rows
+    assert np.array_equal(counted, p["units"]["items"][:n_join]) and not p["done"].any()
+    joined = {}
+    for u, un in enumerate(p["units"]):
+        s = p["segs"][un["seg"]]
+        assert un["row0"] % JOIN_ROWS == 0 and un["row0"] + un["rows"] <= s["rows"]
+        assert un["rows"] == min(JOIN_ROWS, s["rows"] - un["row0"])
+        assert (u < n_join) == (s["rows"] <= THIN_ROWS)
+        own = set()
+        for r in range(un["row0"], un["row0"] + un["rows"]):
+            rq = p["reqs"][p["tok_req"][s["t0"] + r // G]]
+            assert un["seg"] == (rq["pre_seg"] if un["prefix"] else rq["own_seg"])
+            assert un["prefix"] or rq["pre_seg"] < 0
+            own.add(int(rq["own_seg"]))
+            key = (int(s["t0"]) + r // G, int(un["hk"]), r % G)
+            assert key not in joined
+            joined[key] = u
+        if u < n_join:
+            parts = sum(int(p["segs"][x]["nsplit"]) for x in own if x >= 0)
+            assert un["items"] == parts + (int(s["nsplit"]) if un["prefix"] else 0)
     for i, s in enumerate(p["segs"]):
         assert s["rows"] == s["n_tok"] * G
         for hk in range(Hk):
@@ -118,7 +158,6 @@ def test_plan_covers_every_visible_key_once(case):
                     assert sorted(x["part"] + r - x["row0"] for x in its) == \
                         [s["part"] + (hk * s["nsplit"] + m) * s["rows"] + r
                          for m in range(s["nsplit"])]
-    merged = set(p["merge"].tolist())
     t = 0
     for i, r in enumerate(p["reqs"]):
         assert (r["t0"], r["n_new"], r["kv_len"]) == (t, n[i], kv[i])
@@ -144,27 +183,19 @@ def test_plan_covers_every_visible_key_once(case):
                                       np.asarray(kw["prefix_blocks"])[g, :q])
             parts = shared >= 0 or p["segs"][own]["part"] >= 0
             for j in range(t, t + n[i]):
-                assert (j in merged) == parts
+                for hk in range(Hk):
+                    assert all(((j, hk, x) in joined) == parts for x in range(G))
+        assert (p["tok_seg"][t:t + n[i]] == r["own_seg"]).all()
         t += int(n[i])
 
 
 def refused(n, kv, blocks, **kw):
     base = dict(heads=8, kv_heads=2, head_dim=64, block_tokens=16, n_blocks=8)
     b, keep = step.make_batch(n, kv, blocks, **{**base, **kw})
-    n_bytes = step.tas_step_bytes(b)
-    size = ctypes.c_size_t()
-    rc = step.lib().tas_step_plan(ctypes.byref(b), None, 0, ctypes.byref(size))
-    assert (n_bytes == 0) == (rc != 0)
-    ctx = ctypes.c_void_p()
-    if rc:  # refused before anything is copied: the address is never used
-        assert step.lib().tas_step_create(ctypes.byref(b), 1 << 40, 1 << 40,
-                                          ctypes.byref(ctx)) == rc
-    else:
-        assert step.lib().tas_step_create(ctypes.byref(b), 1 << 40, n_bytes - 1,
-                                          ctypes.byref(ctx)) == tas.TAS_ENOMEM
-        assert step.lib().tas_step_create(ctypes.byref(b), (1 << 40) + 16, n_bytes,
-                                          ctypes.byref(ctx)) == tas.TAS_EINVAL
-    assert not ctx.value
+    ctx = ctypes.c_void_p(1)
+    rc = step.lib().tas_step_create(ctypes.byref(b), ctypes.byref(ctx))
+    assert (rc == 0) == bool(ctx.value)
+    step.tas_step_destroy(ctx.value)
     return rc == tas.TAS_EINVAL
 
 
@@ -206,19 +237,31 @@ def test_refused_prefixes():
                         n_blocks=1)
 
 
-def test_null_arguments():
+def test_null_arguments_and_unbound_steps():
     L = step.lib()
-    assert L.tas_step_bytes(None) == 0
-    assert L.tas_step_create(None, None, 0, None) == tas.TAS_EINVAL
+    assert L.tas_step_bytes(None) == 0 and L.tas_step_tokens(None) == -1
+    assert L.tas_step_create(None, None) == tas.TAS_EINVAL
+    assert L.tas_step_bind(None, None, 0, None) == tas.TAS_EINVAL
     assert L.tas_step_append(None, None, None) == tas.TAS_EINVAL
     assert L.tas_step_attention(None, None, None) == tas.TAS_EINVAL
-    assert L.tas_step_tokens(None) == -1
+    assert L.tas_step_plan(None, None, 0, None) == tas.TAS_EINVAL
     L.tas_step_destroy(None)
-    b, keep = step.make_batch([1, 1], [0, 1], [[0], [1]], heads=1, kv_heads=1, head_dim=64,
+    b, keep = step.make_batch([1, 1], [1, 1], [[0], [1]], heads=1, kv_heads=1, head_dim=64,
                               block_tokens=16, n_blocks=2)
-    assert L.tas_step_bytes(ctypes.byref(b)) > 0
+    ctx = step.tas_step_create(b)
+    need, n = step.tas_step_bytes(ctx), ctypes.c_size_t()
+    # refused before the address is used
+    assert L.tas_step_bind(ctx, 1 << 40, need - 1, None) == tas.TAS_ENOMEM
+    assert L.tas_step_bind(ctx, (1 << 40) + 16, need, None) == tas.TAS_EINVAL
+    assert L.tas_step_bind(ctx, None, need, None) == tas.TAS_EINVAL
+    assert L.tas_step_append(ctx, ctypes.byref(step.tas_append()), None) == tas.TAS_ESTATE
+    assert L.tas_step_attention(ctx, ctypes.byref(step.tas_attention()), None) == tas.TAS_ESTATE
+    buf = ctypes.create_string_buffer(8)
+    assert L.tas_step_plan(ctx, buf, 8, ctypes.byref(n)) == tas.TAS_ENOMEM
+    step.tas_step_destroy(ctx)
     b.blocks = None
-    assert L.tas_step_bytes(ctypes.byref(b)) == 0
+    with pytest.raises(tas.TasError):
+        step.tas_step_create(b)
 
 
 def test_library_exports_every_declared_symbol():
