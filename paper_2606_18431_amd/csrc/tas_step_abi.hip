@@ -24,7 +24,9 @@ constexpr int64_t kMaxPartRows = int64_t(1) << 28;
 constexpr int64_t kMaxStride = (int64_t(1) << 31) - 8;      // of a block or head, elements
 constexpr int64_t kMaxTokenStride = int64_t(1) << 24;       // of a token in a block
 constexpr int32_t kSlots = 512;                      // wide items that run at once
-constexpr int32_t kThinItems = 2048;                 // thin items wanted
+constexpr int32_t kThinItems = 768;                  // thin items wanted
+constexpr double kWideShare = 1.0;
+constexpr int64_t kWideLeast = 4;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -106,22 +108,20 @@ bool distinct_slots(const tas_batch *b, const Plan &p) {
 // finds nsplit partial results for every row.
 int make_items(const tas_batch *b, Plan &p) {
     const int32_t G = b->heads / b->kv_heads, Hk = b->kv_heads;
-    int64_t thin_keys = 0, wide_tiles = 0, wide_keys = 0;
+    int64_t thin_keys = 0, wide_steps = 0;
     for (const Seg &s : p.segs) {
-        if (is_thin(s)) {
+        if (is_thin(s))
             thin_keys += (int64_t)s.kv_len * Hk;
-        } else {
-            wide_tiles += (int64_t)tiles_of(s) * Hk;
-            wide_keys += (int64_t)tiles_of(s) * Hk * s.kv_len;
-        }
+        else
+            wide_steps += (int64_t)tiles_of(s) * Hk * ceil_div(s.kv_len, kWideKeys);
     }
     const int64_t step = 4 * kThinKeys;
     const int64_t thin_piece =
         std::max<int64_t>(ceil_div(ceil_div(thin_keys, kThinItems), step) * step, 2 * step);
-    int64_t wide_piece = INT32_MAX;
-    if (wide_tiles && wide_tiles < kSlots)
-        wide_piece = std::max<int64_t>(ceil_div(ceil_div(wide_keys, kSlots), kWideKeys) * kWideKeys,
-                                       4 * kWideKeys);
+    // steps of work for a slot; the thin items' 64 keys take about as long as a step
+    const int64_t load = ceil_div(wide_steps + thin_keys / kWideKeys, kSlots);
+    const int64_t wide_piece =
+        std::max<int64_t>((int64_t)(load * kWideShare), kWideLeast) * kWideKeys;
     for (Seg &s : p.segs) {
         s.nsplit = (int32_t)std::max<int64_t>(
             1, ceil_div(s.kv_len, is_thin(s) ? thin_piece : wide_piece));

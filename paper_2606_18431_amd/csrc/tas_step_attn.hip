@@ -149,6 +149,10 @@ __device__ void store_row(const AttnArgs &a, const Seg &s, const Item &it, int r
     if (d == 0 && a.lse) a.lse[tok * a.heads + head] = lse2(l, m) * kLn2;
 }
 
+// 16 bytes that are read once: they need not stay in the caches (decode of 256 requests,
+// 448k tokens of 8 heads of 128: 282 us, with ordinary loads 311).
+__device__ u4 stream(const char *p) { return __builtin_nontemporal_load((const u4 *)p); }
+
 // Up to 16 rows against a run of keys: each of the four waves takes every fourth
 // 32 keys, K straight into registers as the left operand, V through its own LDS;
 // the waves' results are joined at the end. Memory bound: 16 rows make use of at
@@ -209,11 +213,12 @@ __device__ __forceinline__ void thin_item(const AttnArgs &a, const Item &it, cha
             const char *kp = (const char *)(kbase + page[n] * a.c.k_block + off * a.c.k_token);
             const char *vp = (const char *)(vbase + page[n] * a.c.v_block + off * a.c.v_token);
 #pragma unroll
-            for (int i = 0; i < QS; i++) k[n][i] = *(const V *)(kp + klane + i * 64);
+            for (int i = 0; i < QS; i++)
+                k[n][i] = __builtin_bit_cast(V, stream(kp + klane + i * 64));
 #pragma unroll
             for (int i = 0; i < VL / 2; i++)
                 v[n * VL / 2 + i] =
-                    *(const u4 *)(vp + (int64_t)(i * (64 / LPR)) * a.c.v_token * 2 + vlane);
+                    stream(vp + (int64_t)(i * (64 / LPR)) * a.c.v_token * 2 + vlane);
         }
     };
     int base = __builtin_amdgcn_readfirstlane(it.k0 + wave * kThinKeys);
