@@ -712,8 +712,7 @@ __device__ __forceinline__ void join(const AttnArgs &a, const Unit &u) {
             bad ? NAN : lse2(sum, m) * kLn2;
 }
 
-// One item a workgroup, the wide ones first: they are the long ones. A thin item whose
-// partial results have reached the device is counted for its unit, and the workgroup
+// One item a workgroup. A thin item whose partial results have reached the device is counted for its unit, and the workgroup
 // that counts the last one joins the unit; the count is left at zero for the next
 // launch. (The rows of wide segments are left to the merge kernel: the workgroup that
 // came last would join 128 rows one after another. Decode of 64 requests with a shared
@@ -726,7 +725,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     __shared__ __attribute__((aligned(16))) char v0_lds[WIDE ? TB : 16], v1_lds[WIDE ? TB : 16];
     __shared__ float stat[WIDE ? 1 : 4][kThinRows][2];
     const Item it = a.items[blockIdx.x];
-    if (WIDE && blockIdx.x < (uint32_t)a.n_wide)
+    if (WIDE && a.segs[it.seg].rows > kThinRows)
         wide_item<T, D>(a, it, k0_lds, k1_lds, v0_lds, v1_lds);
     else
         thin_item<T, D>(a, it, k0_lds, k1_lds,

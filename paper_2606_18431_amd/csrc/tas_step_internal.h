@@ -48,8 +48,7 @@ struct PlanHead {
     int64_t bytes;      // of the blob
     int64_t part_rows;  // partial rows
     int32_t n_req, n_tok, n_seg, n_thin, n_wide, n_join, n_merge, n_table;
-    // byte offsets in the blob; the items are the wide ones, then the thin ones; the
-    // units those of thin segments (join), then the others (merge); done holds a
+    // byte offsets in the blob; the items as the workgroups take them; the units those of thin segments (join), then the others (merge); done holds a
     // counter for each of the first, zero between launches
     int64_t req, seg, items, units, tables, tok_req, tok_seg, done;
 };

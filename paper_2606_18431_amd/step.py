@@ -15,7 +15,6 @@ allocating the workspace and outputs as PyTorch tensors.
 from __future__ import annotations
 
 import ctypes
-import math
 import os
 
 import numpy as np
@@ -187,7 +186,10 @@ class Step:
         self.device = torch.device(device)
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self.index = self.device.index
         self.heads, self.kv_heads, self.head_dim = heads, kv_heads, head_dim
+        self.q_shape = (self.tokens, heads, head_dim)
+        self.qkv_shape = (self.tokens, heads + 2 * kv_heads, head_dim)
         self.cache_shape = (n_blocks, kv_heads, block_tokens, head_dim)
         with torch.cuda.device(self.device):
             # the stream whose allocator pool the workspace comes from
@@ -198,31 +200,32 @@ class Step:
 
     # ------------------------------------------------------------ argument checks
 
-    def _rows(self, t, heads, dtype, what):
+    def _rows(self, t, shape, dtype, what):
         """Address and token stride of a [tokens, heads, head_dim] tensor."""
-        if t.dtype != dtype or t.device != self.device:
-            raise ValueError(f"{what} is {t.dtype} on {t.device}, expected {dtype} on "
-                             f"{self.device}")
-        if t.shape != (self.tokens, heads, self.head_dim):
-            raise ValueError(f"{what} has shape {tuple(t.shape)}, expected "
-                             f"{(self.tokens, heads, self.head_dim)}")
-        s = t.stride()
-        if s[2] != 1 or (s[1] != self.head_dim and heads > 1):
-            raise ValueError(f"{what}: the heads of a token have to be adjacent, strides {s}")
+        if t.dtype != dtype or t.get_device() != self.index or t.shape != shape:
+            raise ValueError(f"{what} is {t.dtype} {tuple(t.shape)} on {t.device}, expected "
+                             f"{dtype} {shape} on {self.device}")
+        s0, s1, s2 = t.stride()
+        if s2 != 1 or (s1 != self.head_dim and shape[1] > 1):
+            raise ValueError(f"{what}: the heads of a token have to be adjacent, strides "
+                             f"{t.stride()}")
         # one token: its stride says nothing
-        return t.data_ptr(), s[0] if self.tokens > 1 else heads * self.head_dim
+        return t.data_ptr(), s0 if self.tokens > 1 else shape[1] * self.head_dim
 
     def _cache(self, k, v, dtype):
-        for t, what in ((k, "k_cache"), (v, "v_cache")):
-            if t.dtype != dtype or t.device != self.device:
-                raise ValueError(f"{what} is {t.dtype} on {t.device}, expected {dtype} on "
-                                 f"{self.device}")
-            if t.shape != self.cache_shape:
-                raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {self.cache_shape}")
-        ks, vs = k.stride(), v.stride()
-        if ks[3] != 1 or vs[3] != 1:
-            raise ValueError(f"caches: head_dim is not the fastest, strides {ks} and {vs}")
-        return k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2]
+        if k.dtype != dtype or v.dtype != dtype or k.get_device() != self.index \
+                or v.get_device() != self.index or k.shape != self.cache_shape \
+                or v.shape != self.cache_shape:
+            raise ValueError(
+                f"caches are {k.dtype} {tuple(k.shape)} on {k.device} and {v.dtype} "
+                f"{tuple(v.shape)} on {v.device}, expected {dtype} {self.cache_shape} on "
+                f"{self.device}")
+        k0, k1, k2, k3 = k.stride()
+        v0, v1, v2, v3 = v.stride()
+        if k3 != 1 or v3 != 1:
+            raise ValueError(f"caches: head_dim is not the fastest, strides {k.stride()} and "
+                             f"{v.stride()}")
+        return k.data_ptr(), v.data_ptr(), k0, k1, k2, v0, v1, v2
 
     def _dtype(self, t, what):
         code = DTYPES.get(t.dtype)
@@ -233,16 +236,15 @@ class Step:
     def _out(self, out, like, stream):
         if out is not None:
             return out
-        shape = (self.tokens, self.heads, self.head_dim)
         if stream is None:
-            return like.new_empty(shape)
+            return like.new_empty(self.q_shape)
         with torch.cuda.stream(stream):
-            return like.new_empty(shape)
+            return like.new_empty(self.q_shape)
 
     def _enqueue(self, call, args, stream):
         if self.ctx is None:
             raise ValueError("the step is closed")
-        index = self.device.index
+        index = self.index
         if stream is None:
             raw = torch._C._cuda_getCurrentRawStream(index)
         else:
@@ -266,31 +268,32 @@ class Step:
         16; None: no rotation. ``q_weight``, ``k_weight``: [head_dim], or both
         None. Keys and values go to the caches; returns the queries."""
         dtype = self._dtype(qkv, "qkv")
-        qkv_p, qkv_s = self._rows(qkv, self.heads + 2 * self.kv_heads, qkv.dtype, "qkv")
+        qkv_p, qkv_s = self._rows(qkv, self.qkv_shape, qkv.dtype, "qkv")
         cache = self._cache(k_cache, v_cache, qkv.dtype)
         rot = positions = 0
         cos_p = sin_p = None
         if (cos is None) != (sin is None):
             raise ValueError("cos and sin: both or neither")
         if cos is not None:
+            shape = cos.shape
             for t in (cos, sin):
-                if t.dtype != torch.float32 or t.device != self.device or t.dim() != 2 \
-                        or t.shape != cos.shape or not t.is_contiguous():
+                if t.dtype != torch.float32 or t.get_device() != self.index \
+                        or t.shape != shape or len(shape) != 2 or not t.is_contiguous():
                     raise ValueError("cos and sin: contiguous float32 [positions, rot_dim / 2] "
                                      f"on {self.device}")
-            positions, rot = cos.shape[0], 2 * cos.shape[1]
+            positions, rot = shape[0], 2 * shape[1]
             cos_p, sin_p = cos.data_ptr(), sin.data_ptr()
         if (q_weight is None) != (k_weight is None):
             raise ValueError("q_weight and k_weight: both or neither")
         if q_weight is not None:
             for t in (q_weight, k_weight):
-                if t.dtype != qkv.dtype or t.device != self.device \
+                if t.dtype != qkv.dtype or t.get_device() != self.index \
                         or t.shape != (self.head_dim,) or not t.is_contiguous():
                     raise ValueError(f"weights: contiguous {qkv.dtype} [{self.head_dim}] on "
                                      f"{self.device}")
             q_weight, k_weight = q_weight.data_ptr(), k_weight.data_ptr()
         out = self._out(out, qkv, stream)
-        out_p, out_s = self._rows(out, self.heads, qkv.dtype, "out")
+        out_p, out_s = self._rows(out, self.q_shape, qkv.dtype, "out")
         self._enqueue(tas_step_append,
                       tas_append(dtype, rot, bool(interleaved), eps, qkv_p, qkv_s, out_p, out_s,
                                  q_weight, k_weight, cos_p, sin_p, positions, cache), stream)
@@ -302,18 +305,18 @@ class Step:
         float32 [tokens, heads] to receive the log of the sum of the exponentials.
         ``out`` may be ``q``. Returns [tokens, heads, head_dim]."""
         dtype = self._dtype(q, "q")
-        q_p, q_s = self._rows(q, self.heads, q.dtype, "q")
+        q_p, q_s = self._rows(q, self.q_shape, q.dtype, "q")
         cache = self._cache(k_cache, v_cache, q.dtype)
         out = self._out(out, q, stream)
-        out_p, out_s = self._rows(out, self.heads, q.dtype, "out")
+        out_p, out_s = self._rows(out, self.q_shape, q.dtype, "out")
         if lse is not None:
-            if lse.dtype != torch.float32 or lse.device != self.device \
-                    or lse.shape != (self.tokens, self.heads) or not lse.is_contiguous():
+            if lse.dtype != torch.float32 or lse.get_device() != self.index \
+                    or lse.shape != self.q_shape[:2] or not lse.is_contiguous():
                 raise ValueError(f"lse: contiguous float32 {(self.tokens, self.heads)} on "
                                  f"{self.device}")
             lse = lse.data_ptr()
         if scale is None:
-            scale = 1.0 / math.sqrt(self.head_dim)
+            scale = self.head_dim ** -0.5
         self._enqueue(tas_step_attention,
                       tas_attention(dtype, scale, q_p, q_s, out_p, out_s, lse, cache), stream)
         return out

@@ -42,8 +42,11 @@ def plan(b):
         return np.frombuffer(blob, dtype, int(n), int(off))
 
     items = at(h["items"], ITEM, h["n_wide"] + h["n_thin"])
-    return dict(head=h, reqs=at(h["req"], REQ, h["n_req"]), segs=at(h["seg"], SEG, h["n_seg"]),
-                wide=items[:h["n_wide"]], thin=items[h["n_wide"]:],
+    segs = at(h["seg"], SEG, h["n_seg"])
+    wide = segs["rows"][items["seg"]] > THIN_ROWS
+    assert int(wide.sum()) == h["n_wide"]
+    return dict(head=h, reqs=at(h["req"], REQ, h["n_req"]), segs=segs,
+                wide=items[wide], thin=items[~wide],
                 units=at(h["units"], UNIT, h["n_join"] + h["n_merge"]),
                 tables=at(h["tables"], np.int32, h["n_table"]),
                 tok_req=at(h["tok_req"], np.int32, h["n_tok"]),
