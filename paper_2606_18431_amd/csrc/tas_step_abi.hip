@@ -38,7 +38,8 @@ struct Plan {
     std::vector<Seg> segs;
     std::vector<Item> thin, wide, items;
     std::vector<Unit> join, merge;
-    std::vector<int32_t> tables, tok_req, tok_seg;
+    std::vector<int32_t> tables, tok_req;
+    std::vector<Own> tok_own;  // empty without prefixes
     int64_t max_pos = 0;  // largest position of a new token + 1
     bool appendable = true;
 };
@@ -144,8 +145,8 @@ int make_items(const tas_batch *b, Plan &p) {
         for (int32_t hk = 0; hk < Hk; hk++)
             for (int32_t row0 = 0; row0 < s.rows; row0 += kJoinRows)
                 (is_thin(s) ? p.join : p.merge)
-                    .push_back({seg, hk, row0, std::min(kJoinRows, s.rows - row0), 0,
-                                is_prefix[seg]});
+                    .push_back({s, seg, hk, row0, std::min(kJoinRows, s.rows - row0), 0,
+                                is_prefix[seg], {0, 0}});
         return true;
     };
     std::vector<int32_t> shared(p.segs.size(), -1);  // the prefix that an own segment joins
@@ -157,6 +158,17 @@ int make_items(const tas_batch *b, Plan &p) {
         if ((r.pre_seg >= 0 || p.segs[r.own_seg].nsplit > 1) &&
             !partial(r.own_seg, r.pre_seg < 0))
             return TAS_EINVAL;
+    }
+    if (b->n_prefix) {
+        p.tok_own.reserve(p.tok_req.size());
+        for (const Req &r : p.reqs) {
+            Own own{};
+            if (r.own_seg >= 0) {
+                const Seg &s = p.segs[r.own_seg];
+                own = {s.part, s.nsplit, s.rows, s.t0};
+            }
+            p.tok_own.insert(p.tok_own.end(), (size_t)r.n_new, own);
+        }
     }
     int64_t n_items = 0;
     for (const Seg &s : p.segs) n_items += (int64_t)Hk * tiles_of(s) * s.nsplit;
@@ -175,6 +187,7 @@ int make_items(const tas_batch *b, Plan &p) {
             for (int32_t n = 0; n < s.nsplit; n++)
                 for (int32_t hk = 0; hk < Hk; hk++) {
                     Item it{};
+                    it.s = s;
                     it.seg = (int32_t)i;
                     it.hk = hk;
                     it.row0 = row0;
@@ -272,7 +285,6 @@ int make_plan(const tas_batch *b, Plan &p) {
             }
         }
         p.tok_req.insert(p.tok_req.end(), (size_t)n, i);
-        p.tok_seg.insert(p.tok_seg.end(), (size_t)n, r.own_seg);
         p.reqs.push_back(r);
         t += n;
     }
@@ -297,7 +309,7 @@ int make_plan(const tas_batch *b, Plan &p) {
     place(h.units, (p.join.size() + p.merge.size()) * sizeof(Unit));
     place(h.tables, p.tables.size() * 4);
     place(h.tok_req, p.tok_req.size() * 4);
-    place(h.tok_seg, p.tok_seg.size() * 4);
+    place(h.tok_own, p.tok_own.size() * sizeof(Own));
     place(h.done, p.join.size() * 4);
     h.bytes = (int64_t)at;
     return TAS_OK;
@@ -316,7 +328,7 @@ void write_blob(const Plan &p, char *to) {
     put(h.units + p.join.size() * sizeof(Unit), p.merge.data(), p.merge.size() * sizeof(Unit));
     put(h.tables, p.tables.data(), p.tables.size() * 4);
     put(h.tok_req, p.tok_req.data(), p.tok_req.size() * 4);
-    put(h.tok_seg, p.tok_seg.data(), p.tok_seg.size() * 4);
+    put(h.tok_own, p.tok_own.data(), p.tok_own.size() * sizeof(Own));
 }
 
 
@@ -457,9 +469,8 @@ int tas_step_attention(tas_step *s, const tas_attention *a, void *stream) {
     if (!valid_rows(a->q, a->q_stride, row) || !valid_rows(a->out, a->out_stride, row))
         return TAS_EINVAL;
     AttnArgs k{};
-    k.segs = (const Seg *)(s->ws + s->head.seg);
     k.tables = (const int32_t *)(s->ws + s->head.tables);
-    k.tok_seg = (const int32_t *)(s->ws + s->head.tok_seg);
+    k.tok_own = (const Own *)(s->ws + s->head.tok_own);
     k.items = (const Item *)(s->ws + s->head.items);
     k.units = (const Unit *)(s->ws + s->head.units);
     k.merge = k.units + s->head.n_join;

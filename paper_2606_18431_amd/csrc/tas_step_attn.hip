@@ -124,10 +124,10 @@ __device__ f4 get_part4(const float *from) {
 // Stores should fill whole lines: a wide item's lanes hold rows, so the fours of all its
 // rows are adjacent; a thin segment's few rows are whole.
 template <int D>
-__device__ int64_t part_at(const Seg &s, int64_t first_row, int row, int d) {
-    if (s.rows <= kThinRows) return (first_row + row) * D + d;
+__device__ int64_t part_at(int seg_rows, int64_t first_row, int row, int d) {
+    if (seg_rows <= kThinRows) return (first_row + row) * D + d;
     const int tile = row & ~(kWideRows - 1);
-    return (first_row + tile) * D + d * min(kWideRows, s.rows - tile) + (row - tile) * 4;
+    return (first_row + tile) * D + d * min(kWideRows, seg_rows - tile) + (row - tile) * 4;
 }
 __device__ float lse2(float l, float m) {
     return l > 0 ? m + log2f(l) : (l == l ? -INFINITY : l);  // NaN stays
@@ -167,7 +167,7 @@ __device__ __forceinline__ void thin_item(const AttnArgs &a, const Item &it, cha
     constexpr int VB = kThinKeys * D * 2;  // bytes of a wave's V
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int col = lane & 15, g = lane >> 4;
-    const Seg s = a.segs[it.seg];
+    const Seg &s = it.s;
     const Table tab = (Table)(a.tables + s.table);
 
     const int row = min(col, s.rows - 1), j = row / a.group;
@@ -310,7 +310,7 @@ __device__ __forceinline__ void thin_item(const AttnArgs &a, const Item &it, cha
                 ll += stat[w][r][1] * f;
                 y += *(const f4 *)((const float *)mine(w) + r * D + (d4 ^ r) * 4) * f;
             }
-            put_part(a.part_o + part_at<D>(s, it.part, r, d4 * 4), y * reciprocal(ll),
+            put_part(a.part_o + part_at<D>(s.rows, it.part, r, d4 * 4), y * reciprocal(ll),
                      it.unit >= 0);
             if (d4 == 0) put_part(a.part_lse + it.part + r, lse2(ll, mm), it.unit >= 0);
         }
@@ -380,7 +380,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
-    const Seg s = a.segs[it.seg];
+    const Seg &s = it.s;
     const Table tab = (Table)(a.tables + s.table);
 
     const int r = wave * 32 + col;  // row of the item
@@ -617,7 +617,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
 #pragma unroll
             for (int e = 0; e < 4; e++) {
                 const f4 x = {o[i][e * 4], o[i][e * 4 + 1], o[i][e * 4 + 2], o[i][e * 4 + 3]};
-                put_part(a.part_o + part_at<D>(s, first, it.row0 + r, i * 32 + e * 8 + half * 4),
+                put_part(a.part_o + part_at<D>(s.rows, first, it.row0 + r, i * 32 + e * 8 + half * 4),
                          x * f, false);
             }
         if (half == 0) put_part(a.part_lse + it.part + r, lse2(l, m), false);
@@ -651,20 +651,15 @@ __device__ __forceinline__ void join(const AttnArgs &a, const Unit &u) {
     constexpr int P = 8;
     const int d = threadIdx.x / kJoinRows * 8, r = threadIdx.x % kJoinRows;
     if (r >= u.rows || d >= D) return;
-    const Seg us = a.segs[u.seg];
+    const Seg &us = u.s;
     const int row = u.row0 + r, j = row / a.group, g = row - j * a.group;
     const int tok = us.t0 + j, head = u.hk * a.group + g;
-    const int n0 = us.nsplit;
-    int all = n0;
-    Seg os = us;
-    const int own = u.prefix ? a.tok_seg[tok] : -1;
-    if (own >= 0) {
-        os = a.segs[own];
-        all += os.nsplit;
-    }
+    Own own{};
+    if (u.prefix) own = a.tok_own[tok];
+    const int n0 = us.nsplit, all = n0 + own.nsplit;
     const int64_t first0 = us.part + (int64_t)u.hk * us.nsplit * us.rows;
-    const int64_t first1 = os.part + (int64_t)u.hk * os.nsplit * os.rows;
-    const int own_row = (tok - os.t0) * a.group + g;
+    const int64_t first1 = own.part + (int64_t)u.hk * own.nsplit * own.rows;
+    const int own_row = (tok - own.t0) * a.group + g;
     float m = -INFINITY, sum = 0, y[8] = {};
     bool bad = false;  // a NaN among the parts stays
     for (int n = 0; n < all; n += P) {
@@ -674,14 +669,14 @@ __device__ __forceinline__ void join(const AttnArgs &a, const Unit &u) {
         for (int i = 0; i < P; i++) {
             const int k = min(n + i, all - 1);
             const bool mine = k < n0;
-            const Seg &s = mine ? us : os;
-            const int64_t first =
-                mine ? first0 + (int64_t)k * us.rows : first1 + (int64_t)(k - n0) * os.rows;
+            const int rows = mine ? us.rows : own.rows;
+            const int64_t first = mine ? first0 + (int64_t)k * rows
+                                       : first1 + (int64_t)(k - n0) * rows;
             const int at = mine ? row : own_row;
             lse[i] = get_part<DEVICE>(a.part_lse + first + at);
 #pragma unroll
             for (int e = 0; e < 2; e++)
-                o[i][e] = get_part4<DEVICE>(a.part_o + part_at<D>(s, first, at, d + e * 4));
+                o[i][e] = get_part4<DEVICE>(a.part_o + part_at<D>(rows, first, at, d + e * 4));
         }
         float mn = m;
 #pragma unroll
@@ -725,7 +720,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     __shared__ __attribute__((aligned(16))) char v0_lds[WIDE ? TB : 16], v1_lds[WIDE ? TB : 16];
     __shared__ float stat[WIDE ? 1 : 4][kThinRows][2];
     const Item it = a.items[blockIdx.x];
-    if (WIDE && a.segs[it.seg].rows > kThinRows)
+    if (WIDE && it.s.rows > kThinRows)
         wide_item<T, D>(a, it, k0_lds, k1_lds, v0_lds, v1_lds);
     else
         thin_item<T, D>(a, it, k0_lds, k1_lds,

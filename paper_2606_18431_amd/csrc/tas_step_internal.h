@@ -31,18 +31,26 @@ struct Seg {
                           // results go to the output
     int32_t rows;         // n_tok * heads / kv_heads
 };
-// Rows row0.. of one key head of a segment against its keys k0 .. k1 - 1.
+// Rows row0.. of one key head of a segment against its keys k0 .. k1 - 1. (The segment
+// is held here, not pointed to: a workgroup's first loads wait for it.)
 struct Item {
+    Seg s;
     int32_t seg, hk, row0, k0, k1;
     int32_t part;  // partial row of row0, -1: output
     int32_t unit;  // the join that waits for this item, -1: none
+    int32_t pad;
 };
 // Rows row0 .. row0 + rows - 1 of one key head of a segment, the results of which are
 // partial ones; of a prefix's rows, the parts of the tokens' own segments too. Rows of
 // a thin segment are joined by the last of the `items` items that have a part of them,
 // those of a wide one by a second kernel.
 struct Unit {
-    int32_t seg, hk, row0, rows, items, prefix;
+    Seg s;
+    int32_t seg, hk, row0, rows, items, prefix, pad[2];
+};
+// Of a token under a prefix: where the parts of its own segment lie (nsplit 0: none).
+struct Own {
+    int32_t part, nsplit, rows, t0;
 };
 struct PlanHead {
     int64_t bytes;      // of the blob
@@ -50,7 +58,7 @@ struct PlanHead {
     int32_t n_req, n_tok, n_seg, n_thin, n_wide, n_join, n_merge, n_table;
     // byte offsets in the blob; the items as the workgroups take them; the units those of thin segments (join), then the others (merge); done holds a
     // counter for each of the first, zero between launches
-    int64_t req, seg, items, units, tables, tok_req, tok_seg, done;
+    int64_t req, seg, items, units, tables, tok_req, tok_own, done;
 };
 
 struct AppendArgs {
@@ -68,11 +76,10 @@ struct AppendArgs {
 };
 
 struct AttnArgs {
-    const Seg *segs;
     const Item *items;
     const int32_t *tables;
     const Unit *units, *merge;
-    const int32_t *tok_seg;  // own segments
+    const Own *tok_own;
     uint32_t *done;
     const void *q;
     void *out;

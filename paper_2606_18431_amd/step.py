@@ -176,6 +176,7 @@ class Step:
                  n_blocks, prefix_first=None, prefix_len=None, prefix_blocks=None, causal=True,
                  device="cuda"):
         self.ctx = None
+        self._lib = lib()
         b, keep = make_batch(n_new, kv_len, blocks, heads=heads, kv_heads=kv_heads,
                              head_dim=head_dim, block_tokens=block_tokens, n_blocks=n_blocks,
                              prefix_first=prefix_first, prefix_len=prefix_len,
@@ -244,18 +245,19 @@ class Step:
     def _enqueue(self, call, args, stream):
         if self.ctx is None:
             raise ValueError("the step is closed")
-        index = self.index
         if stream is None:
-            raw = torch._C._cuda_getCurrentRawStream(index)
+            raw = torch._C._cuda_getCurrentRawStream(self.index)
         else:
             raw = stream.cuda_stream
         if raw != self._home:  # the workspace outlives the work there
             self.ws.record_stream(torch.cuda.ExternalStream(raw) if stream is None else stream)
-        if torch.cuda.current_device() == index:
-            call(self.ctx, args, raw)
+        if torch._C._cuda_getDevice() == self.index:
+            rc = call(self.ctx, ctypes.byref(args), raw)
         else:
             with torch.cuda.device(self.device):
-                call(self.ctx, args, raw)
+                rc = call(self.ctx, ctypes.byref(args), raw)
+        if rc != TAS_OK:
+            raise TasError(rc, call.__name__)
 
     # ------------------------------------------------------------ the operators
 
@@ -294,8 +296,8 @@ class Step:
             q_weight, k_weight = q_weight.data_ptr(), k_weight.data_ptr()
         out = self._out(out, qkv, stream)
         out_p, out_s = self._rows(out, self.q_shape, qkv.dtype, "out")
-        self._enqueue(tas_step_append,
-                      tas_append(dtype, rot, bool(interleaved), eps, qkv_p, qkv_s, out_p, out_s,
+        self._enqueue(self._lib.tas_step_append,
+                      tas_append(dtype, rot, 1 if interleaved else 0, eps, qkv_p, qkv_s, out_p, out_s,
                                  q_weight, k_weight, cos_p, sin_p, positions, cache), stream)
         return out
 
@@ -317,7 +319,7 @@ class Step:
             lse = lse.data_ptr()
         if scale is None:
             scale = self.head_dim ** -0.5
-        self._enqueue(tas_step_attention,
+        self._enqueue(self._lib.tas_step_attention,
                       tas_attention(dtype, scale, q_p, q_s, out_p, out_s, lse, cache), stream)
         return out
 

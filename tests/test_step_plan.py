@@ -17,13 +17,16 @@ REQ = np.dtype([(f, np.int32) for f in ("t0", "n_new", "kv_len", "table", "prefi
                                         "pre_seg", "pad")])
 SEG = np.dtype([(f, np.int32) for f in ("t0", "n_tok", "kv_len", "lim0", "table", "nsplit", "part",
                                         "rows")])
-ITEM = np.dtype([(f, np.int32) for f in ("seg", "hk", "row0", "k0", "k1", "part", "unit")])
-UNIT = np.dtype([(f, np.int32) for f in ("seg", "hk", "row0", "rows", "items", "prefix")])
+ITEM = np.dtype([("s", SEG)] + [(f, np.int32) for f in ("seg", "hk", "row0", "k0", "k1", "part",
+                                                        "unit", "pad")])
+UNIT = np.dtype([("s", SEG)] + [(f, np.int32) for f in ("seg", "hk", "row0", "rows", "items",
+                                                        "prefix", "pad0", "pad1")])
+OWN = np.dtype([(f, np.int32) for f in ("part", "nsplit", "rows", "t0")])
 HEAD = np.dtype([("bytes", np.int64), ("part_rows", np.int64)]
                 + [(f, np.int32) for f in ("n_req", "n_tok", "n_seg", "n_thin", "n_wide",
                                            "n_join", "n_merge", "n_table")]
                 + [(f, np.int64) for f in ("req", "seg", "items", "units", "tables", "tok_req",
-                                           "tok_seg", "done")])
+                                           "tok_own", "done")])
 THIN_ROWS, WIDE_ROWS, JOIN_ROWS = 16, 128, 16
 
 
@@ -50,7 +53,7 @@ def plan(b):
                 units=at(h["units"], UNIT, h["n_join"] + h["n_merge"]),
                 tables=at(h["tables"], np.int32, h["n_table"]),
                 tok_req=at(h["tok_req"], np.int32, h["n_tok"]),
-                tok_seg=at(h["tok_seg"], np.int32, h["n_tok"]),
+                tok_own=at(h["tok_own"], OWN, h["n_tok"] if b.n_prefix else 0),
                 done=at(h["done"], np.int32, h["n_join"]))
 
 
@@ -107,6 +110,7 @@ def test_plan_covers_every_visible_key_once(case):
     for kind, tile in (("thin", THIN_ROWS), ("wide", WIDE_ROWS)):
         for it in p[kind]:
             s = p["segs"][it["seg"]]
+            assert s == it["s"]
             assert (s["rows"] <= THIN_ROWS) == (kind == "thin")
             assert 0 <= it["hk"] < Hk and it["row0"] % tile == 0 and it["row0"] < s["rows"]
             rows = min(tile, s["rows"] - it["row0"])
@@ -130,6 +134,7 @@ def test_plan_covers_every_visible_key_once(case):
     joined = {}
     for u, un in enumerate(p["units"]):
         s = p["segs"][un["seg"]]
+        assert s == un["s"]
         assert un["row0"] % JOIN_ROWS == 0 and un["row0"] + un["rows"] <= s["rows"]
         assert un["rows"] == min(JOIN_ROWS, s["rows"] - un["row0"])
         assert (u < n_join) == (s["rows"] <= THIN_ROWS)
@@ -188,7 +193,11 @@ def test_plan_covers_every_visible_key_once(case):
             for j in range(t, t + n[i]):
                 for hk in range(Hk):
                     assert all(((j, hk, x) in joined) == parts for x in range(G))
-        assert (p["tok_seg"][t:t + n[i]] == r["own_seg"]).all()
+        for own in p["tok_own"][t:t + n[i]]:
+            if r["own_seg"] < 0:
+                assert own["nsplit"] == 0
+            else:
+                assert all(own[f] == p["segs"][r["own_seg"]][f] for f in OWN.names)
         t += int(n[i])
 
 
