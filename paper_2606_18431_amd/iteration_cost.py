@@ -1,0 +1,199 @@
+"""What an iteration's attention costs on this GPU, in the cost model's terms.
+
+The simulator prices an iteration as base + tok * sum(n) + sum(ctx) / div
+microseconds (``workloads.Engine``). This command forms iterations of a workload
+as its scheduler would have them in progress, runs their attention part on the
+GPU as a model's layers do (``step.Step``: norm, rotate and append the new tokens,
+then attend over the pages) and fits the three coefficients to the times:
+
+    python -m paper_2606_18431_amd.iteration_cost --cfg 4 --layers 32
+
+``--prefix N`` puts N shared tokens (a system prompt, computed once) before every
+request's own context. The weights' part of an iteration (its matrix products)
+is not in the times: add it to base and tok from the model's own measurements.
+"""
+from __future__ import annotations
+
+import argparse
+import dataclasses
+
+import numpy as np
+
+from . import workloads as W
+
+
+@dataclasses.dataclass
+class Iteration:
+    """One iteration's batch: new tokens and context of every request in it (the
+    new ones included), and the blocks that hold the contexts."""
+
+    n_new: np.ndarray
+    kv_len: np.ndarray
+    blocks: np.ndarray  # [requests, pages], -1 beyond a context
+
+    @property
+    def tokens(self) -> int:
+        return int(self.n_new.sum())
+
+    @property
+    def context(self) -> int:
+        return int(self.kv_len.sum())
+
+
+def form_iteration(w: W.Workload, trace: int, first: int, rng, prefix_blocks: int = 0) -> Iteration:
+    """An iteration in the middle of a run: requests from ``first`` on, each somewhere
+    in its life (every one of its prefill chunks and decode steps is equally likely),
+    admitted while the engine's sequence cap, token budget and KV blocks last.
+    ``prefix_blocks`` of the pool are taken by shared tokens."""
+    e = w.engine
+    n_new, kv_len = [], []
+    used = prefix_blocks
+    budget = e.max_tokens
+    for i in range(first, first + 4 * e.max_seqs):
+        p, d = int(w.prompt[trace, i % w.n_req]), int(w.decode[trace, i % w.n_req])
+        chunks = -(-p // e.chunk)
+        at = int(rng.integers(0, chunks + d - 1)) if chunks + d > 1 else 0
+        if at < chunks:
+            kv = min((at + 1) * e.chunk, p)
+            n = kv - at * e.chunk
+        else:
+            kv, n = p + at - chunks + 1, 1
+        n_pages = -(-kv // e.block_tokens)
+        if n > budget or used + n_pages > e.kv_blocks or len(n_new) == e.max_seqs:
+            break
+        n_new.append(n)
+        kv_len.append(kv)
+        used += n_pages
+        budget -= n
+    if not n_new:
+        raise ValueError("no request fits the engine's budgets")
+    n_new, kv_len = np.asarray(n_new), np.asarray(kv_len)
+    pages = -(-kv_len // e.block_tokens)
+    ids = prefix_blocks + rng.permutation(e.kv_blocks - prefix_blocks)
+    blocks = np.full((len(n_new), int(pages.max())), -1, np.int32)
+    at = 0
+    for i, n in enumerate(pages):
+        blocks[i, :n] = ids[at:at + n]
+        at += n
+    return Iteration(n_new, kv_len, blocks)
+
+
+class Layer:
+    """One layer's cache and the inputs of its attention, random values."""
+
+    def __init__(self, e: W.Engine, heads, kv_heads, head_dim, dtype, device, positions):
+        import torch
+
+        self.torch = torch
+        shape = (e.kv_blocks, kv_heads, e.block_tokens, head_dim)
+        g = torch.Generator(device=device)
+        g.manual_seed(0)
+        self.k_cache = torch.randn(shape, generator=g, device=device, dtype=dtype)
+        self.v_cache = torch.randn(shape, generator=g, device=device, dtype=dtype)
+        self.qkv = torch.randn((e.max_tokens, heads + 2 * kv_heads, head_dim), generator=g,
+                               device=device, dtype=dtype)
+        self.weight = torch.ones(head_dim, device=device, dtype=dtype)
+        freq = 1e4 ** (-torch.arange(0, head_dim, 2, device=device, dtype=torch.float64) / head_dim)
+        angle = torch.arange(positions, device=device, dtype=torch.float64)[:, None] * freq
+        self.cos, self.sin = angle.cos().float(), angle.sin().float()
+
+    def run(self, step):
+        """The attention of one layer for the step's batch; returns its output."""
+        q = step.append(self.qkv[:step.tokens], self.k_cache, self.v_cache, self.cos, self.sin,
+                        q_weight=self.weight, k_weight=self.weight)
+        return step.attention(q, self.k_cache, self.v_cache)
+
+    def time_us(self, step, layers: int, repeats: int = 3) -> float:
+        """Microseconds of ``layers`` layers, one after another."""
+        torch = self.torch
+        self.run(step)
+        best = float("inf")
+        for _ in range(repeats):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            for _ in range(layers):
+                self.run(step)
+            b.record()
+            b.synchronize()
+            best = min(best, a.elapsed_time(b) * 1e3)
+        return best
+
+
+def fit(tokens, context, us):
+    """(base, tok, div, share of the variance explained) of us = base + tok * tokens
+    + context / div, by least squares with no coefficient below zero."""
+    x = np.stack([np.ones(len(us)), np.asarray(tokens, float), np.asarray(context, float)], 1)
+    y = np.asarray(us, float)
+    keep = [0, 1, 2]
+    while True:
+        c, *_ = np.linalg.lstsq(x[:, keep], y, rcond=None)
+        if (c >= 0).all() or len(keep) == 1:
+            break
+        keep.remove(keep[int(np.argmin(c))])
+    full = np.zeros(3)
+    full[keep] = np.maximum(c, 0)
+    left = ((y - x @ full) ** 2).sum()
+    var = ((y - y.mean()) ** 2).sum()
+    return full[0], full[1], (1 / full[2] if full[2] > 0 else float("inf")), \
+        1 - left / var if var > 0 else 1.0
+
+
+def measure(w: W.Workload, *, iterations=24, layers=32, heads=32, kv_heads=8, head_dim=128,
+            dtype="bf16", prefix=0, seed=0, device="cuda", say=lambda line: None):
+    """Times of ``iterations`` iterations of the workload; a list of (requests, tokens,
+    context, microseconds), context with the prefix counted for every request."""
+    import torch
+
+    from . import step as S
+
+    e = w.engine
+    rng = np.random.default_rng([seed, 31])
+    prefix_pages = -(-prefix // e.block_tokens)
+    positions = prefix + int((w.prompt.astype(np.int64) + w.decode).max())
+    layer = Layer(e, heads, kv_heads, head_dim,
+                  {"bf16": torch.bfloat16, "f16": torch.float16}[dtype], device, positions)
+    rows = []
+    for i in range(iterations):
+        it = form_iteration(w, int(rng.integers(0, w.n_traces)), int(rng.integers(0, w.n_req)), rng,
+                            prefix_pages)
+        shared = dict(prefix_first=[0, len(it.n_new)], prefix_len=[prefix],
+                      prefix_blocks=np.arange(prefix_pages)[None]) if prefix else {}
+        step = S.Step(it.n_new, it.kv_len, it.blocks, heads=heads, kv_heads=kv_heads,
+                      head_dim=head_dim, block_tokens=e.block_tokens, n_blocks=e.kv_blocks,
+                      device=device, **shared)
+        us = layer.time_us(step, layers)
+        step.close()
+        rows.append((len(it.n_new), it.tokens, it.context + prefix * len(it.n_new), us))
+        say(f"{rows[-1][0]:4d} requests {rows[-1][1]:6d} tokens {rows[-1][2]:8d} context "
+            f"{us:10.1f} us")
+    return rows
+
+
+def main(argv=None):
+    p = argparse.ArgumentParser(description=__doc__.split("\n")[0])
+    p.add_argument("--cfg", type=int, default=4, help="workload (0 to 5)")
+    p.add_argument("--iterations", type=int, default=24)
+    p.add_argument("--layers", type=int, default=32)
+    p.add_argument("--heads", type=int, default=32)
+    p.add_argument("--kv-heads", type=int, default=8)
+    p.add_argument("--head-dim", type=int, default=128)
+    p.add_argument("--dtype", choices=["bf16", "f16"], default="bf16")
+    p.add_argument("--prefix", type=int, default=0, help="shared tokens before every request")
+    p.add_argument("--seed", type=int, default=0)
+    a = p.parse_args(argv)
+    w = W.make(a.cfg, n_traces=1, n_settings=4 if a.cfg != 0 else None)
+    rows = measure(w, iterations=a.iterations, layers=a.layers, heads=a.heads,
+                   kv_heads=a.kv_heads, head_dim=a.head_dim, dtype=a.dtype, prefix=a.prefix,
+                   seed=a.seed, say=lambda line: print(line, flush=True))
+    _, tokens, context, us = zip(*rows)
+    base, tok, div, r2 = fit(tokens, context, us)
+    print(f"{w.name}, {a.layers} layers of {a.heads}/{a.kv_heads} heads of {a.head_dim}, "
+          f"{a.dtype}: attention of an iteration = {base:.0f} + {tok:.4f} * tokens + context / "
+          f"{div:.1f} us ({100 * r2:.1f}% of the variance)")
+    e = w.engine
+    print(f"the workload's engine prices the whole iteration at {e.iter_base_us} + "
+          f"{e.iter_tok_us} * tokens + context / {e.iter_ctx_div} us")
+
+
+if __name__ == "__main__":
+    main()

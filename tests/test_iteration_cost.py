@@ -1,0 +1,57 @@
+"""Iterations formed from a workload keep the engine's budgets, and the fit returns
+the coefficients that made its data (no GPU); on a GPU, a short measurement."""
+import numpy as np
+import pytest
+
+from paper_2606_18431_amd import iteration_cost as C
+from paper_2606_18431_amd import workloads as W
+
+
+@pytest.mark.parametrize("cfg", [0, 2, 4, 5])
+@pytest.mark.parametrize("prefix_blocks", [0, 33])
+def test_iterations_keep_the_budgets(cfg, prefix_blocks):
+    w = W.make(cfg, n_traces=1, n_req=400)
+    e = w.engine
+    rng = np.random.default_rng(5)
+    mixed = 0
+    for first in (0, 17, 390):
+        it = C.form_iteration(w, 0, first, rng, prefix_blocks)
+        assert 1 <= len(it.n_new) <= e.max_seqs
+        assert it.tokens <= e.max_tokens and (it.n_new >= 1).all() and (it.n_new <= e.chunk).all()
+        assert (it.kv_len >= it.n_new).all()
+        used = it.blocks[it.blocks >= 0]
+        assert len(used) == len(set(used.tolist())) == (-(-it.kv_len // e.block_tokens)).sum()
+        assert len(used) + prefix_blocks <= e.kv_blocks
+        assert used.min() >= prefix_blocks and used.max() < e.kv_blocks
+        for i, kv in enumerate(it.kv_len):
+            r = (first + i) % w.n_req
+            p, d = int(w.prompt[0, r]), int(w.decode[0, r])
+            # a chunk of the prompt, or a decode step that is not the last token's
+            assert (it.n_new[i] == 1 and p < kv <= p + d - 1) or \
+                (kv <= p and (kv == p or kv % e.chunk == 0)
+                 and it.n_new[i] == kv - (kv - 1) // e.chunk * e.chunk)
+            mixed |= 1 if it.n_new[i] == 1 else 2
+    assert mixed & 1
+
+
+def test_fit_returns_the_coefficients():
+    rng = np.random.default_rng(1)
+    tokens, context = rng.integers(1, 8192, 40), rng.integers(1, 400_000, 40)
+    base, tok, div, r2 = C.fit(tokens, context, 300 + 0.5 * tokens + context / 64)
+    assert abs(base - 300) < 1e-6 and abs(tok - 0.5) < 1e-9 and abs(div - 64) < 1e-6 and r2 > 1 - 1e-9
+    base, tok, div, r2 = C.fit(tokens, context, 100 - 0.001 * tokens + context / 50)
+    assert tok == 0 and base > 0 and abs(div - 50) < 2 and r2 > 0.9
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prefix", [0, 100])
+def test_measure_runs_the_operators(prefix):
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    w = W.make(1, n_traces=1, n_settings=4, n_req=200)
+    rows = C.measure(w, iterations=4, layers=2, heads=8, kv_heads=2, head_dim=64, dtype="f16",
+                     prefix=prefix)
+    assert len(rows) == 4
+    for n, tokens, context, us in rows:
+        assert n >= 1 and tokens >= n and context >= tokens and 0 < us < 1e6
