@@ -149,6 +149,30 @@ __device__ void store_row(const AttnArgs &a, const Seg &s, const Item &it, int r
     if (d == 0 && a.lse) a.lse[tok * a.heads + head] = lse2(l, m) * kLn2;
 }
 
+// Keys that some of an item's rows see and others do not: a weight of 0 does not take
+// out a value of V that is not finite, so such values are zeroed there and the key is
+// marked; a row that sees a marked key becomes NaN.
+template <typename T>
+__device__ uint32_t not_finite(uint32_t x) {  // bits 15 and 31: of the two values
+    constexpr uint32_t E = sizeof(T) == 2 && __is_same(T, _Float16) ? 0x7c00u : 0x7f80u;
+    constexpr uint32_t ONE = E & (0u - E);
+    return ((x & (E | E << 16)) + (ONE | ONE << 16)) & 0x80008000u;
+}
+template <typename T>
+__device__ bool any_not_finite(u4 x) {
+    return (not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) |
+            not_finite<T>(x[3])) != 0;
+}
+template <typename T>
+__device__ u4 zero_not_finite(u4 x) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const uint32_t b = not_finite<T>(x[i]);
+        x[i] &= ~((b >> 15 & 0x10001u) * 0xffffu);
+    }
+    return x;
+}
+
 // 16 bytes that are read once: they need not stay in the caches (decode of 256 requests,
 // 448k tokens of 8 heads of 128: 282 us, with ordinary loads 311).
 __device__ u4 stream(const char *p) { return __builtin_nontemporal_load((const u4 *)p); }
@@ -240,6 +264,19 @@ __device__ __forceinline__ void thin_item(const AttnArgs &a, const Item &it, cha
 #pragma unroll
             for (int i = 0; i < VL; i++)
                 if (base + i * (64 / LPR) + vrow >= it.k1) v[i] = u4{0, 0, 0, 0};
+        uint32_t marked = 0;  // of the 32 keys
+        if (base + kThinKeys > full && full < it.k1) {
+#pragma unroll
+            for (int i = 0; i < VL; i++) {
+                const uint64_t lanes = __ballot(any_not_finite<T>(v[i]));
+                if (lanes) {
+                    v[i] = zero_not_finite<T>(v[i]);
+                    for (int y = 0; y < 64 / LPR; y++)
+                        if (lanes >> (y * LPR) & ((1u << LPR) - 1))
+                            marked |= 1u << (i * (64 / LPR) + y);
+                }
+            }
+        }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int i = 0; i < VL; i++)
@@ -256,6 +293,12 @@ __device__ __forceinline__ void thin_item(const AttnArgs &a, const Item &it, cha
 #pragma unroll
                 for (int i = 0; i < 4; i++)
                     if (base + n * 16 + g * 4 + i >= lim) sc[n][i] = -INFINITY;
+        if (marked)
+#pragma unroll
+            for (int n = 0; n < 2; n++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    if ((marked >> (n * 16 + g * 4 + i) & 1) && sc[n][i] != -INFINITY) l = NAN;
         float mt = -INFINITY;
 #pragma unroll
         for (int n = 0; n < 2; n++)
@@ -360,6 +403,7 @@ __device__ __forceinline__ void mix() {
         mix<N - 1, VECTOR, READS>();
     }
 }
+constexpr int kMarks = 8;  // words of 32 keys
 constexpr int kWaitLoads = 0x0F70;  // s_waitcnt: no load or store outstanding
 
 // 128 rows against a run of keys, 64 keys a step: 32 rows to a wave, K and V of a
@@ -370,7 +414,8 @@ constexpr int kWaitLoads = 0x0F70;  // s_waitcnt: no load or store outstanding
 // whole step to arrive.
 template <typename T, int D>
 __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, char *k0_lds,
-                                          char *k1_lds, char *v0_lds, char *v1_lds) {
+                                          char *k1_lds, char *v0_lds, char *v1_lds,
+                                          uint32_t *marked) {
     using V = vec8<T>;
     constexpr int QS = D / 16;             // steps of 16 over d
     constexpr int LPR = D / 8;             // chunks of 16 bytes of a row
@@ -435,15 +480,29 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
     };
     auto load_k = [&](char *to) { load(to, kbase + klane, 0); };
     auto load_v = [&](char *to) { load(to, vbase + vlane, 4); };
+    // The rows see the keys from here on to the end differently (at most 128 + 63 keys;
+    // a bit each in `marked`).
+    const int differ = full < it.k1 ? full & ~31 : it.k1;
+    if (full < it.k1) {
+        if (tid < kMarks) marked[tid] = 0;
+        __syncthreads();
+    }
     // Waits for the loads; slots past the keys hold anything, and weight 0 times it
     // has to be 0: a wave clears what it loaded of them.
-    auto arrive = [&](char *v, int base) {
+    auto arrive = [&](char *v, int base, bool edge) {
         __builtin_amdgcn_s_waitcnt(kWaitLoads);
-        if (base + kWideKeys > it.k1)
+        if (edge && base + kWideKeys > differ)
 #pragma unroll
-            for (int i = 0; i < NL; i++)
-                if (base + y0(i) + lrow >= it.k1)
-                    *(u4 *)(v + (i * 4 + wave) * 1024 + lane * 16) = u4{0, 0, 0, 0};
+            for (int i = 0; i < NL; i++) {
+                u4 *at = (u4 *)(v + (i * 4 + wave) * 1024 + lane * 16);
+                const int y = base + y0(i) + lrow;
+                if (y >= it.k1) {
+                    *at = u4{0, 0, 0, 0};
+                } else if (y >= differ && any_not_finite<T>(*at)) {
+                    *at = zero_not_finite<T>(*at);
+                    atomicOr(marked + ((y - differ) >> 5), 1u << (y & 31));
+                }
+            }
         __syncthreads();
     };
 
@@ -487,6 +546,16 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
 #pragma unroll
         for (int e = 0; e < 16; e++)
             if (base + (e >> 2) * 8 + half * 4 + (e & 3) >= lim) sc[e] = -INFINITY;
+    };
+    // (the V of these keys has arrived, so their marks are complete)
+    auto poison = [&](const f16x &sc, int base) {
+        if (base < differ || base >= it.k1) return;
+        const uint32_t bits = marked[(base - differ) >> 5];
+        if (bits)
+#pragma unroll
+            for (int e = 0; e < 16; e++)
+                if ((bits >> ((e >> 2) * 8 + half * 4 + (e & 3)) & 1) && sc[e] != -INFINITY)
+                    l = NAN;
     };
     auto largest = [&](const f16x &sc) {
         float mt = -INFINITY;
@@ -532,10 +601,12 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
     constexpr int HB = TB / 2;  // bytes of 32 rows
     f16x sa, sb;
     V p[2];
-    auto step = [&](auto which, int base) {
-        constexpr int B = decltype(which)::value;
+    // EDGE: its keys and the next ones may be seen by some rows only.
+    auto step = [&](auto which, auto edge, int base) {
+        constexpr int B = decltype(which)::value, EDGE = decltype(edge)::value;
         const char *kl = B ? k1_lds : k0_lds, *vl = B ? v1_lds : v0_lds;
         const int next = base + kWideKeys;
+        if (EDGE) poison(sa, base);
         read_k(kl);
         place();
         load_v(B ? v0_lds : v1_lds);
@@ -547,24 +618,25 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
         read_v(vl);
         mix<QS, 56 / QS, D / 8 / QS>();
         __builtin_amdgcn_sched_barrier(0);
-        if (next > full) hide(sb, base + 32);
+        if (EDGE) hide(sb, base + 32);
         products(p);
         read_k(kl + HB);
         const float mb = largest(sb);
         mix<D / 16, 4, QS / (D / 16)>();
         raise(mb);
+        if (EDGE) poison(sb, base + 32);
         __builtin_amdgcn_sched_barrier(0);
         scores(sa);
         weights(p, sb);
         read_v(vl + HB);
         mix<QS, 56 / QS, D / 8 / QS>();
         __builtin_amdgcn_sched_barrier(0);
-        if (next + 32 > full) hide(sa, next);
+        if (EDGE) hide(sa, next);
         products(p);
         const float ma = largest(sa);
         mix<D / 16, 4, 0>();
         raise(ma);
-        arrive(B ? v0_lds : v1_lds, next);
+        arrive(B ? v0_lds : v1_lds, next, EDGE);
     };
     if (it.k0 < it.k1) {
         int base = it.k0;
@@ -576,23 +648,29 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
         place();
         load_k(k0_lds);
         look_up(base + kWideKeys, base + kWideKeys + 32);
-        arrive(v0_lds, base);
+        arrive(v0_lds, base, true);
         read_k(k1_lds);
         scores(sa);
         hide(sa, base);
         raise(largest(sa));
         __syncthreads();  // the first step loads K where these were
         int steps = (it.k1 - base - 1) / kWideKeys;
+        for (; steps >= 2 && base + 3 * kWideKeys <= differ; steps -= 2) {
+            step(Const<0>{}, Const<0>{}, base);
+            step(Const<1>{}, Const<0>{}, base + kWideKeys);
+            base += 2 * kWideKeys;
+        }
         for (; steps >= 2; steps -= 2) {
-            step(Const<0>{}, base);
-            step(Const<1>{}, base + kWideKeys);
+            step(Const<0>{}, Const<1>{}, base);
+            step(Const<1>{}, Const<1>{}, base + kWideKeys);
             base += 2 * kWideKeys;
         }
         if (steps) {
-            step(Const<0>{}, base);
+            step(Const<0>{}, Const<1>{}, base);
             base += kWideKeys;
         }
         const char *kl = steps ? k1_lds : k0_lds, *vl = steps ? v1_lds : v0_lds;
+        poison(sa, base);
         weights(p, sa);
         read_v(vl);
         products(p);
@@ -600,6 +678,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
             read_k(kl);
             scores(sa);
             hide(sa, base + 32);
+            poison(sa, base + 32);
             raise(largest(sa));
             weights(p, sa);
             read_v(vl + HB);
@@ -707,21 +786,22 @@ __device__ __forceinline__ void join(const AttnArgs &a, const Unit &u) {
             bad ? NAN : lse2(sum, m) * kLn2;
 }
 
-// One item a workgroup. A thin item whose partial results have reached the device is counted for its unit, and the workgroup
-// that counts the last one joins the unit; the count is left at zero for the next
-// launch. (The rows of wide segments are left to the merge kernel: the workgroup that
+// One item a workgroup. A thin item whose partial results have reached the device is
+// counted for its unit, and the workgroup that counts the last one joins the unit; the
+// count is left at zero for the next launch. (The rows of wide segments are left to the merge kernel: the workgroup that
 // came last would join 128 rows one after another. Decode of 64 requests with a shared
 // prefix of 2048, 32/8 heads of 128: 71 us so, 25 us with the merge kernel.)
 template <typename T, int D, bool WIDE>
-__global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, WIDE ? 2 : 3) void attn_kernel(AttnArgs a) {
     constexpr int TB = kWideKeys * D * 2;
     // four objects, so that the compiler sees which loads a read has to wait for
     __shared__ __attribute__((aligned(16))) char k0_lds[TB], k1_lds[TB];
     __shared__ __attribute__((aligned(16))) char v0_lds[WIDE ? TB : 16], v1_lds[WIDE ? TB : 16];
     __shared__ float stat[WIDE ? 1 : 4][kThinRows][2];
+    __shared__ uint32_t marked[kMarks];
     const Item it = a.items[blockIdx.x];
     if (WIDE && it.s.rows > kThinRows)
-        wide_item<T, D>(a, it, k0_lds, k1_lds, v0_lds, v1_lds);
+        wide_item<T, D>(a, it, k0_lds, k1_lds, v0_lds, v1_lds, marked);
     else
         thin_item<T, D>(a, it, k0_lds, k1_lds,
                         WIDE ? (float (*)[kThinRows][2])(void *)v0_lds : stat);

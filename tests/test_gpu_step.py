@@ -278,6 +278,31 @@ def test_infinite_and_nan_keys_stay_with_their_rows(torch):
     assert torch.equal(got[0, 2:], want[0, 2:])
 
 
+@pytest.mark.parametrize("name", ["bf16", "f16"])
+@pytest.mark.parametrize("size", [64, 128])
+@pytest.mark.parametrize("n,kv,heads", [(5, 40, 2), (3, 90, 10), (70, 70, 1), (200, 333, 2),
+                                        (150, 160, 8)])
+def test_values_after_a_token_do_not_reach_it(torch, name, size, n, kv, heads):
+    """A new token's V that is infinite or NaN makes the tokens from it on NaN (a row as
+    a whole, or the element) and leaves those before it as they were."""
+    b = Batch(33, [n], [kv], heads, 1, size)
+    k, v = caches(torch, b, dtype_of(torch, name), 3)
+    q = torch.randn((n, heads, size)).to(k.dtype).cuda()
+    s = b.step()
+    clean = s.attention(q, k, v)
+    for bad in (n - 1, n // 2, n // 3):
+        for value in (math.nan, math.inf, -math.inf):
+            y = kv - n + bad
+            v2 = v.clone()
+            v2[b.blocks[0, y // 16], 0, y % 16, 7] = value
+            got = s.attention(q, k, v2)
+            assert torch.equal(got[:bad], clean[:bad])
+            assert not torch.isfinite(got[bad:, :, 7]).any()
+            k2 = k.clone()
+            k2[b.blocks[0, y // 16], 0, y % 16] = value
+            assert torch.equal(s.attention(q, k2, v)[:bad], clean[:bad])
+
+
 def test_strided_queries_output_in_place_and_determinism(torch):
     b = Batch(14, [1, 60, 3], [3000, 80, 700], 8, 2, 128)
     k, v = caches(torch, b, torch.bfloat16, 4)
