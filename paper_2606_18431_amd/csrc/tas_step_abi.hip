@@ -288,7 +288,8 @@ int make_plan(const tas_batch *b, Plan &p) {
         p.reqs.push_back(r);
         t += n;
     }
-    if (t * G > INT32_MAX / 2) return TAS_EINVAL;
+    // rows and heads of the batch are counted in 32 bits
+    if (t * (b->heads + 2 * b->kv_heads) > INT32_MAX / 2) return TAS_EINVAL;
     if (p.appendable && !distinct_slots(b, p)) return TAS_EINVAL;
     const int rc = make_items(b, p);
     if (rc != TAS_OK) return rc;

@@ -16,6 +16,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 import torch
@@ -54,6 +55,14 @@ class tas_attention(ctypes.Structure):
     _fields_ = [("dtype", _i32), ("scale", ctypes.c_float), ("q", _P), ("q_stride", _i64),
                 ("out", _P), ("out_stride", _i64), ("lse", _P), ("cache", tas_cache)]
 
+
+# The same two structs for Step's calls, which are made for every layer: packing takes
+# a third of the time of a ctypes constructor.
+_CACHE = "PPqqqqqq"
+_APPEND = struct.Struct("iiifPqPqPPPPq" + _CACHE)
+_ATTENTION = struct.Struct("ifPqPqP" + _CACHE)
+assert _APPEND.size == ctypes.sizeof(tas_append)
+assert _ATTENTION.size == ctypes.sizeof(tas_attention)
 
 EXPORTS = ["tas_step_create", "tas_step_bytes", "tas_step_bind", "tas_step_destroy",
            "tas_step_tokens", "tas_step_append", "tas_step_attention", "tas_step_plan"]
@@ -170,13 +179,16 @@ class Step:
     (a permuted view serves other orders) whose last is 1. Calls are enqueued on
     ``stream`` (a torch stream; default: the current one); outputs are allocated
     on that stream unless given. Attention calls of one step share its
-    workspace: keep them on one stream, or order them."""
+    workspace: keep them on one stream, or order them. A step is used by one host thread
+    at a time."""
 
     def __init__(self, n_new, kv_len, blocks, *, heads, kv_heads, head_dim, block_tokens,
                  n_blocks, prefix_first=None, prefix_len=None, prefix_blocks=None, causal=True,
                  device="cuda"):
         self.ctx = None
         self._lib = lib()
+        self._args = ctypes.create_string_buffer(max(_APPEND.size, _ATTENTION.size))
+        self._args_p = ctypes.addressof(self._args)
         b, keep = make_batch(n_new, kv_len, blocks, heads=heads, kv_heads=kv_heads,
                              head_dim=head_dim, block_tokens=block_tokens, n_blocks=n_blocks,
                              prefix_first=prefix_first, prefix_len=prefix_len,
@@ -235,14 +247,17 @@ class Step:
         return code
 
     def _out(self, out, like, stream):
+        """The output, its address and its token stride."""
         if out is not None:
-            return out
+            return (out, *self._rows(out, self.q_shape, like.dtype, "out"))
         if stream is None:
-            return like.new_empty(self.q_shape)
-        with torch.cuda.stream(stream):
-            return like.new_empty(self.q_shape)
+            out = like.new_empty(self.q_shape)
+        else:
+            with torch.cuda.stream(stream):
+                out = like.new_empty(self.q_shape)
+        return out, out.data_ptr(), self.heads * self.head_dim
 
-    def _enqueue(self, call, args, stream):
+    def _enqueue(self, call, stream):
         if self.ctx is None:
             raise ValueError("the step is closed")
         if stream is None:
@@ -252,10 +267,10 @@ class Step:
         if raw != self._home:  # the workspace outlives the work there
             self.ws.record_stream(torch.cuda.ExternalStream(raw) if stream is None else stream)
         if torch._C._cuda_getDevice() == self.index:
-            rc = call(self.ctx, ctypes.byref(args), raw)
+            rc = call(self.ctx, self._args_p, raw)
         else:
             with torch.cuda.device(self.device):
-                rc = call(self.ctx, ctypes.byref(args), raw)
+                rc = call(self.ctx, self._args_p, raw)
         if rc != TAS_OK:
             raise TasError(rc, call.__name__)
 
@@ -272,17 +287,17 @@ class Step:
         dtype = self._dtype(qkv, "qkv")
         qkv_p, qkv_s = self._rows(qkv, self.qkv_shape, qkv.dtype, "qkv")
         cache = self._cache(k_cache, v_cache, qkv.dtype)
-        rot = positions = 0
-        cos_p = sin_p = None
+        rot = positions = cos_p = sin_p = qw_p = kw_p = 0
         if (cos is None) != (sin is None):
             raise ValueError("cos and sin: both or neither")
         if cos is not None:
             shape = cos.shape
-            for t in (cos, sin):
-                if t.dtype != torch.float32 or t.get_device() != self.index \
-                        or t.shape != shape or len(shape) != 2 or not t.is_contiguous():
-                    raise ValueError("cos and sin: contiguous float32 [positions, rot_dim / 2] "
-                                     f"on {self.device}")
+            if len(shape) != 2 or sin.shape != shape or cos.dtype != torch.float32 \
+                    or sin.dtype != torch.float32 or cos.get_device() != self.index \
+                    or sin.get_device() != self.index or not cos.is_contiguous() \
+                    or not sin.is_contiguous():
+                raise ValueError("cos and sin: contiguous float32 [positions, rot_dim / 2] "
+                                 f"on {self.device}")
             positions, rot = shape[0], 2 * shape[1]
             cos_p, sin_p = cos.data_ptr(), sin.data_ptr()
         if (q_weight is None) != (k_weight is None):
@@ -290,15 +305,14 @@ class Step:
         if q_weight is not None:
             for t in (q_weight, k_weight):
                 if t.dtype != qkv.dtype or t.get_device() != self.index \
-                        or t.shape != (self.head_dim,) or not t.is_contiguous():
+                        or t.shape != self.q_shape[2:] or not t.is_contiguous():
                     raise ValueError(f"weights: contiguous {qkv.dtype} [{self.head_dim}] on "
                                      f"{self.device}")
-            q_weight, k_weight = q_weight.data_ptr(), k_weight.data_ptr()
-        out = self._out(out, qkv, stream)
-        out_p, out_s = self._rows(out, self.q_shape, qkv.dtype, "out")
-        self._enqueue(self._lib.tas_step_append,
-                      tas_append(dtype, rot, 1 if interleaved else 0, eps, qkv_p, qkv_s, out_p, out_s,
-                                 q_weight, k_weight, cos_p, sin_p, positions, cache), stream)
+            qw_p, kw_p = q_weight.data_ptr(), k_weight.data_ptr()
+        out, out_p, out_s = self._out(out, qkv, stream)
+        _APPEND.pack_into(self._args, 0, dtype, rot, 1 if interleaved else 0, eps, qkv_p, qkv_s,
+                          out_p, out_s, qw_p, kw_p, cos_p, sin_p, positions, *cache)
+        self._enqueue(self._lib.tas_step_append, stream)
         return out
 
     def attention(self, q, k_cache, v_cache, *, scale=None, out=None, lse=None, stream=None):
@@ -309,18 +323,18 @@ class Step:
         dtype = self._dtype(q, "q")
         q_p, q_s = self._rows(q, self.q_shape, q.dtype, "q")
         cache = self._cache(k_cache, v_cache, q.dtype)
-        out = self._out(out, q, stream)
-        out_p, out_s = self._rows(out, self.q_shape, q.dtype, "out")
+        out, out_p, out_s = self._out(out, q, stream)
+        lse_p = 0
         if lse is not None:
             if lse.dtype != torch.float32 or lse.get_device() != self.index \
                     or lse.shape != self.q_shape[:2] or not lse.is_contiguous():
                 raise ValueError(f"lse: contiguous float32 {(self.tokens, self.heads)} on "
                                  f"{self.device}")
-            lse = lse.data_ptr()
+            lse_p = lse.data_ptr()
         if scale is None:
             scale = self.head_dim ** -0.5
-        self._enqueue(self._lib.tas_step_attention,
-                      tas_attention(dtype, scale, q_p, q_s, out_p, out_s, lse, cache), stream)
+        _ATTENTION.pack_into(self._args, 0, dtype, scale, q_p, q_s, out_p, out_s, lse_p, *cache)
+        self._enqueue(self._lib.tas_step_attention, stream)
         return out
 
     def close(self):

@@ -230,6 +230,9 @@ def test_refused_batches():
     assert not refused([1, 1], [20, 32], [[0, 1], [0, 3]])    # read by both, written by neither
     assert refused([20, 1], [20, 1], [[5, 5], [2, 3]])
     assert refused([1 << 25, 1], [1 << 25, 1], pages)
+    many = np.arange(1 << 16).reshape(1, -1)
+    assert not refused([1 << 19], [1 << 19], many, n_blocks=1 << 16, heads=32)
+    assert refused([1 << 20], [1 << 20], many, n_blocks=1 << 16, heads=1024, kv_heads=1024)
 
 
 def test_refused_prefixes():
