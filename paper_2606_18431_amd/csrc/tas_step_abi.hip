@@ -104,6 +104,23 @@ bool distinct_slots(const tas_batch *b, const Plan &p) {
     return std::adjacent_find(written.begin(), written.end()) == written.end();
 }
 
+// Pieces of a thin segment's keys: as many as give every slot its share of the batch,
+// but no more than pay. I steps of 128 keys in n pieces take about 0.9 I / n us, and
+// joining the n parts 2.2 us for every eight, in each of the sets of rows that a join
+// has threads for: that is least at n = 1.8 sqrt(I sets). A join as such costs some
+// 2 us, what three steps take. (One decode of 32/8 heads of 128: context 777 in pieces
+// of 256 keys 9.3 us, of 128 8.6; 32000 in 125 pieces 49 us, in 57 35.) Parts that the
+// merge kernel joins are one set, and two steps long at least.
+int64_t thin_pieces(const Seg &s, int64_t share, bool merged) {
+    const int64_t step = 4 * kThinKeys, steps = ceil_div(s.kv_len, step);
+    if (steps <= 3 && !merged) return 1;
+    int sets = 1;
+    while (!merged && sets * 2 * s.rows <= kJoinRows) sets *= 2;
+    const int64_t pay = (int64_t)(1.8 * std::sqrt((double)steps * sets));
+    const int64_t piece = merged ? std::max(share, 2 * step) : share;
+    return std::min(ceil_div(s.kv_len, piece), pay);
+}
+
 // Cuts the keys of the segments into items. A segment's keys are split into
 // nsplit pieces (the last ones shorter, or empty); every tile of its rows has an
 // item for each piece, an empty one where causality leaves nothing, so that a join
@@ -118,15 +135,19 @@ int make_items(const tas_batch *b, Plan &p) {
             wide_steps += (int64_t)tiles_of(s) * Hk * ceil_div(s.kv_len, kWideKeys);
     }
     const int64_t step = 4 * kThinKeys;
-    const int64_t thin_piece =
-        std::max<int64_t>(ceil_div(ceil_div(thin_keys, kThinItems), step) * step, 2 * step);
+    const int64_t thin_piece = ceil_div(ceil_div(thin_keys, kThinItems), step) * step;
     // steps of work for a slot; the thin items' 64 keys take about as long as a step
     const int64_t load = ceil_div(wide_steps + thin_keys / kWideKeys, kSlots);
     const int64_t wide_piece =
         std::max<int64_t>((int64_t)(load * kWideShare), kWideLeast) * kWideKeys;
-    for (Seg &s : p.segs) {
+    std::vector<char> joined(p.segs.size(), 0);  // with a prefix, by the merge kernel
+    for (const Req &r : p.reqs)
+        if (r.pre_seg >= 0 && r.own_seg >= 0) joined[r.own_seg] = !is_thin(p.segs[r.pre_seg]);
+    for (size_t i = 0; i < p.segs.size(); i++) {
+        Seg &s = p.segs[i];
         s.nsplit = (int32_t)std::max<int64_t>(
-            1, ceil_div(s.kv_len, is_thin(s) ? thin_piece : wide_piece));
+            1, is_thin(s) ? thin_pieces(s, thin_piece, joined[i])
+                          : ceil_div(s.kv_len, wide_piece));
         s.part = -1;
     }
     // a result goes straight to the output where it has one part only

@@ -724,14 +724,18 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
 
 // Joins the partial results of a unit's rows, weights 2^(lse_n - max), in a fixed order
 // whoever is last. D / 8 threads to a row, adjacent threads to adjacent rows. What it
-// takes is the latency of the loads, so those of eight parts are under way at once.
+// takes is the latency of the loads, so those of eight parts are under way at once, and
+// where a unit has fewer than 16 rows, the threads of the others take parts too.
 template <typename T, int D, bool DEVICE>
 __device__ __forceinline__ void join(const AttnArgs &a, const Unit &u) {
     constexpr int P = 8;
-    const int d = threadIdx.x / kJoinRows * 8, r = threadIdx.x % kJoinRows;
-    if (r >= u.rows || d >= D) return;
+    const int d = threadIdx.x / kJoinRows * 8;
+    if (d >= D) return;  // whole waves
+    int width = kJoinRows;  // lanes of one set of the rows
+    while (width / 2 >= u.rows) width /= 2;
+    const int r = threadIdx.x % width, set = threadIdx.x % kJoinRows / width;
     const Seg &us = u.s;
-    const int row = u.row0 + r, j = row / a.group, g = row - j * a.group;
+    const int row = u.row0 + min(r, u.rows - 1), j = row / a.group, g = row - j * a.group;
     const int tok = us.t0 + j, head = u.hk * a.group + g;
     Own own{};
     if (u.prefix) own = a.tok_own[tok];
@@ -741,7 +745,7 @@ __device__ __forceinline__ void join(const AttnArgs &a, const Unit &u) {
     const int own_row = (tok - own.t0) * a.group + g;
     float m = -INFINITY, sum = 0, y[8] = {};
     bool bad = false;  // a NaN among the parts stays
-    for (int n = 0; n < all; n += P) {
+    for (int n = set * P; n < all; n += kJoinRows / width * P) {
         float lse[P];
         f4 o[P][2];
 #pragma unroll
@@ -776,6 +780,17 @@ __device__ __forceinline__ void join(const AttnArgs &a, const Unit &u) {
             for (int e = 0; e < 8; e++) y[e] += o[i][e >> 2][e & 3] * w;
         }
     }
+    for (int w = width; w < kJoinRows; w *= 2) {
+        const float om = __shfl_xor(m, w), mn = fmaxf(m, om);
+        const float mu = mn == -INFINITY ? 0.0f : mn;
+        const float f = exp2_(m - mu), of = exp2_(om - mu);
+        m = mn;
+        sum = sum * f + __shfl_xor(sum, w) * of;
+#pragma unroll
+        for (int e = 0; e < 8; e++) y[e] = y[e] * f + __shfl_xor(y[e], w) * of;
+        bad |= __shfl_xor((int)bad, w) != 0;
+    }
+    if (set || r >= u.rows) return;
     const float f = sum > 0 ? 1.0f / sum : 0.0f;
     vec8<T> x;
 #pragma unroll
