@@ -23,11 +23,9 @@ constexpr int64_t kMaxTokens = int64_t(1) << 24;     // of a batch
 constexpr int64_t kMaxPartRows = int64_t(1) << 28;
 constexpr int64_t kMaxStride = (int64_t(1) << 31) - 8;      // of a block or head, elements
 constexpr int64_t kMaxTokenStride = int64_t(1) << 24;       // of a token in a block
-constexpr size_t kUnits = 256;                       // compute units
-constexpr int32_t kSlots = 2 * kUnits;               // wide items that run at once
+constexpr int64_t kUnits = 256;                      // compute units
+constexpr int64_t kSlots = 2 * kUnits;               // wide items that run at once
 constexpr int32_t kThinItems = 768;                  // thin items wanted
-constexpr double kWideShare = 1.0;
-constexpr int64_t kWideLeast = 4;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -121,6 +119,59 @@ int64_t thin_pieces(const Seg &s, int64_t share, bool merged) {
     return std::min(ceil_div(s.kv_len, piece), pay);
 }
 
+// Pieces of a wide segment's keys, each of `piece` steps, but (as above, with one set
+// and 1 us for a step) no more than pay.
+int64_t wide_pieces(const Seg &s, int64_t piece) {
+    const int64_t steps = ceil_div(s.kv_len, kWideKeys);
+    return std::max<int64_t>(
+        1, std::min(ceil_div(steps, piece), (int64_t)(1.9 * std::sqrt((double)steps))));
+}
+
+// Steps of a piece of the wide segments' keys, by what the batch then takes. Measured: a
+// step of 64 keys lasts 1.16 us where a compute unit has one item, 2.06 us where it has
+// two (head size 64: 0.80, 1.34); the thin items' keys stream at 6 TB/s beside that; a
+// merge takes 2 us, 2.2 for every eight parts of a row, and the time to write and read
+// the parts at 10 TB/s (they stay in caches for the most part). (One chunk of 1024, 32/8 heads of 128, nothing before it: whole
+// 25 us, in two pieces 32; 16/16 heads of 64 over 4096 keys: whole 56 us, in four 33.)
+int64_t choose_wide_piece(const tas_batch *b, const Plan &p, const std::vector<char> &joined,
+                          int64_t thin_keys) {
+    const int64_t Hk = b->kv_heads;
+    const double step_us[2] = {b->head_dim == 64 ? 0.80 : 1.16, b->head_dim == 64 ? 1.34 : 2.06};
+    const double thin_us = (double)thin_keys * b->head_dim * 4 / 6e6;
+    int64_t most = 0, n_thin = 0;
+    for (const Seg &s : p.segs) {
+        if (is_thin(s))
+            n_thin += Hk;
+        else
+            most = std::max(most, ceil_div(s.kv_len, kWideKeys));
+    }
+    int64_t best = 1;
+    double least = 0;
+    for (int64_t n : {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 15, 20, 24, 32, 48, 64}) {
+        const int64_t piece = std::max<int64_t>(1, ceil_div(most, n));
+        int64_t items = n_thin, longest = 0, parts = 0;
+        double steps = 0, part_bytes = 0;
+        for (size_t i = 0; i < p.segs.size(); i++) {
+            const Seg &s = p.segs[i];
+            if (is_thin(s)) continue;
+            const int64_t all = ceil_div(s.kv_len, kWideKeys), k = wide_pieces(s, piece);
+            items += tiles_of(s) * Hk * k;
+            steps += (double)(tiles_of(s) * Hk * all);
+            longest = std::max(longest, ceil_div(all, k));
+            if (k > 1 || joined[i]) {
+                parts = std::max(parts, k + joined[i]);  // (and of the own keys)
+                part_bytes += (double)(s.rows * Hk * k) * b->head_dim * 4;
+            }
+        }
+        double us = std::max(longest * step_us[items > kUnits],
+                             steps * step_us[1] / kSlots + thin_us);
+        if (parts) us += 2 + 2.2 * ceil_div(parts, 8) + part_bytes * 2 / 10e6;
+        if (n == 1 || us < least) least = us, best = piece;
+        if (piece == 1) break;
+    }
+    return best;
+}
+
 // Cuts the keys of the segments into items. A segment's keys are split into
 // nsplit pieces (the last ones shorter, or empty); every tile of its rows has an
 // item for each piece, an empty one where causality leaves nothing, so that a join
@@ -136,18 +187,19 @@ int make_items(const tas_batch *b, Plan &p) {
     }
     const int64_t step = 4 * kThinKeys;
     const int64_t thin_piece = ceil_div(ceil_div(thin_keys, kThinItems), step) * step;
-    // steps of work for a slot; the thin items' 64 keys take about as long as a step
-    const int64_t load = ceil_div(wide_steps + thin_keys / kWideKeys, kSlots);
-    const int64_t wide_piece =
-        std::max<int64_t>((int64_t)(load * kWideShare), kWideLeast) * kWideKeys;
-    std::vector<char> joined(p.segs.size(), 0);  // with a prefix, by the merge kernel
+    // whose parts the merge kernel joins though they are not split
+    std::vector<char> joined(p.segs.size(), 0);
     for (const Req &r : p.reqs)
-        if (r.pre_seg >= 0 && r.own_seg >= 0) joined[r.own_seg] = !is_thin(p.segs[r.pre_seg]);
+        if (r.pre_seg >= 0 && !is_thin(p.segs[r.pre_seg])) {
+            joined[r.pre_seg] = 1;
+            if (r.own_seg >= 0) joined[r.own_seg] = 1;
+        }
+    const int64_t wide_piece = wide_steps ? choose_wide_piece(b, p, joined, thin_keys) : 1;
     for (size_t i = 0; i < p.segs.size(); i++) {
         Seg &s = p.segs[i];
         s.nsplit = (int32_t)std::max<int64_t>(
             1, is_thin(s) ? thin_pieces(s, thin_piece, joined[i])
-                          : ceil_div(s.kv_len, wide_piece));
+                          : wide_pieces(s, wide_piece));
         s.part = -1;
     }
     // a result goes straight to the output where it has one part only
@@ -233,9 +285,9 @@ int make_items(const tas_batch *b, Plan &p) {
     // alternately, one of each to a compute unit (60 decodes and 4 chunks, 28/4 heads of
     // 128: 132 us, with all the wide items first 146 us).
     p.items.reserve(p.wide.size() + p.thin.size());
-    for (size_t i = 0; i < std::max(p.wide.size(), p.thin.size()); i += kUnits)
+    for (size_t i = 0; i < std::max(p.wide.size(), p.thin.size()); i += (size_t)kUnits)
         for (const std::vector<Item> *from : {&p.wide, &p.thin})
-            for (size_t k = i; k < std::min(from->size(), i + kUnits); k++)
+            for (size_t k = i; k < std::min(from->size(), i + (size_t)kUnits); k++)
                 p.items.push_back((*from)[k]);
     p.head.part_rows = part_rows;
     return TAS_OK;
