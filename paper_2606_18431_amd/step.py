@@ -98,14 +98,22 @@ def _check(rc: int, what: str):
         raise TasError(rc, what)
 
 
+def _int32(x, what):
+    """A contiguous int32 array of whole numbers (no value changes on the way)."""
+    a = np.asarray(x)
+    if a.size and a.dtype.kind not in "iu":
+        raise ValueError(f"{what} holds {a.dtype}, expected whole numbers")
+    if a.size and (a.min() < -2 ** 31 or a.max() >= 2 ** 31):
+        raise ValueError(f"{what} holds values beyond 32 bits")
+    return np.ascontiguousarray(a, np.int32)
+
+
 def make_batch(n_new, kv_len, blocks, *, heads, kv_heads, head_dim, block_tokens, n_blocks,
                prefix_first=None, prefix_len=None, prefix_blocks=None, causal=True):
     """tas_batch over host arrays; returns (struct, keepalive). ``blocks`` is
     [n_req, pages] and ``prefix_blocks`` [groups, pages], rows as long as the
     longest context needs."""
-    n = np.ascontiguousarray(n_new, np.int32)
-    kv = np.ascontiguousarray(kv_len, np.int32)
-    bl = np.ascontiguousarray(blocks, np.int32)
+    n, kv, bl = _int32(n_new, "n_new"), _int32(kv_len, "kv_len"), _int32(blocks, "blocks")
     if n.ndim != 1 or kv.shape != n.shape:
         raise ValueError(f"n_new has shape {n.shape}, kv_len {kv.shape}")
     if bl.ndim != 2 or bl.shape[0] != len(n):
@@ -114,9 +122,9 @@ def make_batch(n_new, kv_len, blocks, *, heads, kv_heads, head_dim, block_tokens
     b = tas_batch(heads, kv_heads, head_dim, block_tokens, len(n), n_blocks, int(bool(causal)), 0,
                   n.ctypes.data, kv.ctypes.data, bl.ctypes.data, bl.shape[1])
     if prefix_first is not None:
-        pf = np.ascontiguousarray(prefix_first, np.int32)
-        pl = np.ascontiguousarray(prefix_len, np.int32)
-        pb = np.ascontiguousarray(prefix_blocks, np.int32)
+        pf = _int32(prefix_first, "prefix_first")
+        pl = _int32(prefix_len, "prefix_len")
+        pb = _int32(prefix_blocks, "prefix_blocks")
         if pf.ndim != 1 or len(pf) < 2 or pl.shape != (len(pf) - 1,):
             raise ValueError(f"prefix_first has shape {pf.shape}, prefix_len {pl.shape}")
         if pb.ndim != 2 or pb.shape[0] != len(pl):

@@ -252,6 +252,17 @@ def test_refused_prefixes():
                         n_blocks=1)
 
 
+def test_refused_values():
+    """Nothing is cut to 32 bits or rounded on the way to the C structs."""
+    kw = dict(heads=1, kv_heads=1, head_dim=64, block_tokens=16, n_blocks=4)
+    step.make_batch(np.array([1], np.int64), np.array([1], np.uint8), [[0]], **kw)
+    for n, kv, bl in (([1], [2 ** 32 + 1], [[0]]), ([2 ** 31], [1], [[0]]),
+                      ([1], [1], [[-2 ** 31 - 1]]), ([1.5], [1], [[0]]), ([1], [1], [[0.0]]),
+                      ([True], [1], [[0]])):
+        with pytest.raises(ValueError):
+            step.make_batch(n, kv, bl, **kw)
+
+
 def test_null_arguments_and_unbound_steps():
     L = step.lib()
     assert L.tas_step_bytes(None) == 0 and L.tas_step_tokens(None) == -1
