@@ -392,15 +392,16 @@ template <int N>
 struct Const {
     static constexpr int value = N;
 };
-// The order of a stretch: N times a matrix product, vector work that does not wait for
-// it, and LDS reads for the next stretch.
-template <int N, int VECTOR, int READS>
+// The order of a stretch: N times a matrix product, a load to LDS at every other of
+// them, vector work that does not wait for it, and LDS reads for the next stretch.
+template <int N, int VECTOR, int READS, bool LOADS = false>
 __device__ __forceinline__ void mix() {
     if constexpr (N > 0) {
         __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        if (LOADS && N % 2 == 0) __builtin_amdgcn_sched_group_barrier(0x10, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x2, VECTOR, 0);
         if (READS) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
-        mix<N - 1, VECTOR, READS>();
+        mix<N - 1, VECTOR, READS, LOADS>();
     }
 }
 constexpr int kMarks = 8;  // words of 32 keys
@@ -410,8 +411,12 @@ constexpr int kWaitLoads = 0x0F70;  // s_waitcnt: no load or store outstanding
 // step in LDS for all four waves, loaded there directly and double buffered. A step
 // is two stretches in which the matrix unit and the vector unit have independent
 // work: S of the next keys beside the exponentials of these, then P V of these beside
-// the maximum of the next. One barrier ends a step; the loads it waits for had the
-// whole step to arrive.
+// the maximum of the next. One barrier ends a step; the loads it waits for had most of
+// the step to arrive. In a stretch the products, the vector work, the LDS reads and the
+// loads to LDS alternate: V is read before the weights are worked out, whose end no read
+// passes, and the loads go between the products, V's in the first stretch and K's in the
+// second. (16 chunks of 11777 tokens, 32/8 heads of 128: 927 us with the products behind
+// the vector work, 908 with V read first, 897 with the loads spread as well.)
 template <typename T, int D>
 __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, char *k0_lds,
                                           char *k1_lds, char *v0_lds, char *v1_lds,
@@ -609,26 +614,26 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
         if (EDGE) poison(sa, base);
         read_k(kl);
         place();
-        load_v(B ? v0_lds : v1_lds);
-        load_k(B ? k0_lds : k1_lds);
         look_up(next + kWideKeys, next + kWideKeys + 32);
         __builtin_amdgcn_sched_barrier(0);
+        load_v(B ? v0_lds : v1_lds);
         scores(sb);
-        weights(p, sa);
         read_v(vl);
-        mix<QS, 56 / QS, D / 8 / QS>();
+        weights(p, sa);
+        mix<QS, 56 / QS, D / 8 / QS, true>();
         __builtin_amdgcn_sched_barrier(0);
         if (EDGE) hide(sb, base + 32);
+        load_k(B ? k0_lds : k1_lds);
         products(p);
         read_k(kl + HB);
         const float mb = largest(sb);
-        mix<D / 16, 4, QS / (D / 16)>();
+        mix<D / 16, 4, QS / (D / 16), true>();
         raise(mb);
         if (EDGE) poison(sb, base + 32);
         __builtin_amdgcn_sched_barrier(0);
         scores(sa);
-        weights(p, sb);
         read_v(vl + HB);
+        weights(p, sb);
         mix<QS, 56 / QS, D / 8 / QS>();
         __builtin_amdgcn_sched_barrier(0);
         if (EDGE) hide(sa, next);
