@@ -281,14 +281,31 @@ int make_items(const tas_batch *b, Plan &p) {
     }
     longest_first(p.thin, (int32_t)step);
     longest_first(p.wide, kWideKeys);
-    // A wide item keeps the matrix cores busy and a thin one the memory: they start
-    // alternately, one of each to a compute unit (60 decodes and 4 chunks, 28/4 heads of
-    // 128: 132 us, with all the wide items first 146 us).
+    // A wide item keeps the matrix cores busy and a thin one the memory, so that a compute
+    // unit is to have one of each as long as there are both: either kind has half of the
+    // slots, or what the other leaves, and the items are listed as those slots come free
+    // (the work of the kind before an item, over its slots; in steps of a wide item, of
+    // which a thin item's last 1.5, and one for the start). (60 decodes and 4 chunks, 28/4
+    // heads of 128: 130 us; 256 of each alternately 136, all the wide items first 146.)
+    struct Kind {
+        const std::vector<Item> &items;
+        double step, slots;  // keys of a step's time
+        size_t next = 0;
+        double before = 0;
+        double start() const { return next < slots ? 0 : before / slots; }
+    };
+    const double n_wide = (double)p.wide.size(), n_thin = (double)p.thin.size();
+    Kind wide{p.wide, kWideKeys, kSlots - std::min<double>(n_thin, kUnits)};
+    Kind thin{p.thin, (double)step / 1.5, kSlots - std::min<double>(n_wide, kUnits)};
     p.items.reserve(p.wide.size() + p.thin.size());
-    for (size_t i = 0; i < std::max(p.wide.size(), p.thin.size()); i += (size_t)kUnits)
-        for (const std::vector<Item> *from : {&p.wide, &p.thin})
-            for (size_t k = i; k < std::min(from->size(), i + (size_t)kUnits); k++)
-                p.items.push_back((*from)[k]);
+    while (p.items.size() < p.wide.size() + p.thin.size()) {
+        const bool w = wide.next < p.wide.size() &&
+                       (thin.next == p.thin.size() || wide.start() <= thin.start());
+        Kind &from = w ? wide : thin;
+        const Item &it = from.items[from.next++];
+        from.before += (it.k1 - it.k0) / from.step + 1;
+        p.items.push_back(it);
+    }
     p.head.part_rows = part_rows;
     return TAS_OK;
 }
