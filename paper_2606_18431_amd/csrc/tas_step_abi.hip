@@ -119,6 +119,29 @@ int64_t thin_pieces(const Seg &s, int64_t share, bool merged) {
     return std::min(ceil_div(s.kv_len, piece), pay);
 }
 
+// Keys of a piece of the thin segments: a slot's share of all keys. As every segment has
+// a last piece that is shorter, these are somewhat more items than slots, and the rest
+// takes a round of its own: where a piece that is longer by a third at most fills the
+// slots once, all but a sixteenth, that one. (16/16 heads of 64, 8 contexts of about
+// 20039: 816 items 136 us, 752 items 121; 32/8 heads of 128, 64 of about 1200: 928 items
+// 66, 760 items 64. With more slots left empty that loses: 16/2 heads of 128, 28 of about
+// 14830: 786 items 77 us, 694 items 82.)
+int64_t choose_thin_piece(const Plan &p, const std::vector<char> &joined, int64_t kv_heads,
+                          int64_t keys, bool any_wide) {
+    const int64_t step = 4 * kThinKeys;
+    const int64_t share = ceil_div(ceil_div(keys, kThinItems), step) * step;
+    if (any_wide || (int64_t)p.segs.size() * kv_heads > kThinItems) return share;
+    for (int64_t piece = share; piece <= share + share / 3; piece += step) {
+        int64_t items = 0;
+        for (size_t i = 0; i < p.segs.size(); i++)
+            items += kv_heads *
+                     std::max<int64_t>(1, thin_pieces(p.segs[i], piece, joined[i]));
+        if (items <= kThinItems)
+            return items >= kThinItems - kThinItems / 16 ? piece : share;
+    }
+    return share;
+}
+
 // Pieces of a wide segment's keys, each of `piece` steps, but (as above, with one set
 // and 1 us for a step) no more than pay.
 int64_t wide_pieces(const Seg &s, int64_t piece) {
@@ -186,7 +209,6 @@ int make_items(const tas_batch *b, Plan &p) {
             wide_steps += (int64_t)tiles_of(s) * Hk * ceil_div(s.kv_len, kWideKeys);
     }
     const int64_t step = 4 * kThinKeys;
-    const int64_t thin_piece = ceil_div(ceil_div(thin_keys, kThinItems), step) * step;
     // whose parts the merge kernel joins though they are not split
     std::vector<char> joined(p.segs.size(), 0);
     for (const Req &r : p.reqs)
@@ -194,6 +216,7 @@ int make_items(const tas_batch *b, Plan &p) {
             joined[r.pre_seg] = 1;
             if (r.own_seg >= 0) joined[r.own_seg] = 1;
         }
+    const int64_t thin_piece = choose_thin_piece(p, joined, Hk, thin_keys, wide_steps > 0);
     const int64_t wide_piece = wide_steps ? choose_wide_piece(b, p, joined, thin_keys) : 1;
     for (size_t i = 0; i < p.segs.size(); i++) {
         Seg &s = p.segs[i];
