@@ -384,9 +384,10 @@ __device__ int64_t run_offset(int page, int run, int64_t block_stride, int64_t t
                      (uint64_t)(uint32_t)run * (uint32_t)(token_stride * 32));
 }
 
-__device__ void load_to_lds(const char *from, char *to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
-                                     (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+typedef const __attribute__((address_space(1))) char *Global;
+__device__ void load_to_lds(Global from, char *to) {
+    __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, 0,
+                                     0);
 }
 template <int N>
 struct Const {
@@ -449,42 +450,48 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
     const char *kbase = (const char *)((const T *)a.c.k + it.hk * a.c.k_head);
     const char *vbase = (const char *)((const T *)a.c.v + it.hk * a.c.v_head);
 
-    // Load i of a wave fills 1 KB, RPL rows from row y0(i) on; a lane's place is fixed,
-    // so it fetches the chunk that belongs there: chunk c of row y of K lies at
-    // c ^ (y mod LPR), which spreads the rows of a column over the banks.
-    auto y0 = [&](int i) { return (i * 4 + wave) * RPL; };
+    // A wave loads a run of 16 keys of a tile: load i fills 1 KB, rows i RPL on of the run
+    // (so that a wave works out two addresses a step: with rows of four runs, and eight
+    // addresses, the 16 chunks took 3 % longer). Chunk c of row y of K lies at
+    // c ^ (y mod LPR), which spreads the rows of a column over the banks; a lane's place
+    // is fixed, so it fetches the chunk that belongs there.
     const int lrow = lane / LPR, lch = lane % LPR;
-    // (y mod 16, and so the place in the row, is the same for all i)
-    const int yl = (y0(0) + lrow) & 15;
-    const uint32_t klane = yl * (uint32_t)(a.c.k_token * 2) + (lch ^ (yl & (LPR - 1))) * 16;
-    const uint32_t vlane = yl * (uint32_t)(a.c.v_token * 2) + (v_chunk<D>(yl, lch) - yl * LPR) * 16;
-    // Lanes 0 .. 3 (mod 8) work out where the next four runs of 16 keys of K lie,
-    // lanes 4 .. 7 those of V; the block numbers are read a step before that.
-    const int which_run = lane & 3;
-    const bool of_v = lane & 4;
+    uint32_t klane[NL], vlane[NL];
+#pragma unroll
+    for (int i = 0; i < NL; i++) {
+        const int y = i * RPL + lrow;
+        klane[i] = y * (uint32_t)(a.c.k_token * 2) + (lch ^ (y & (LPR - 1))) * 16;
+        vlane[i] = y * (uint32_t)(a.c.v_token * 2) + (v_chunk<D>(y, lch) - y * LPR) * 16;
+    }
+    // Even lanes work out where the wave's next run of K lies, odd lanes that of V; the
+    // block number is read a step before that.
+    const bool of_v = lane & 1;
+    const uint64_t base_of = (uint64_t)(of_v ? vbase : kbase);
     const uint32_t block_bytes = (uint32_t)((of_v ? a.c.v_block : a.c.k_block) * 2);
     const uint32_t run_bytes = (uint32_t)((of_v ? a.c.v_token : a.c.k_token) * 32);
     int page = 0, run = 0;
     auto look_up = [&](int v_base, int k_base) {
-        const int sub = min(((of_v ? v_base : k_base) >> 4) + which_run, last_sub);
+        const int sub = min(((of_v ? v_base : k_base) >> 4) + wave, last_sub);
         page = tab[sub >> a.sub_shift];
         run = sub & sub_mask;
     };
-    uint64_t off = 0;
+    uint64_t k_from = 0, v_from = 0;
     auto place = [&]() {
-        off = (uint64_t)(uint32_t)page * block_bytes + (uint64_t)(uint32_t)run * run_bytes;
+        const uint64_t at = base_of + (uint64_t)(uint32_t)page * block_bytes +
+                            (uint64_t)(uint32_t)run * run_bytes;
+        const uint32_t lo = (uint32_t)at, hi = (uint32_t)(at >> 32);
+        k_from = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, 0) << 32 |
+                 (uint32_t)__builtin_amdgcn_readlane(lo, 0);
+        v_from = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, 1) << 32 |
+                 (uint32_t)__builtin_amdgcn_readlane(lo, 1);
     };
-    auto load = [&](char *to, const char *from, int first) {
+    auto load = [&](char *to, uint64_t from, const uint32_t (&at)[NL]) {
 #pragma unroll
-        for (int i = 0; i < NL; i++) {
-            const int n = first + (y0(i) >> 4);
-            const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)off, n);
-            const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(off >> 32), n);
-            load_to_lds(from + (((uint64_t)hi << 32) | lo), to + (i * 4 + wave) * 1024);
-        }
+        for (int i = 0; i < NL; i++)
+            load_to_lds((Global)from + at[i], to + (wave * NL + i) * 1024);
     };
-    auto load_k = [&](char *to) { load(to, kbase + klane, 0); };
-    auto load_v = [&](char *to) { load(to, vbase + vlane, 4); };
+    auto load_k = [&](char *to) { load(to, k_from, klane); };
+    auto load_v = [&](char *to) { load(to, v_from, vlane); };
     // The rows see the keys from here on to the end differently (at most 128 + 63 keys;
     // a bit each in `marked`).
     const int differ = full < it.k1 ? full & ~31 : it.k1;
@@ -499,8 +506,8 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
         if (edge && base + kWideKeys > differ)
 #pragma unroll
             for (int i = 0; i < NL; i++) {
-                u4 *at = (u4 *)(v + (i * 4 + wave) * 1024 + lane * 16);
-                const int y = base + y0(i) + lrow;
+                u4 *at = (u4 *)(v + (wave * NL + i) * 1024 + lane * 16);
+                const int y = base + wave * 16 + i * RPL + lrow;
                 if (y >= it.k1) {
                     *at = u4{0, 0, 0, 0};
                 } else if (y >= differ && any_not_finite<T>(*at)) {
