@@ -63,7 +63,9 @@ typedef struct tas_batch {
 /* One layer's cache: element (block, head, token of the block, d) of K lies at
  * k + block * k_block + head * k_head + token * k_token + d (elements); V
  * likewise. Pointers 16-byte aligned, strides multiples of 8, below 2^31, of a
- * token at most 2^24. */
+ * token at most 2^24. For tas_step_append no two elements of K, or of V, may lie in
+ * one place: in the order of the strides, each is at least as long as what the
+ * shorter ones span. */
 typedef struct tas_cache {
     void *k, *v;
     int64_t k_block, k_head, k_token;
@@ -92,7 +94,7 @@ typedef struct tas_append {
 /* Arguments of tas_step_attention. */
 typedef struct tas_attention {
     int32_t dtype;
-    float scale;                   /* of the scores, finite                                  */
+    float scale;                   /* of the scores, positive and finite                     */
     const void *q;                 /* [T][heads][head_dim]                                   */
     int64_t q_stride;
     void *out;                     /* [T][heads][head_dim]; may be q                         */
@@ -122,7 +124,7 @@ int64_t tas_step_tokens(const tas_step *step);
  *     (a, b) <- (a cos - b sin, b cos + a sin)      (each rotated pair)
  * queries go to q_out, keys and the unchanged values to the token's slot of the
  * cache. In 32 bits, rounded once. TAS_EINVAL: an argument out of range or
- * unaligned, a batch with kv_len[i] < n_new[i], positions too small;
+ * unaligned, a cache whose slots overlap, a batch with kv_len[i] < n_new[i], positions too small;
  * TAS_ESTATE: not bound (also below). */
 int tas_step_append(tas_step *step, const tas_append *a, void *stream);
 

@@ -458,6 +458,23 @@ bool valid_cache(const tas_cache &c) {
     return true;
 }
 
+// No two slots of K, or of V, share an element, so that the new tokens' writes do not
+// race: in the order of the strides, each is at least what the shorter ones span.
+bool disjoint_slots(int64_t block, int64_t head, int64_t token, int64_t n_blocks,
+                    int64_t kv_heads, int64_t block_tokens, int64_t head_dim) {
+    struct Axis {
+        int64_t stride, n;
+    } axes[3] = {{token, block_tokens}, {head, kv_heads}, {block, n_blocks}};
+    std::sort(axes, axes + 3, [](const Axis &x, const Axis &y) { return x.stride < y.stride; });
+    int64_t span = head_dim;
+    for (const Axis &x : axes) {
+        if (x.n == 1) continue;  // its stride says nothing
+        if (x.stride < span) return false;
+        span += (x.n - 1) * x.stride;
+    }
+    return true;
+}
+
 bool valid_rows(const void *p, int64_t stride, int64_t row) {
     return aligned16(p) && stride >= row && stride % 8 == 0;
 }
@@ -467,7 +484,7 @@ bool valid_rows(const void *p, int64_t stride, int64_t row) {
 struct tas_step {
     std::vector<char> blob;  // the plan
     PlanHead head{};
-    int32_t heads = 0, kv_heads = 0, head_dim = 0, blk_shift = 0;
+    int32_t heads = 0, kv_heads = 0, head_dim = 0, blk_shift = 0, n_blocks = 0;
     int64_t max_pos = 0;
     bool appendable = false;
     char *ws = nullptr;  // null: not bound
@@ -494,6 +511,7 @@ int tas_step_create(const tas_batch *b, tas_step **out) try {
     s->heads = b->heads;
     s->kv_heads = b->kv_heads;
     s->head_dim = b->head_dim;
+    s->n_blocks = b->n_blocks;
     while ((1 << s->blk_shift) < b->block_tokens) s->blk_shift++;
     s->max_pos = p.max_pos;
     s->appendable = p.appendable;
@@ -544,6 +562,12 @@ int tas_step_append(tas_step *s, const tas_append *a, void *stream) {
         (!aligned16(a->cos) || !aligned16(a->sin) || a->positions < s->max_pos))
         return TAS_EINVAL;
     if (!valid_cache(a->cache)) return TAS_EINVAL;
+    const tas_cache &c = a->cache;
+    const int64_t bt = int64_t(1) << s->blk_shift;
+    if (c.k == c.v ||
+        !disjoint_slots(c.k_block, c.k_head, c.k_token, s->n_blocks, s->kv_heads, bt, D) ||
+        !disjoint_slots(c.v_block, c.v_head, c.v_token, s->n_blocks, s->kv_heads, bt, D))
+        return TAS_EINVAL;
     if (s->head.n_tok == 0) return TAS_OK;
     if (!valid_rows(a->qkv, a->qkv_stride, (s->heads + 2 * s->kv_heads) * D) ||
         !valid_rows(a->q_out, a->q_out_stride, s->heads * D))

@@ -541,3 +541,36 @@ def test_batch_without_new_tokens(torch):
     assert s.attention(q, k, v).shape == (0, 4, 64)
     assert s.append(torch.empty((0, 8, 64), device="cuda", dtype=torch.float16), k, v).shape == \
         (0, 4, 64)
+
+
+@pytest.mark.parametrize("shared", ["block", "head", "token", "half a token", "k is v"])
+def test_append_refuses_slots_that_share_elements(torch, shared):
+    """A broadcast cache can be attended to; its slots cannot be written."""
+    b = Batch(33, [1, 4], [30, 20], 4, 2, 64)
+    k, v = caches(torch, b, torch.bfloat16, 9, poison=False)
+    s = b.step()
+    qkv = torch.zeros((5, 8, 64), device="cuda", dtype=torch.bfloat16)
+    bk, bv = {
+        "block": (k[:1].expand_as(k), v),
+        "head": (k, v[:, :1].expand_as(v)),
+        "token": (k[:, :, :1].expand_as(k), v),
+        "half a token": (k, v.as_strided(v.shape, (v.stride(0), v.stride(1), 32, 1))),
+        "k is v": (k, k),
+    }[shared]
+    before = k.clone(), v.clone()
+    with pytest.raises(tas.TasError) as e:
+        s.append(qkv, bk, bv)
+    assert e.value.code == tas.TAS_EINVAL
+    assert torch.equal(k, before[0]) and torch.equal(v, before[1])
+    s.attention(qkv[:, :4].contiguous(), bk, bv)
+    s.append(qkv, k, v)
+
+
+def test_append_takes_any_order_of_disjoint_slots(torch):
+    """One block and one key head: their strides say nothing."""
+    s = step.Step([2], [9], [[0]], heads=2, kv_heads=1, head_dim=64, block_tokens=16, n_blocks=1)
+    qkv = torch.randn((2, 4, 64), device="cuda", dtype=torch.float16)
+    k, v = torch.zeros((2, 16, 64), device="cuda", dtype=torch.float16)
+    s.append(qkv, k.as_strided((1, 1, 16, 64), (0, 0, 64, 1)),
+             v.as_strided((1, 1, 16, 64), (8, 8, 64, 1)))
+    assert torch.equal(k[7:9], qkv[:, 2]) and torch.equal(v[7:9], qkv[:, 3])
