@@ -112,7 +112,10 @@ def make_batch(n_new, kv_len, blocks, *, heads, kv_heads, head_dim, block_tokens
                prefix_first=None, prefix_len=None, prefix_blocks=None, causal=True):
     """tas_batch over host arrays; returns (struct, keepalive). ``blocks`` is
     [n_req, pages] and ``prefix_blocks`` [groups, pages], rows as long as the
-    longest context needs."""
+    longest context needs. The three prefix arguments: all or none."""
+    given = [x is not None for x in (prefix_first, prefix_len, prefix_blocks)]
+    if any(given) != all(given):
+        raise ValueError("prefix_first, prefix_len and prefix_blocks: all or none")
     n, kv, bl = _int32(n_new, "n_new"), _int32(kv_len, "kv_len"), _int32(blocks, "blocks")
     if n.ndim != 1 or kv.shape != n.shape:
         raise ValueError(f"n_new has shape {n.shape}, kv_len {kv.shape}")

@@ -319,3 +319,18 @@ def test_struct_layouts_match_header(tmp_path):
         assert int(got[st.__name__]) == ctypes.sizeof(st)
         for f, _ in st._fields_:
             assert int(got[f"{st.__name__}.{f}"]) == getattr(st, f).offset, f
+
+
+@pytest.mark.parametrize("left_out", ["prefix_first", "prefix_len", "prefix_blocks"])
+def test_prefix_arguments_go_together(left_out):
+    """A prefix that is only half described is refused, not left out."""
+    kw = dict(heads=1, kv_heads=1, head_dim=64, block_tokens=16, n_blocks=4)
+    prefix = dict(prefix_first=[0, 1], prefix_len=[20], prefix_blocks=[[1, 2]])
+    b, keep = step.make_batch([1], [1], [[0]], **kw, **prefix)
+    assert b.n_prefix == 1
+    del prefix[left_out]
+    with pytest.raises(ValueError):
+        step.make_batch([1], [1], [[0]], **kw, **prefix)
+    for name, value in prefix.items():
+        with pytest.raises(ValueError):
+            step.make_batch([1], [1], [[0]], **kw, **{name: value})
