@@ -15,6 +15,7 @@ allocating the workspace and outputs as PyTorch tensors.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 import struct
 
@@ -108,6 +109,14 @@ def _int32(x, what):
     return np.ascontiguousarray(a, np.int32)
 
 
+def _size(x, what):
+    """A whole number of 32 bits (ctypes would cut a longer one)."""
+    x = operator.index(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{what} is {x}, beyond 32 bits")
+    return x
+
+
 def make_batch(n_new, kv_len, blocks, *, heads, kv_heads, head_dim, block_tokens, n_blocks,
                prefix_first=None, prefix_len=None, prefix_blocks=None, causal=True):
     """tas_batch over host arrays; returns (struct, keepalive). ``blocks`` is
@@ -122,8 +131,9 @@ def make_batch(n_new, kv_len, blocks, *, heads, kv_heads, head_dim, block_tokens
     if bl.ndim != 2 or bl.shape[0] != len(n):
         raise ValueError(f"blocks has shape {bl.shape} for {len(n)} requests")
     keep = [n, kv, bl]
-    b = tas_batch(heads, kv_heads, head_dim, block_tokens, len(n), n_blocks, int(bool(causal)), 0,
-                  n.ctypes.data, kv.ctypes.data, bl.ctypes.data, bl.shape[1])
+    b = tas_batch(_size(heads, "heads"), _size(kv_heads, "kv_heads"), _size(head_dim, "head_dim"),
+                  _size(block_tokens, "block_tokens"), len(n), _size(n_blocks, "n_blocks"),
+                  int(bool(causal)), 0, n.ctypes.data, kv.ctypes.data, bl.ctypes.data, bl.shape[1])
     if prefix_first is not None:
         pf = _int32(prefix_first, "prefix_first")
         pl = _int32(prefix_len, "prefix_len")

@@ -334,3 +334,17 @@ def test_prefix_arguments_go_together(left_out):
     for name, value in prefix.items():
         with pytest.raises(ValueError):
             step.make_batch([1], [1], [[0]], **kw, **{name: value})
+
+
+@pytest.mark.parametrize("name", ["heads", "kv_heads", "head_dim", "block_tokens", "n_blocks"])
+def test_refused_sizes(name):
+    """No size is cut to 32 bits on the way to the C struct either."""
+    kw = dict(heads=1, kv_heads=1, head_dim=64, block_tokens=16, n_blocks=4)
+    b, keep = step.make_batch([1], [1], [[0]], **{**kw, name: np.int64(kw[name])})
+    assert getattr(b, name) == kw[name]
+    for value in (2 ** 32 + kw[name], 2 ** 31, -2 ** 31 - 1, -2 ** 32 + kw[name]):
+        with pytest.raises(ValueError):
+            step.make_batch([1], [1], [[0]], **{**kw, name: value})
+    for value in (float(kw[name]), str(kw[name]), None):
+        with pytest.raises(TypeError):
+            step.make_batch([1], [1], [[0]], **{**kw, name: value})
