@@ -106,8 +106,9 @@ typedef struct tas_attention {
 typedef struct tas_step tas_step;
 
 /* Validate and plan a batch (host only). TAS_EINVAL: a field out of range, a
- * block number outside the pool, two new tokens that would be written to one
- * slot; TAS_ENOMEM: no host memory. */
+ * block number outside the pool, in a causal batch a block that new tokens of two
+ * requests, or two pages of one, would be written to (without causality such a
+ * batch can be attended, not appended); TAS_ENOMEM: no host memory. */
 int tas_step_create(const tas_batch *batch, tas_step **out);
 /* Bytes of device workspace that the step needs (plan and partial results). */
 size_t tas_step_bytes(const tas_step *step);
@@ -124,7 +125,8 @@ int64_t tas_step_tokens(const tas_step *step);
  *     (a, b) <- (a cos - b sin, b cos + a sin)      (each rotated pair)
  * queries go to q_out, keys and the unchanged values to the token's slot of the
  * cache. In 32 bits, rounded once. TAS_EINVAL: an argument out of range or
- * unaligned, a cache whose slots overlap, a batch with kv_len[i] < n_new[i], positions too small;
+ * unaligned, a cache whose slots overlap, a batch with kv_len[i] < n_new[i] or new
+ * tokens in one block, positions too small;
  * TAS_ESTATE: not bound (also below). */
 int tas_step_append(tas_step *step, const tas_append *a, void *stream);
 

@@ -88,8 +88,8 @@ int64_t add_table(const tas_batch *b, const int32_t *pages, int64_t stride, int6
     return at;
 }
 
-// Two new tokens in one slot would race: the blocks that new tokens go to are
-// distinct, over all requests and within one.
+// Two new tokens appended to one slot would race: the blocks that new tokens go to are
+// distinct, over all requests and within one (a block has one request that fills it).
 bool distinct_slots(const tas_batch *b, const Plan &p) {
     std::vector<int32_t> written;
     for (const Req &r : p.reqs) {
@@ -403,7 +403,13 @@ int make_plan(const tas_batch *b, Plan &p) {
     }
     // rows and heads of the batch are counted in 32 bits
     if (t * (b->heads + 2 * b->kv_heads) > INT32_MAX / 2) return TAS_EINVAL;
-    if (p.appendable && !distinct_slots(b, p)) return TAS_EINVAL;
+    if (p.appendable && !distinct_slots(b, p)) {
+        // A causal batch's new tokens are the last ones of contexts of their own: a block
+        // that two of them end in is an error of the tables. Without causality they may
+        // be queries over any pages, and only append would race.
+        if (b->causal) return TAS_EINVAL;
+        p.appendable = false;
+    }
     const int rc = make_items(b, p);
     if (rc != TAS_OK) return rc;
     PlanHead &h = p.head;

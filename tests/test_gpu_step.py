@@ -574,3 +574,23 @@ def test_append_takes_any_order_of_disjoint_slots(torch):
     s.append(qkv, k.as_strided((1, 1, 16, 64), (0, 0, 64, 1)),
              v.as_strided((1, 1, 16, 64), (8, 8, 64, 1)))
     assert torch.equal(k[7:9], qkv[:, 2]) and torch.equal(v[7:9], qkv[:, 3])
+
+
+def test_requests_over_the_same_pages(torch):
+    """Queries of two requests over one context (no causality): attended as each by
+    itself, and not appended, which would race."""
+    kv, pages = [40, 40, 33], [[3, 1, 4], [3, 1, 4], [3, 1, 4]]
+    kw = dict(heads=4, kv_heads=2, head_dim=64, block_tokens=16, n_blocks=5, causal=False)
+    k, v = torch.randn((2, 5, 2, 16, 64), device="cuda", dtype=torch.bfloat16)
+    q = torch.randn((23, 4, 64), device="cuda", dtype=torch.bfloat16)
+    n = [1, 20, 2]
+    s = step.Step(n, kv, pages, **kw)
+    got = s.attention(q, k, v)
+    t = 0
+    for i in range(3):
+        one = step.Step([n[i]], [kv[i]], [pages[i]], **kw)
+        assert torch.equal(got[t:t + n[i]], one.attention(q[t:t + n[i]], k, v)), i
+        t += n[i]
+    with pytest.raises(tas.TasError) as e:
+        s.append(torch.zeros((23, 8, 64), device="cuda", dtype=torch.bfloat16), k, v)
+    assert e.value.code == tas.TAS_EINVAL

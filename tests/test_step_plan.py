@@ -348,3 +348,14 @@ def test_refused_sizes(name):
     for value in (float(kw[name]), str(kw[name]), None):
         with pytest.raises(TypeError):
             step.make_batch([1], [1], [[0]], **{**kw, name: value})
+
+
+def test_new_tokens_in_one_block_without_causality():
+    """Without causality new tokens may be queries over any pages, shared ones too: the
+    batch is planned. Only append would race; a causal batch stays refused."""
+    pages = [[0, 1], [0, 1]]
+    assert not refused([1, 1], [20, 20], pages, causal=False)
+    assert not refused([1, 2], [20, 32], pages, causal=False)
+    assert not refused([20], [20], [[5, 5]], causal=False)
+    assert refused([1, 1], [20, 20], pages)
+    assert refused([1, 2], [20, 32], pages)
