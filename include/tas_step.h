@@ -132,7 +132,9 @@ int tas_step_append(tas_step *step, const tas_append *a, void *stream);
 
 /* out = softmax(scale * q K^T) V of every new token and head, over the group's
  * prefix and the keys y < kv_len[i] of its own context (causal: y <= kv_len[i] -
- * n_new[i] + j); query head h reads key head h / (heads / kv_heads). A row
+ * n_new[i] + j); query head h reads key head h / (heads / kv_heads). Scores, maxima
+ * and sums are held in 32 bits; the softmax's weights are rounded to the tensors'
+ * type for the product with V, and the result once. A row
  * without keys gives 0 and lse -inf. What a row does not see does not reach it,
  * whatever the slots hold; a value that it sees and that is not finite makes its
  * element not finite, or the whole row NaN. */

@@ -8,7 +8,8 @@
 // operand of O^T = V^T P^T (which keys its k-slots stand for is free, as long as both
 // operands agree). The left operand V^T is read from the rows of V in LDS by the
 // transposing LDS read. Scores, statistics and sums are held in 32 bits; the weights
-// are rounded to the inputs' type for the second product, as its operands have to be.
+// are rounded to the inputs' type for the second product, as its operands have to be
+// (kHeadroom: what a 16-bit float has left of its exponent).
 #include <hip/hip_runtime.h>
 
 #include "tas_step_internal.h"
@@ -45,8 +46,16 @@ __device__ f16x mfma32(vec8<_Float16> a, vec8<_Float16> b, f16x c) {
 }
 
 // The running maximum is raised only where it falls behind by more than this (a
-// weight is at most 2^8 then): the rescaling of o, as long as it is, is rare.
+// weight is at most 2^8 of the largest's then): the rescaling of o, as long as it is, is rare.
 constexpr float kLazy = 8.0f;
+
+// The m of a row is this far below its maximum, so that its weights are that much larger:
+// a 16-bit float holds none below 2^-25, and would lose from the row, but not from its
+// sum, what many small ones add (8000 keys at 2^-25.5 of the largest: 1.7e-4 of V). With
+// 2^7 the largest is at most 2^15, and 2^20 keys below the smallest add 2^-12 at most,
+// less than the result's rounding. A bfloat16 has the exponents of 32 bits.
+template <typename T>
+constexpr float kHeadroom = __is_same(T, _Float16) ? 7.0f : 0.0f;
 
 __device__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -304,7 +313,7 @@ __device__ __forceinline__ void thin_item(const AttnArgs &a, const Item &it, cha
         for (int n = 0; n < 2; n++)
 #pragma unroll
             for (int i = 0; i < 4; i++) mt = fmaxf(mt, sc[n][i]);
-        mt = max32(max16(mt)) * a.scale2;
+        mt = max32(max16(mt)) * a.scale2 - kHeadroom<T>;
         if (__any(mt > m + kLazy)) {
             const float mn = mt > m + kLazy ? mt : m, f = mn == m ? 1.0f : exp2_(m - mn);
             m = mn;
@@ -568,7 +577,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
         float mt = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 16; e++) mt = fmaxf(mt, sc[e]);
-        return max32(mt) * a.scale2;
+        return max32(mt) * a.scale2 - kHeadroom<T>;
     };
     auto raise = [&](float mt) {
         if (__any(mt > m + kLazy)) {

@@ -594,3 +594,32 @@ def test_requests_over_the_same_pages(torch):
     with pytest.raises(tas.TasError) as e:
         s.append(torch.zeros((23, 8, 64), device="cuda", dtype=torch.bfloat16), k, v)
     assert e.value.code == tas.TAS_EINVAL
+
+
+@pytest.mark.parametrize("name", ["bf16", "f16"])
+@pytest.mark.parametrize("size", [64, 128])
+@pytest.mark.parametrize("n,group", [(1, 4), (3, 8)])
+def test_many_small_weights(torch, name, size, n, group):
+    """One key has nearly all of the weight, and 8000 others 2^-25.5 of its each, which a
+    16-bit float cannot hold beside 1: what they add to the row is not lost. (96 requests
+    over the same pages, so that the keys of a row stay in one piece.)"""
+    dt, keys, heads = dtype_of(torch, name), 8000, 8
+    g = torch.Generator().manual_seed(5)
+    k, v = torch.zeros((2, 500, heads, 16, size), dtype=dt)
+    k[0, :, 0, 3] = 4.41796875                  # scores 17.67 = 25.5 log(2), and 0
+    v[:] = (50 + 100 * torch.rand(v.shape, generator=g)).to(dt)
+    v[0, :, 0] = 0
+    q = torch.zeros((96 * n, heads * group, size), dtype=dt)
+    q[..., 3] = 4
+    s = step.Step([n] * 96, [keys] * 96, np.tile(np.arange(500), (96, 1)), heads=heads * group,
+                  kv_heads=heads, head_dim=size, block_tokens=16, n_blocks=500, causal=False)
+    got = s.attention(q.cuda(), k.cuda(), v.cuda(), scale=1.0)
+    w = math.exp(-4 * float(k[0, 0, 0, 3]))
+    flat = v.double().permute(1, 0, 2, 3).reshape(heads, keys, size)
+    want = w * flat.sum(1) / (1 + w * (keys - 1))
+    want = want.repeat_interleave(group, 0).expand(96 * n, -1, -1)
+    # rounding of the result and of the weights; 16-bit floats keep weights of 2^7 down
+    # to 2^-25, with an error of 2^-32 of the largest
+    u = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}[name]
+    tol = 2.01 * u * want + 2.0 ** -15 * want + (keys * 2.0 ** -32 * 150 if name == "f16" else 0)
+    near(got, want, tol, "out")
