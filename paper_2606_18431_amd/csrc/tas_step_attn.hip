@@ -307,7 +307,8 @@ __device__ __forceinline__ void thin_item(const AttnArgs &a, const Item &it, cha
             for (int n = 0; n < 2; n++)
 #pragma unroll
                 for (int i = 0; i < 4; i++)
-                    if ((marked >> (n * 16 + g * 4 + i) & 1) && sc[n][i] != -INFINITY) l = NAN;
+                    if ((marked >> (n * 16 + g * 4 + i) & 1) && base + n * 16 + g * 4 + i < lim)
+                        l = NAN;
         float mt = -INFINITY;
 #pragma unroll
         for (int n = 0; n < 2; n++)
@@ -564,13 +565,14 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
             if (base + (e >> 2) * 8 + half * 4 + (e & 3) >= lim) sc[e] = -INFINITY;
     };
     // (the V of these keys has arrived, so their marks are complete)
-    auto poison = [&](const f16x &sc, int base) {
+    auto poison = [&](int base) {
         if (base < differ || base >= it.k1) return;
         const uint32_t bits = marked[(base - differ) >> 5];
         if (bits)
 #pragma unroll
             for (int e = 0; e < 16; e++)
-                if ((bits >> ((e >> 2) * 8 + half * 4 + (e & 3)) & 1) && sc[e] != -INFINITY)
+                if ((bits >> ((e >> 2) * 8 + half * 4 + (e & 3)) & 1) &&
+                    base + (e >> 2) * 8 + half * 4 + (e & 3) < lim)
                     l = NAN;
     };
     auto largest = [&](const f16x &sc) {
@@ -622,7 +624,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
         constexpr int B = decltype(which)::value, EDGE = decltype(edge)::value;
         const char *kl = B ? k1_lds : k0_lds, *vl = B ? v1_lds : v0_lds;
         const int next = base + kWideKeys;
-        if (EDGE) poison(sa, base);
+        if (EDGE) poison(base);
         read_k(kl);
         place();
         look_up(next + kWideKeys, next + kWideKeys + 32);
@@ -640,7 +642,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
         const float mb = largest(sb);
         mix<D / 16, 4, QS / (D / 16), true>();
         raise(mb);
-        if (EDGE) poison(sb, base + 32);
+        if (EDGE) poison(base + 32);
         __builtin_amdgcn_sched_barrier(0);
         scores(sa);
         read_v(vl + HB);
@@ -686,7 +688,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
             base += kWideKeys;
         }
         const char *kl = steps ? k1_lds : k0_lds, *vl = steps ? v1_lds : v0_lds;
-        poison(sa, base);
+        poison(base);
         weights(p, sa);
         read_v(vl);
         products(p);
@@ -694,7 +696,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
             read_k(kl);
             scores(sa);
             hide(sa, base + 32);
-            poison(sa, base + 32);
+            poison(base + 32);
             raise(largest(sa));
             weights(p, sa);
             read_v(vl + HB);

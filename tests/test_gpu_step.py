@@ -623,3 +623,22 @@ def test_many_small_weights(torch, name, size, n, group):
     u = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}[name]
     tol = 2.01 * u * want + 2.0 ** -15 * want + (keys * 2.0 ** -32 * 150 if name == "f16" else 0)
     near(got, want, tol, "out")
+
+
+@pytest.mark.parametrize("name", ["bf16", "f16"])
+@pytest.mark.parametrize("n,heads", [(5, 2), (40, 1)])
+def test_value_under_a_weight_of_zero(torch, name, n, heads):
+    """A key of -inf (score -inf, weight 0) does not hide its value from the rows that see
+    it: 0 times NaN is NaN."""
+    b = Batch(34, [n], [n + 50], heads, 1, 64)
+    k, v = caches(torch, b, dtype_of(torch, name), 3)
+    q = (torch.rand((n, heads, 64)) + 0.1).to(k.dtype).cuda()
+    s = b.step()
+    clean = s.attention(q, k, v)
+    bad = n // 2
+    page, at = b.blocks[0, (50 + bad) // 16], (50 + bad) % 16
+    k[page, 0, at] = -math.inf
+    v[page, 0, at, 7] = math.nan
+    got = s.attention(q, k, v)
+    assert torch.equal(got[:bad], clean[:bad])
+    assert not torch.isfinite(got[bad:, :, 7]).any()
