@@ -101,8 +101,7 @@ hipError_t launch(const AppendArgs &a, hipStream_t s) {
     constexpr int HPW = 64 / (D / 16);
     const int64_t units =
         (int64_t)a.n_tok * ((a.heads + 2 * a.kv_heads + HPW - 1) / HPW);
-    append_kernel<T, D><<<dim3((uint32_t)((units + 3) / 4)), 256, 0, s>>>(a);
-    return hipGetLastError();
+    return launch_kernel(append_kernel<T, D>, (units + 3) / 4, a, s);
 }
 
 }  // namespace

@@ -862,14 +862,10 @@ __global__ __launch_bounds__(256) void merge_kernel(AttnArgs a) {
 
 template <typename T, int D>
 hipError_t launch(const AttnArgs &a, int n, int n_merge, hipStream_t s) {
-    if (a.n_wide)
-        attn_kernel<T, D, true><<<dim3(n), 256, 0, s>>>(a);
-    else
-        attn_kernel<T, D, false><<<dim3(n), 256, 0, s>>>(a);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = launch_kernel(
+        a.n_wide ? attn_kernel<T, D, true> : attn_kernel<T, D, false>, n, a, s);
     if (e != hipSuccess || !n_merge) return e;
-    merge_kernel<T, D><<<dim3(n_merge), 256, 0, s>>>(a);
-    return hipGetLastError();
+    return launch_kernel(merge_kernel<T, D>, n_merge, a, s);
 }
 
 }  // namespace

@@ -94,6 +94,15 @@ struct AttnArgs {
     float scale2;       // scale * log2(e)
 };
 
+// Launches n workgroups of 256; the launch's own error. (hipGetLastError would also
+// return one that an earlier call of the program left.)
+template <typename Args>
+hipError_t launch_kernel(void (*kernel)(Args), int64_t n, const Args &a, hipStream_t s) {
+    Args copy = a;
+    void *args[] = {&copy};
+    return hipLaunchKernel((const void *)kernel, dim3((uint32_t)n), dim3(256), args, 0, s);
+}
+
 // Return hipSuccess or the launch's error.
 hipError_t launch_append(const AppendArgs &a, int dtype, int head_dim, hipStream_t s);
 hipError_t launch_attention(const AttnArgs &a, int n_items, int n_merge, int dtype, int head_dim,

@@ -642,3 +642,20 @@ def test_value_under_a_weight_of_zero(torch, name, n, heads):
     got = s.attention(q, k, v)
     assert torch.equal(got[:bad], clean[:bad])
     assert not torch.isfinite(got[bad:, :, 7]).any()
+
+
+def test_error_of_an_earlier_call_is_not_reported(torch):
+    """A call that failed before, and whose error nobody took, is not this one's."""
+    b = Batch(35, [1, 20], [30, 40], 4, 2, 64)
+    k, v = caches(torch, b, torch.bfloat16, 9)
+    s = b.step()
+    qkv = torch.randn((21, 8, 64), device="cuda", dtype=torch.bfloat16)
+    q, out = torch.empty((2, 21, 4, 64), device="cuda", dtype=torch.bfloat16)
+    L = step.lib()
+    try:
+        assert L.hipSetDevice(1 << 20) != 0
+        s.append(qkv, k, v, out=q)
+        s.attention(q, k, v, out=out)
+    finally:
+        L.hipGetLastError()
+    torch.cuda.synchronize()
