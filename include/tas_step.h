@@ -94,7 +94,7 @@ typedef struct tas_append {
 /* Arguments of tas_step_attention. */
 typedef struct tas_attention {
     int32_t dtype;
-    float scale;                   /* of the scores, positive and finite                     */
+    float scale;                   /* of the scores, positive; scale * log2(e) finite         */
     const void *q;                 /* [T][heads][head_dim]                                   */
     int64_t q_stride;
     void *out;                     /* [T][heads][head_dim]; may be q                         */

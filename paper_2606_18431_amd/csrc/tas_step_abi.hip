@@ -606,7 +606,8 @@ int tas_step_attention(tas_step *s, const tas_attention *a, void *stream) {
     if (!s || !a) return TAS_EINVAL;
     if (!s->ws) return TAS_ESTATE;
     if (a->dtype != TAS_F16 && a->dtype != TAS_BF16) return TAS_EINVAL;
-    if (!(a->scale > 0) || std::isinf(a->scale)) return TAS_EINVAL;
+    const float scale2 = a->scale * 1.4426950408889634f;
+    if (!(a->scale > 0) || std::isinf(scale2)) return TAS_EINVAL;
     if (!valid_cache(a->cache)) return TAS_EINVAL;
     if (s->head.n_tok == 0) return TAS_OK;
     const int64_t row = (int64_t)s->heads * s->head_dim;
@@ -630,7 +631,7 @@ int tas_step_attention(tas_step *s, const tas_attention *a, void *stream) {
     k.group = s->heads / s->kv_heads;
     k.heads = s->heads;
     k.sub_shift = s->blk_shift - 4;
-    k.scale2 = a->scale * 1.4426950408889634f;
+    k.scale2 = scale2;
     k.n_wide = s->head.n_wide;
     return launch_attention(k, s->head.n_wide + s->head.n_thin, s->head.n_merge, a->dtype,
                             s->head_dim, (hipStream_t)stream) == hipSuccess

@@ -659,3 +659,17 @@ def test_error_of_an_earlier_call_is_not_reported(torch):
     finally:
         L.hipGetLastError()
     torch.cuda.synchronize()
+
+
+def test_scale_beyond_the_exponent(torch):
+    """A scale that is finite itself, but not in the base 2 of the kernels: refused, where
+    every row would be NaN."""
+    b = Batch(37, [1, 20], [30, 40], 4, 2, 64)
+    k, v = caches(torch, b, torch.bfloat16, 9)
+    q = torch.randn((21, 4, 64), device="cuda", dtype=torch.bfloat16)
+    s = b.step()
+    s.attention(q, k, v, scale=2.3e38)
+    for scale in (2.4e38, 3e38, 3.4e38):
+        with pytest.raises(tas.TasError) as e:
+            s.attention(q, k, v, scale=scale)
+        assert e.value.code == tas.TAS_EINVAL
