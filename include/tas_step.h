@@ -106,9 +106,10 @@ typedef struct tas_attention {
 typedef struct tas_step tas_step;
 
 /* Validate and plan a batch (host only). TAS_EINVAL: a field out of range, a
- * block number outside the pool, in a causal batch a block that new tokens of two
- * requests, or two pages of one, would be written to (without causality such a
- * batch can be attended, not appended); TAS_ENOMEM: no host memory. */
+ * block number outside the pool, more than 2^24 tokens or work for as many
+ * workgroups, in a causal batch a block that new tokens of two requests, or two
+ * pages of one, would be written to (without causality such a batch can be
+ * attended, not appended); TAS_ENOMEM: no host memory. */
 int tas_step_create(const tas_batch *batch, tas_step **out);
 /* Bytes of device workspace that the step needs (plan and partial results). */
 size_t tas_step_bytes(const tas_step *step);

@@ -23,6 +23,7 @@ constexpr int64_t kMaxTokens = int64_t(1) << 24;     // of a batch
 constexpr int64_t kMaxPartRows = int64_t(1) << 28;
 constexpr int64_t kMaxStride = (int64_t(1) << 31) - 8;      // of a block or head, elements
 constexpr int64_t kMaxTokenStride = int64_t(1) << 24;       // of a token in a block
+constexpr int64_t kMaxGroups = (int64_t(1) << 24) - 1;      // of a launch: 2^32 threads
 constexpr int64_t kUnits = 256;                      // compute units
 constexpr int64_t kSlots = 2 * kUnits;               // wide items that run at once
 constexpr int32_t kThinItems = 768;                  // thin items wanted
@@ -237,7 +238,10 @@ int make_items(const tas_batch *b, Plan &p) {
         part_rows += (int64_t)Hk * s.nsplit * s.rows;
         if (part_rows > kMaxPartRows) return false;
         if (!joins) return true;
-        if (is_thin(s)) unit0[seg] = (int32_t)p.join.size();
+        if (is_thin(s))
+            unit0[seg] = (int32_t)p.join.size();
+        else if ((int64_t)p.merge.size() + Hk * ceil_div(s.rows, kJoinRows) > kMaxGroups)
+            return false;
         for (int32_t hk = 0; hk < Hk; hk++)
             for (int32_t row0 = 0; row0 < s.rows; row0 += kJoinRows)
                 (is_thin(s) ? p.join : p.merge)
@@ -268,7 +272,7 @@ int make_items(const tas_batch *b, Plan &p) {
     }
     int64_t n_items = 0;
     for (const Seg &s : p.segs) n_items += (int64_t)Hk * tiles_of(s) * s.nsplit;
-    if (n_items > INT32_MAX / 2) return TAS_EINVAL;
+    if (n_items > kMaxGroups) return TAS_EINVAL;
     for (size_t i = 0; i < p.segs.size(); i++) {
         const Seg &s = p.segs[i];
         const int32_t tile = tile_rows(s);
@@ -403,6 +407,7 @@ int make_plan(const tas_batch *b, Plan &p) {
     }
     // rows and heads of the batch are counted in 32 bits
     if (t * (b->heads + 2 * b->kv_heads) > INT32_MAX / 2) return TAS_EINVAL;
+    if (append_groups(t, b->heads, b->kv_heads, b->head_dim) > kMaxGroups) return TAS_EINVAL;
     if (p.appendable && !distinct_slots(b, p)) {
         // A causal batch's new tokens are the last ones of contexts of their own: a block
         // that two of them end in is an error of the tables. Without causality they may

@@ -25,7 +25,7 @@ using vec8 = T __attribute__((ext_vector_type(8)));
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
-    constexpr int LPH = D / 16, HPW = 64 / LPH;  // lanes of a head, heads of a wave
+    constexpr int LPH = D / 16, HPW = heads_of_wave(D);  // lanes of a head, heads of a wave
     using V = vec8<T>;
     const int lane = threadIdx.x & 63, i = lane % LPH;
     const uint32_t per_tok = (a.heads + 2 * a.kv_heads + HPW - 1) / HPW;
@@ -98,10 +98,8 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
 
 template <typename T, int D>
 hipError_t launch(const AppendArgs &a, hipStream_t s) {
-    constexpr int HPW = 64 / (D / 16);
-    const int64_t units =
-        (int64_t)a.n_tok * ((a.heads + 2 * a.kv_heads + HPW - 1) / HPW);
-    return launch_kernel(append_kernel<T, D>, (units + 3) / 4, a, s);
+    return launch_kernel(append_kernel<T, D>, append_groups(a.n_tok, a.heads, a.kv_heads, D), a,
+                         s);
 }
 
 }  // namespace

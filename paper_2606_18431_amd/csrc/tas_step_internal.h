@@ -75,6 +75,13 @@ struct AppendArgs {
     float eps;
 };
 
+constexpr int heads_of_wave(int head_dim) { return 1024 / head_dim; }  // 16 elements a lane
+// Workgroups of an append: four waves, each for some heads of one token.
+inline int64_t append_groups(int64_t n_tok, int heads, int kv_heads, int head_dim) {
+    const int n = heads_of_wave(head_dim);
+    return (n_tok * ((heads + 2 * kv_heads + n - 1) / n) + 3) / 4;
+}
+
 struct AttnArgs {
     const Item *items;
     const int32_t *tables;

@@ -359,3 +359,20 @@ def test_new_tokens_in_one_block_without_causality():
     assert not refused([20], [20], [[5, 5]], causal=False)
     assert refused([1, 1], [20, 20], pages)
     assert refused([1, 2], [20, 32], pages)
+
+
+def test_batches_of_more_workgroups_than_a_launch_takes():
+    """A launch has fewer than 2^32 threads, 2^24 workgroups of 256: batches beyond that
+    are refused when they are planned, not after append has written the cache."""
+    # as many items: one for each request and key head
+    n = 1 << 15
+    one = np.arange(n).reshape(n, 1)
+    assert refused(np.ones(n, int), np.ones(n, int), one, n_blocks=n, heads=512, kv_heads=512)
+    # as many groups of 16 rows whose parts of a prefix are merged
+    assert refused([1 << 22], [0], [[0]], heads=64, kv_heads=64, causal=False,
+                   prefix_first=[0, 1], prefix_len=[16], prefix_blocks=[[1]])
+    # tokens and heads to append, at 8 heads of a token to a wave
+    n = 1 << 21
+    kw = dict(heads=128, kv_heads=128, head_dim=128, block_tokens=4096, n_blocks=512)
+    assert refused([n], [n], np.arange(512).reshape(1, -1), **kw)
+    assert not refused([n // 8], [n // 8], np.arange(512).reshape(1, -1), **kw)
