@@ -63,9 +63,10 @@ typedef struct tas_batch {
 /* One layer's cache: element (block, head, token of the block, d) of K lies at
  * k + block * k_block + head * k_head + token * k_token + d (elements); V
  * likewise. Pointers 16-byte aligned, strides multiples of 8, below 2^31, of a
- * token at most 2^24. For tas_step_append no two elements of K, or of V, may lie in
- * one place: in the order of the strides, each is at least as long as what the
- * shorter ones span. */
+ * token at most 2^24. For tas_step_append no two elements of the pool's K and V may
+ * lie in one place: in the order of the strides, each is at least as long as what the
+ * shorter ones span, and K and V have no element in common (they may alternate, by
+ * blocks, heads, tokens or halves of a row). */
 typedef struct tas_cache {
     void *k, *v;
     int64_t k_block, k_head, k_token;

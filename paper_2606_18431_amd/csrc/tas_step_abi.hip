@@ -14,6 +14,7 @@
 
 #include "tas_step.h"
 #include "tas_step_internal.h"
+#include "tas_step_overlap.h"
 
 using namespace tas_step_impl;
 
@@ -486,6 +487,13 @@ bool disjoint_slots(int64_t block, int64_t head, int64_t token, int64_t n_blocks
     return true;
 }
 
+// The memory of one of a cache's tensors (aligned, strides in elements).
+Region region_of(const void *p, int64_t block, int64_t head, int64_t token, int64_t n_blocks,
+                 int64_t kv_heads, int64_t block_tokens, int64_t head_dim) {
+    return {(int64_t)((uintptr_t)p / 16), head_dim / 8, {block / 8, head / 8, token / 8},
+            {n_blocks, kv_heads, block_tokens}};
+}
+
 bool valid_rows(const void *p, int64_t stride, int64_t row) {
     return aligned16(p) && stride >= row && stride % 8 == 0;
 }
@@ -575,10 +583,14 @@ int tas_step_append(tas_step *s, const tas_append *a, void *stream) {
     if (!valid_cache(a->cache)) return TAS_EINVAL;
     const tas_cache &c = a->cache;
     const int64_t bt = int64_t(1) << s->blk_shift;
-    if (c.k == c.v ||
-        !disjoint_slots(c.k_block, c.k_head, c.k_token, s->n_blocks, s->kv_heads, bt, D) ||
+    if (!disjoint_slots(c.k_block, c.k_head, c.k_token, s->n_blocks, s->kv_heads, bt, D) ||
         !disjoint_slots(c.v_block, c.v_head, c.v_token, s->n_blocks, s->kv_heads, bt, D))
         return TAS_EINVAL;
+    const Region kr =
+        region_of(c.k, c.k_block, c.k_head, c.k_token, s->n_blocks, s->kv_heads, bt, D);
+    const Region vr =
+        region_of(c.v, c.v_block, c.v_head, c.v_token, s->n_blocks, s->kv_heads, bt, D);
+    if (Overlap()(kr, vr)) return TAS_EINVAL;  // (K of a token and V of another would race)
     if (s->head.n_tok == 0) return TAS_OK;
     if (!valid_rows(a->qkv, a->qkv_stride, (s->heads + 2 * s->kv_heads) * D) ||
         !valid_rows(a->q_out, a->q_out_stride, s->heads * D))

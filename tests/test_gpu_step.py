@@ -673,3 +673,29 @@ def test_scale_beyond_the_exponent(torch):
         with pytest.raises(tas.TasError) as e:
             s.attention(q, k, v, scale=scale)
         assert e.value.code == tas.TAS_EINVAL
+
+
+def test_append_refuses_k_and_v_in_one_place(torch):
+    """K and V that are parts of one pool: a block further on their slots are the same
+    memory, which new keys and values would race for; beside each other they are not."""
+    b = Batch(39, [1, 4], [30, 20], 4, 2, 64)
+    n = b.n_blocks
+    s = b.step()
+    qkv = torch.randn((5, 8, 64), device="cuda", dtype=torch.bfloat16)
+    pool = torch.zeros((2 * n, 2, 16, 64), device="cuda", dtype=torch.bfloat16)
+    for k, v in ((pool[:n], pool[1:n + 1]), (pool[1:n + 1], pool[:n]), (pool[:n], pool[:n]),
+                 (pool.flatten()[8:8 + pool[:n].numel()].view_as(pool[:n]), pool[n:])):
+        with pytest.raises(tas.TasError) as e:
+            s.append(qkv, k, v)
+        assert e.value.code == tas.TAS_EINVAL
+        assert not pool.any()
+    wide = torch.zeros((n, 2, 16, 128), device="cuda", dtype=torch.bfloat16)
+    beside = torch.zeros((n, 2, 2, 16, 64), device="cuda", dtype=torch.bfloat16)
+    last = torch.zeros((n, 2, 16, 2, 64), device="cuda", dtype=torch.bfloat16)
+    want = None
+    for k, v in ((pool[:n], pool[n:]), (pool[::2], pool[1::2]), (wide[..., :64], wide[..., 64:]),
+                 (beside[:, 1], beside[:, 0]), (last[:, :, :, 0], last[:, :, :, 1])):
+        k.zero_(), v.zero_()
+        s.append(qkv, k, v)
+        want = want or (k.clone(), v.clone())
+        assert torch.equal(k, want[0]) and torch.equal(v, want[1])
