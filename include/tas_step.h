@@ -84,7 +84,7 @@ typedef struct tas_append {
     float eps;                     /* of the norm, >= 0                                      */
     const void *qkv;               /* [T][heads + 2 kv_heads][head_dim]: queries, keys, values */
     int64_t qkv_stride;
-    void *q_out;                   /* [T][heads][head_dim]; may not overlap qkv              */
+    void *q_out;                   /* [T][heads][head_dim]; may be qkv, with its stride      */
     int64_t q_out_stride;
     const void *q_weight, *k_weight; /* [head_dim] norm weights; both, or both NULL: no norm */
     const float *cos, *sin;        /* float [positions][rot_dim / 2], rows adjacent          */
@@ -95,10 +95,10 @@ typedef struct tas_append {
 /* Arguments of tas_step_attention. */
 typedef struct tas_attention {
     int32_t dtype;
-    float scale;                   /* of the scores, positive; scale * log2(e) finite         */
+    float scale;                   /* of the scores, positive; scale * log2(e) finite        */
     const void *q;                 /* [T][heads][head_dim]                                   */
     int64_t q_stride;
-    void *out;                     /* [T][heads][head_dim]; may be q                         */
+    void *out;                     /* [T][heads][head_dim]; may be q, with its stride        */
     int64_t out_stride;
     float *lse;                    /* float [T][heads]: log of the sum of exp(scores), or NULL */
     tas_cache cache;
@@ -127,8 +127,8 @@ int64_t tas_step_tokens(const tas_step *step);
  *     (a, b) <- (a cos - b sin, b cos + a sin)      (each rotated pair)
  * queries go to q_out, keys and the unchanged values to the token's slot of the
  * cache. In 32 bits, rounded once. TAS_EINVAL: an argument out of range or
- * unaligned, a cache whose slots overlap, a batch with kv_len[i] < n_new[i] or new
- * tokens in one block, positions too small;
+ * unaligned, a cache whose slots overlap, tensors that overlap, a batch with
+ * kv_len[i] < n_new[i] or new tokens in one block, positions too small;
  * TAS_ESTATE: not bound (also below). */
 int tas_step_append(tas_step *step, const tas_append *a, void *stream);
 
@@ -136,10 +136,11 @@ int tas_step_append(tas_step *step, const tas_append *a, void *stream);
  * prefix and the keys y < kv_len[i] of its own context (causal: y <= kv_len[i] -
  * n_new[i] + j); query head h reads key head h / (heads / kv_heads). Scores, maxima
  * and sums are held in 32 bits; the softmax's weights are rounded to the tensors'
- * type for the product with V, and the result once. A row
- * without keys gives 0 and lse -inf. What a row does not see does not reach it,
- * whatever the slots hold; a value that it sees and that is not finite makes its
- * element not finite, or the whole row NaN. */
+ * type for the product with V, and the result once. A row without keys gives 0 and
+ * lse -inf. What a row does not see does not reach it, whatever the slots hold; a
+ * value that it sees and that is not finite makes its element not finite, or the
+ * whole row NaN. TAS_EINVAL: an argument out of range or
+ * unaligned, out over a part of q or of the cache. */
 int tas_step_attention(tas_step *step, const tas_attention *a, void *stream);
 
 /* The plan that tas_step_bind copies to the device, for inspection: writes it to

@@ -494,6 +494,22 @@ Region region_of(const void *p, int64_t block, int64_t head, int64_t token, int6
             {n_blocks, kv_heads, block_tokens}};
 }
 
+// The rows of n_tok tokens (aligned, the stride in elements).
+Region region_of(const void *p, int64_t stride, int64_t row, int64_t n_tok) {
+    return {(int64_t)((uintptr_t)p / 16), row / 8, {stride / 8, 0, 0}, {n_tok, 1, 1}};
+}
+
+// Whether an output's rows are in memory that is read or written besides. They may be the
+// input's own rows: a row is read before it is written.
+bool clash(const void *out, int64_t out_stride, int64_t out_row, const void *in,
+           int64_t in_stride, int64_t in_row, int64_t n_tok, const Region &k, const Region &v) {
+    const Region o = region_of(out, out_stride, out_row, n_tok);
+    Overlap overlap;
+    const bool in_place = out == in && (out_stride == in_stride || n_tok == 1);
+    return (!in_place && overlap(o, region_of(in, in_stride, in_row, n_tok))) || overlap(o, k) ||
+           overlap(o, v);
+}
+
 bool valid_rows(const void *p, int64_t stride, int64_t row) {
     return aligned16(p) && stride >= row && stride % 8 == 0;
 }
@@ -592,8 +608,14 @@ int tas_step_append(tas_step *s, const tas_append *a, void *stream) {
         region_of(c.v, c.v_block, c.v_head, c.v_token, s->n_blocks, s->kv_heads, bt, D);
     if (Overlap()(kr, vr)) return TAS_EINVAL;  // (K of a token and V of another would race)
     if (s->head.n_tok == 0) return TAS_OK;
-    if (!valid_rows(a->qkv, a->qkv_stride, (s->heads + 2 * s->kv_heads) * D) ||
-        !valid_rows(a->q_out, a->q_out_stride, s->heads * D))
+    const int64_t in_row = (s->heads + 2 * s->kv_heads) * D, out_row = s->heads * D;
+    if (!valid_rows(a->qkv, a->qkv_stride, in_row) ||
+        !valid_rows(a->q_out, a->q_out_stride, out_row))
+        return TAS_EINVAL;
+    const Region in = region_of(a->qkv, a->qkv_stride, in_row, s->head.n_tok);
+    if (clash(a->q_out, a->q_out_stride, out_row, a->qkv, a->qkv_stride, in_row, s->head.n_tok, kr,
+              vr) ||
+        Overlap()(in, kr) || Overlap()(in, vr))
         return TAS_EINVAL;
     AppendArgs k{};
     k.reqs = (const Req *)(s->ws + s->head.req);
@@ -629,6 +651,12 @@ int tas_step_attention(tas_step *s, const tas_attention *a, void *stream) {
     if (s->head.n_tok == 0) return TAS_OK;
     const int64_t row = (int64_t)s->heads * s->head_dim;
     if (!valid_rows(a->q, a->q_stride, row) || !valid_rows(a->out, a->out_stride, row))
+        return TAS_EINVAL;
+    const tas_cache &c = a->cache;
+    const int64_t bt = int64_t(1) << s->blk_shift, D = s->head_dim;
+    if (clash(a->out, a->out_stride, row, a->q, a->q_stride, row, s->head.n_tok,
+              region_of(c.k, c.k_block, c.k_head, c.k_token, s->n_blocks, s->kv_heads, bt, D),
+              region_of(c.v, c.v_block, c.v_head, c.v_token, s->n_blocks, s->kv_heads, bt, D)))
         return TAS_EINVAL;
     AttnArgs k{};
     k.tables = (const int32_t *)(s->ws + s->head.tables);

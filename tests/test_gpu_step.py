@@ -699,3 +699,49 @@ def test_append_refuses_k_and_v_in_one_place(torch):
         s.append(qkv, k, v)
         want = want or (k.clone(), v.clone())
         assert torch.equal(k, want[0]) and torch.equal(v, want[1])
+
+
+def test_outputs_over_other_tensors(torch):
+    """An output may be its input's own rows, or lie between rows; over other rows, heads
+    or the cache it is refused, and nothing is written."""
+    b = Batch(40, [1, 4, 60], [300, 20, 90], 4, 2, 64)
+    k, v = caches(torch, b, torch.bfloat16, 9, poison=False)
+    s = b.step()
+    T = b.T
+    buf = torch.randn((T + 1, 16, 64), device="cuda", dtype=torch.bfloat16)
+    qkv = buf[:T, :8]
+    ke, ve = k.clone(), v.clone()
+    cos, sin = torch.rand((2, 300, 32), device="cuda")
+    want_q = s.append(qkv.contiguous(), ke, ve, cos, sin)
+    want = s.attention(want_q, ke, ve)
+    first = buf.clone(), k.clone(), v.clone()
+    flat = k.flatten()[:T * 4 * 64].view(T, 4, 64)
+    for out in (qkv[:, 1:5], qkv[:, 4:8], buf[1:, :4], buf[:T, 6:10], flat,
+                buf.flatten()[8:].as_strided((T, 4, 64), (1024, 64, 1)),
+                buf.flatten()[:T * 256].view(T, 4, 64)):
+        with pytest.raises(tas.TasError) as e:
+            s.append(qkv, k, v, cos, sin, out=out)
+        assert e.value.code == tas.TAS_EINVAL
+    inside = v.flatten()[:T * 8 * 64].view(T, 8, 64)
+    with pytest.raises(tas.TasError):
+        s.append(inside, k, v, cos, sin)
+    assert all(torch.equal(x, y) for x, y in zip(first, (buf, k, v)))
+    k1, v1 = k.clone(), v.clone()
+    s.append(qkv, k1, v1, cos, sin, out=buf[:T, 8:12])
+    assert torch.equal(buf[:T, 8:12], want_q) and torch.equal(k1, ke) and torch.equal(v1, ve)
+    k1, v1 = k.clone(), v.clone()
+    s.append(qkv, k1, v1, cos, sin, out=qkv[:, :4])  # in place
+    assert torch.equal(qkv[:, :4], want_q) and torch.equal(k1, ke) and torch.equal(v1, ve)
+    assert torch.equal(buf[:T, 4:8], first[0][:T, 4:8])
+
+    q, first = buf[:T, :4], buf.clone()
+    for out in (buf[1:, :4], buf[:T, 1:5], ke.flatten()[:T * 256].view(T, 4, 64),
+                buf.flatten()[:T * 256].view(T, 4, 64)):
+        with pytest.raises(tas.TasError) as e:
+            s.attention(q, ke, ve, out=out)
+        assert e.value.code == tas.TAS_EINVAL
+    assert torch.equal(buf, first) and torch.equal(k1, ke)
+    s.attention(q, ke, ve, out=buf[:T, 4:8])
+    assert torch.equal(buf[:T, 4:8], want)
+    s.attention(q, ke, ve, out=q)
+    assert torch.equal(q, want)
