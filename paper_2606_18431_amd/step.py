@@ -199,7 +199,8 @@ class Step:
     Caches are tensors [n_blocks, kv_heads, block_tokens, head_dim], any strides
     (a permuted view serves other orders) whose last is 1. Calls are enqueued on
     ``stream`` (a torch stream; default: the current one); outputs are allocated
-    on that stream unless given. Attention calls of one step share its
+    on that stream unless given, and the tensors of a call may be dropped while it is
+    under way there (what it reads has to be written before: order the streams). Attention calls of one step share its
     workspace: keep them on one stream, or order them. A step is used by one host thread
     at a time."""
 
@@ -278,13 +279,15 @@ class Step:
                 out = like.new_empty(self.q_shape)
         return out, out.data_ptr(), self.heads * self.head_dim
 
-    def _enqueue(self, call, stream):
+    def _enqueue(self, call, stream, used):
         if self.ctx is None:
             raise ValueError("the step is closed")
-        if stream is None:
-            raw = torch._C._cuda_getCurrentRawStream(self.index)
-        else:
+        raw = torch._C._cuda_getCurrentRawStream(self.index)
+        if stream is not None and stream.cuda_stream != raw:
             raw = stream.cuda_stream
+            for t in used:  # their memory is not given away before the work there is done
+                if t is not None:
+                    t.record_stream(stream)
         if raw != self._home:  # the workspace outlives the work there
             self.ws.record_stream(torch.cuda.ExternalStream(raw) if stream is None else stream)
         if torch._C._cuda_getDevice() == self.index:
@@ -333,7 +336,8 @@ class Step:
         out, out_p, out_s = self._out(out, qkv, stream)
         _APPEND.pack_into(self._args, 0, dtype, rot, 1 if interleaved else 0, eps, qkv_p, qkv_s,
                           out_p, out_s, qw_p, kw_p, cos_p, sin_p, positions, *cache)
-        self._enqueue(self._lib.tas_step_append, stream)
+        self._enqueue(self._lib.tas_step_append, stream,
+                      (qkv, k_cache, v_cache, cos, sin, q_weight, k_weight, out))
         return out
 
     def attention(self, q, k_cache, v_cache, *, scale=None, out=None, lse=None, stream=None):
@@ -355,7 +359,7 @@ class Step:
         if scale is None:
             scale = self.head_dim ** -0.5
         _ATTENTION.pack_into(self._args, 0, dtype, scale, q_p, q_s, out_p, out_s, lse_p, *cache)
-        self._enqueue(self._lib.tas_step_attention, stream)
+        self._enqueue(self._lib.tas_step_attention, stream, (q, k_cache, v_cache, lse, out))
         return out
 
     def close(self):

@@ -745,3 +745,43 @@ def test_outputs_over_other_tensors(torch):
     assert torch.equal(buf[:T, 4:8], want)
     s.attention(q, ke, ve, out=q)
     assert torch.equal(q, want)
+
+
+def test_tensors_dropped_while_another_stream_uses_them(torch):
+    """Memory of a call's tensors is not reused before the call on its stream is done."""
+    b = Batch(41, [1, 40], [300, 90], 4, 2, 64)
+    k, v = caches(torch, b, torch.bfloat16, 9, poison=False)
+    s = b.step()
+    qkv = torch.randn((b.T, 8, 64), device="cuda", dtype=torch.bfloat16)
+    cos, sin = torch.rand((2, 300, 32), device="cuda")
+    ke, ve = k.clone(), v.clone()
+    want_q = s.append(qkv, ke, ve, cos, sin)
+    want = s.attention(want_q, ke, ve)
+    a = torch.randn((8192, 8192), device="cuda", dtype=torch.bfloat16)
+    a @ a
+    side = torch.cuda.Stream()
+
+    def busy():
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for _ in range(50):
+                torch.mm(a, a)
+
+    def dropped(call, tensors):
+        """The call's result on the busy stream; the tensors' memory asked for again."""
+        torch.cuda.synchronize()
+        tensors = [t.clone() for t in tensors]
+        busy()
+        out = call(*tensors)
+        places = {t.data_ptr() for t in tensors}
+        sizes = [t.numel() * t.element_size() for t in tensors]
+        del tensors
+        again = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes]
+        assert not places & {t.data_ptr() for t in again}
+        side.synchronize()
+        return out
+
+    got = dropped(lambda *t: s.append(*t, stream=side), [qkv, k, v, cos, sin])
+    assert torch.equal(got, want_q)
+    got = dropped(lambda *t: s.attention(*t, stream=side), [want_q, ke, ve])
+    assert torch.equal(got, want)
