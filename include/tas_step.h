@@ -115,7 +115,8 @@ int tas_step_create(const tas_batch *batch, tas_step **out);
 /* Bytes of device workspace that the step needs (plan and partial results). */
 size_t tas_step_bytes(const tas_step *step);
 /* Copy the plan to d_ws (256-byte aligned, at least tas_step_bytes) on the
- * stream, and wait for that. d_ws must outlive the step's last call and stay
+ * stream, and wait for that (and so for all that the stream was given before: use a
+ * stream of its own where planning is not to wait for work). d_ws must outlive the step's last call and stay
  * untouched by others. TAS_EINVAL, TAS_ENOMEM (ws_bytes too small), TAS_EHIP. */
 int tas_step_bind(tas_step *step, void *d_ws, size_t ws_bytes, void *stream);
 void tas_step_destroy(tas_step *step);

@@ -192,6 +192,16 @@ def tas_step_destroy(ctx):
         lib().tas_step_destroy(ctx)
 
 
+_plan_streams = {}  # of a device
+
+
+def _plan_stream(index):
+    """The stream on which plans are copied to a device."""
+    if index not in _plan_streams:
+        _plan_streams[index] = torch.cuda.Stream(torch.device("cuda", index))
+    return _plan_streams[index]
+
+
 class Step:
     """The plan of one batch on one GPU: made once when the scheduler has
     formed the batch, used for every layer.
@@ -226,12 +236,15 @@ class Step:
         self.q_shape = (self.tokens, heads, head_dim)
         self.qkv_shape = (self.tokens, heads + 2 * kv_heads, head_dim)
         self.cache_shape = (n_blocks, kv_heads, block_tokens, head_dim)
-        with torch.cuda.device(self.device):
-            # the stream whose allocator pool the workspace comes from
-            self._home = torch.cuda.current_stream().cuda_stream
+        # Binding waits for its stream: one of its own, so that planning the next batch does
+        # not wait for the layers of this one. The workspace is that stream's memory, as
+        # memory of another might still be in use there.
+        side = _plan_stream(self.index)
+        with torch.cuda.stream(side):
             self.ws = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=self.device)
             tas_step_bind(self.ctx, self.ws.data_ptr() + (-self.ws.data_ptr()) % 256,
-                          self.ws_bytes, self._home)
+                          self.ws_bytes, side.cuda_stream)
+        self._streams = set()  # that the workspace is recorded on
 
     # ------------------------------------------------------------ argument checks
 
@@ -288,8 +301,10 @@ class Step:
             for t in used:  # their memory is not given away before the work there is done
                 if t is not None:
                     t.record_stream(stream)
-        if raw != self._home:  # the workspace outlives the work there
-            self.ws.record_stream(torch.cuda.ExternalStream(raw) if stream is None else stream)
+        if raw not in self._streams:  # the workspace outlives the work there
+            self.ws.record_stream(torch.cuda.ExternalStream(raw, self.device) if stream is None
+                                  else stream)
+            self._streams.add(raw)
         if torch._C._cuda_getDevice() == self.index:
             rc = call(self.ctx, self._args_p, raw)
         else:

@@ -785,3 +785,22 @@ def test_tensors_dropped_while_another_stream_uses_them(torch):
     assert torch.equal(got, want_q)
     got = dropped(lambda *t: s.attention(*t, stream=side), [want_q, ke, ve])
     assert torch.equal(got, want)
+
+
+def test_planning_does_not_wait_for_the_device(torch):
+    """A step is made while the device still works on what came before; its calls come
+    after that, and its workspace is not one that the work before still uses."""
+    b = Batch(36, [1, 20], [30, 40], 4, 2, 64)
+    k, v = caches(torch, b, torch.bfloat16, 9, poison=False)
+    q = torch.randn((21, 4, 64), device="cuda", dtype=torch.bfloat16)
+    want = b.step().attention(q, k, v)
+    a = torch.randn((8192, 8192), device="cuda", dtype=torch.bfloat16)
+    a @ a
+    torch.cuda.synchronize()
+    done = torch.cuda.Event()
+    for _ in range(100):
+        a @ a
+    done.record()
+    got = [b.step().attention(q, k, v) for _ in range(5)]
+    assert not done.query()
+    assert all(torch.equal(x, want) for x in got)
