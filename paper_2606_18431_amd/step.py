@@ -192,6 +192,18 @@ def tas_step_destroy(ctx):
         lib().tas_step_destroy(ctx)
 
 
+class _NoBackward(torch.autograd.Function):
+    """Outputs of inputs that require a gradient say so, and refuse to compute it."""
+
+    @staticmethod
+    def forward(ctx, out, *inputs):
+        return out.detach()
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise NotImplementedError("the serving step has no backward pass")
+
+
 _plan_streams = {}  # of a device
 
 
@@ -209,10 +221,14 @@ class Step:
     Caches are tensors [n_blocks, kv_heads, block_tokens, head_dim], any strides
     (a permuted view serves other orders) whose last is 1. Calls are enqueued on
     ``stream`` (a torch stream; default: the current one); outputs are allocated
-    on that stream unless given, and the tensors of a call may be dropped while it is
-    under way there (what it reads has to be written before: order the streams). Attention calls of one step share its
-    workspace: keep them on one stream, or order them. A step is used by one host thread
-    at a time."""
+    on that stream unless given, and the tensors of a call may be dropped while it
+    is under way there (what it reads has to be written before: order the streams).
+    Attention calls of one step share its workspace: keep them on one stream, or
+    order them. A step is used by one host thread at a time. A graph that captured
+    its calls reads its workspace: keep the step as long as the graph.
+
+    There is no backward pass: where an input requires a gradient (and grad mode is on),
+    the output does too, and a backward pass through it raises NotImplementedError."""
 
     def __init__(self, n_new, kv_len, blocks, *, heads, kv_heads, head_dim, block_tokens,
                  n_blocks, prefix_first=None, prefix_len=None, prefix_blocks=None, causal=True,
@@ -353,6 +369,10 @@ class Step:
                           out_p, out_s, qw_p, kw_p, cos_p, sin_p, positions, *cache)
         self._enqueue(self._lib.tas_step_append, stream,
                       (qkv, k_cache, v_cache, cos, sin, q_weight, k_weight, out))
+        if (qkv.requires_grad or qw_p and (q_weight.requires_grad or k_weight.requires_grad)
+                or cos_p and (cos.requires_grad or sin.requires_grad)) \
+                and torch.is_grad_enabled():
+            return _NoBackward.apply(out, qkv, q_weight, k_weight, cos, sin)
         return out
 
     def attention(self, q, k_cache, v_cache, *, scale=None, out=None, lse=None, stream=None):
@@ -375,6 +395,9 @@ class Step:
             scale = self.head_dim ** -0.5
         _ATTENTION.pack_into(self._args, 0, dtype, scale, q_p, q_s, out_p, out_s, lse_p, *cache)
         self._enqueue(self._lib.tas_step_attention, stream, (q, k_cache, v_cache, lse, out))
+        if (q.requires_grad or k_cache.requires_grad or v_cache.requires_grad) \
+                and torch.is_grad_enabled():
+            return _NoBackward.apply(out, q, k_cache, v_cache)
         return out
 
     def close(self):

@@ -804,3 +804,45 @@ def test_planning_does_not_wait_for_the_device(torch):
     got = [b.step().attention(q, k, v) for _ in range(5)]
     assert not done.query()
     assert all(torch.equal(x, want) for x in got)
+
+
+def test_a_backward_pass_is_refused(torch):
+    """An input's gradient is not lost without a word; values are those without one."""
+    b = Batch(38, [1, 20], [30, 40], 4, 2, 64)
+    k, v = caches(torch, b, torch.bfloat16, 9)
+    s = b.step()
+    q = torch.randn((21, 4, 64), device="cuda", dtype=torch.bfloat16)
+    qkv = torch.randn((21, 8, 64), device="cuda", dtype=torch.bfloat16)
+    w = torch.ones(64, device="cuda", dtype=torch.bfloat16)
+    cos = torch.rand((40, 32), device="cuda")
+    want = s.attention(q, k, v)
+    assert not want.requires_grad
+
+    def grad(t):
+        return t.detach().clone().requires_grad_()
+
+    for args in ((grad(q), k, v), (q, grad(k), v), (q, k, grad(v))):
+        out = s.attention(*args)
+        assert out.requires_grad and torch.equal(out, want)
+        with pytest.raises(NotImplementedError):
+            out.float().sum().backward()
+        given = torch.empty_like(q)
+        assert s.attention(*args, out=given).data_ptr() == given.data_ptr()
+        assert torch.equal(given, want) and not given.requires_grad
+        with torch.no_grad():
+            assert not s.attention(*args).requires_grad
+        with torch.inference_mode():
+            assert torch.equal(s.attention(*args), want)
+    x = s.append(qkv, k, v, cos, cos, q_weight=w, k_weight=w)
+    assert not x.requires_grad
+    for args in ((grad(qkv), cos, cos, w, w), (qkv, grad(cos), cos, w, w),
+                 (qkv, cos, grad(cos), w, w), (qkv, cos, cos, grad(w), w),
+                 (qkv, cos, cos, w, grad(w))):
+        out = s.append(args[0], k, v, args[1], args[2], q_weight=args[3], k_weight=args[4])
+        assert out.requires_grad and torch.equal(out, x)
+        with pytest.raises(NotImplementedError):
+            out.float().sum().backward()
+        with torch.no_grad():
+            assert not s.append(args[0], k, v, args[1], args[2], q_weight=args[3],
+                                k_weight=args[4]).requires_grad
+    assert not s.append(grad(qkv).detach(), k, v).requires_grad
