@@ -16,6 +16,7 @@ from __future__ import annotations
 
 import argparse
 import dataclasses
+import math
 
 import numpy as np
 
@@ -78,45 +79,53 @@ def form_iteration(w: W.Workload, trace: int, first: int, rng, prefix_blocks: in
     return Iteration(n_new, kv_len, blocks)
 
 
-class Layer:
-    """One layer's cache and the inputs of its attention, random values."""
+class Layers:
+    """The layers' caches, one of each layer's own as in a model (as many as the memory
+    holds, in turn), and the inputs of their attention; random values."""
 
-    def __init__(self, e: W.Engine, heads, kv_heads, head_dim, dtype, device, positions):
+    def __init__(self, e: W.Engine, layers, heads, kv_heads, head_dim, dtype, device, positions):
         import torch
 
         self.torch = torch
         shape = (e.kv_blocks, kv_heads, e.block_tokens, head_dim)
         g = torch.Generator(device=device)
         g.manual_seed(0)
-        self.k_cache = torch.randn(shape, generator=g, device=device, dtype=dtype)
-        self.v_cache = torch.randn(shape, generator=g, device=device, dtype=dtype)
-        self.qkv = torch.randn((e.max_tokens, heads + 2 * kv_heads, head_dim), generator=g,
-                               device=device, dtype=dtype)
+
+        def random(*shape):
+            return torch.randn(shape, generator=g, device=device, dtype=dtype)
+
+        self.layers, caches = layers, layers
+        if torch.device(device).type == "cuda":
+            layer_bytes = 2 * random(1).element_size() * math.prod(shape)
+            caches = min(layers, max(1, torch.cuda.mem_get_info(device)[0] * 3 // 4 // layer_bytes))
+        self.caches = [(random(*shape), random(*shape)) for _ in range(caches)]
+        self.qkv = random(e.max_tokens, heads + 2 * kv_heads, head_dim)
         self.weight = torch.ones(head_dim, device=device, dtype=dtype)
         freq = 1e4 ** (-torch.arange(0, head_dim, 2, device=device, dtype=torch.float64) / head_dim)
         angle = torch.arange(positions, device=device, dtype=torch.float64)[:, None] * freq
         self.cos, self.sin = angle.cos().float(), angle.sin().float()
 
     def run(self, step):
-        """The attention of one layer for the step's batch; returns its output."""
-        q = step.append(self.qkv[:step.tokens], self.k_cache, self.v_cache, self.cos, self.sin,
-                        q_weight=self.weight, k_weight=self.weight)
-        return step.attention(q, self.k_cache, self.v_cache)
+        """The attention of all layers, one after another, for the step's batch."""
+        for i in range(self.layers):
+            k_cache, v_cache = self.caches[i % len(self.caches)]
+            q = step.append(self.qkv[:step.tokens], k_cache, v_cache, self.cos, self.sin,
+                            q_weight=self.weight, k_weight=self.weight)
+            step.attention(q, k_cache, v_cache)
 
-    def time_us(self, step, layers: int, repeats: int = 3) -> float:
-        """Microseconds of ``layers`` layers, one after another."""
+    def time_us(self, step, repeats: int = 3) -> float:
+        """Microseconds of the layers, the median of some passes."""
         torch = self.torch
         self.run(step)
-        best = float("inf")
+        times = []
         for _ in range(repeats):
             a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
             a.record()
-            for _ in range(layers):
-                self.run(step)
+            self.run(step)
             b.record()
             b.synchronize()
-            best = min(best, a.elapsed_time(b) * 1e3)
-        return best
+            times.append(a.elapsed_time(b) * 1e3)
+        return float(np.median(times))
 
 
 def fit(tokens, context, us):
@@ -150,8 +159,8 @@ def measure(w: W.Workload, *, iterations=24, layers=32, heads=32, kv_heads=8, he
     rng = np.random.default_rng([seed, 31])
     prefix_pages = -(-prefix // e.block_tokens)
     positions = prefix + int((w.prompt.astype(np.int64) + w.decode).max())
-    layer = Layer(e, heads, kv_heads, head_dim,
-                  {"bf16": torch.bfloat16, "f16": torch.float16}[dtype], device, positions)
+    model = Layers(e, layers, heads, kv_heads, head_dim,
+                   {"bf16": torch.bfloat16, "f16": torch.float16}[dtype], device, positions)
     rows = []
     for i in range(iterations):
         it = form_iteration(w, int(rng.integers(0, w.n_traces)), int(rng.integers(0, w.n_req)), rng,
@@ -161,7 +170,7 @@ def measure(w: W.Workload, *, iterations=24, layers=32, heads=32, kv_heads=8, he
         step = S.Step(it.n_new, it.kv_len, it.blocks, heads=heads, kv_heads=kv_heads,
                       head_dim=head_dim, block_tokens=e.block_tokens, n_blocks=e.kv_blocks,
                       device=device, **shared)
-        us = layer.time_us(step, layers)
+        us = model.time_us(step)
         step.close()
         rows.append((len(it.n_new), it.tokens, it.context + prefix * len(it.n_new), us))
         say(f"{rows[-1][0]:4d} requests {rows[-1][1]:6d} tokens {rows[-1][2]:8d} context "

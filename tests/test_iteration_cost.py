@@ -55,3 +55,35 @@ def test_measure_runs_the_operators(prefix):
     assert len(rows) == 4
     for n, tokens, context, us in rows:
         assert n >= 1 and tokens >= n and context >= tokens and 0 < us < 1e6
+
+
+class FakeStep:
+    """A step that notes the caches of its calls."""
+
+    tokens = 3
+
+    def __init__(self):
+        self.calls = []
+
+    def append(self, qkv, k_cache, v_cache, *args, **kw):
+        assert qkv.shape[0] == self.tokens
+        self.calls.append(("append", k_cache.data_ptr(), v_cache.data_ptr()))
+        return "queries"
+
+    def attention(self, q, k_cache, v_cache):
+        assert q == "queries"
+        self.calls.append(("attention", k_cache.data_ptr(), v_cache.data_ptr()))
+
+
+def test_every_layer_has_a_cache_of_its_own():
+    """As a model's layers have: what a layer reads was not read by the one before it, and
+    is not in the caches of the chip for that."""
+    torch = pytest.importorskip("torch")
+    e = W.Engine(kv_blocks=4, max_tokens=64)
+    m = C.Layers(e, 5, heads=2, kv_heads=1, head_dim=64, dtype=torch.float16, device="cpu",
+                 positions=10)
+    s = FakeStep()
+    m.run(s)
+    assert [c[0] for c in s.calls] == ["append", "attention"] * 5
+    assert all(s.calls[i][1:] == s.calls[i + 1][1:] for i in range(0, 10, 2))
+    assert len({p for c in s.calls for p in c[1:]}) == 10
