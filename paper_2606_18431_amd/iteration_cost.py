@@ -9,14 +9,19 @@ then attend over the pages) and fits the three coefficients to the times:
     python -m paper_2606_18431_amd.iteration_cost --cfg 4 --layers 32
 
 ``--prefix N`` puts N shared tokens (a system prompt, computed once) before every
-request's own context. The weights' part of an iteration (its matrix products)
-is not in the times: add it to base and tok from the model's own measurements.
+request's own context. The times hold the layers' two calls, made from the host one
+layer after another. Not in them: the weights' part of an iteration (its matrix
+products; add it to base and tok from the model's own measurements), and the plan of
+the batch, which the host makes once an iteration and which is printed by itself (an
+engine that plans while the GPU works does not wait for it; one that plans in between
+adds it to base).
 """
 from __future__ import annotations
 
 import argparse
 import dataclasses
 import math
+import time
 
 import numpy as np
 
@@ -148,9 +153,10 @@ def fit(tokens, context, us):
 
 
 def measure(w: W.Workload, *, iterations=24, layers=32, heads=32, kv_heads=8, head_dim=128,
-            dtype="bf16", prefix=0, seed=0, device="cuda", say=lambda line: None):
+            dtype="bf16", prefix=0, seed=0, device="cuda", say=lambda line: None, plans=None):
     """Times of ``iterations`` iterations of the workload; a list of (requests, tokens,
-    context, microseconds), context with the prefix counted for every request."""
+    context, microseconds), context with the prefix counted for every request. ``plans``:
+    a list that receives the microseconds that the host took for each iteration's plan."""
     import torch
 
     from . import step as S
@@ -167,14 +173,18 @@ def measure(w: W.Workload, *, iterations=24, layers=32, heads=32, kv_heads=8, he
                             prefix_pages)
         shared = dict(prefix_first=[0, len(it.n_new)], prefix_len=[prefix],
                       prefix_blocks=np.arange(prefix_pages)[None]) if prefix else {}
+        start = time.perf_counter()
         step = S.Step(it.n_new, it.kv_len, it.blocks, heads=heads, kv_heads=kv_heads,
                       head_dim=head_dim, block_tokens=e.block_tokens, n_blocks=e.kv_blocks,
                       device=device, **shared)
+        plan_us = (time.perf_counter() - start) * 1e6
+        if plans is not None:
+            plans.append(plan_us)
         us = model.time_us(step)
         step.close()
         rows.append((len(it.n_new), it.tokens, it.context + prefix * len(it.n_new), us))
         say(f"{rows[-1][0]:4d} requests {rows[-1][1]:6d} tokens {rows[-1][2]:8d} context "
-            f"{us:10.1f} us")
+            f"{us:10.1f} us, plan {plan_us:6.1f}")
     return rows
 
 
@@ -191,7 +201,8 @@ def main(argv=None):
     p.add_argument("--seed", type=int, default=0)
     a = p.parse_args(argv)
     w = W.make(a.cfg, n_traces=1, n_settings=4 if a.cfg != 0 else None)
-    rows = measure(w, iterations=a.iterations, layers=a.layers, heads=a.heads,
+    plans = []
+    rows = measure(w, plans=plans, iterations=a.iterations, layers=a.layers, heads=a.heads,
                    kv_heads=a.kv_heads, head_dim=a.head_dim, dtype=a.dtype, prefix=a.prefix,
                    seed=a.seed, say=lambda line: print(line, flush=True))
     _, tokens, context, us = zip(*rows)
@@ -199,6 +210,8 @@ def main(argv=None):
     print(f"{w.name}, {a.layers} layers of {a.heads}/{a.kv_heads} heads of {a.head_dim}, "
           f"{a.dtype}: attention of an iteration = {base:.0f} + {tok:.4f} * tokens + context / "
           f"{div:.1f} us ({100 * r2:.1f}% of the variance)")
+    print(f"the host plans an iteration in {np.median(plans):.0f} us (median), beside the GPU's "
+          "work or before it")
     e = w.engine
     print(f"the workload's engine prices the whole iteration at {e.iter_base_us} + "
           f"{e.iter_tok_us} * tokens + context / {e.iter_ctx_div} us")

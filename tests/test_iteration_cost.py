@@ -87,3 +87,16 @@ def test_every_layer_has_a_cache_of_its_own():
     assert [c[0] for c in s.calls] == ["append", "attention"] * 5
     assert all(s.calls[i][1:] == s.calls[i + 1][1:] for i in range(0, 10, 2))
     assert len({p for c in s.calls for p in c[1:]}) == 10
+
+
+@pytest.mark.gpu
+def test_measure_gives_the_times_of_the_plans():
+    """Each iteration's plan is timed too: it is made once an iteration, by the host."""
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    w = W.make(1, n_traces=1, n_settings=4, n_req=200)
+    plans = []
+    rows = C.measure(w, iterations=4, layers=2, heads=8, kv_heads=2, head_dim=64, dtype="f16",
+                     plans=plans)
+    assert len(plans) == len(rows) == 4 and all(0 < us < 1e6 for us in plans)
