@@ -9,12 +9,13 @@ then attend over the pages) and fits the three coefficients to the times:
     python -m paper_2606_18431_amd.iteration_cost --cfg 4 --layers 32
 
 ``--prefix N`` puts N shared tokens (a system prompt, computed once) before every
-request's own context. The times hold the layers' two calls, made from the host one
-layer after another. Not in them: the weights' part of an iteration (its matrix
-products; add it to base and tok from the model's own measurements), and the plan of
-the batch, which the host makes once an iteration and which is printed by itself (an
-engine that plans while the GPU works does not wait for it; one that plans in between
-adds it to base).
+request's own context. In an iteration's context they count once, as they are read
+(each new token's work on them is in tok). The times hold the layers' two calls, made
+from the host one layer after another. Not in them: the weights' part of an iteration
+(its matrix products; add it to base and tok from the model's own measurements), and
+the plan of the batch, which the host makes once an iteration and which is printed by
+itself (an engine that plans while the GPU works does not wait for it; one that plans
+in between adds it to base).
 """
 from __future__ import annotations
 
@@ -133,6 +134,11 @@ class Layers:
         return float(np.median(times))
 
 
+def context_read(it: Iteration, prefix: int) -> int:
+    """Tokens of context that an iteration's attention reads: shared ones once."""
+    return it.context + prefix
+
+
 def fit(tokens, context, us):
     """(base, tok, div, share of the variance explained) of us = base + tok * tokens
     + context / div, by least squares with no coefficient below zero."""
@@ -155,8 +161,8 @@ def fit(tokens, context, us):
 def measure(w: W.Workload, *, iterations=24, layers=32, heads=32, kv_heads=8, head_dim=128,
             dtype="bf16", prefix=0, seed=0, device="cuda", say=lambda line: None, plans=None):
     """Times of ``iterations`` iterations of the workload; a list of (requests, tokens,
-    context, microseconds), context with the prefix counted for every request. ``plans``:
-    a list that receives the microseconds that the host took for each iteration's plan."""
+    context, microseconds), the prefix once in the context. ``plans``: a list that
+    receives the microseconds that the host took for each iteration's plan."""
     import torch
 
     from . import step as S
@@ -182,7 +188,7 @@ def measure(w: W.Workload, *, iterations=24, layers=32, heads=32, kv_heads=8, he
             plans.append(plan_us)
         us = model.time_us(step)
         step.close()
-        rows.append((len(it.n_new), it.tokens, it.context + prefix * len(it.n_new), us))
+        rows.append((len(it.n_new), it.tokens, context_read(it, prefix), us))
         say(f"{rows[-1][0]:4d} requests {rows[-1][1]:6d} tokens {rows[-1][2]:8d} context "
             f"{us:10.1f} us, plan {plan_us:6.1f}")
     return rows

@@ -100,3 +100,10 @@ def test_measure_gives_the_times_of_the_plans():
     rows = C.measure(w, iterations=4, layers=2, heads=8, kv_heads=2, head_dim=64, dtype="f16",
                      plans=plans)
     assert len(plans) == len(rows) == 4 and all(0 < us < 1e6 for us in plans)
+
+
+def test_a_shared_prefix_is_read_once():
+    """The context that a batch costs: its requests' own, and the shared tokens once."""
+    it = C.Iteration(np.array([1, 1, 40]), np.array([100, 7, 40]), np.zeros((3, 7), np.int32))
+    assert it.context == 147
+    assert C.context_read(it, 0) == 147 and C.context_read(it, 2048) == 147 + 2048
