@@ -139,23 +139,49 @@ def context_read(it: Iteration, prefix: int) -> int:
     return it.context + prefix
 
 
+def _nonnegative(x, y):
+    """Least squares with no coefficient below zero."""
+    keep = list(range(x.shape[1]))
+    while keep:
+        c, *_ = np.linalg.lstsq(x[:, keep], y, rcond=None)
+        if (c >= 0).all():
+            break
+        keep.remove(keep[int(np.argmin(c))])
+    full = np.zeros(x.shape[1])
+    if keep:
+        full[keep] = c
+    return full
+
+
 def fit(tokens, context, us):
     """(base, tok, div, share of the variance explained) of us = base + tok * tokens
     + context / div, by least squares with no coefficient below zero."""
     x = np.stack([np.ones(len(us)), np.asarray(tokens, float), np.asarray(context, float)], 1)
     y = np.asarray(us, float)
-    keep = [0, 1, 2]
-    while True:
-        c, *_ = np.linalg.lstsq(x[:, keep], y, rcond=None)
-        if (c >= 0).all() or len(keep) == 1:
-            break
-        keep.remove(keep[int(np.argmin(c))])
-    full = np.zeros(3)
-    full[keep] = np.maximum(c, 0)
-    left = ((y - x @ full) ** 2).sum()
+    c = _nonnegative(x, y)
+    left = ((y - x @ c) ** 2).sum()
     var = ((y - y.mean()) ** 2).sum()
-    return full[0], full[1], (1 / full[2] if full[2] > 0 else float("inf")), \
-        1 - left / var if var > 0 else 1.0
+    return c[0], c[1], (1 / c[2] if c[2] > 0 else float("inf")), 1 - left / var if var > 0 else 1.0
+
+
+NO_PRICE = 2 ** 31 - 1  # the divisor of a context without a price
+
+
+def whole_terms(tokens, context, us):
+    """(base, tok, div) as the engine holds them, whole numbers: for either neighbour of
+    the fitted tok the base and div that fit what is left, the closer of the two."""
+    tokens, context, y = (np.asarray(a, float) for a in (tokens, context, us))
+    x = np.stack([np.ones(len(y)), context], 1)
+    low = int(fit(tokens, context, us)[1])
+    best = None
+    for tok in (low, low + 1):
+        base, slope = _nonnegative(x, y - tok * tokens)
+        base = round(base)
+        div = min(NO_PRICE, max(1, round(1 / slope))) if slope > 0 else NO_PRICE
+        off = ((y - base - tok * tokens - context / div) ** 2).sum()
+        if best is None or off < best[0]:
+            best = (off, (base, tok, div))
+    return best[1]
 
 
 def measure(w: W.Workload, *, iterations=24, layers=32, heads=32, kv_heads=8, head_dim=128,
@@ -216,6 +242,8 @@ def main(argv=None):
     print(f"{w.name}, {a.layers} layers of {a.heads}/{a.kv_heads} heads of {a.head_dim}, "
           f"{a.dtype}: attention of an iteration = {base:.0f} + {tok:.4f} * tokens + context / "
           f"{div:.1f} us ({100 * r2:.1f}% of the variance)")
+    whole = whole_terms(tokens, context, us)
+    print("in whole numbers, for Engine(iter_base_us, iter_tok_us, iter_ctx_div): %d, %d, %d" % whole)
     print(f"the host plans an iteration in {np.median(plans):.0f} us (median), beside the GPU's "
           "work or before it")
     e = w.engine

@@ -107,3 +107,26 @@ def test_a_shared_prefix_is_read_once():
     it = C.Iteration(np.array([1, 1, 40]), np.array([100, 7, 40]), np.zeros((3, 7), np.int32))
     assert it.context == 147
     assert C.context_read(it, 0) == 147 and C.context_read(it, 2048) == 147 + 2048
+
+
+def test_whole_terms_fit_the_engine():
+    """The engine's terms are whole numbers: the ones that fit best with the tokens' price
+    rounded, not each rounded by itself."""
+    rng = np.random.default_rng(2)
+    tokens, context = rng.integers(1, 8192, 60), rng.integers(1, 400_000, 60)
+    assert C.whole_terms(tokens, context, 300 + 2 * tokens + context / 64) == (300, 2, 64)
+    us = 100 + 0.66 * tokens + context / 46
+    base, tok, div = C.whole_terms(tokens, context, us)
+    assert (tok, type(base), type(tok), type(div)) == (1, int, int, int)
+    assert base >= 0 and div >= 1
+    W.Engine(iter_base_us=base, iter_tok_us=tok, iter_ctx_div=div)
+
+    def off(b, t, d):
+        return ((us - b - t * tokens - context / d) ** 2).sum()
+
+    for t in (0, 1):
+        for b in (0, 100, base - 50, base + 50):
+            for d in (46, div - 2, div + 2):
+                assert b < 0 or off(base, tok, div) <= off(b, t, d)
+    base, tok, div = C.whole_terms(tokens, context, 5.0 * tokens)  # no price of context
+    assert (base, tok) == (0, 5) and div == 2 ** 31 - 1
