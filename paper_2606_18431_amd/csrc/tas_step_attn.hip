@@ -45,10 +45,6 @@ __device__ f16x mfma32(vec8<_Float16> a, vec8<_Float16> b, f16x c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
-// The running maximum is raised only where it falls behind by more than this (a
-// weight is at most 2^8 of the largest's then): the rescaling of o, as long as it is, is rare.
-constexpr float kLazy = 8.0f;
-
 // The m of a row is this far below its maximum, so that its weights are that much larger:
 // a 16-bit float holds none below 2^-25, and would lose from the row, but not from its
 // sum, what many small ones add (8000 keys at 2^-25.5 of the largest: 1.7e-4 of V). With
@@ -56,6 +52,11 @@ constexpr float kLazy = 8.0f;
 // less than the result's rounding. A bfloat16 has the exponents of 32 bits.
 template <typename T>
 constexpr float kHeadroom = __is_same(T, _Float16) ? 7.0f : 0.0f;
+
+// m is raised only where it falls behind by 8 more (a weight is then at most 2^8 of what
+// it would be): the rescaling of o, as long as it is, is rare.
+template <typename T>
+constexpr float kRaise = kHeadroom<T> + 8.0f;
 
 __device__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -314,9 +315,10 @@ __device__ __forceinline__ void thin_item(const AttnArgs &a, const Item &it, cha
         for (int n = 0; n < 2; n++)
 #pragma unroll
             for (int i = 0; i < 4; i++) mt = fmaxf(mt, sc[n][i]);
-        mt = max32(max16(mt)) * a.scale2 - kHeadroom<T>;
-        if (__any(mt > m + kLazy)) {
-            const float mn = mt > m + kLazy ? mt : m, f = mn == m ? 1.0f : exp2_(m - mn);
+        mt = max32(max16(mt)) * a.scale2;
+        if (__any(mt > m + kRaise<T>)) {
+            const float mn = mt > m + kRaise<T> ? mt - kHeadroom<T> : m;
+            const float f = mn == m ? 1.0f : exp2_(m - mn);
             m = mn;
             l *= f;
 #pragma unroll
@@ -579,11 +581,12 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
         float mt = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 16; e++) mt = fmaxf(mt, sc[e]);
-        return max32(mt) * a.scale2 - kHeadroom<T>;
+        return max32(mt) * a.scale2;
     };
     auto raise = [&](float mt) {
-        if (__any(mt > m + kLazy)) {
-            const float mn = mt > m + kLazy ? mt : m, f = mn == m ? 1.0f : exp2_(m - mn);
+        if (__any(mt > m + kRaise<T>)) {
+            const float mn = mt > m + kRaise<T> ? mt - kHeadroom<T> : m;
+            const float f = mn == m ? 1.0f : exp2_(m - mn);
             m = mn;
             l *= f;
 #pragma unroll
