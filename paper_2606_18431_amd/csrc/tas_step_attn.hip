@@ -183,6 +183,8 @@ __device__ u4 zero_not_finite(u4 x) {
     return x;
 }
 
+__device__ uint32_t first_bits(int n) { return n >= 32 ? ~0u : n > 0 ? (1u << n) - 1 : 0; }
+
 // 16 bytes that are read once: they need not stay in the caches (decode of 256 requests,
 // 448k tokens of 8 heads of 128: 282 us, with ordinary loads 311).
 __device__ u4 stream(const char *p) { return __builtin_nontemporal_load((const u4 *)p); }
@@ -303,13 +305,8 @@ __device__ __forceinline__ void thin_item(const AttnArgs &a, const Item &it, cha
 #pragma unroll
                 for (int i = 0; i < 4; i++)
                     if (base + n * 16 + g * 4 + i >= lim) sc[n][i] = -INFINITY;
-        if (marked)
-#pragma unroll
-            for (int n = 0; n < 2; n++)
-#pragma unroll
-                for (int i = 0; i < 4; i++)
-                    if ((marked >> (n * 16 + g * 4 + i) & 1) && base + n * 16 + g * 4 + i < lim)
-                        l = NAN;
+        // (this lane's keys: 4 g .. 4 g + 3 and 16 on)
+        if (marked && (marked & first_bits(lim - base) & (0xf000fu << (g * 4)))) l = NAN;
         float mt = -INFINITY;
 #pragma unroll
         for (int n = 0; n < 2; n++)
@@ -569,13 +566,9 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, cha
     // (the V of these keys has arrived, so their marks are complete)
     auto poison = [&](int base) {
         if (base < differ || base >= it.k1) return;
-        const uint32_t bits = marked[(base - differ) >> 5];
-        if (bits)
-#pragma unroll
-            for (int e = 0; e < 16; e++)
-                if ((bits >> ((e >> 2) * 8 + half * 4 + (e & 3)) & 1) &&
-                    base + (e >> 2) * 8 + half * 4 + (e & 3) < lim)
-                    l = NAN;
+        // (this lane's keys: 4 half .. 4 half + 3, and 8, 16 and 24 on)
+        if (marked[(base - differ) >> 5] & first_bits(lim - base) & (0xf0f0f0fu << (half * 4)))
+            l = NAN;
     };
     auto largest = [&](const f16x &sc) {
         float mt = -INFINITY;
