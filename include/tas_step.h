@@ -19,8 +19,8 @@
  *     prefix_len[g] + kv_len[i] - n_new[i] + j.
  *
  * A STEP context is the plan of one batch: made by tas_step_create when the
- * scheduler has formed the batch, bound to device memory by tas_step_bind, used
- * for every layer of the model.
+ * scheduler has formed the batch, bound to device memory by tas_step_bind (or
+ * tas_step_attach), used for every layer of the model.
  *
  * Conventions as in tas.h: negative return codes (TAS_E*), no exceptions;
  * batch arrays are host memory, read only during the call; d_* and the tensor
@@ -115,10 +115,14 @@ int tas_step_create(const tas_batch *batch, tas_step **out);
 /* Bytes of device workspace that the step needs (plan and partial results). */
 size_t tas_step_bytes(const tas_step *step);
 /* Copy the plan to d_ws (256-byte aligned, at least tas_step_bytes) on the
- * stream, and wait for that (and so for all that the stream was given before: use a
- * stream of its own where planning is not to wait for work). d_ws must outlive the step's last call and stay
- * untouched by others. TAS_EINVAL, TAS_ENOMEM (ws_bytes too small), TAS_EHIP. */
+ * stream, and wait for that: for all that the stream was given before, too. d_ws
+ * must outlive the step's last call and stay untouched by others. TAS_EINVAL,
+ * TAS_ENOMEM (ws_bytes too small), TAS_EHIP. */
 int tas_step_bind(tas_step *step, void *d_ws, size_t ws_bytes, void *stream);
+/* As tas_step_bind, for a caller that copies the plan itself and does not wait: host
+ * only. What tas_step_plan gives has to lie at d_ws before the step's first call runs
+ * (enqueued before it on its stream, or waited for). */
+int tas_step_attach(tas_step *step, void *d_ws, size_t ws_bytes);
 void tas_step_destroy(tas_step *step);
 /* New tokens of the batch (T). */
 int64_t tas_step_tokens(const tas_step *step);
@@ -144,7 +148,7 @@ int tas_step_append(tas_step *step, const tas_append *a, void *stream);
  * unaligned, out over a part of q or of the cache. */
 int tas_step_attention(tas_step *step, const tas_attention *a, void *stream);
 
-/* The plan that tas_step_bind copies to the device, for inspection: writes it to
+/* The plan that tas_step_bind copies to the device: writes it to
  * host memory `buf` and its size to *bytes (with buf NULL, the size only). Host
  * only. TAS_EINVAL, TAS_ENOMEM (buf_bytes too small). */
 int tas_step_plan(const tas_step *step, void *buf, size_t buf_bytes, size_t *bytes);

@@ -530,6 +530,11 @@ struct tas_step {
     size_t bytes() const { return part_lse() + align256((size_t)head.part_rows * 4); }
 };
 
+static int valid_workspace(const tas_step *s, const void *d_ws, size_t ws_bytes) {
+    if (!s || !d_ws || ((uintptr_t)d_ws & 255)) return TAS_EINVAL;
+    return ws_bytes < s->bytes() ? TAS_ENOMEM : TAS_OK;
+}
+
 extern "C" {
 
 int tas_step_create(const tas_batch *b, tas_step **out) try {
@@ -559,8 +564,8 @@ int tas_step_create(const tas_batch *b, tas_step **out) try {
 size_t tas_step_bytes(const tas_step *s) { return s ? s->bytes() : 0; }
 
 int tas_step_bind(tas_step *s, void *d_ws, size_t ws_bytes, void *stream) {
-    if (!s || !d_ws || ((uintptr_t)d_ws & 255)) return TAS_EINVAL;
-    if (ws_bytes < s->bytes()) return TAS_ENOMEM;
+    const int rc = valid_workspace(s, d_ws, ws_bytes);
+    if (rc != TAS_OK) return rc;
     const hipStream_t st = (hipStream_t)stream;
     if (hipMemcpyAsync(d_ws, s->blob.data(), s->blob.size(), hipMemcpyHostToDevice, st) !=
             hipSuccess ||
@@ -568,6 +573,12 @@ int tas_step_bind(tas_step *s, void *d_ws, size_t ws_bytes, void *stream) {
         return TAS_EHIP;
     s->ws = (char *)d_ws;
     return TAS_OK;
+}
+
+int tas_step_attach(tas_step *s, void *d_ws, size_t ws_bytes) {
+    const int rc = valid_workspace(s, d_ws, ws_bytes);
+    if (rc == TAS_OK) s->ws = (char *)d_ws;
+    return rc;
 }
 
 void tas_step_destroy(tas_step *s) { delete s; }

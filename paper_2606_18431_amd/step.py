@@ -65,8 +65,9 @@ _ATTENTION = struct.Struct("ifPqPqP" + _CACHE)
 assert _APPEND.size == ctypes.sizeof(tas_append)
 assert _ATTENTION.size == ctypes.sizeof(tas_attention)
 
-EXPORTS = ["tas_step_create", "tas_step_bytes", "tas_step_bind", "tas_step_destroy",
-           "tas_step_tokens", "tas_step_append", "tas_step_attention", "tas_step_plan"]
+EXPORTS = ["tas_step_create", "tas_step_bytes", "tas_step_bind", "tas_step_attach",
+           "tas_step_destroy", "tas_step_tokens", "tas_step_append", "tas_step_attention",
+           "tas_step_plan"]
 
 _lib = None
 
@@ -83,6 +84,7 @@ def lib():
         L.tas_step_bytes.restype = ctypes.c_size_t
         L.tas_step_create.argtypes = [_P, ctypes.POINTER(_P)]
         L.tas_step_bind.argtypes = [_P, _P, ctypes.c_size_t, _P]
+        L.tas_step_attach.argtypes = [_P, _P, ctypes.c_size_t]
         L.tas_step_destroy.argtypes = [_P]
         L.tas_step_destroy.restype = None
         L.tas_step_tokens.argtypes = [_P]
@@ -165,6 +167,11 @@ def tas_step_bind(ctx, ws: int, ws_bytes: int, stream=None):
     _check(lib().tas_step_bind(ctx, ws, ws_bytes, _stream(stream)), "tas_step_bind")
 
 
+def tas_step_attach(ctx, ws: int, ws_bytes: int):
+    """``ws``: a device address, where the caller puts the plan."""
+    _check(lib().tas_step_attach(ctx, ws, ws_bytes), "tas_step_attach")
+
+
 def tas_step_tokens(ctx) -> int:
     return int(lib().tas_step_tokens(ctx))
 
@@ -202,16 +209,6 @@ class _NoBackward(torch.autograd.Function):
     @staticmethod
     def backward(ctx, *grads):
         raise NotImplementedError("the serving step has no backward pass")
-
-
-_plan_streams = {}  # of a device
-
-
-def _plan_stream(index):
-    """The stream on which plans are copied to a device."""
-    if index not in _plan_streams:
-        _plan_streams[index] = torch.cuda.Stream(torch.device("cuda", index))
-    return _plan_streams[index]
 
 
 class Step:
@@ -252,15 +249,25 @@ class Step:
         self.q_shape = (self.tokens, heads, head_dim)
         self.qkv_shape = (self.tokens, heads + 2 * kv_heads, head_dim)
         self.cache_shape = (n_blocks, kv_heads, block_tokens, head_dim)
-        # Binding waits for its stream: one of its own, so that planning the next batch does
-        # not wait for the layers of this one. The workspace is that stream's memory, as
-        # memory of another might still be in use there.
-        side = _plan_stream(self.index)
-        with torch.cuda.stream(side):
+        with torch.cuda.device(self.device):
+            if torch.cuda.is_current_stream_capturing():
+                raise ValueError("a step is made outside of a graph's capture")
+            # The plan goes through pinned memory (which torch keeps until it is copied)
+            # without waiting: planning the next batch does not wait for the layers of this.
+            n = ctypes.c_size_t()
+            _check(self._lib.tas_step_plan(self.ctx, None, 0, ctypes.byref(n)), "tas_step_plan")
+            plan = torch.empty(n.value, dtype=torch.uint8, pin_memory=True)
+            _check(self._lib.tas_step_plan(self.ctx, plan.data_ptr(), n.value, ctypes.byref(n)),
+                   "tas_step_plan")
+            self._home = torch._C._cuda_getCurrentRawStream(self.index)
             self.ws = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=self.device)
-            tas_step_bind(self.ctx, self.ws.data_ptr() + (-self.ws.data_ptr()) % 256,
-                          self.ws_bytes, side.cuda_stream)
-        self._streams = set()  # that the workspace is recorded on
+            at = -self.ws.data_ptr() % 256
+            self.ws[at:at + n.value].copy_(plan, non_blocking=True)
+            self._copied = torch.cuda.Event()
+            self._copied.record()
+        tas_step_attach(self.ctx, self.ws.data_ptr() + at, self.ws_bytes)
+        self._there = False  # the plan, as far as the host knows
+        self._streams = {self._home}  # that the workspace is recorded on
 
     # ------------------------------------------------------------ argument checks
 
@@ -308,19 +315,23 @@ class Step:
                 out = like.new_empty(self.q_shape)
         return out, out.data_ptr(), self.heads * self.head_dim
 
-    def _enqueue(self, call, stream, used):
-        if self.ctx is None:
-            raise ValueError("the step is closed")
-        raw = torch._C._cuda_getCurrentRawStream(self.index)
-        if stream is not None and stream.cuda_stream != raw:
-            raw = stream.cuda_stream
-            for t in used:  # their memory is not given away before the work there is done
+    def _keep(self, stream, *tensors):
+        """The memory of tensors used on another stream than the current one is not given
+        away before the work there is done."""
+        if stream.cuda_stream != torch._C._cuda_getCurrentRawStream(self.index):
+            for t in tensors:
                 if t is not None:
                     t.record_stream(stream)
-        if raw not in self._streams:  # the workspace outlives the work there
-            self.ws.record_stream(torch.cuda.ExternalStream(raw, self.device) if stream is None
-                                  else stream)
-            self._streams.add(raw)
+
+    def _enqueue(self, call, stream):
+        if self.ctx is None:
+            raise ValueError("the step is closed")
+        if stream is None:
+            raw = torch._C._cuda_getCurrentRawStream(self.index)
+        else:
+            raw = stream.cuda_stream
+        if not self._there or raw not in self._streams:
+            self._admit(raw, stream)
         if torch._C._cuda_getDevice() == self.index:
             rc = call(self.ctx, self._args_p, raw)
         else:
@@ -328,6 +339,23 @@ class Step:
                 rc = call(self.ctx, self._args_p, raw)
         if rc != TAS_OK:
             raise TasError(rc, call.__name__)
+
+    def _admit(self, raw, stream):
+        """Orders a call's stream behind the plan's copy, and the end of the workspace behind
+        the stream."""
+        on = torch.cuda.ExternalStream(raw, self.device) if stream is None else stream
+        self._there = self._there or self._copied.query()
+        if not self._there:
+            with torch.cuda.stream(on):
+                capturing = torch.cuda.is_current_stream_capturing()
+            if capturing:  # its replays would not wait for the copy
+                raise ValueError("the step's plan is still under way to the device: synchronize "
+                                 "before the capture")
+            if raw != self._home:
+                on.wait_event(self._copied)
+        if raw not in self._streams:
+            self.ws.record_stream(on)
+            self._streams.add(raw)
 
     # ------------------------------------------------------------ the operators
 
@@ -367,8 +395,9 @@ class Step:
         out, out_p, out_s = self._out(out, qkv, stream)
         _APPEND.pack_into(self._args, 0, dtype, rot, 1 if interleaved else 0, eps, qkv_p, qkv_s,
                           out_p, out_s, qw_p, kw_p, cos_p, sin_p, positions, *cache)
-        self._enqueue(self._lib.tas_step_append, stream,
-                      (qkv, k_cache, v_cache, cos, sin, q_weight, k_weight, out))
+        self._enqueue(self._lib.tas_step_append, stream)
+        if stream is not None:
+            self._keep(stream, qkv, k_cache, v_cache, cos, sin, q_weight, k_weight, out)
         if (qkv.requires_grad or qw_p and (q_weight.requires_grad or k_weight.requires_grad)
                 or cos_p and (cos.requires_grad or sin.requires_grad)) \
                 and torch.is_grad_enabled():
@@ -394,7 +423,9 @@ class Step:
         if scale is None:
             scale = self.head_dim ** -0.5
         _ATTENTION.pack_into(self._args, 0, dtype, scale, q_p, q_s, out_p, out_s, lse_p, *cache)
-        self._enqueue(self._lib.tas_step_attention, stream, (q, k_cache, v_cache, lse, out))
+        self._enqueue(self._lib.tas_step_attention, stream)
+        if stream is not None:
+            self._keep(stream, q, k_cache, v_cache, lse, out)
         if (q.requires_grad or k_cache.requires_grad or v_cache.requires_grad) \
                 and torch.is_grad_enabled():
             return _NoBackward.apply(out, q, k_cache, v_cache)

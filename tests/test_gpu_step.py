@@ -846,3 +846,48 @@ def test_a_backward_pass_is_refused(torch):
             assert not s.append(args[0], k, v, args[1], args[2], q_weight=args[3],
                                 k_weight=args[4]).requires_grad
     assert not s.append(grad(qkv).detach(), k, v).requires_grad
+
+
+def test_plan_under_way(torch):
+    """While a step's plan waits behind the device's work, calls on other streams wait for
+    it, and a capture, whose replays would not, is refused."""
+    b = Batch(42, [1, 20], [30, 40], 4, 2, 64)
+    k, v = caches(torch, b, torch.bfloat16, 9, poison=False)
+    q = torch.randn((21, 4, 64), device="cuda", dtype=torch.bfloat16)
+    want = b.step().attention(q, k, v)
+    a = torch.randn((8192, 8192), device="cuda", dtype=torch.bfloat16)
+    a @ a
+    other, side = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(50):
+        a @ a
+    s = b.step()                      # its copy is behind the products
+    with torch.cuda.stream(other):
+        x = s.attention(q, k, v)
+    y = s.attention(q, k, v, stream=side)
+    z = s.attention(q, k, v)
+    graph = torch.cuda.CUDAGraph()
+    out = torch.empty_like(q)
+    with torch.cuda.stream(other):
+        graph.capture_begin()
+        out.zero_()
+        refused = False
+        try:
+            s.attention(q, k, v, out=out)
+        except ValueError:
+            refused = True
+        graph.capture_end()
+    late = s._copied.query()
+    torch.cuda.synchronize()
+    assert refused and not late
+    assert all(torch.equal(t, want) for t in (x, y, z))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):     # (it synchronizes first)
+        s.attention(q, k, v, out=out)
+        with pytest.raises(ValueError):
+            b.step()
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)

@@ -376,3 +376,21 @@ def test_batches_of_more_workgroups_than_a_launch_takes():
     kw = dict(heads=128, kv_heads=128, head_dim=128, block_tokens=4096, n_blocks=512)
     assert refused([n], [n], np.arange(512).reshape(1, -1), **kw)
     assert not refused([n // 8], [n // 8], np.arange(512).reshape(1, -1), **kw)
+
+
+def test_workspace_of_the_callers_own_copy():
+    """tas_step_attach takes what tas_step_bind takes, and copies nothing (host only)."""
+    L = step.lib()
+    b, keep = step.make_batch([1, 1], [1, 1], [[0], [1]], heads=1, kv_heads=1, head_dim=64,
+                              block_tokens=16, n_blocks=2)
+    ctx = step.tas_step_create(b)
+    need = step.tas_step_bytes(ctx)
+    assert L.tas_step_attach(None, 1 << 40, need) == tas.TAS_EINVAL
+    assert L.tas_step_attach(ctx, None, need) == tas.TAS_EINVAL
+    assert L.tas_step_attach(ctx, (1 << 40) + 16, need) == tas.TAS_EINVAL
+    assert L.tas_step_attach(ctx, 1 << 40, need - 1) == tas.TAS_ENOMEM
+    assert L.tas_step_append(ctx, ctypes.byref(step.tas_append()), None) == tas.TAS_ESTATE
+    step.tas_step_attach(ctx, 1 << 40, need)  # (an address that nothing here uses)
+    a = step.tas_append(dtype=7)
+    assert L.tas_step_append(ctx, ctypes.byref(a), None) == tas.TAS_EINVAL  # bound: checked
+    step.tas_step_destroy(ctx)
