@@ -26,7 +26,9 @@ constexpr int64_t kMaxStride = (int64_t(1) << 31) - 8;      // of a block or hea
 constexpr int64_t kMaxTokenStride = int64_t(1) << 24;       // of a token in a block
 constexpr int64_t kMaxGroups = (int64_t(1) << 24) - 1;      // of a launch: 2^32 threads
 constexpr int64_t kUnits = 256;                      // compute units
-constexpr int64_t kSlots = 2 * kUnits;               // wide items that run at once
+// By registers a compute unit holds two wide or three thin items of head size 128, and
+// three or four of head size 64; the numbers below are those of 128 for both.
+constexpr int64_t kSlots = 2 * kUnits;               // wide items taken to run at once
 constexpr int32_t kThinItems = 768;                  // thin items wanted
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -121,13 +123,14 @@ int64_t thin_pieces(const Seg &s, int64_t share, bool merged) {
     return std::min(ceil_div(s.kv_len, piece), pay);
 }
 
-// Keys of a piece of the thin segments: a slot's share of all keys. As every segment has
-// a last piece that is shorter, these are somewhat more items than slots, and the rest
-// takes a round of its own: where a piece that is longer by a third at most fills the
-// slots once, all but a sixteenth, that one. (16/16 heads of 64, 8 contexts of about
-// 20039: 816 items 136 us, 752 items 121; 32/8 heads of 128, 64 of about 1200: 928 items
-// 66, 760 items 64. With more slots left empty that loses: 16/2 heads of 128, 28 of about
-// 14830: 786 items 77 us, 694 items 82.)
+// Keys of a piece of the thin segments: the share of all keys that makes kThinItems. As
+// every segment has a last piece that is shorter, these are somewhat more items than that:
+// where a piece that is longer by a third at most makes that many, or a sixteenth fewer,
+// that one. At head size 128 the rest would take a round of its own (32/8 heads, 64
+// contexts of about 1200: 928 items 66 us, 760 items 64; with more slots left empty it
+// loses: 16/2 heads, 28 of about 14830: 786 items 77 us, 694 items 82). At 64, where
+// either number runs at once, the fewer items measured faster too (16/16 heads, 8 contexts
+// of about 20039: 816 items 136 us, 752 items 121).
 int64_t choose_thin_piece(const Plan &p, const std::vector<char> &joined, int64_t kv_heads,
                           int64_t keys, bool any_wide) {
     const int64_t step = 4 * kThinKeys;
@@ -154,10 +157,11 @@ int64_t wide_pieces(const Seg &s, int64_t piece) {
 
 // Steps of a piece of the wide segments' keys, by what the batch then takes. Measured: a
 // step of 64 keys lasts 1.16 us where a compute unit has one item, 2.06 us where it has
-// two (head size 64: 0.80, 1.34); the thin items' keys stream at 6 TB/s beside that; a
-// merge takes 2 us, 2.2 for every eight parts of a row, and the time to write and read
-// the parts at 10 TB/s (they stay in caches for the most part). (One chunk of 1024, 32/8 heads of 128, nothing before it: whole
-// 25 us, in two pieces 32; 16/16 heads of 64 over 4096 keys: whole 56 us, in four 33.)
+// two (head size 64: 0.80, 1.34; three are not taken into account); the thin items' keys
+// stream at 6 TB/s beside that; a merge takes 2 us, 2.2 for every eight parts of a row,
+// and the time to write and read the parts at 10 TB/s (they stay in caches for the most
+// part). (One chunk of 1024, 32/8 heads of 128, nothing before it: whole 25 us, in two
+// pieces 32; 16/16 heads of 64 over 4096 keys: whole 56 us, in four 33.)
 int64_t choose_wide_piece(const tas_batch *b, const Plan &p, const std::vector<char> &joined,
                           int64_t thin_keys) {
     const int64_t Hk = b->kv_heads;

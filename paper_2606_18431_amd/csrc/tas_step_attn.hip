@@ -420,8 +420,8 @@ constexpr int kWaitLoads = 0x0F70;  // s_waitcnt: no load or store outstanding
 // loads to LDS alternate: V is read before the weights are worked out, whose end no read
 // passes, and the loads go between the products, V's in the first stretch and K's in the
 // second. (16 chunks of 11777 tokens, 32/8 heads of 128: 927 us with the products behind
-// the vector work, 908 with V read first, 897 with the loads spread as well; 870 now,
-// 1007 TFLOP/s.)
+// the vector work, 908 with V read first, 897 with the loads spread as well; 850 to 891 now,
+// by the card, 1030 to 983 TFLOP/s.)
 template <typename T, int D>
 __device__ __forceinline__ void wide_item(const AttnArgs &a, const Item &it, char *k0_lds,
                                           char *k1_lds, char *v0_lds, char *v1_lds,
@@ -819,7 +819,7 @@ __device__ __forceinline__ void join(const AttnArgs &a, const Unit &u) {
 // counted for its unit, and the workgroup that counts the last one joins the unit; the
 // count is left at zero for the next launch. (The rows of wide segments are left to the merge kernel: the workgroup that
 // came last would join 128 rows one after another. Decode of 64 requests with a shared
-// prefix of 2048, 32/8 heads of 128: 71 us so, 25 us with the merge kernel.)
+// prefix of 2048, 32/8 heads of 128: 71 us so, 23.5 us with the merge kernel.)
 template <typename T, int D, bool WIDE>
 __global__ __launch_bounds__(256, WIDE ? 2 : 3) void attn_kernel(AttnArgs a) {
     constexpr int TB = kWideKeys * D * 2;
