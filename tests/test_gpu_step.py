@@ -764,7 +764,7 @@ def test_tensors_dropped_while_another_stream_uses_them(torch):
     def busy():
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
-            for _ in range(50):
+            for _ in range(250):
                 torch.mm(a, a)
 
     def dropped(call, tensors):
@@ -798,7 +798,7 @@ def test_planning_does_not_wait_for_the_device(torch):
     a @ a
     torch.cuda.synchronize()
     done = torch.cuda.Event()
-    for _ in range(100):
+    for _ in range(250):
         a @ a
     done.record()
     got = [b.step().attention(q, k, v) for _ in range(5)]
@@ -859,7 +859,7 @@ def test_plan_under_way(torch):
     a @ a
     other, side = torch.cuda.Stream(), torch.cuda.Stream()
     torch.cuda.synchronize()
-    for _ in range(50):
+    for _ in range(250):
         a @ a
     s = b.step()                      # its copy is behind the products
     with torch.cuda.stream(other):
