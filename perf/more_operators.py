@@ -290,7 +290,7 @@ def _code4(x, e):
     code = torch.zeros(x.shape, dtype=torch.uint8, device=x.device)
     for i, border in enumerate(BORDERS):
         code += t > border if i % 2 == 0 else t >= border
-    return code + 8 * torch.signbit(x)
+    return code + 8 * torch.signbit(x).to(torch.uint8)
 
 
 def _round4(x, exponents):
@@ -299,7 +299,7 @@ def _round4(x, exponents):
     if blocks.dtype != torch.float64:
         blocks = blocks.float()
     e, finite = _scale4(blocks, exponents)
-    code = torch.where(finite[..., None], _code4(blocks, e), 0).flatten(-2)
+    code = (_code4(blocks, e) * finite[..., None]).flatten(-2)
     scale = torch.where(finite, e + 127, 255).to(torch.uint8)
     return code[..., ::2] | code[..., 1::2] << 4, scale
 
