@@ -1,7 +1,7 @@
 """Build the HIP libraries for gfx950 with hipcc, in-tree: libtas.so;
 libtas_check.so, the same entry points with every batch, every run of
 repeated iterations and every instance's state verified (TAS_CHECK_INVARIANTS);
-and libtas_step.so, the operators of a serving iteration (tas_step.h)."""
+and libtas_step.so, the operators of a serving iteration (tas_step.h, tas_fp4.h)."""
 from __future__ import annotations
 
 import os
@@ -15,7 +15,9 @@ LIB = os.path.join(PKG, "libtas.so")
 CHECK_LIB = os.path.join(PKG, "libtas_check.so")
 STEP_LIB = os.path.join(PKG, "libtas_step.so")
 SOURCES = ["tas_abi.hip", "tas_sim.hip", "tas_pctl.hip", "tas_order.hip"]
-STEP_SOURCES = ["tas_step_abi.hip", "tas_step_append.hip", "tas_step_attn.hip"]
+STEP_SOURCES = ["tas_step_abi.hip", "tas_step_append.hip", "tas_step_attn.hip",
+                "tas_fp4_abi.hip", "tas_fp4_append.hip", "tas_fp4_attn.hip", "tas_fp4_pack.hip",
+                "tas_fp4_linear.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 

@@ -1,0 +1,522 @@
+// tas_fp4_attn.hip - attention of a step's new tokens over a paged cache in four bits.
+//
+// The mathematics, the items and the joins are those of tas_step_attn.hip. What differs is
+// the way of K and V to the matrix unit: codes are loaded to registers (a third to a quarter
+// of the bytes), converted there to the 16-bit type, exactly, two elements an instruction,
+// and go on as 16-bit rows. A lane always has a quarter of a row, D / 8 bytes, which lies in
+// one block: one scale to a lane and row.
+#include <hip/hip_runtime.h>
+
+#include "tas_fp4_convert.h"
+#include "tas_fp4_internal.h"
+#include "tas_step_attn.h"
+
+namespace tas_step_impl {
+namespace {
+
+// The four bytes of a lane's quarter of a row.
+template <int D>
+struct Quarter {
+    static constexpr int W = D / 32;  // words, of eight elements
+    uint32_t w[W];
+};
+
+template <int D>
+__device__ Quarter<D> load_quarter(const char *p) {
+    typedef uint32_t words __attribute__((ext_vector_type(D / 32)));
+    const words x = __builtin_nontemporal_load((const words *)p);
+    Quarter<D> q;
+#pragma unroll
+    for (int i = 0; i < D / 32; i++) q.w[i] = x[i];
+    return q;
+}
+
+// The block of a row that quarter i lies in.
+template <int D>
+__device__ int block_of(int i) {
+    return D == 128 ? i : i >> 1;
+}
+
+// Places in LDS (in 16-byte chunks of eight elements) of chunk c of row y. Lanes write
+// quarters of rows, chunks D / 32 apart; eight lanes (two rows) write to different banks
+// because a chunk's low bits are turned by its quarter, and the rows of a pair differ in
+// the lowest bit.
+template <int D>
+__device__ constexpr int turned(int c) {
+    return D == 128 ? c ^ (c >> 2) : c;
+}
+// V: read by the transposing read, which takes pairs of chunks of four rows: those lie in
+// different quarters of the banks.
+template <int D>
+__device__ int v_place(int y, int c) {
+    return y * (D / 8) + (turned<D>(c) ^ ((y & 3) << 1) ^ (y & 1));
+}
+// K: read by columns of chunks.
+template <int D>
+__device__ int k_place(int y, int c) {
+    return y * (D / 8) + (turned<D>(c) ^ (y & (D / 8 - 1)));
+}
+
+// Up to 16 rows against a run of keys: each of the four waves takes every fourth 32 keys.
+// K goes straight into registers as the left operand: lane 16 g + r has the quarter g of key
+// r, so that the k-slots of step i stand for elements g D / 4 + 8 i + 0..7, for the queries
+// too. V goes through the wave's own LDS. Memory bound.
+template <typename T, int D>
+__device__ __forceinline__ void thin_item4(const Attn4Args &a, const Item &it, char *lds01,
+                                           char *lds23, float (*stat)[kThinRows][2]) {
+    using V = vec8<T>;
+    constexpr int QS = D / 32;             // steps of 32 over d, words of a quarter
+    constexpr int VB = kThinKeys * D * 2;  // bytes of a wave's V
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int col = lane & 15, g = lane >> 4;
+    const Seg &s = it.s;
+    const Table tab = (Table)(a.tables + s.table);
+
+    const int row = min(col, s.rows - 1), j = row / a.group;
+    const int lim = min(min(s.kv_len, s.lim0 + j), it.k1);
+    V q[QS];
+    {
+        const T *src = (const T *)a.q + (int64_t)(s.t0 + j) * a.q_stride +
+                       (int64_t)(it.hk * a.group + row - j * a.group) * D + g * (D / 4);
+#pragma unroll
+        for (int i = 0; i < QS; i++) q[i] = *(const V *)(src + i * 8);
+    }
+    const int full = min(min(s.kv_len, s.lim0), it.k1);  // keys that the first row sees
+    const int sub_mask = (1 << a.sub_shift) - 1;
+    const int vrow = lane >> 2, vq = lane & 3;
+    auto head_of = [&](const tas_rows &r) { return (const char *)r.p + it.hk * r.stride[1]; };
+    const char *kbase = head_of(a.f.k), *vbase = head_of(a.f.v);
+    const char *ksbase = head_of(a.f.k_scale), *vsbase = head_of(a.f.v_scale);
+    const uint32_t klane = col * (uint32_t)a.f.k.stride[2] + g * (D / 8);
+    const uint32_t kslane = col * (uint32_t)a.f.k_scale.stride[2] + block_of<D>(g);
+    const uint32_t vlane = vrow * (uint32_t)a.f.v.stride[2] + vq * (D / 8);
+    const uint32_t vslane = vrow * (uint32_t)a.f.v_scale.stride[2] + block_of<D>(vq);
+    // a wave's 32 rows of V, and in the end its sums (16 rows of floats, as many bytes)
+    auto mine = [&](int w) { return (w < 2 ? lds01 : lds23) + (w & 1) * VB; };
+    char *vl = mine(wave);
+    // (another pair of chunks is an exclusive or, a row 16 on an addition)
+    const uint32_t v_at = v_place<D>(4 * g + (col >> 2), (col >> 1) & 1) * 16 + (col & 1) * 8;
+
+    f4 o[D / 16];
+#pragma unroll
+    for (int i = 0; i < D / 16; i++) o[i] = f4{0, 0, 0, 0};
+    float m = -INFINITY, l = 0;
+    Quarter<D> k[2], v[2];
+    uint32_t ks[2], vs[2];
+    int page[2];
+    const int last_sub = it.k1 > 0 ? (it.k1 - 1) >> 4 : 0;
+
+    auto look_up = [&](int base) {
+#pragma unroll
+        for (int n = 0; n < 2; n++)
+            page[n] = tab[min((base >> 4) + n, last_sub) >> a.sub_shift];
+    };
+    auto load = [&](int base) {
+#pragma unroll
+        for (int n = 0; n < 2; n++) {
+            const int64_t off = (min((base >> 4) + n, last_sub) & sub_mask) * 16;
+            auto run = [&](const char *p, const tas_rows &r) {
+                return p + page[n] * r.stride[0] + off * r.stride[2];
+            };
+            k[n] = load_quarter<D>(run(kbase, a.f.k) + klane);
+            ks[n] = *(const uint8_t *)(run(ksbase, a.f.k_scale) + kslane);
+            v[n] = load_quarter<D>(run(vbase, a.f.v) + vlane);
+            vs[n] = *(const uint8_t *)(run(vsbase, a.f.v_scale) + vslane);
+        }
+    };
+    int base = __builtin_amdgcn_readfirstlane(it.k0 + wave * kThinKeys);
+    const int stride = 4 * kThinKeys;
+    if (base < it.k1) {
+        look_up(base);
+        load(base);
+        look_up(base + stride);
+    }
+    for (; base < it.k1; base += stride) {
+        f4 sc[2];
+#pragma unroll
+        for (int n = 0; n < 2; n++) {
+            sc[n] = f4{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < QS; i++)
+                sc[n] = mfma16(values_of<T>(k[n].w[i], scale_of(ks[n])), q[i], sc[n]);
+        }
+        u4 x[2][QS];
+#pragma unroll
+        for (int n = 0; n < 2; n++)
+#pragma unroll
+            for (int i = 0; i < QS; i++)
+                x[n][i] = __builtin_bit_cast(u4, values_of<T>(v[n].w[i], scale_of(vs[n])));
+        if (base + kThinKeys > it.k1)  // slots past the keys hold anything: weight 0 times it
+#pragma unroll
+            for (int n = 0; n < 2; n++)
+                if (base + n * 16 + vrow >= it.k1)
+#pragma unroll
+                    for (int i = 0; i < QS; i++) x[n][i] = u4{0, 0, 0, 0};
+        uint32_t marked = 0;  // of the 32 keys
+        if (base + kThinKeys > full && full < it.k1) {
+#pragma unroll
+            for (int n = 0; n < 2; n++)
+#pragma unroll
+                for (int i = 0; i < QS; i++) {
+                    const uint64_t lanes = __ballot(any_not_finite<T>(x[n][i]));
+                    if (lanes) {
+                        x[n][i] = zero_not_finite<T>(x[n][i]);
+                        for (int y = 0; y < 16; y++)
+                            if (lanes >> (y * 4) & 15) marked |= 1u << (n * 16 + y);
+                    }
+                }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int n = 0; n < 2; n++)
+#pragma unroll
+            for (int i = 0; i < QS; i++)
+                *(u4 *)(vl + v_place<D>(n * 16 + vrow, vq * QS + i) * 16) = x[n][i];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (base + stride < it.k1) {
+            load(base + stride);
+            look_up(base + 2 * stride);
+        }
+
+        if (base + kThinKeys > full)
+#pragma unroll
+            for (int n = 0; n < 2; n++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    if (base + n * 16 + g * 4 + i >= lim) sc[n][i] = -INFINITY;
+        // (this lane's keys: 4 g .. 4 g + 3 and 16 on)
+        if (marked && (marked & first_bits(lim - base) & (0xf000fu << (g * 4)))) l = NAN;
+        float mt = -INFINITY;
+#pragma unroll
+        for (int n = 0; n < 2; n++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) mt = fmaxf(mt, sc[n][i]);
+        mt = max32(max16(mt)) * a.scale2;
+        if (__any(mt > m + kRaise<T>)) {
+            const float mn = mt > m + kRaise<T> ? mt - kHeadroom<T> : m;
+            const float f = mn == m ? 1.0f : exp2_(m - mn);
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < D / 16; i++) o[i] *= f;
+        }
+        const float mu = m == -INFINITY ? 0.0f : m;
+        V p;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float y = exp2_(sc[i >> 2][i & 3] * a.scale2 - mu);
+            l += y;
+            p[i] = (T)y;
+        }
+#pragma unroll
+        for (int i = 0; i < D / 16; i++) {
+            // lane c of group g: column d = 16 i + c of the rows 4 g .. 4 g + 3 and 16 on
+            const char *at = vl + (v_at ^ (turned<D>(2 * i) * 16));
+            const s4 lo = read_tr(at), hi = read_tr(at + 32 * D);
+            const s8 t = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            o[i] = mfma16(__builtin_bit_cast(V, t), p, o[i]);
+        }
+    }
+    thin_end<T, D>(a, it, l, m, o, lds01, lds23, stat);
+}
+
+// 128 rows against a run of keys, as the 16-bit kernel's wide item: 64 keys a step, 32 rows
+// to a wave, K and V of a step in LDS as 16-bit rows for all four waves, double buffered.
+// A wave fetches a run of 16 keys of K and of V a whole step before it converts them and
+// writes them to LDS.
+template <typename T, int D>
+__device__ __forceinline__ void wide_item4(const Attn4Args &a, const Item &it, char *k0_lds,
+                                           char *k1_lds, char *v0_lds, char *v1_lds,
+                                           uint32_t *marked) {
+    using V = vec8<T>;
+    constexpr int QS = D / 16;             // steps of 16 over d
+    constexpr int W = D / 32;              // words of a quarter of a row
+    constexpr int LPR = D / 8;             // chunks of 16 bytes of a row
+    constexpr int TB = kWideKeys * D * 2;  // bytes of a tile
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const Seg &s = it.s;
+    const Table tab = (Table)(a.tables + s.table);
+
+    const int r = wave * 32 + col;  // row of the item
+    const int row = min(it.row0 + r, s.rows - 1), j = row / a.group;
+    const int lim = min(min(s.kv_len, s.lim0 + j), it.k1);
+    V q[QS];
+    {
+        const T *src = (const T *)a.q + (int64_t)(s.t0 + j) * a.q_stride +
+                       (int64_t)(it.hk * a.group + row - j * a.group) * D + half * 8;
+#pragma unroll
+        for (int i = 0; i < QS; i++) q[i] = *(const V *)(src + i * 16);
+    }
+    const int full = min(min(s.kv_len, s.lim0 + it.row0 / a.group), it.k1);
+    const int sub_mask = (1 << a.sub_shift) - 1;
+    const int last_sub = it.k1 > 0 ? (it.k1 - 1) >> 4 : 0;
+
+    const int lrow = lane >> 2, lq = lane & 3;
+    const uint32_t klane = lrow * (uint32_t)a.f.k.stride[2] + lq * (D / 8);
+    const uint32_t vlane = lrow * (uint32_t)a.f.v.stride[2] + lq * (D / 8);
+    const uint32_t kslane = lrow * (uint32_t)a.f.k_scale.stride[2] + block_of<D>(lq);
+    const uint32_t vslane = lrow * (uint32_t)a.f.v_scale.stride[2] + block_of<D>(lq);
+    // Lanes 0 to 3 work out where the wave's next run lies, of K, V and their scales; the
+    // block number is read a step before that.
+    const bool of_v = lane & 1;
+    const tas_rows &mine = lane & 2 ? (of_v ? a.f.v_scale : a.f.k_scale) : (of_v ? a.f.v : a.f.k);
+    const uint64_t base_of = (uint64_t)mine.p + it.hk * mine.stride[1];
+    const uint32_t block_bytes = (uint32_t)mine.stride[0];
+    const uint32_t run_bytes = (uint32_t)mine.stride[2] * 16;
+    int page = 0, run = 0;
+    auto look_up = [&](int v_base, int k_base) {
+        const int sub = min(((of_v ? v_base : k_base) >> 4) + wave, last_sub);
+        page = tab[sub >> a.sub_shift];
+        run = sub & sub_mask;
+    };
+    Quarter<D> kq, vq;
+    uint32_t ks, vs;
+    auto fetch = [&]() {
+        const uint64_t at = base_of + (uint64_t)(uint32_t)page * block_bytes +
+                            (uint64_t)(uint32_t)run * run_bytes;
+        const uint32_t lo = (uint32_t)at, hi = (uint32_t)(at >> 32);
+        auto from = [&](int l) {
+            return (const char *)((uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, l) << 32 |
+                                  (uint32_t)__builtin_amdgcn_readlane(lo, l));
+        };
+        kq = load_quarter<D>(from(0) + klane);
+        vq = load_quarter<D>(from(1) + vlane);
+        ks = *(const uint8_t *)(from(2) + kslane);
+        vs = *(const uint8_t *)(from(3) + vslane);
+    };
+    // The rows see the keys from here on to the end differently (at most 128 + 63 keys;
+    // a bit each in `marked`).
+    const int differ = full < it.k1 ? full & ~31 : it.k1;
+    if (full < it.k1) {
+        if (tid < kMarks) marked[tid] = 0;
+        __syncthreads();
+    }
+    const int y0 = wave * 16 + lrow;  // this lane's row of a tile
+    auto put_k = [&](char *to) {
+#pragma unroll
+        for (int i = 0; i < W; i++)
+            *(u4 *)(to + k_place<D>(y0, lq * W + i) * 16) =
+                __builtin_bit_cast(u4, values_of<T>(kq.w[i], scale_of(ks)));
+    };
+    // Slots past the keys hold anything, and weight 0 times it has to be 0.
+    auto put_v = [&](char *to, int base, bool edge) {
+#pragma unroll
+        for (int i = 0; i < W; i++) {
+            u4 x = __builtin_bit_cast(u4, values_of<T>(vq.w[i], scale_of(vs)));
+            if (edge && base + kWideKeys > differ) {
+                const int y = base + y0;
+                if (y >= it.k1) {
+                    x = u4{0, 0, 0, 0};
+                } else if (y >= differ && any_not_finite<T>(x)) {
+                    x = zero_not_finite<T>(x);
+                    atomicOr(marked + ((y - differ) >> 5), 1u << (y & 31));
+                }
+            }
+            *(u4 *)(to + v_place<D>(y0, lq * W + i) * 16) = x;
+        }
+    };
+
+    f16x o[D / 32];
+#pragma unroll
+    for (int i = 0; i < D / 32; i++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) o[i][e] = 0;
+    float m = -INFINITY, l = 0;
+
+    // The chunk's number is in bits 4 and up of an address, so another chunk is an
+    // exclusive or, another row (of the same place) an addition.
+    const uint32_t k_at = k_place<D>(col, half) * 16;
+    const int tr = (lane & 15) >> 2, tc = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
+    const uint32_t v_at = v_place<D>(half * 4 + tr, tc) * 16 + (lane & 1) * 8;
+    V kf[QS], vf[2][D / 32];
+    auto read_k = [&](const char *kl) {
+#pragma unroll
+        for (int i = 0; i < QS; i++)
+            kf[i] = *(const V *)(kl + (k_at ^ (turned<D>(i * 2) * 16)));
+    };
+    auto read_v = [&](const char *vl) {
+#pragma unroll
+        for (int n = 0; n < 2; n++)
+#pragma unroll
+            for (int i = 0; i < D / 32; i++) {
+                const char *at = vl + (v_at ^ (turned<D>(i * 4) * 16)) + n * 256 * LPR;
+                const s4 lo = read_tr(at), hi = read_tr(at + 128 * LPR);
+                const s8 t = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                vf[n][i] = __builtin_bit_cast(V, t);
+            }
+    };
+    auto scores = [&](f16x &sc) {
+#pragma unroll
+        for (int e = 0; e < 16; e++) sc[e] = 0;
+#pragma unroll
+        for (int i = 0; i < QS; i++) sc = mfma32(kf[i], q[i], sc);
+    };
+    auto hide = [&](f16x &sc, int base) {
+#pragma unroll
+        for (int e = 0; e < 16; e++)
+            if (base + (e >> 2) * 8 + half * 4 + (e & 3) >= lim) sc[e] = -INFINITY;
+    };
+    // (the V of these keys is in LDS, so their marks are complete)
+    auto poison = [&](int base) {
+        if (base < differ || base >= it.k1) return;
+        // (this lane's keys: 4 half .. 4 half + 3, and 8, 16 and 24 on)
+        if (marked[(base - differ) >> 5] & first_bits(lim - base) & (0xf0f0f0fu << (half * 4)))
+            l = NAN;
+    };
+    auto largest = [&](const f16x &sc) {
+        float mt = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 16; e++) mt = fmaxf(mt, sc[e]);
+        return max32(mt) * a.scale2;
+    };
+    auto raise = [&](float mt) {
+        if (__any(mt > m + kRaise<T>)) {
+            const float mn = mt > m + kRaise<T> ? mt - kHeadroom<T> : m;
+            const float f = mn == m ? 1.0f : exp2_(m - mn);
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < D / 32; i++) o[i] *= f;
+        }
+    };
+    auto weights = [&](V (&p)[2], const f16x &sc) {
+        const float mu = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+            const float y = exp2_(sc[e] * a.scale2 - mu);
+            l += y;
+            p[e >> 3][e & 7] = (T)y;
+        }
+    };
+    auto products = [&](const V (&p)[2]) {
+#pragma unroll
+        for (int n = 0; n < 2; n++)
+#pragma unroll
+            for (int i = 0; i < D / 32; i++) o[i] = mfma32(vf[n][i], p[n], o[i]);
+    };
+
+    // The K of a buffer is 32 keys ahead of its V: on entry of a step sa are the scores
+    // of the keys base .. + 31, m covers them, buffer B holds the V from base on and the K
+    // from base + 32 on, and the next ones' codes are in registers.
+    constexpr int HB = TB / 2;  // bytes of 32 rows
+    f16x sa, sb;
+    V p[2];
+    // EDGE: its keys and the next ones may be seen by some rows only.
+    auto step = [&](auto which, auto edge, int base) {
+        constexpr int B = decltype(which)::value, EDGE = decltype(edge)::value;
+        const char *kl = B ? k1_lds : k0_lds, *vl = B ? v1_lds : v0_lds;
+        const int next = base + kWideKeys;
+        if (EDGE) poison(base);
+        read_k(kl);
+        put_v(B ? v0_lds : v1_lds, next, EDGE);
+        put_k(B ? k0_lds : k1_lds);
+        fetch();
+        look_up(next + 2 * kWideKeys, next + 2 * kWideKeys + 32);
+        scores(sb);
+        read_v(vl);
+        weights(p, sa);
+        if (EDGE) hide(sb, base + 32);
+        products(p);
+        read_k(kl + HB);
+        raise(largest(sb));
+        if (EDGE) poison(base + 32);
+        scores(sa);
+        read_v(vl + HB);
+        weights(p, sb);
+        if (EDGE) hide(sa, next);
+        products(p);
+        raise(largest(sa));
+        __syncthreads();
+    };
+    if (it.k0 < it.k1) {
+        int base = it.k0;
+        look_up(base, base);
+        fetch();
+        look_up(base, base + 32);
+        put_k(k1_lds);
+        put_v(v0_lds, base, true);
+        fetch();
+        look_up(base + kWideKeys, base + kWideKeys + 32);
+        put_k(k0_lds);
+        fetch();
+        look_up(base + 2 * kWideKeys, base + 2 * kWideKeys + 32);
+        __syncthreads();
+        read_k(k1_lds);
+        scores(sa);
+        hide(sa, base);
+        raise(largest(sa));
+        __syncthreads();  // the first step writes K where these were
+        int steps = (it.k1 - base - 1) / kWideKeys;
+        for (; steps >= 2 && base + 3 * kWideKeys <= differ; steps -= 2) {
+            step(Const<0>{}, Const<0>{}, base);
+            step(Const<1>{}, Const<0>{}, base + kWideKeys);
+            base += 2 * kWideKeys;
+        }
+        for (; steps >= 2; steps -= 2) {
+            step(Const<0>{}, Const<1>{}, base);
+            step(Const<1>{}, Const<1>{}, base + kWideKeys);
+            base += 2 * kWideKeys;
+        }
+        if (steps) {
+            step(Const<0>{}, Const<1>{}, base);
+            base += kWideKeys;
+        }
+        const char *kl = steps ? k1_lds : k0_lds, *vl = steps ? v1_lds : v0_lds;
+        poison(base);
+        weights(p, sa);
+        read_v(vl);
+        products(p);
+        if (base + 32 < it.k1) {
+            read_k(kl);
+            scores(sa);
+            hide(sa, base + 32);
+            poison(base + 32);
+            raise(largest(sa));
+            weights(p, sa);
+            read_v(vl + HB);
+            products(p);
+        }
+    }
+    wide_end<T, D>(a, it, l, m, o);
+}
+
+// One item a workgroup.
+template <typename T, int D, bool WIDE>
+__global__ __launch_bounds__(256, WIDE ? 2 : 3) void attn4_kernel(Attn4Args a) {
+    constexpr int TB = kWideKeys * D * 2;
+    // four objects, so that the compiler sees which loads a read has to wait for
+    __shared__ __attribute__((aligned(16))) char k0_lds[TB], k1_lds[TB];
+    __shared__ __attribute__((aligned(16))) char v0_lds[WIDE ? TB : 16], v1_lds[WIDE ? TB : 16];
+    __shared__ float stat[WIDE ? 1 : 4][kThinRows][2];
+    __shared__ uint32_t marked[kMarks];
+    const Item it = a.items[blockIdx.x];
+    if (WIDE && it.s.rows > kThinRows)
+        wide_item4<T, D>(a, it, k0_lds, k1_lds, v0_lds, v1_lds, marked);
+    else
+        thin_item4<T, D>(a, it, k0_lds, k1_lds,
+                         WIDE ? (float (*)[kThinRows][2])(void *)v0_lds : stat);
+    if (it.unit >= 0) count_item<T, D>(a, it, (int *)k0_lds);
+}
+
+template <typename T, int D>
+hipError_t launch(const Attn4Args &a, int n, int n_merge, int dtype, hipStream_t s) {
+    const hipError_t e = launch_kernel(
+        a.n_wide ? attn4_kernel<T, D, true> : attn4_kernel<T, D, false>, n, a, s);
+    if (e != hipSuccess || !n_merge) return e;
+    return launch_merge(a, n_merge, dtype, D, s);
+}
+
+}  // namespace
+
+hipError_t launch_attention4(const Attn4Args &a, int n, int n_merge, int dtype, int head_dim,
+                             hipStream_t s) {
+    if (dtype == TAS_F16)
+        return head_dim == 64 ? launch<_Float16, 64>(a, n, n_merge, dtype, s)
+                              : launch<_Float16, 128>(a, n, n_merge, dtype, s);
+    return head_dim == 64 ? launch<__bf16, 64>(a, n, n_merge, dtype, s)
+                          : launch<__bf16, 128>(a, n, n_merge, dtype, s);
+}
+
+}  // namespace tas_step_impl

@@ -1,0 +1,81 @@
+// tas_fp4_pack.hip - tensors to four bits and back, and the layout of weights.
+//
+// All three move data: a thread has eight elements (16 bytes in 16 bits, 4 in four), so
+// that the wider side's accesses are whole lines; a block is four adjacent threads. Each
+// is bound by the bytes.
+#include <hip/hip_runtime.h>
+
+#include "tas_fp4_convert.h"
+#include "tas_fp4_internal.h"
+
+namespace tas_step_impl {
+namespace {
+
+__device__ char *row_at(const tas_rows &r, uint32_t row, uint32_t n1, uint32_t n2) {
+    const uint32_t i2 = row % n2, i01 = row / n2, i1 = i01 % n1, i0 = i01 / n1;
+    return (char *)r.p + i0 * r.stride[0] + i1 * r.stride[1] + i2 * r.stride[2];
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(Tensor4Args a) {
+    const uint32_t u = blockIdx.x * 256 + threadIdx.x;
+    if (u >= a.units) return;  // whole blocks
+    const uint32_t row = u / a.per_row, c = u - row * a.per_row;
+    const vec8<T> v = *(const vec8<T> *)(row_at(a.x, row, a.n1, a.n2) + c * 16ull);
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) x[e] = (float)v[e];
+    uint32_t most = largest(x);
+    most = max(most, __shfl_xor(most, 1));
+    most = max(most, __shfl_xor(most, 2));
+    const uint32_t byte = scale_byte<T>(most);
+    *(uint32_t *)(row_at(a.codes, row, a.n1, a.n2) + c * 4ull) = codes_of(x, byte);
+    if (c % 4 == 0) *(uint8_t *)(row_at(a.scales, row, a.n1, a.n2) + c / 4) = (uint8_t)byte;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void values_kernel(Tensor4Args a) {
+    const uint32_t u = blockIdx.x * 256 + threadIdx.x;
+    if (u >= a.units) return;
+    const uint32_t row = u / a.per_row, c = u - row * a.per_row;
+    const uint32_t codes = *(const uint32_t *)(row_at(a.codes, row, a.n1, a.n2) + c * 4ull);
+    const uint32_t byte = *(const uint8_t *)(row_at(a.scales, row, a.n1, a.n2) + c / 4);
+    *(vec8<T> *)(row_at(a.x, row, a.n1, a.n2) + c * 16ull) = values_of<T>(codes, scale_of(byte));
+}
+
+// A thread's 16 bytes are those of one lane and tile.
+__global__ __launch_bounds__(256) void weights_kernel(Weights4Args a) {
+    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t tile = u >> 6, tn = tile / a.w.tiles_k, tk = tile - tn * a.w.tiles_k;
+    if (tn >= a.w.tiles_n) return;
+    const int lane = u & 63;
+    const int64_t row = tn * kTileRows + (lane & 15), block = tk * 4 + (lane >> 4);
+    u4 codes = {0, 0, 0, 0};
+    char scale = 0;
+    if (row < a.rows && block < a.blocks) {
+        codes = *(const u4 *)(a.codes + row * a.codes_stride + block * 16);
+        scale = a.scales[row * a.scales_stride + block];
+    }
+    *(u4 *)(a.out + tile * 1024 + lane * 16) = codes;
+    char *s = a.out + a.w.scales_at + (tn * a.w.units_k + tk / 4) * 256 + lane * 4;
+    s[tk & 3] = scale;
+    if (tk == a.w.tiles_k - 1)  // of the last unit, tiles that there are not
+        for (int i = (tk & 3) + 1; i < 4; i++) s[i] = 0;
+}
+
+}  // namespace
+
+hipError_t launch_pack4(const Tensor4Args &a, int dtype, hipStream_t s) {
+    const int64_t n = ((int64_t)a.units + 255) / 256;
+    return launch_kernel(dtype == TAS_F16 ? pack_kernel<_Float16> : pack_kernel<__bf16>, n, a, s);
+}
+hipError_t launch_values4(const Tensor4Args &a, int dtype, hipStream_t s) {
+    const int64_t n = ((int64_t)a.units + 255) / 256;
+    return launch_kernel(dtype == TAS_F16 ? values_kernel<_Float16> : values_kernel<__bf16>, n, a,
+                         s);
+}
+hipError_t launch_weights4(const Weights4Args &a, hipStream_t s) {
+    return launch_kernel(weights_kernel, (a.w.tiles_n * a.w.tiles_k + 3) / 4, a, s);
+}
+
+}  // namespace tas_step_impl

@@ -114,5 +114,7 @@ hipError_t launch_kernel(void (*kernel)(Args), int64_t n, const Args &a, hipStre
 hipError_t launch_append(const AppendArgs &a, int dtype, int head_dim, hipStream_t s);
 hipError_t launch_attention(const AttnArgs &a, int n_items, int n_merge, int dtype, int head_dim,
                             hipStream_t s);
+// Joins the parts of the merge units alone.
+hipError_t launch_merge(const AttnArgs &a, int n_merge, int dtype, int head_dim, hipStream_t s);
 
 }  // namespace tas_step_impl

@@ -62,6 +62,9 @@ class tas_attention(ctypes.Structure):
 _CACHE = "PPqqqqqq"
 _APPEND = struct.Struct("iiifPqPqPPPPq" + _CACHE)
 _ATTENTION = struct.Struct("ifPqPqP" + _CACHE)
+_CACHE_FP4 = 4 * "Pqqq"
+_APPEND_FP4 = struct.Struct("iiifPqPqPPPPq" + _CACHE_FP4)  # those of include/tas_fp4.h
+_ATTENTION_FP4 = struct.Struct("ifPqPqP" + _CACHE_FP4)
 assert _APPEND.size == ctypes.sizeof(tas_append)
 assert _ATTENTION.size == ctypes.sizeof(tas_attention)
 
@@ -92,6 +95,14 @@ def lib():
         L.tas_step_append.argtypes = [_P, _P, _P]
         L.tas_step_attention.argtypes = [_P, _P, _P]
         L.tas_step_plan.argtypes = [_P, _P, ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)]
+        L.tas_fp4_append.argtypes = [_P, _P, _P]
+        L.tas_fp4_attention.argtypes = [_P, _P, _P]
+        L.tas_fp4_pack.argtypes = [_P, _P]
+        L.tas_fp4_values.argtypes = [_P, _P]
+        L.tas_fp4_weights_bytes.argtypes = [_i64, _i64]
+        L.tas_fp4_weights_bytes.restype = ctypes.c_size_t
+        L.tas_fp4_weights.argtypes = [_i64, _i64, _P, _i64, _P, _i64, _P, _P]
+        L.tas_fp4_linear.argtypes = [_P, _P]
         _lib = L
     return _lib
 
@@ -232,7 +243,7 @@ class Step:
                  device="cuda"):
         self.ctx = None
         self._lib = lib()
-        self._args = ctypes.create_string_buffer(max(_APPEND.size, _ATTENTION.size))
+        self._args = ctypes.create_string_buffer(_APPEND_FP4.size)  # the longest
         self._args_p = ctypes.addressof(self._args)
         b, keep = make_batch(n_new, kv_len, blocks, heads=heads, kv_heads=kv_heads,
                              head_dim=head_dim, block_tokens=block_tokens, n_blocks=n_blocks,
@@ -249,6 +260,8 @@ class Step:
         self.q_shape = (self.tokens, heads, head_dim)
         self.qkv_shape = (self.tokens, heads + 2 * kv_heads, head_dim)
         self.cache_shape = (n_blocks, kv_heads, block_tokens, head_dim)
+        self.codes_shape = (n_blocks, kv_heads, block_tokens, head_dim // 2)
+        self.scales_shape = (n_blocks, kv_heads, block_tokens, head_dim // 32)
         with torch.cuda.device(self.device):
             if torch.cuda.is_current_stream_capturing():
                 raise ValueError("a step is made outside of a graph's capture")
@@ -298,11 +311,57 @@ class Step:
                              f"{v.stride()}")
         return k.data_ptr(), v.data_ptr(), k0, k1, k2, v0, v1, v2
 
+    def _cache_fp4(self, cache):
+        got = []
+        for t, shape in ((cache.k, self.codes_shape), (cache.v, self.codes_shape),
+                         (cache.k_scale, self.scales_shape), (cache.v_scale, self.scales_shape)):
+            s0, s1, s2, s3 = t.stride() if t.dim() == 4 else (0, 0, 0, 0)
+            if t.dtype != torch.uint8 or t.get_device() != self.index or t.shape != shape \
+                    or s3 != 1:
+                raise ValueError(f"the cache holds {t.dtype} {tuple(t.shape)}, strides "
+                                 f"{t.stride()}, on {t.device}, expected adjacent uint8 {shape} "
+                                 f"on {self.device}")
+            got += t.data_ptr(), s0, s1, s2
+        return got
+
     def _dtype(self, t, what):
         code = DTYPES.get(t.dtype)
         if code is None:
             raise ValueError(f"{what} is {t.dtype}: float16 or bfloat16")
         return code
+
+    def _turn(self, dtype, cos, sin, q_weight, k_weight):
+        """rot_dim, the addresses of the weights and angles, and their positions."""
+        rot = positions = cos_p = sin_p = qw_p = kw_p = 0
+        if (cos is None) != (sin is None):
+            raise ValueError("cos and sin: both or neither")
+        if cos is not None:
+            shape = cos.shape
+            if len(shape) != 2 or sin.shape != shape or cos.dtype != torch.float32 \
+                    or sin.dtype != torch.float32 or cos.get_device() != self.index \
+                    or sin.get_device() != self.index or not cos.is_contiguous() \
+                    or not sin.is_contiguous():
+                raise ValueError("cos and sin: contiguous float32 [positions, rot_dim / 2] "
+                                 f"on {self.device}")
+            positions, rot = shape[0], 2 * shape[1]
+            cos_p, sin_p = cos.data_ptr(), sin.data_ptr()
+        if (q_weight is None) != (k_weight is None):
+            raise ValueError("q_weight and k_weight: both or neither")
+        if q_weight is not None:
+            for t in (q_weight, k_weight):
+                if t.dtype != dtype or t.get_device() != self.index \
+                        or t.shape != self.q_shape[2:] or not t.is_contiguous():
+                    raise ValueError(f"weights: contiguous {dtype} [{self.head_dim}] on "
+                                     f"{self.device}")
+            qw_p, kw_p = q_weight.data_ptr(), k_weight.data_ptr()
+        return rot, qw_p, kw_p, cos_p, sin_p, positions
+
+    def _lse(self, lse):
+        if lse.dtype != torch.float32 or lse.get_device() != self.index \
+                or lse.shape != self.q_shape[:2] or not lse.is_contiguous():
+            raise ValueError(f"lse: contiguous float32 {(self.tokens, self.heads)} on "
+                             f"{self.device}")
+        return lse.data_ptr()
 
     def _out(self, out, like, stream):
         """The output, its address and its token stride."""
@@ -322,6 +381,12 @@ class Step:
             for t in tensors:
                 if t is not None:
                     t.record_stream(stream)
+
+    def _no_backward(self, out, *inputs):
+        for t in inputs:
+            if t is not None and t.requires_grad and torch.is_grad_enabled():
+                return _NoBackward.apply(out, *inputs)
+        return out
 
     def _enqueue(self, call, stream):
         if self.ctx is None:
@@ -370,39 +435,14 @@ class Step:
         dtype = self._dtype(qkv, "qkv")
         qkv_p, qkv_s = self._rows(qkv, self.qkv_shape, qkv.dtype, "qkv")
         cache = self._cache(k_cache, v_cache, qkv.dtype)
-        rot = positions = cos_p = sin_p = qw_p = kw_p = 0
-        if (cos is None) != (sin is None):
-            raise ValueError("cos and sin: both or neither")
-        if cos is not None:
-            shape = cos.shape
-            if len(shape) != 2 or sin.shape != shape or cos.dtype != torch.float32 \
-                    or sin.dtype != torch.float32 or cos.get_device() != self.index \
-                    or sin.get_device() != self.index or not cos.is_contiguous() \
-                    or not sin.is_contiguous():
-                raise ValueError("cos and sin: contiguous float32 [positions, rot_dim / 2] "
-                                 f"on {self.device}")
-            positions, rot = shape[0], 2 * shape[1]
-            cos_p, sin_p = cos.data_ptr(), sin.data_ptr()
-        if (q_weight is None) != (k_weight is None):
-            raise ValueError("q_weight and k_weight: both or neither")
-        if q_weight is not None:
-            for t in (q_weight, k_weight):
-                if t.dtype != qkv.dtype or t.get_device() != self.index \
-                        or t.shape != self.q_shape[2:] or not t.is_contiguous():
-                    raise ValueError(f"weights: contiguous {qkv.dtype} [{self.head_dim}] on "
-                                     f"{self.device}")
-            qw_p, kw_p = q_weight.data_ptr(), k_weight.data_ptr()
+        turn = self._turn(qkv.dtype, cos, sin, q_weight, k_weight)
         out, out_p, out_s = self._out(out, qkv, stream)
-        _APPEND.pack_into(self._args, 0, dtype, rot, 1 if interleaved else 0, eps, qkv_p, qkv_s,
-                          out_p, out_s, qw_p, kw_p, cos_p, sin_p, positions, *cache)
+        _APPEND.pack_into(self._args, 0, dtype, turn[0], 1 if interleaved else 0, eps, qkv_p,
+                          qkv_s, out_p, out_s, *turn[1:], *cache)
         self._enqueue(self._lib.tas_step_append, stream)
         if stream is not None:
             self._keep(stream, qkv, k_cache, v_cache, cos, sin, q_weight, k_weight, out)
-        if (qkv.requires_grad or qw_p and (q_weight.requires_grad or k_weight.requires_grad)
-                or cos_p and (cos.requires_grad or sin.requires_grad)) \
-                and torch.is_grad_enabled():
-            return _NoBackward.apply(out, qkv, q_weight, k_weight, cos, sin)
-        return out
+        return self._no_backward(out, qkv, q_weight, k_weight, cos, sin)
 
     def attention(self, q, k_cache, v_cache, *, scale=None, out=None, lse=None, stream=None):
         """softmax(scale q K^T) V of every new token and head over its request's
@@ -413,23 +453,46 @@ class Step:
         q_p, q_s = self._rows(q, self.q_shape, q.dtype, "q")
         cache = self._cache(k_cache, v_cache, q.dtype)
         out, out_p, out_s = self._out(out, q, stream)
-        lse_p = 0
-        if lse is not None:
-            if lse.dtype != torch.float32 or lse.get_device() != self.index \
-                    or lse.shape != self.q_shape[:2] or not lse.is_contiguous():
-                raise ValueError(f"lse: contiguous float32 {(self.tokens, self.heads)} on "
-                                 f"{self.device}")
-            lse_p = lse.data_ptr()
+        lse_p = 0 if lse is None else self._lse(lse)
         if scale is None:
             scale = self.head_dim ** -0.5
         _ATTENTION.pack_into(self._args, 0, dtype, scale, q_p, q_s, out_p, out_s, lse_p, *cache)
         self._enqueue(self._lib.tas_step_attention, stream)
         if stream is not None:
             self._keep(stream, q, k_cache, v_cache, lse, out)
-        if (q.requires_grad or k_cache.requires_grad or v_cache.requires_grad) \
-                and torch.is_grad_enabled():
-            return _NoBackward.apply(out, q, k_cache, v_cache)
-        return out
+        return self._no_backward(out, q, k_cache, v_cache)
+
+    def append_fp4(self, qkv, cache, cos=None, sin=None, *, q_weight=None, k_weight=None,
+                   eps=1e-6, interleaved=False, out=None, stream=None):
+        """``append`` to a cache in four bits (``fp4.Cache``): keys and values are
+        rounded to it. Returns the queries."""
+        dtype = self._dtype(qkv, "qkv")
+        qkv_p, qkv_s = self._rows(qkv, self.qkv_shape, qkv.dtype, "qkv")
+        tensors = self._cache_fp4(cache)
+        turn = self._turn(qkv.dtype, cos, sin, q_weight, k_weight)
+        out, out_p, out_s = self._out(out, qkv, stream)
+        _APPEND_FP4.pack_into(self._args, 0, dtype, turn[0], 1 if interleaved else 0, eps, qkv_p,
+                              qkv_s, out_p, out_s, *turn[1:], *tensors)
+        self._enqueue(self._lib.tas_fp4_append, stream)
+        if stream is not None:
+            self._keep(stream, qkv, *cache, cos, sin, q_weight, k_weight, out)
+        return self._no_backward(out, qkv, q_weight, k_weight, cos, sin)
+
+    def attention_fp4(self, q, cache, *, scale=None, out=None, lse=None, stream=None):
+        """``attention`` over a cache in four bits (``fp4.Cache``)."""
+        dtype = self._dtype(q, "q")
+        q_p, q_s = self._rows(q, self.q_shape, q.dtype, "q")
+        tensors = self._cache_fp4(cache)
+        out, out_p, out_s = self._out(out, q, stream)
+        lse_p = 0 if lse is None else self._lse(lse)
+        if scale is None:
+            scale = self.head_dim ** -0.5
+        _ATTENTION_FP4.pack_into(self._args, 0, dtype, scale, q_p, q_s, out_p, out_s, lse_p,
+                                 *tensors)
+        self._enqueue(self._lib.tas_fp4_attention, stream)
+        if stream is not None:
+            self._keep(stream, q, *cache, lse, out)
+        return self._no_backward(out, q)
 
     def close(self):
         if getattr(self, "ctx", None):

@@ -1,0 +1,217 @@
+"""The C ABI of the operators in four bits, without a GPU: declared symbols, struct layouts,
+and arguments that are refused before any address is used."""
+import ctypes
+import os
+import re
+import subprocess
+
+import pytest
+
+from paper_2606_18431_amd import fp4, step, tas
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+AT = 1 << 40  # an address that nothing here uses
+
+
+def test_library_exports_every_declared_symbol():
+    src = open(os.path.join(ROOT, "include", "tas_fp4.h")).read()
+    src = re.sub(r"/\*.*?\*/", "", src, flags=re.S)
+    names = sorted(set(re.findall(r"\b(tas_fp4_[a-z_]+)\s*\(", src)))
+    assert names == sorted(fp4.EXPORTS)
+    for n in names:
+        assert hasattr(step.lib(), n), n
+
+
+def test_struct_layouts_match_header(tmp_path):
+    structs = [fp4.tas_rows, fp4.tas_cache_fp4, fp4.tas_append_fp4, fp4.tas_attention_fp4,
+               fp4.tas_tensor_fp4, fp4.tas_linear_fp4]
+    lines = ['#include <stddef.h>', '#include <stdio.h>', '#include "tas_fp4.h"',
+             'int main(void) {']
+    for st in structs:
+        n = st.__name__
+        lines.append(f'printf("{n} %zu\\n", sizeof({n}));')
+        for f, _ in st._fields_:
+            lines.append(f'printf("{n}.{f} %zu\\n", offsetof({n}, {f}));')
+    lines.append('return 0; }')
+    src = tmp_path / "layout.c"
+    src.write_text("\n".join(lines))
+    exe = tmp_path / "layout"
+    subprocess.check_call(["gcc", "-std=c11", "-I", os.path.join(ROOT, "include"), "-o", str(exe),
+                           str(src)])
+    got = dict(x.split() for x in subprocess.check_output([str(exe)], text=True).splitlines())
+    for st in structs:
+        assert int(got[st.__name__]) == ctypes.sizeof(st)
+        for f, _ in st._fields_:
+            assert int(got[f"{st.__name__}.{f}"]) == getattr(st, f).offset, f
+    assert step._APPEND_FP4.size == ctypes.sizeof(fp4.tas_append_fp4)
+    assert step._ATTENTION_FP4.size == ctypes.sizeof(fp4.tas_attention_fp4)
+
+
+def rows(p, *stride):
+    return fp4.tas_rows(p, (ctypes.c_int64 * 3)(*stride))
+
+
+@pytest.fixture
+def bound():
+    b, keep = step.make_batch([1, 3], [20, 3], [[0, 1], [2, 3]], heads=4, kv_heads=2, head_dim=64,
+                              block_tokens=16, n_blocks=4)
+    ctx = step.tas_step_create(b)
+    step.tas_step_attach(ctx, AT, step.tas_step_bytes(ctx))
+    yield ctx
+    step.tas_step_destroy(ctx)
+
+
+def cache(**kw):
+    """Blocks of 2 heads of 16 tokens of 64: 32 bytes of codes and 2 of scales a row."""
+    c = dict(k=rows(AT + (1 << 20), 1024, 512, 32), v=rows(AT + (2 << 20), 1024, 512, 32),
+             k_scale=rows(AT + (3 << 20), 64, 32, 2), v_scale=rows(AT + (4 << 20), 64, 32, 2))
+    c.update(kw)
+    return fp4.tas_cache_fp4(*(c[n] for n in ("k", "v", "k_scale", "v_scale")))
+
+
+def refused(call, ctx, args):
+    return call(ctx, ctypes.byref(args), None) == tas.TAS_EINVAL
+
+
+BAD_CACHES = [dict(k=rows(AT + 8, 1024, 512, 32)), dict(k=rows(None, 1024, 512, 32)),
+              dict(v=rows(AT + (2 << 20), 1024, 512, 24)), dict(v=rows(AT, -1024, 512, 32)),
+              dict(v=rows(AT, 1 << 31, 512, 32)), dict(v=rows(AT, 1024, 512, (1 << 24) + 16)),
+              dict(k_scale=rows(AT + 1, 64, 32, 2)), dict(v_scale=rows(AT, 64, 31, 2)),
+              dict(v_scale=rows(None, 64, 32, 2))]
+
+
+def test_refused_attention(bound):
+    """(The last argument that is looked at is refused in each: nothing is launched.)"""
+    L = step.lib()
+
+    def args(**kw):
+        a = dict(dtype=1, scale=0.125, q=AT + (8 << 20), q_stride=256, out=AT + (9 << 20),
+                 out_stride=256, lse=AT + (9 << 20), cache=cache())  # lse over out
+        a.update(kw)
+        return fp4.tas_attention_fp4(**a)
+
+    assert L.tas_fp4_attention(None, None, None) == tas.TAS_EINVAL
+    assert refused(L.tas_fp4_attention, bound, args())
+    for kw in [dict(dtype=2), dict(scale=0), dict(scale=float("nan")), dict(scale=3e38),
+               dict(q=AT + 8), dict(q=None), dict(q_stride=255), dict(q_stride=260),
+               dict(out=None), dict(out_stride=248), dict(lse=AT + (10 << 20) + 2),
+               dict(lse=AT + (1 << 20)), dict(lse=AT + (4 << 20)), dict(lse=AT + (8 << 20)),
+               dict(out=AT + (8 << 20) + 16, lse=None), dict(out=AT + (2 << 20), lse=None),
+               dict(out=AT + (4 << 20), lse=None)] + [dict(cache=cache(**c), lse=None)
+                                                     for c in BAD_CACHES]:
+        assert refused(L.tas_fp4_attention, bound, args(**kw)), kw
+
+
+def test_refused_append(bound):
+    L = step.lib()
+
+    def args(**kw):
+        a = dict(dtype=0, rot_dim=32, interleaved=0, eps=1e-6, qkv=AT + (8 << 20), qkv_stride=512,
+                 q_out=AT + (9 << 20), q_out_stride=256, q_weight=AT + (10 << 20),
+                 k_weight=AT + (11 << 20), cos=AT + (12 << 20), sin=AT + (9 << 20) + 1024,
+                 positions=20, cache=cache())  # sin over q_out
+        a.update(kw)
+        return fp4.tas_append_fp4(**a)
+
+    assert L.tas_fp4_append(None, None, None) == tas.TAS_EINVAL
+    assert refused(L.tas_fp4_append, bound, args())
+    apart = dict(sin=AT + (13 << 20))
+    for kw in [dict(dtype=2), dict(rot_dim=24), dict(rot_dim=80), dict(interleaved=2),
+               dict(eps=-1), dict(k_weight=None), dict(q_weight=AT + 8), dict(cos=None),
+               dict(positions=19), dict(qkv=None), dict(qkv_stride=504), dict(q_out_stride=252),
+               dict(qkv=AT + (9 << 20)), dict(q_out=AT + (8 << 20) + 512),
+               dict(q_out=AT + (3 << 20)), dict(qkv=AT + (2 << 20)),
+               dict(q_weight=AT + (9 << 20) + 256), dict(k_weight=AT + (1 << 20)),
+               dict(cos=AT + (4 << 20))]:
+        assert refused(L.tas_fp4_append, bound, args(**{**apart, **kw})), kw
+    for c in BAD_CACHES + [dict(k=rows(AT + (1 << 20), 0, 512, 32)),
+                           dict(k=rows(AT + (1 << 20), 1024, 256, 32)),
+                           dict(k=rows(AT + (1 << 20), 1024, 512, 16)),
+                           dict(v_scale=rows(AT + (4 << 20), 64, 0, 2)),
+                           dict(k=rows(AT + (2 << 20) + 512, 1024, 512, 32)),
+                           dict(k_scale=rows(AT + (4 << 20) + 64, 64, 32, 2)),
+                           dict(k_scale=rows(AT + (1 << 20) + 64, 64, 32, 2))]:
+        assert refused(L.tas_fp4_append, bound, args(**apart, cache=cache(**c))), c
+
+
+def test_unbound_steps_and_batches_that_cannot_be_appended():
+    L = step.lib()
+    b, keep = step.make_batch([1], [1], [[0]], heads=1, kv_heads=1, head_dim=64, block_tokens=16,
+                              n_blocks=1)
+    ctx = step.tas_step_create(b)
+    assert L.tas_fp4_append(ctx, ctypes.byref(fp4.tas_append_fp4()), None) == tas.TAS_ESTATE
+    assert L.tas_fp4_attention(ctx, ctypes.byref(fp4.tas_attention_fp4()), None) == tas.TAS_ESTATE
+    step.tas_step_destroy(ctx)
+    b, keep = step.make_batch([3], [2], [[0]], heads=1, kv_heads=1, head_dim=64, block_tokens=16,
+                              n_blocks=1)
+    ctx = step.tas_step_create(b)
+    assert L.tas_fp4_append(ctx, ctypes.byref(fp4.tas_append_fp4()), None) == tas.TAS_EINVAL
+    step.tas_step_destroy(ctx)
+
+
+def test_refused_tensors():
+    L = step.lib()
+
+    def tensor(**kw):
+        t = dict(dtype=1, reserved=0, n=(2, 3, 5), cols=64, x=rows(AT, 1920, 640, 128),
+                 codes=rows(AT + (1 << 20), 480, 160, 32), scales=rows(AT + (1 << 20), 30, 10, 2))
+        t.update(kw)
+        t["n"] = (ctypes.c_int64 * 3)(*t["n"])
+        return ctypes.byref(fp4.tas_tensor_fp4(**t))  # scales over codes
+
+    apart = dict(scales=rows(AT + (2 << 20), 30, 10, 2))
+    assert L.tas_fp4_pack(None, None) == L.tas_fp4_values(None, None) == tas.TAS_EINVAL
+    assert L.tas_fp4_pack(tensor(), None) == tas.TAS_EINVAL
+    assert L.tas_fp4_pack(tensor(n=(2, 0, 5)), None) == 0
+    both = [dict(dtype=2), dict(reserved=1), dict(cols=48), dict(cols=0), dict(cols=-32),
+            dict(n=(-1, 3, 5)), dict(n=(1 << 20, 1 << 20, 1)), dict(n=(1 << 62, 1 << 62, 4)),
+            dict(cols=1 << 36), dict(x=rows(AT + 8, 1920, 640, 128)),
+            dict(x=rows(AT, 1920, 640, 136)), dict(x=rows(AT, -1920, 640, 128)),
+            dict(x=rows(None, 1920, 640, 128)), dict(codes=rows(AT + 2, 480, 160, 32)),
+            dict(codes=rows(AT + (1 << 20), 480, 1 << 50, 32)), dict(scales=rows(None, 30, 10, 2)),
+            dict(codes=rows(AT + 1900, 480, 160, 32)), dict(scales=rows(AT + 3800, 30, 10, 2))]
+    for kw in both:
+        assert L.tas_fp4_pack(tensor(**{**apart, **kw}), None) == tas.TAS_EINVAL, kw
+        assert L.tas_fp4_values(tensor(**{**apart, **kw}), None) == tas.TAS_EINVAL, kw
+    for kw in (dict(codes=rows(AT + (1 << 20), 480, 160, 16)), dict(scales=rows(AT + (2 << 20), 30, 0, 2)),
+               dict(scales=rows(AT + (1 << 20) + 957, 30, 10, 2))):
+        assert L.tas_fp4_pack(tensor(**{**apart, **kw}), None) == tas.TAS_EINVAL, kw
+    assert L.tas_fp4_values(tensor(**apart, x=rows(AT, 1920, 0, 128)), None) == tas.TAS_EINVAL
+
+
+def test_weights_bytes():
+    L = step.lib()
+    assert L.tas_fp4_weights_bytes(1, 32) == 1024 + 256
+    assert L.tas_fp4_weights_bytes(17, 160) == 4 * 1024 + 2 * 256
+    assert L.tas_fp4_weights_bytes(4096, 4096) == 4096 * 4096 * 17 // 32
+    for bad in ((0, 32), (-1, 32), (1, 0), (1, 16), (1, 48), (1, -32), (1 << 25, 32),
+                (1, (1 << 20) + 32), (1 << 24, 1 << 20)):
+        assert L.tas_fp4_weights_bytes(*bad) == 0, bad
+
+
+def test_refused_weights_and_products():
+    L = step.lib()
+    ok = [40, 64, AT, 32, AT + (1 << 20), 2, AT + (1 << 20)]  # (onto the scales)
+    assert L.tas_fp4_weights(*ok, None) == tas.TAS_EINVAL
+    for i, bad in ((0, 0), (1, 48), (2, None), (2, AT + 8), (3, 24), (3, -32), (3, (1 << 31) + 16),
+                   (4, None), (5, -1), (6, None), (6, AT + 128), (6, AT)):
+        args = ok[:6] + [AT + (2 << 20)]
+        args[i] = bad
+        assert L.tas_fp4_weights(*args, None) == tas.TAS_EINVAL, (i, bad)
+
+    def linear(**kw):
+        a = dict(dtype=1, reserved=0, tokens=3, rows=40, cols=64, x=AT, x_stride=64,
+                 weights=AT + (1 << 20), y=AT + 128, y_stride=40)  # y over x
+        a.update(kw)
+        return L.tas_fp4_linear(ctypes.byref(fp4.tas_linear_fp4(**a)), None)
+
+    assert L.tas_fp4_linear(None, None) == tas.TAS_EINVAL
+    assert linear() == tas.TAS_EINVAL
+    assert linear(tokens=0, x=None, y=None) == 0
+    apart = dict(y=AT + (3 << 20))
+    for kw in (dict(dtype=2), dict(reserved=1), dict(tokens=-1), dict(tokens=1 << 25),
+               dict(rows=0), dict(cols=48), dict(x=None), dict(x=AT + 8), dict(x_stride=56),
+               dict(x_stride=68), dict(x_stride=1 << 31), dict(weights=None),
+               dict(weights=AT + 128), dict(y=None), dict(y=AT + (3 << 20) + 1),
+               dict(y_stride=39), dict(y_stride=1 << 31), dict(y=AT + (1 << 20) + 3000)):
+        assert linear(**{**apart, **kw}) == tas.TAS_EINVAL, kw
