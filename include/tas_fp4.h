@@ -123,7 +123,7 @@ typedef struct tas_linear_fp4 {
     int32_t reserved;              /* 0                                                      */
     int64_t tokens, rows, cols;    /* tokens 0 .. 2^24                                       */
     const void *x;                 /* [tokens][cols], 16-byte aligned                        */
-    int64_t x_stride;              /* elements, a multiple of 8, below 2^31                  */
+    int64_t x_stride;              /* elements, a multiple of 8, at most 2^24                */
     const void *weights;           /* as tas_fp4_weights laid them out                       */
     void *y;                       /* [tokens][rows], 2-byte aligned                         */
     int64_t y_stride;              /* elements, below 2^31                                   */
@@ -131,7 +131,8 @@ typedef struct tas_linear_fp4 {
 
 /* The products of x's and W's values (W's are exact in 16 bits) are summed in 32
  * bits in an order that depends on the sizes alone, and rounded once. TAS_EINVAL:
- * an argument out of range or unaligned, y over x or the weights. */
+ * an argument out of range or unaligned, y over x or the weights, more than 2^33 elements
+ * of y (about: 2^21 tiles of 64 by 64). */
 int tas_fp4_linear(const tas_linear_fp4 *a, void *stream);
 
 #ifdef __cplusplus

@@ -300,9 +300,12 @@ int tas_fp4_linear(const tas_linear_fp4 *a, void *stream) {
     if (!bytes || !a->weights || (uintptr_t)a->weights & 255) return TAS_EINVAL;
     if (a->tokens < 0 || a->tokens > (int64_t(1) << 24)) return TAS_EINVAL;
     if (!a->tokens) return TAS_OK;
-    const int64_t most = int64_t(1) << 31;
-    if (!valid_rows(a->x, a->x_stride, a->cols) || a->x_stride >= most) return TAS_EINVAL;
-    if (!a->y || (uintptr_t)a->y % 2 || a->y_stride < a->rows || a->y_stride >= most)
+    // (the smallest tiles, of 32 by 32, are not taken where there are many)
+    if (ceil_div(a->rows, 64) * ceil_div(a->tokens, 64) > kMaxGroups / 8) return TAS_EINVAL;
+    if (!valid_rows(a->x, a->x_stride, a->cols) || a->x_stride > kMaxTokenStride)
+        return TAS_EINVAL;
+    if (!a->y || (uintptr_t)a->y % 2 || a->y_stride < a->rows ||
+        a->y_stride >= int64_t(1) << 31)
         return TAS_EINVAL;
     const Region y = tokens_of(a->y, a->y_stride, a->rows, a->tokens);
     if (Overlap()(y, tokens_of(a->x, a->x_stride, a->cols, a->tokens)) ||
@@ -321,7 +324,6 @@ int tas_fp4_linear(const tas_linear_fp4 *a, void *stream) {
     k.blocks = (int32_t)(a->cols / 32);
     k.tiles_n = (int32_t)w.tiles_n;
     k.tiles_k = (int32_t)w.tiles_k;
-    k.units_k = (int32_t)w.units_k;
     k.y_fours = a->rows % 4 == 0 && a->y_stride % 4 == 0 && (uintptr_t)a->y % 8 == 0;
     return done(launch_linear4(k, a->dtype, (hipStream_t)stream));
 }

@@ -22,21 +22,21 @@ struct Tensor4Args {
 };
 
 // Weights as the products read them: tiles of 16 rows and 128 columns, the tiles of a run
-// of rows one after another. Lane 16 g + r of a wave has the 16 bytes of row r's block g,
-// so that a tile is one load of adjacent 16 bytes a lane; the scales of four tiles are one
-// load of four bytes a lane. Rows and blocks beyond the matrix are zeros.
+// of rows one after another, so that a tile is one load of adjacent 16 bytes a lane. Lane
+// 16 g + r has the words g (elements 8 g .. 8 g + 7) of row r's four blocks: a product's 32
+// k-slots are one block, and adjacent in x. A tile's scales are 64 bytes, byte 4 r + j that of
+// row r, block j. Rows and blocks beyond the matrix are zeros.
 constexpr int kTileRows = 16, kTileCols = 128;
 struct WeightsShape {
-    int64_t tiles_n, tiles_k, units_k;  // units: four tiles along a row
-    int64_t scales_at, bytes;           // byte offset of the scales; size
+    int64_t tiles_n, tiles_k;
+    int64_t scales_at, bytes;  // byte offset of the scales; size
 };
 inline WeightsShape weights_shape(int64_t rows, int64_t cols) {
     WeightsShape w;
     w.tiles_n = (rows + kTileRows - 1) / kTileRows;
     w.tiles_k = (cols + kTileCols - 1) / kTileCols;
-    w.units_k = (w.tiles_k + 3) / 4;
     w.scales_at = w.tiles_n * w.tiles_k * 1024;
-    w.bytes = w.scales_at + w.tiles_n * w.units_k * 256;
+    w.bytes = w.scales_at + w.tiles_n * w.tiles_k * 64;
     return w;
 }
 struct Weights4Args {
@@ -51,7 +51,7 @@ struct Linear4Args {
     void *y;
     int64_t x_stride, y_stride;
     int32_t tokens, rows, blocks;  // blocks of a row
-    int32_t tiles_n, tiles_k, units_k;
+    int32_t tiles_n, tiles_k;
     int32_t y_fours;  // y can be written four elements at once
 };
 

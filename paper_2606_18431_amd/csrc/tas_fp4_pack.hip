@@ -43,24 +43,26 @@ __global__ __launch_bounds__(256) void values_kernel(Tensor4Args a) {
     *(vec8<T> *)(row_at(a.x, row, a.n1, a.n2) + c * 16ull) = values_of<T>(codes, scale_of(byte));
 }
 
-// A thread's 16 bytes are those of one lane and tile.
+// A thread's 16 bytes of codes are those of one lane and tile, its byte of scale that of a
+// row and block of it.
 __global__ __launch_bounds__(256) void weights_kernel(Weights4Args a) {
     const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t tile = u >> 6, tn = tile / a.w.tiles_k, tk = tile - tn * a.w.tiles_k;
     if (tn >= a.w.tiles_n) return;
-    const int lane = u & 63;
-    const int64_t row = tn * kTileRows + (lane & 15), block = tk * 4 + (lane >> 4);
+    const int lane = u & 63, r = lane & 15, g = lane >> 4;
+    const int64_t row = tn * kTileRows + r;
     u4 codes = {0, 0, 0, 0};
-    char scale = 0;
-    if (row < a.rows && block < a.blocks) {
-        codes = *(const u4 *)(a.codes + row * a.codes_stride + block * 16);
-        scale = a.scales[row * a.scales_stride + block];
+    uint8_t scale = 0;
+    if (row < a.rows) {
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+            if (tk * 4 + j < a.blocks)
+                codes[j] = *(const uint32_t *)(a.codes + row * a.codes_stride +
+                                               (tk * 4 + j) * 16 + g * 4);
+        if (tk * 4 + g < a.blocks) scale = a.scales[row * a.scales_stride + tk * 4 + g];
     }
     *(u4 *)(a.out + tile * 1024 + lane * 16) = codes;
-    char *s = a.out + a.w.scales_at + (tn * a.w.units_k + tk / 4) * 256 + lane * 4;
-    s[tk & 3] = scale;
-    if (tk == a.w.tiles_k - 1)  // of the last unit, tiles that there are not
-        for (int i = (tk & 3) + 1; i < 4; i++) s[i] = 0;
+    a.out[a.w.scales_at + tile * 64 + r * 4 + g] = (char)scale;
 }
 
 }  // namespace

@@ -181,8 +181,8 @@ def test_refused_tensors():
 
 def test_weights_bytes():
     L = step.lib()
-    assert L.tas_fp4_weights_bytes(1, 32) == 1024 + 256
-    assert L.tas_fp4_weights_bytes(17, 160) == 4 * 1024 + 2 * 256
+    assert L.tas_fp4_weights_bytes(1, 32) == 1024 + 64
+    assert L.tas_fp4_weights_bytes(17, 160) == 4 * (1024 + 64)
     assert L.tas_fp4_weights_bytes(4096, 4096) == 4096 * 4096 * 17 // 32
     for bad in ((0, 32), (-1, 32), (1, 0), (1, 16), (1, 48), (1, -32), (1 << 25, 32),
                 (1, (1 << 20) + 32), (1 << 24, 1 << 20)):
@@ -211,7 +211,7 @@ def test_refused_weights_and_products():
     apart = dict(y=AT + (3 << 20))
     for kw in (dict(dtype=2), dict(reserved=1), dict(tokens=-1), dict(tokens=1 << 25),
                dict(rows=0), dict(cols=48), dict(x=None), dict(x=AT + 8), dict(x_stride=56),
-               dict(x_stride=68), dict(x_stride=1 << 31), dict(weights=None),
+               dict(x_stride=68), dict(x_stride=(1 << 24) + 8), dict(weights=None),
                dict(weights=AT + 128), dict(y=None), dict(y=AT + (3 << 20) + 1),
                dict(y_stride=39), dict(y_stride=1 << 31), dict(y=AT + (1 << 20) + 3000)):
         assert linear(**{**apart, **kw}) == tas.TAS_EINVAL, kw
