@@ -75,9 +75,12 @@ bool disjoint(const tas_cache_fp4 &c, const CacheShape &s, const CacheRegions &r
 bool valid_dtype(int32_t dtype) { return dtype == TAS_F16 || dtype == TAS_BF16; }
 int done(hipError_t e) { return e == hipSuccess ? TAS_OK : TAS_EHIP; }
 
-// A tensor's sizes, and what its sides have in common.
-bool valid_tensor(const tas_tensor_fp4 *a, int64_t &rows) {
-    if (!a || !valid_dtype(a->dtype) || a->reserved) return false;
+// A tensor's rows, and what its sides have in common; the stride of a dimension of one says
+// nothing.
+bool valid_tensor(const tas_tensor_fp4 *from, tas_tensor_fp4 *a, int64_t &rows) {
+    if (!from) return false;
+    *a = *from;
+    if (!valid_dtype(a->dtype) || a->reserved) return false;
     if (a->cols < 32 || a->cols % 32) return false;
     rows = 1;
     int64_t most = (int64_t(1) << 35) / a->cols;
@@ -87,12 +90,14 @@ bool valid_tensor(const tas_tensor_fp4 *a, int64_t &rows) {
         if (n) most /= n;
     }
     if (!rows) return true;
-    auto strides = [&](const tas_rows &r, int64_t align) {
+    auto strides = [&](tas_rows &r, int64_t align) {
         if (!r.p || (uintptr_t)r.p % align) return false;
-        for (int i = 0; i < 3; i++)  // (places stay far below 2^63)
+        for (int i = 0; i < 3; i++) {  // (places stay far below 2^63)
+            if (a->n[i] == 1) r.stride[i] = 0;
             if (r.stride[i] < 0 || r.stride[i] % align ||
                 r.stride[i] > (int64_t(1) << 50) / a->n[i])
                 return false;
+        }
         return true;
     };
     return strides(a->x, 16) && strides(a->codes, 4) && strides(a->scales, 1);
@@ -225,9 +230,10 @@ int tas_fp4_attention(tas_step *s, const tas_attention_fp4 *a, void *stream) {
                                   s->head_dim, (hipStream_t)stream));
 }
 
-int tas_fp4_pack(const tas_tensor_fp4 *a, void *stream) {
+int tas_fp4_pack(const tas_tensor_fp4 *from, void *stream) {
+    tas_tensor_fp4 tensor, *const a = &tensor;
     int64_t rows;
-    if (!valid_tensor(a, rows)) return TAS_EINVAL;
+    if (!valid_tensor(from, a, rows)) return TAS_EINVAL;
     if (!rows) return TAS_OK;
     const int64_t(&n)[3] = a->n;
     const int64_t cb = a->cols / 2, sb = a->cols / 32;
@@ -242,9 +248,10 @@ int tas_fp4_pack(const tas_tensor_fp4 *a, void *stream) {
     return done(launch_pack4(tensor_args(a, rows), a->dtype, (hipStream_t)stream));
 }
 
-int tas_fp4_values(const tas_tensor_fp4 *a, void *stream) {
+int tas_fp4_values(const tas_tensor_fp4 *from, void *stream) {
+    tas_tensor_fp4 tensor, *const a = &tensor;
     int64_t rows;
-    if (!valid_tensor(a, rows)) return TAS_EINVAL;
+    if (!valid_tensor(from, a, rows)) return TAS_EINVAL;
     if (!rows) return TAS_OK;
     const int64_t(&n)[3] = a->n;
     if (!disjoint_slots(a->x.stride[0], a->x.stride[1], a->x.stride[2], n[0], n[1], n[2],

@@ -6,9 +6,15 @@
 //     (a, b) <- (a cos x - b sin x, b cos x + a sin x)    x: the position's angles
 // Queries in 32 bits, rounded once. Keys and values are rounded to four bits by blocks of
 // 32. A key that lies within a rounding error of the border of two codes would get either,
-// by the order of the norm's sum, and an error of half a step; so keys are worked out in 64
-// bits, which this chip computes at half the rate of 32. Nothing is read twice and nothing in
-// between is written, so the bound is the copy of the queries and the reading of the rest.
+// by the order of the norm's sum, and an error of half a step: such keys are worked out again
+// in 64 bits. In 32 bits a key is off by 13 roundings of |a cos x| + |b sin x| at most: a term
+// of the norm's sum passes 10 in its lane and 3 over the lanes, eps is one more, the root
+// halves them to 7 and is one itself, as the division, two products and the rotation's two.
+// With two for the comparison that is less than 2^-20; 2^-19 is taken. Where so much moves a
+// code or a block's scale (of some hundredths of the waves), or the range of 32 bits may not
+// do, the wave's keys take the long way. Nothing else is read twice and nothing in between is
+// written, so the bound is the copy of the queries and the reading of the rest. (13321 tokens
+// of 32/8 heads of 128: with all keys in 64 bits 76 us, 65 so.)
 //
 // A head is D / 16 lanes with two chunks of eight elements each, chosen so that a lane
 // holds both members of its rotated pairs: chunks i and i + R / 16 of the halves (R / 8
@@ -25,54 +31,133 @@ namespace {
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 
-__device__ float root(float x) { return sqrtf(x); }
-__device__ double root(double x) { return sqrt(x); }
+// A lane's part of a head.
+struct Part {
+    int c0, c1;   // its chunks
+    int i;        // the lane of the head
+    bool turned;  // whether they are rotated
+    int pos;      // of the token
+};
 
-// Chunks c0 and c1 (y0, y1) of a head whose chunks the D / 16 lanes i hold: normed, with
-// weights, and rotated by the angles of position `pos`, if `turned`.
-template <typename T, int D, typename F>
-__device__ __forceinline__ void norm_and_turn(const AppendArgs &a, const void *weight, int c0,
-                                              int c1, int i, bool turned, int pos, F (&y0)[8],
-                                              F (&y1)[8]) {
+// Chunks c0 and c1 (x0, x1) of a head: normed, with weights, and rotated; and how far the
+// results may be off.
+template <int D, typename T>
+__device__ __forceinline__ float norm_and_turn(const AppendArgs &a, const void *weight,
+                                               const Part &p, const vec8<T> &x0,
+                                               const vec8<T> &x1, float (&y0)[8], float (&y1)[8]) {
     using V = vec8<T>;
+    bool in_range = true;  // where roundings are relative ones
+#pragma unroll
+    for (int e = 0; e < 8; e++) y0[e] = (float)x0[e], y1[e] = (float)x1[e];
     if (weight) {
-        F sum = 0;
+        float sum = 0;
+#pragma unroll
         for (int e = 0; e < 8; e++) sum += y0[e] * y0[e] + y1[e] * y1[e];
         for (int m = 1; m < D / 16; m *= 2) sum += __shfl_xor(sum, m);
-        const F f = F(1) / root(sum / D + a.eps);
-        const V w0 = *(const V *)((const T *)weight + c0 * 8);
-        const V w1 = *(const V *)((const T *)weight + c1 * 8);
-        for (int e = 0; e < 8; e++) y0[e] *= f * (F)w0[e], y1[e] *= f * (F)w1[e];
+        const float mean = sum / D + a.eps, f = 1.0f / sqrtf(mean);
+        in_range = mean > 0x1p-100f && mean < 0x1p120f;
+        const V w0 = *(const V *)((const T *)weight + p.c0 * 8);
+        const V w1 = *(const V *)((const T *)weight + p.c1 * 8);
+#pragma unroll
+        for (int e = 0; e < 8; e++) y0[e] *= f * (float)w0[e], y1[e] *= f * (float)w1[e];
     }
-    if (turned) {
-        const int64_t p = (int64_t)pos * (a.rot / 2) + i * 8;
+    float most = 0;
+    if (p.turned) {
+        const int64_t at = (int64_t)p.pos * (a.rot / 2) + p.i * 8;
         float c[8], s[8];
-        *(f4 *)c = *(const f4 *)(a.cos + p), *(f4 *)(c + 4) = *(const f4 *)(a.cos + p + 4);
-        *(f4 *)s = *(const f4 *)(a.sin + p), *(f4 *)(s + 4) = *(const f4 *)(a.sin + p + 4);
+        *(f4 *)c = *(const f4 *)(a.cos + at), *(f4 *)(c + 4) = *(const f4 *)(a.cos + at + 4);
+        *(f4 *)s = *(const f4 *)(a.sin + at), *(f4 *)(s + 4) = *(const f4 *)(a.sin + at + 4);
+        auto turn = [&](float &x, float &y, float c, float s) {
+            const float u = x, v = y;
+            most = fmaxf(most, fmaxf(fabsf(u * c) + fabsf(v * s), fabsf(v * c) + fabsf(u * s)));
+            x = u * c - v * s;
+            y = v * c + u * s;
+        };
         if (a.interleaved) {
+#pragma unroll
             for (int e = 0; e < 4; e++) {
-                const F u = y0[2 * e], v = y0[2 * e + 1];
-                y0[2 * e] = u * c[e] - v * s[e];
-                y0[2 * e + 1] = v * c[e] + u * s[e];
-                const F w = y1[2 * e], z = y1[2 * e + 1];
-                y1[2 * e] = w * c[4 + e] - z * s[4 + e];
-                y1[2 * e + 1] = z * c[4 + e] + w * s[4 + e];
+                turn(y0[2 * e], y0[2 * e + 1], c[e], s[e]);
+                turn(y1[2 * e], y1[2 * e + 1], c[4 + e], s[4 + e]);
             }
         } else {
-            for (int e = 0; e < 8; e++) {
-                const F u = y0[e], v = y1[e];
-                y0[e] = u * c[e] - v * s[e];
-                y1[e] = v * c[e] + u * s[e];
-            }
+#pragma unroll
+            for (int e = 0; e < 8; e++) turn(y0[e], y1[e], c[e], s[e]);
         }
+    } else if (weight) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) most = fmaxf(most, fmaxf(fabsf(y0[e]), fabsf(y1[e])));
     }
+    in_range &= most == 0 || (most > 0x1p-100f && most < 0x1p120f);
+    return in_range ? most * 0x1p-19f : INFINITY;
+}
+
+// The same in 64 bits, to floats on the same side of every border; `to`: 16 floats of the
+// lane in LDS. (Element after element: of doubles, few are held at once.)
+template <int D, typename T>
+__device__ __forceinline__ void norm_and_turn_exact(const AppendArgs &a, const T *weight,
+                                                    const Part &p, vec8<T> x0, vec8<T> x1,
+                                                    float *to) {
+    using V = vec8<T>;
+    double f = 1;
+    V w0, w1;
+#pragma unroll
+    for (int e = 0; e < 8; e++) w0[e] = w1[e] = (T)1.0f;
+    if (weight) {
+        w0 = *(const V *)(weight + p.c0 * 8);
+        w1 = *(const V *)(weight + p.c1 * 8);
+        double sum = 0;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const double u = (float)x0[e], v = (float)x1[e];
+            sum += u * u + v * v;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        for (int m = 1; m < D / 16; m *= 2) sum += __shfl_xor(sum, m);
+        f = 1.0 / sqrt(sum / D + a.eps);
+    }
+    const float *cos = a.cos + (int64_t)p.pos * (a.rot / 2) + p.i * 8;
+    const float *sin = a.sin + (int64_t)p.pos * (a.rot / 2) + p.i * 8;
+    const bool halves = p.turned && !a.interleaved;
+    // converted again below, not kept
+    u4 k0 = __builtin_bit_cast(u4, x0), k1 = __builtin_bit_cast(u4, x1);
+    asm volatile("" : "+v"(k0), "+v"(k1));
+    x0 = __builtin_bit_cast(V, k0), x1 = __builtin_bit_cast(V, k1);
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        // a rotated pair, or two elements: (c0, e) and (c1, e), or the two of 16 from 2 e on
+        const int pair = 2 * e % 8;
+        const V &xp = e < 4 ? x0 : x1, &wp = e < 4 ? w0 : w1;
+        const float ux = halves ? (float)x0[e] : (float)xp[pair];
+        const float vx = halves ? (float)x1[e] : (float)xp[pair + 1];
+        const float uw = halves ? (float)w0[e] : (float)wp[pair];
+        const float vw = halves ? (float)w1[e] : (float)wp[pair + 1];
+        const double u = ux * (f * uw), v = vx * (f * vw);
+        double x = u, y = v;
+        if (p.turned) {
+            const double c = cos[e], s = sin[e];
+            x = u * c - v * s;
+            y = v * c + u * s;
+        }
+        to[halves ? e : 2 * e] = odd_float(x);
+        to[halves ? 8 + e : 2 * e + 1] = odd_float(y);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// Whether two words of codes differ in more than the sign of zeros.
+__device__ bool differ(uint32_t x, uint32_t y) {
+    const uint32_t signs = 0x88888888u;
+    const uint32_t not_zero = (((x | y) & ~signs) + ~signs) & signs;
+    return ((x ^ y) & (not_zero | ~signs)) != 0;
 }
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void append4_kernel(Append4Args a) {
     constexpr int LPH = D / 16, HPW = heads_of_wave(D);  // lanes of a head, heads of a wave
     using V = vec8<T>;
-    __shared__ __attribute__((aligned(16))) uint32_t most[4][HPW][D / 8];
+    // of a wave's heads: the chunks' largest magnitudes, at least and at most
+    __shared__ __attribute__((aligned(16))) uint32_t least[4][HPW][D / 8], most[4][HPW][D / 8];
+    __shared__ __attribute__((aligned(16))) float exact[4][64][16];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, i = lane % LPH;
     const uint32_t per_tok = (a.heads + 2 * a.kv_heads + HPW - 1) / HPW;
     const uint32_t unit = blockIdx.x * 4 + wave;
@@ -82,56 +167,86 @@ __global__ __launch_bounds__(256) void append4_kernel(Append4Args a) {
     if (h >= a.heads + 2 * a.kv_heads) return;  // whole heads: all exchanges stay in one
 
     const int RL = a.rot / 16;
-    const bool turned = i < RL;
-    int c0 = 2 * i, c1 = 2 * i + 1;
-    if (!a.interleaved && turned) c0 = i, c1 = i + RL;
+    Part p;
+    p.i = i;
+    p.turned = i < RL;
+    p.c0 = 2 * i, p.c1 = 2 * i + 1;
+    if (!a.interleaved && p.turned) p.c0 = i, p.c1 = i + RL;
     const T *src = (const T *)a.qkv + tok * a.qkv_stride + (int64_t)h * D;
-    const V x0 = *(const V *)(src + c0 * 8), x1 = *(const V *)(src + c1 * 8);
+    const V x0 = *(const V *)(src + p.c0 * 8), x1 = *(const V *)(src + p.c1 * 8);
 
     const Req &r = a.reqs[a.tok_req[tok]];
     const int j = (int)tok - r.t0, own = r.kv_len - r.n_new + j;
+    p.pos = r.prefix_len + own;
+    float y0[8], y1[8], off = 0;
     if (h < a.heads) {
-        float y0[8], y1[8];
-        for (int e = 0; e < 8; e++) y0[e] = (float)x0[e], y1[e] = (float)x1[e];
-        norm_and_turn<T, D>(a, a.q_weight, c0, c1, i, turned, r.prefix_len + own, y0, y1);
+        norm_and_turn<D, T>(a, a.q_weight, p, x0, x1, y0, y1);
         V z0, z1;
+#pragma unroll
         for (int e = 0; e < 8; e++) z0[e] = (T)y0[e], z1[e] = (T)y1[e];
         T *to = (T *)a.q_out + tok * a.q_out_stride + (int64_t)h * D;
-        *(V *)(to + c0 * 8) = z0;
-        *(V *)(to + c1 * 8) = z1;
+        *(V *)(to + p.c0 * 8) = z0;
+        *(V *)(to + p.c1 * 8) = z1;
         return;
     }
     const int page = a.tables[r.table + (own >> a.blk_shift)];
     const int at = own & ((1 << a.blk_shift) - 1);
     const bool is_v = h >= a.heads + a.kv_heads;
-    float y0[8], y1[8];
-    if (is_v) {
+    if (is_v)
+#pragma unroll
         for (int e = 0; e < 8; e++) y0[e] = (float)x0[e], y1[e] = (float)x1[e];
-    } else {
-        double z0[8], z1[8];
-        for (int e = 0; e < 8; e++) z0[e] = (double)(float)x0[e], z1[e] = (double)(float)x1[e];
-        norm_and_turn<T, D>(a, a.k_weight, c0, c1, i, turned, r.prefix_len + own, z0, z1);
-        for (int e = 0; e < 8; e++) y0[e] = odd_float(z0[e]), y1[e] = odd_float(z1[e]);
-    }
-    uint32_t *mine = most[wave][lane / LPH];
-    mine[c0] = largest(y0);
-    mine[c1] = largest(y1);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    auto byte_of = [&](int c) {
-        const u4 m = *(const u4 *)(mine + (c & ~3));
+    else
+        off = norm_and_turn<D, T>(a, a.k_weight, p, x0, x1, y0, y1);
+
+    uint32_t *lo = least[wave][lane / LPH], *hi = most[wave][lane / LPH];
+    auto byte_of = [&](const uint32_t *from, int c) {
+        const u4 m = *(const u4 *)(from + (c & ~3));
         return scale_byte<T>(max(max(m[0], m[1]), max(m[2], m[3])));
     };
-    const uint32_t b0 = byte_of(c0), b1 = byte_of(c1);
+    const float most0 = __builtin_bit_cast(float, largest(y0));
+    const float most1 = __builtin_bit_cast(float, largest(y1));
+    auto bits = [](float x) { return __builtin_bit_cast(uint32_t, x); };
+    hi[p.c0] = bits(most0 + off);
+    hi[p.c1] = bits(most1 + off);
+    lo[p.c0] = bits(most0 < off ? 0.0f : most0 - off);
+    lo[p.c1] = bits(most1 < off ? 0.0f : most1 - off);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    uint32_t b0 = byte_of(hi, p.c0), b1 = byte_of(hi, p.c1);
+    uint32_t k0 = codes_of(y0, b0), k1 = codes_of(y1, b1);
+    bool unsure = b0 != byte_of(lo, p.c0) || b1 != byte_of(lo, p.c1);
+    if (off != 0) {
+        float u0[8], u1[8], v0[8], v1[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            u0[e] = y0[e] - off, u1[e] = y1[e] - off;
+            v0[e] = y0[e] + off, v1[e] = y1[e] + off;
+        }
+        unsure |= differ(codes_of(u0, b0), codes_of(v0, b0)) ||
+                  differ(codes_of(u1, b1), codes_of(v1, b1));
+    }
+    if (__any(unsure)) {
+        if (!is_v) {
+            float *to = exact[wave][lane];
+            norm_and_turn_exact<D, T>(a, (const T *)a.k_weight, p, x0, x1, to);
+#pragma unroll
+            for (int e = 0; e < 8; e++) y0[e] = to[e], y1[e] = to[8 + e];
+            hi[p.c0] = largest(y0);
+            hi[p.c1] = largest(y1);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        b0 = byte_of(hi, p.c0), b1 = byte_of(hi, p.c1);
+        k0 = codes_of(y0, b0), k1 = codes_of(y1, b1);
+    }
     const tas_rows &codes = is_v ? a.f.v : a.f.k, &scales = is_v ? a.f.v_scale : a.f.k_scale;
     const int64_t hk = is_v ? h - a.heads - a.kv_heads : h - a.heads;
     char *to = (char *)codes.p + page * codes.stride[0] + hk * codes.stride[1] +
                at * codes.stride[2];
-    *(uint32_t *)(to + c0 * 4) = codes_of(y0, b0);
-    *(uint32_t *)(to + c1 * 4) = codes_of(y1, b1);
+    *(uint32_t *)(to + p.c0 * 4) = k0;
+    *(uint32_t *)(to + p.c1 * 4) = k1;
     uint8_t *st = (uint8_t *)scales.p + page * scales.stride[0] + hk * scales.stride[1] +
                   at * scales.stride[2];
-    if (c0 % 4 == 0) st[c0 / 4] = (uint8_t)b0;
-    if (c1 % 4 == 0) st[c1 / 4] = (uint8_t)b1;
+    if (p.c0 % 4 == 0) st[p.c0 / 4] = (uint8_t)b0;
+    if (p.c1 % 4 == 0) st[p.c1 / 4] = (uint8_t)b1;
 }
 
 template <typename T, int D>

@@ -220,6 +220,19 @@ __device__ __forceinline__ void thin_item4(const Attn4Args &a, const Item &it, c
     thin_end<T, D>(a, it, l, m, o, lds01, lds23, stat);
 }
 
+// The order of a stretch: N times a matrix product, vector work that does not wait for it, LDS
+// reads for the next stretch and, at every other, an LDS write.
+template <int N, int VECTOR, int READS, int WRITES>
+__device__ __forceinline__ void mix4() {
+    if constexpr (N > 0) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, VECTOR, 0);
+        if (READS) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+        if (WRITES && N % 2 == 0) __builtin_amdgcn_sched_group_barrier(0x200, WRITES, 0);
+        mix4<N - 1, VECTOR, READS, WRITES>();
+    }
+}
+
 // 128 rows against a run of keys, as the 16-bit kernel's wide item: 64 keys a step, 32 rows
 // to a wave, K and V of a step in LDS as 16-bit rows for all four waves, double buffered.
 // A wave fetches a run of 16 keys of K and of V a whole step before it converts them and
@@ -271,19 +284,24 @@ __device__ __forceinline__ void wide_item4(const Attn4Args &a, const Item &it, c
         page = tab[sub >> a.sub_shift];
         run = sub & sub_mask;
     };
-    Quarter<D> kq, vq;
-    uint32_t ks, vs;
-    auto fetch = [&]() {
+    uint32_t at_lo = 0, at_hi = 0;
+    auto place = [&]() {
         const uint64_t at = base_of + (uint64_t)(uint32_t)page * block_bytes +
                             (uint64_t)(uint32_t)run * run_bytes;
-        const uint32_t lo = (uint32_t)at, hi = (uint32_t)(at >> 32);
-        auto from = [&](int l) {
-            return (const char *)((uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, l) << 32 |
-                                  (uint32_t)__builtin_amdgcn_readlane(lo, l));
-        };
+        at_lo = (uint32_t)at, at_hi = (uint32_t)(at >> 32);
+    };
+    auto from = [&](int l) {
+        return (const char *)((uint64_t)(uint32_t)__builtin_amdgcn_readlane(at_hi, l) << 32 |
+                              (uint32_t)__builtin_amdgcn_readlane(at_lo, l));
+    };
+    Quarter<D> kq, vq;
+    uint32_t ks, vs;
+    auto fetch_k = [&]() {
         kq = load_quarter<D>(from(0) + klane);
-        vq = load_quarter<D>(from(1) + vlane);
         ks = *(const uint8_t *)(from(2) + kslane);
+    };
+    auto fetch_v = [&]() {
+        vq = load_quarter<D>(from(1) + vlane);
         vs = *(const uint8_t *)(from(3) + vslane);
     };
     // The rows see the keys from here on to the end differently (at most 128 + 63 keys;
@@ -389,6 +407,13 @@ __device__ __forceinline__ void wide_item4(const Attn4Args &a, const Item &it, c
             l += y;
             p[e >> 3][e & 7] = (T)y;
         }
+        // computed here, beside the scores, and not where they are used
+#pragma unroll
+        for (int n = 0; n < 2; n++) {
+            u4 x = __builtin_bit_cast(u4, p[n]);
+            asm volatile("" : "+v"(x));
+            p[n] = __builtin_bit_cast(V, x);
+        }
     };
     auto products = [&](const V (&p)[2]) {
 #pragma unroll
@@ -410,37 +435,54 @@ __device__ __forceinline__ void wide_item4(const Attn4Args &a, const Item &it, c
         const int next = base + kWideKeys;
         if (EDGE) poison(base);
         read_k(kl);
-        put_v(B ? v0_lds : v1_lds, next, EDGE);
-        put_k(B ? k0_lds : k1_lds);
-        fetch();
+        place();
         look_up(next + 2 * kWideKeys, next + 2 * kWideKeys + 32);
+        __builtin_amdgcn_sched_barrier(0);
         scores(sb);
         read_v(vl);
         weights(p, sa);
+        mix4<QS, 56 / QS, D / 8 / QS, 0>();
+        __builtin_amdgcn_sched_barrier(0);
         if (EDGE) hide(sb, base + 32);
+        put_k(B ? k0_lds : k1_lds);
+        fetch_k();
         products(p);
         read_k(kl + HB);
-        raise(largest(sb));
+        const float mb = largest(sb);
+        mix4<D / 16, 6, QS / (D / 16), 1>();
+        raise(mb);
         if (EDGE) poison(base + 32);
+        __builtin_amdgcn_sched_barrier(0);
         scores(sa);
         read_v(vl + HB);
         weights(p, sb);
+        mix4<QS, 56 / QS, D / 8 / QS, 0>();
+        __builtin_amdgcn_sched_barrier(0);
         if (EDGE) hide(sa, next);
+        put_v(B ? v0_lds : v1_lds, next, EDGE);
+        fetch_v();
         products(p);
-        raise(largest(sa));
+        const float ma = largest(sa);
+        mix4<D / 16, 6, 0, 1>();
+        raise(ma);
         __syncthreads();
     };
     if (it.k0 < it.k1) {
         int base = it.k0;
         look_up(base, base);
-        fetch();
-        look_up(base, base + 32);
+        place();
+        fetch_k();
+        fetch_v();
+        look_up(base + kWideKeys, base + 32);
         put_k(k1_lds);
         put_v(v0_lds, base, true);
-        fetch();
-        look_up(base + kWideKeys, base + kWideKeys + 32);
+        place();
+        fetch_k();
+        fetch_v();
+        look_up(base, base + kWideKeys + 32);
         put_k(k0_lds);
-        fetch();
+        place();
+        fetch_k();
         look_up(base + 2 * kWideKeys, base + 2 * kWideKeys + 32);
         __syncthreads();
         read_k(k1_lds);

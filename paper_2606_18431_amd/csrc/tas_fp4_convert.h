@@ -40,13 +40,14 @@ __device__ uint32_t largest(const float (&x)[8]) {
     for (int e = 0; e < 8; e++) m = max(m, magnitude(x[e]));
     return m;
 }
-// The scale's byte for a block's largest magnitude. 7 * 2^e is 1.75 * 2^(e + 2), so adding
+// The scale's byte for a block's largest magnitude, given as bits (of a number that is not
+// negative). 7 * 2^e is 1.75 * 2^(e + 2), so adding
 // a quarter to the mantissa carries into the exponent where it is reached.
 template <typename T>
 __device__ uint32_t scale_byte(uint32_t most) {
     constexpr bool F16 = __is_same(T, _Float16);
     constexpr int lo = 127 + (F16 ? -23 : -125), hi = 127 + (F16 ? 13 : 125);
-    if (most >= 0x7f800000u) return 255;
+    if (most >= 0x7f800000u) return 255;  // (a NaN's sign too)
     return (uint32_t)min(max((int)((most + 0x200000u) >> 23) - 2, lo), hi);
 }
 // Eight elements' codes. The conversion rounds to nearest, halves to the even code, and

@@ -91,7 +91,7 @@ def _call(index, stream, call, *args):
 def _keep(index, stream, *tensors):
     """The memory of tensors used on another stream than the current one is not given away
     before the work there is done."""
-    if stream is not None and stream.cuda_stream != torch._C._cuda_getCurrentRawStream(index):
+    if stream.cuda_stream != torch._C._cuda_getCurrentRawStream(index):
         for t in tensors:
             t.record_stream(stream)
 
@@ -115,19 +115,24 @@ def _gpu(t, what):
     return t.get_device()
 
 
-def _rows(t, what):
-    """(sizes of three leading dimensions, row's length, address, strides in bytes)."""
-    d = t.dim()
+def _rows(t, size, what):
+    """(sizes of three leading dimensions, row's length, address and strides in bytes) of a
+    tensor of elements of ``size`` bytes."""
+    shape, stride = t.shape, t.stride()
+    d = len(shape)
     if not 1 <= d <= 4:
         raise ValueError(f"{what} has {d} dimensions: one to four")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise ValueError(f"{what}: the elements of a row have to be adjacent, strides "
-                         f"{t.stride()}")
-    size = t.element_size()
-    n = (1,) * (4 - d) + tuple(t.shape[:-1])
-    # a dimension of one: its stride says nothing
-    s = (0,) * (4 - d) + tuple(size * x if m > 1 else 0 for m, x in zip(t.shape, t.stride()[:-1]))
-    return n, t.shape[-1], (t.data_ptr(), *s)
+    if stride[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{what}: the elements of a row have to be adjacent, strides {stride}")
+    if d < 4:
+        shape, stride = (1,) * (4 - d) + tuple(shape), (0,) * (4 - d) + stride
+    a, b, c, cols = shape
+    return (a, b, c), cols, (t.data_ptr(), size * stride[0], size * stride[1], size * stride[2])
+
+
+def _adjacent(t, n, row):
+    """Address and strides of a new tensor of n rows of so many bytes."""
+    return t.data_ptr(), row * n[1] * n[2], row * n[2], row
 
 
 def pack(x, *, stream=None):
@@ -139,15 +144,17 @@ def pack(x, *, stream=None):
     if x.requires_grad and torch.is_grad_enabled():
         raise NotImplementedError("rounding to four bits has no gradient: detach x")
     index = _gpu(x, "x")
-    n, cols, at = _rows(x, "x")
+    n, cols, at = _rows(x, 2, "x")
     if cols % BLOCK or not cols:
         raise ValueError(f"rows of {cols} elements: a multiple of {BLOCK}")
-    codes = _empty((*x.shape[:-1], cols // 2), torch.uint8, x.device, stream)
-    scales = _empty((*x.shape[:-1], cols // BLOCK), torch.uint8, x.device, stream)
-    args = _TENSOR.pack(dtype, 0, *n, cols, *at, *_rows(codes, "codes")[2],
-                        *_rows(scales, "scales")[2])
+    lead = x.shape[:-1]
+    codes = _empty((*lead, cols // 2), torch.uint8, x.device, stream)
+    scales = _empty((*lead, cols // BLOCK), torch.uint8, x.device, stream)
+    args = _TENSOR.pack(dtype, 0, *n, cols, *at, *_adjacent(codes, n, cols // 2),
+                        *_adjacent(scales, n, cols // BLOCK))
     _call(index, stream, lib().tas_fp4_pack, args)
-    _keep(index, stream, x, codes, scales)
+    if stream is not None:
+        _keep(index, stream, x, codes, scales)
     return codes, scales
 
 
@@ -158,18 +165,19 @@ def values(codes, scales, dtype, *, stream=None):
     if code is None:
         raise ValueError(f"{dtype}: float16 or bfloat16")
     index = _gpu(codes, "codes")
-    n, half, at = _rows(codes, "codes")
-    _, _, scales_at = _rows(scales, "scales")
-    shape = (*codes.shape[:-1], half // 16)
-    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or half % 16 or not half \
-            or scales.shape != shape or scales.get_device() != index:
+    n, half, at = _rows(codes, 1, "codes")
+    scales_n, blocks, scales_at = _rows(scales, 1, "scales")
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or not half \
+            or half != 16 * blocks or scales_n != n or codes.dim() != scales.dim() \
+            or scales.get_device() != index:
         raise ValueError(f"codes are {codes.dtype} {tuple(codes.shape)} on {codes.device}, scales "
                          f"{scales.dtype} {tuple(scales.shape)} on {scales.device}: uint8, 16 "
                          "bytes of codes to one of scales")
     x = _empty((*codes.shape[:-1], 2 * half), dtype, codes.device, stream)
-    args = _TENSOR.pack(code, 0, *n, 2 * half, *_rows(x, "x")[2], *at, *scales_at)
+    args = _TENSOR.pack(code, 0, *n, 2 * half, *_adjacent(x, n, 4 * half), *at, *scales_at)
     _call(index, stream, lib().tas_fp4_values, args)
-    _keep(index, stream, codes, scales, x)
+    if stream is not None:
+        _keep(index, stream, codes, scales, x)
     return x
 
 
@@ -231,7 +239,8 @@ class Weights:
                   scales.stride(0) if many else 0, self._at)
             self._laid = torch.cuda.Event()
             self._laid.record()
-        _keep(index, stream, codes, scales)
+        if stream is not None:
+            _keep(index, stream, codes, scales)
         self._home = on.cuda_stream
         self._there = False  # laid out, as far as the host knows
         self._streams = {self._home}  # that the memory is recorded on
@@ -281,5 +290,6 @@ def linear(x, weights, *, out=None, stream=None):
                         x.stride(0) if many else weights.cols, weights._at, out.data_ptr(),
                         out.stride(0) if many else rows)
     _call(index, stream, lib().tas_fp4_linear, args)
-    _keep(index, stream, x, out)
+    if stream is not None:
+        _keep(index, stream, x, out)
     return _no_backward(out, x)

@@ -267,6 +267,37 @@ def test_append_without_norm_and_rotation_is_pack(torch, name):
             t += 1
 
 
+@pytest.mark.parametrize("name", ["bf16", "f16"])
+@pytest.mark.parametrize("scale", [1.0, 2.0 ** -10, 2.0 ** 14, 2.0 ** -70, 2.0 ** 62])
+def test_append_keys_at_borders(torch, name, scale):
+    """Two million keys, some of which lie within a rounding error of 32 bits of the border
+    of two codes or scales: each has the code of the formula in 64 bits. Also where squares
+    leave the range of 32 bits."""
+    if name == "f16" and not 2.0 ** -12 < scale < 2.0 ** 12:
+        pytest.skip("beyond the type")
+    dt, T = dtype_of(torch, name), 2000
+    b = Batch(24, [T], [T], 8, 8, 128)
+    cache = fp4.Cache.zeros(b.n_blocks, 8, 16, 128)
+    g = torch.Generator().manual_seed(12)
+    qkv = (scale * torch.randn((T, 24, 128), generator=g)).to(dt)
+    qkv[::3, 8:16] = qkv[::3, 8:16].sign() * scale                   # norms that are powers of two
+    qkv[1::3, 8:16, 32:64] *= 2.0 ** -6
+    a = torch.rand((T, 64), generator=g) * 6.3
+    a[::2] = torch.randint(0, 9, (T // 2, 64), generator=g) * (math.pi / 4)
+    cos, sin = a.cos(), a.sin()
+    qw, kw = (torch.randint(1, 9, (2, 128), generator=g) / 4).to(dt)
+    want, _ = append_reference(torch, b, qkv, cos, sin, qw, kw, 0.0, False)
+    b.step().append_fp4(qkv.cuda(), cache, cos.cuda(), sin.cuda(), q_weight=qw.cuda(),
+                        k_weight=kw.cuda(), eps=0.0)
+    k, _ = cache.values(dt)
+    page = torch.from_numpy(b.blocks[0]).long()[torch.arange(T) // 16]
+    got = k.double().cpu()[page, :, torch.arange(T) % 16]
+    keys, close = rounded(torch, want[:, 8:16], name)
+    # 64 bits: some 150 roundings of 2^-53, on terms a few times the result
+    assert bool(((got == keys) | (close < 2.0 ** -40)).all())
+    assert bool((close < 2.0 ** -22).any())
+
+
 # ------------------------------------------------------------------ attention
 
 
