@@ -96,11 +96,12 @@ def _keep(index, stream, *tensors):
             t.record_stream(stream)
 
 
-def _empty(shape, dtype, device, stream):
+def _empty(like, shape, dtype, stream):
+    """A new tensor on the device of another, for the stream's use."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _no_backward(out, x):
@@ -148,8 +149,8 @@ def pack(x, *, stream=None):
     if cols % BLOCK or not cols:
         raise ValueError(f"rows of {cols} elements: a multiple of {BLOCK}")
     lead = x.shape[:-1]
-    codes = _empty((*lead, cols // 2), torch.uint8, x.device, stream)
-    scales = _empty((*lead, cols // BLOCK), torch.uint8, x.device, stream)
+    codes = _empty(x, (*lead, cols // 2), torch.uint8, stream)
+    scales = _empty(x, (*lead, cols // BLOCK), torch.uint8, stream)
     args = _TENSOR.pack(dtype, 0, *n, cols, *at, *_adjacent(codes, n, cols // 2),
                         *_adjacent(scales, n, cols // BLOCK))
     _call(index, stream, lib().tas_fp4_pack, args)
@@ -173,7 +174,7 @@ def values(codes, scales, dtype, *, stream=None):
         raise ValueError(f"codes are {codes.dtype} {tuple(codes.shape)} on {codes.device}, scales "
                          f"{scales.dtype} {tuple(scales.shape)} on {scales.device}: uint8, 16 "
                          "bytes of codes to one of scales")
-    x = _empty((*codes.shape[:-1], 2 * half), dtype, codes.device, stream)
+    x = _empty(codes, (*codes.shape[:-1], 2 * half), dtype, stream)
     args = _TENSOR.pack(code, 0, *n, 2 * half, *_adjacent(x, n, 4 * half), *at, *scales_at)
     _call(index, stream, lib().tas_fp4_values, args)
     if stream is not None:
@@ -267,28 +268,30 @@ def linear(x, weights, *, out=None, stream=None):
     """x W^T of float16 or bfloat16 tokens [tokens, cols] (adjacent rows, any stride that is
     a multiple of 8) and ``Weights`` of [rows, cols]: [tokens, rows] of x's type. The
     products are summed in 32 bits, in an order that depends on the sizes alone."""
-    dtype = DTYPES.get(x.dtype)
-    index = weights.index
-    if dtype is None or x.dim() != 2 or x.get_device() != index or x.shape[1] != weights.cols \
-            or x.stride(1) != 1:
-        raise ValueError(f"x is {x.dtype} {tuple(x.shape)}, strides {x.stride()}, on {x.device}, "
-                         f"expected float16 or bfloat16 [tokens, {weights.cols}], rows adjacent, "
-                         f"on {weights.device}")
-    tokens, rows = x.shape[0], weights.rows
+    dtype, index, rows, cols = DTYPES.get(x.dtype), weights.index, weights.rows, weights.cols
+    shape, stride = x.shape, x.stride()
+    if dtype is None or len(shape) != 2 or x.get_device() != index or shape[1] != cols \
+            or stride[1] != 1:
+        raise ValueError(f"x is {x.dtype} {tuple(shape)}, strides {stride}, on {x.device}, "
+                         f"expected float16 or bfloat16 [tokens, {cols}], rows adjacent, on "
+                         f"{weights.device}")
+    tokens = shape[0]
     if out is None:
-        out = _empty((tokens, rows), x.dtype, x.device, stream)
+        out = _empty(x, (tokens, rows), x.dtype, stream)
+        out_stride = rows
     elif out.dtype != x.dtype or out.get_device() != index or out.shape != (tokens, rows) \
             or (out.stride(1) != 1 and rows > 1):
         raise ValueError(f"out is {out.dtype} {tuple(out.shape)}, strides {out.stride()}, on "
                          f"{out.device}, expected {x.dtype} {(tokens, rows)}, rows adjacent, on "
                          f"{weights.device}")
+    else:  # one token: its stride says nothing
+        out_stride = out.stride(0) if tokens > 1 else rows
     raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
     if not weights._there or raw not in weights._streams:
         weights._admit(raw, stream)
-    many = tokens > 1  # one token: its stride says nothing
-    args = _LINEAR.pack(dtype, 0, tokens, rows, weights.cols, x.data_ptr(),
-                        x.stride(0) if many else weights.cols, weights._at, out.data_ptr(),
-                        out.stride(0) if many else rows)
+    args = _LINEAR.pack(dtype, 0, tokens, rows, cols, x.data_ptr(),
+                        stride[0] if tokens > 1 else cols, weights._at, out.data_ptr(),
+                        out_stride)
     _call(index, stream, lib().tas_fp4_linear, args)
     if stream is not None:
         _keep(index, stream, x, out)

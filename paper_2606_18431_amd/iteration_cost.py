@@ -7,15 +7,20 @@ GPU as a model's layers do (``step.Step``: norm, rotate and append the new token
 then attend over the pages) and fits the three coefficients to the times:
 
     python -m paper_2606_18431_amd.iteration_cost --cfg 4 --layers 32
+    python -m paper_2606_18431_amd.iteration_cost --cfg 4 --layers 32 --cache-bits 4 --hidden 4096
 
 ``--prefix N`` puts N shared tokens (a system prompt, computed once) before every
 request's own context. In an iteration's context they count once, as they are read
 (each new token's work on them is in tok). The times hold the layers' two calls, made
-from the host one layer after another. Not in them: the weights' part of an iteration
-(its matrix products; add it to base and tok from the model's own measurements), and
-the plan of the batch, which the host makes once an iteration and which is printed by
-itself (an engine that plans while the GPU works does not wait for it; one that plans
-in between adds it to base).
+from the host one layer after another. ``--cache-bits 4`` holds the caches in four bits
+(``fp4.Cache``); their blocks take 3.8 times less memory. ``--hidden N`` adds the products
+with a layer's weights, held in four bits (``fp4.Weights``): of a state of N to the heads,
+from the heads back, and to ``--ffn`` (4 N) and back; the norms and the activation between
+them are not in the times. Without it the weights' part of an iteration is not in them
+(add it to base and tok from the model's own measurements). Never in them is the plan of
+the batch, which the host makes once an iteration and which is printed by itself (an engine
+that plans while the GPU works does not wait for it; one that plans in between adds it to
+base).
 """
 from __future__ import annotations
 
@@ -87,12 +92,14 @@ def form_iteration(w: W.Workload, trace: int, first: int, rng, prefix_blocks: in
 
 class Layers:
     """The layers' caches, one of each layer's own as in a model (as many as the memory
-    holds, in turn), and the inputs of their attention; random values."""
+    holds, in turn), and the inputs of their attention; random values. ``hidden`` and
+    ``ffn``: with the layers' weights, in four bits, each layer's own as well."""
 
-    def __init__(self, e: W.Engine, layers, heads, kv_heads, head_dim, dtype, device, positions):
+    def __init__(self, e: W.Engine, layers, heads, kv_heads, head_dim, dtype, device, positions,
+                 cache_bits=16, hidden=0, ffn=0):
         import torch
 
-        self.torch = torch
+        self.torch, self.cache_bits = torch, cache_bits
         shape = (e.kv_blocks, kv_heads, e.block_tokens, head_dim)
         g = torch.Generator(device=device)
         g.manual_seed(0)
@@ -100,11 +107,40 @@ class Layers:
         def random(*shape):
             return torch.randn(shape, generator=g, device=device, dtype=dtype)
 
-        self.layers, caches = layers, layers
+        def random_fp4(*shape, scale=0):
+            """Codes, and scales of 2^scale."""
+            *lead, n = shape
+            codes = torch.randint(0, 256, (*lead, n // 2), generator=g, device=device,
+                                  dtype=torch.uint8)
+            return codes, torch.full((*lead, n // 32), 127 + scale, device=device,
+                                     dtype=torch.uint8)
+
+        def cache():
+            if cache_bits == 16:
+                return random(*shape), random(*shape)
+            from . import fp4
+
+            (k, k_scale), (v, v_scale) = random_fp4(*shape), random_fp4(*shape)
+            return fp4.Cache(k, v, k_scale, v_scale)
+
+        self.layers = layers
+        self.weights = []
+        if hidden:
+            from . import fp4
+
+            ffn = ffn or 4 * hidden
+            rows = (heads + 2 * kv_heads) * head_dim
+            sizes = ((rows, hidden), (hidden, heads * head_dim), (ffn, hidden), (hidden, ffn))
+            # values of some 2 * 2^scale: about 1 / sqrt(cols), so that the states stay near 1
+            self.weights = [[fp4.Weights(*random_fp4(n, k, scale=-round(math.log2(3 * k ** 0.5))))
+                             for n, k in sizes] for _ in range(layers)]
+            self.x = random(e.max_tokens, hidden)
+        caches = layers
         if torch.device(device).type == "cuda":
-            layer_bytes = 2 * random(1).element_size() * math.prod(shape)
+            per_value = 2.0 if cache_bits == 16 else 0.5 + 1 / 32
+            layer_bytes = int(2 * per_value * math.prod(shape))
             caches = min(layers, max(1, torch.cuda.mem_get_info(device)[0] * 3 // 4 // layer_bytes))
-        self.caches = [(random(*shape), random(*shape)) for _ in range(caches)]
+        self.caches = [cache() for _ in range(caches)]
         self.qkv = random(e.max_tokens, heads + 2 * kv_heads, head_dim)
         self.weight = torch.ones(head_dim, device=device, dtype=dtype)
         freq = 1e4 ** (-torch.arange(0, head_dim, 2, device=device, dtype=torch.float64) / head_dim)
@@ -112,12 +148,26 @@ class Layers:
         self.cos, self.sin = angle.cos().float(), angle.sin().float()
 
     def run(self, step):
-        """The attention of all layers, one after another, for the step's batch."""
+        """All layers, one after another, for the step's batch."""
+        qkv = self.qkv[:step.tokens]
         for i in range(self.layers):
-            k_cache, v_cache = self.caches[i % len(self.caches)]
-            q = step.append(self.qkv[:step.tokens], k_cache, v_cache, self.cos, self.sin,
-                            q_weight=self.weight, k_weight=self.weight)
-            step.attention(q, k_cache, v_cache)
+            cache = self.caches[i % len(self.caches)]
+            if self.weights:
+                from .fp4 import linear
+
+                of_heads, from_heads, up, down = self.weights[i]
+                qkv = linear(self.x[:step.tokens], of_heads).view(qkv.shape)
+            turn = (self.cos, self.sin)
+            norm = dict(q_weight=self.weight, k_weight=self.weight)
+            if self.cache_bits == 16:
+                k_cache, v_cache = cache
+                q = step.append(qkv, k_cache, v_cache, *turn, **norm)
+                o = step.attention(q, k_cache, v_cache)
+            else:
+                q = step.append_fp4(qkv, cache, *turn, **norm)
+                o = step.attention_fp4(q, cache)
+            if self.weights:
+                linear(linear(linear(o.flatten(1), from_heads), up), down)
 
     def time_us(self, step, repeats: int = 3) -> float:
         """Microseconds of the layers, the median of some passes."""
@@ -185,7 +235,8 @@ def whole_terms(tokens, context, us):
 
 
 def measure(w: W.Workload, *, iterations=24, layers=32, heads=32, kv_heads=8, head_dim=128,
-            dtype="bf16", prefix=0, seed=0, device="cuda", say=lambda line: None, plans=None):
+            dtype="bf16", prefix=0, seed=0, device="cuda", say=lambda line: None, plans=None,
+            cache_bits=16, hidden=0, ffn=0):
     """Times of ``iterations`` iterations of the workload; a list of (requests, tokens,
     context, microseconds), the prefix once in the context. ``plans``: a list that
     receives the microseconds that the host took for each iteration's plan."""
@@ -198,7 +249,8 @@ def measure(w: W.Workload, *, iterations=24, layers=32, heads=32, kv_heads=8, he
     prefix_pages = -(-prefix // e.block_tokens)
     positions = prefix + int((w.prompt.astype(np.int64) + w.decode).max())
     model = Layers(e, layers, heads, kv_heads, head_dim,
-                   {"bf16": torch.bfloat16, "f16": torch.float16}[dtype], device, positions)
+                   {"bf16": torch.bfloat16, "f16": torch.float16}[dtype], device, positions,
+                   cache_bits, hidden, ffn)
     rows = []
     for i in range(iterations):
         it = form_iteration(w, int(rng.integers(0, w.n_traces)), int(rng.integers(0, w.n_req)), rng,
@@ -229,6 +281,10 @@ def main(argv=None):
     p.add_argument("--kv-heads", type=int, default=8)
     p.add_argument("--head-dim", type=int, default=128)
     p.add_argument("--dtype", choices=["bf16", "f16"], default="bf16")
+    p.add_argument("--cache-bits", type=int, choices=[16, 4], default=16)
+    p.add_argument("--hidden", type=int, default=0,
+                   help="with the products with a layer's weights in four bits, of a state of so many")
+    p.add_argument("--ffn", type=int, default=0, help="of the layer's second half (4 * hidden)")
     p.add_argument("--prefix", type=int, default=0, help="shared tokens before every request")
     p.add_argument("--seed", type=int, default=0)
     a = p.parse_args(argv)
@@ -236,11 +292,13 @@ def main(argv=None):
     plans = []
     rows = measure(w, plans=plans, iterations=a.iterations, layers=a.layers, heads=a.heads,
                    kv_heads=a.kv_heads, head_dim=a.head_dim, dtype=a.dtype, prefix=a.prefix,
-                   seed=a.seed, say=lambda line: print(line, flush=True))
+                   seed=a.seed, cache_bits=a.cache_bits, hidden=a.hidden, ffn=a.ffn,
+                   say=lambda line: print(line, flush=True))
     _, tokens, context, us = zip(*rows)
     base, tok, div, r2 = fit(tokens, context, us)
     print(f"{w.name}, {a.layers} layers of {a.heads}/{a.kv_heads} heads of {a.head_dim}, "
-          f"{a.dtype}: attention of an iteration = {base:.0f} + {tok:.4f} * tokens + context / "
+          f"{a.dtype}, cache of {a.cache_bits} bits: {'attention and products' if a.hidden else 'attention'}"
+          f" of an iteration = {base:.0f} + {tok:.4f} * tokens + context / "
           f"{div:.1f} us ({100 * r2:.1f}% of the variance)")
     whole = whole_terms(tokens, context, us)
     print("in whole numbers, for Engine(iter_base_us, iter_tok_us, iter_ctx_div): %d, %d, %d" % whole)

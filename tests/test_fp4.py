@@ -215,3 +215,31 @@ def test_refused_weights_and_products():
                dict(weights=AT + 128), dict(y=None), dict(y=AT + (3 << 20) + 1),
                dict(y_stride=39), dict(y_stride=1 << 31), dict(y=AT + (1 << 20) + 3000)):
         assert linear(**{**apart, **kw}) == tas.TAS_EINVAL, kw
+
+
+def test_every_layer_has_a_cache_of_its_own():
+    """As with caches of 16 bits: what a layer reads was not read by the one before it."""
+    torch = pytest.importorskip("torch")
+    from paper_2606_18431_amd import iteration_cost as C
+    from paper_2606_18431_amd import workloads as W
+
+    class Step:
+        tokens = 3
+        calls = []
+
+        def append_fp4(self, qkv, cache, *args, **kw):
+            assert qkv.shape[0] == self.tokens and isinstance(cache, fp4.Cache)
+            self.calls.append(("append", *(t.data_ptr() for t in cache)))
+            return "queries"
+
+        def attention_fp4(self, q, cache):
+            assert q == "queries"
+            self.calls.append(("attention", *(t.data_ptr() for t in cache)))
+
+    m = C.Layers(W.Engine(kv_blocks=4, max_tokens=64), 5, heads=2, kv_heads=1, head_dim=64,
+                 dtype=torch.float16, device="cpu", positions=10, cache_bits=4)
+    s = Step()
+    m.run(s)
+    assert [c[0] for c in s.calls] == ["append", "attention"] * 5
+    assert all(s.calls[i][1:] == s.calls[i + 1][1:] for i in range(0, 10, 2))
+    assert len({p for c in s.calls for p in c[1:]}) == 20

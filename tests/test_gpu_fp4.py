@@ -870,3 +870,39 @@ def test_a_backward_pass_is_refused(torch):
         fp4.pack(grad(x))
     with torch.no_grad():
         fp4.pack(grad(x))
+
+
+# ------------------------------------------------------------------ the command
+
+
+@pytest.mark.parametrize("prefix", [0, 100])
+def test_measure_in_four_bits(torch, prefix):
+    """Iterations over caches in four bits, with the products of the weights."""
+    from paper_2606_18431_amd import iteration_cost as C
+    from paper_2606_18431_amd import workloads as W
+
+    w = W.make(1, n_traces=1, n_settings=4, n_req=200)
+    rows = C.measure(w, iterations=4, layers=2, heads=8, kv_heads=2, head_dim=64, dtype="f16",
+                     prefix=prefix, cache_bits=4, hidden=256)
+    assert len(rows) == 4
+    for n, tokens, context, us in rows:
+        assert n >= 1 and tokens >= n and context >= tokens and 0 < us < 1e6
+
+
+def test_layers_run_the_operators_in_order(torch):
+    """A layer's run: heads' product, append, attention, and three products from its result."""
+    from paper_2606_18431_amd import iteration_cost as C
+    from paper_2606_18431_amd import workloads as W
+
+    e = W.Engine(kv_blocks=16, max_tokens=64)
+    m = C.Layers(e, 1, heads=4, kv_heads=2, head_dim=64, dtype=torch.bfloat16, device="cuda",
+                 positions=100, cache_bits=4, hidden=128, ffn=160)
+    assert [(w.rows, w.cols) for w in m.weights[0]] == [(512, 128), (128, 256), (160, 128), (128, 160)]
+    s = step.Step([1, 3], [40, 3], [[3, 1, 4], [0, 0, 0]], heads=4, kv_heads=2, head_dim=64,
+                  block_tokens=e.block_tokens, n_blocks=16)
+    qkv = fp4.linear(m.x[:4], m.weights[0][0]).view(4, 8, 64)
+    cache = fp4.Cache(*(t.clone() for t in m.caches[0]))
+    q = s.append_fp4(qkv, cache, m.cos, m.sin, q_weight=m.weight, k_weight=m.weight)
+    m.run(s)
+    assert all(torch.equal(t, u) for t, u in zip(cache, m.caches[0]))
+    assert torch.isfinite(s.attention_fp4(q, cache)).all()
