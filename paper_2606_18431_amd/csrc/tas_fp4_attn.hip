@@ -94,8 +94,12 @@ __device__ __forceinline__ void thin_item4(const Attn4Args &a, const Item &it, c
     // a wave's 32 rows of V, and in the end its sums (16 rows of floats, as many bytes)
     auto mine = [&](int w) { return (w < 2 ? lds01 : lds23) + (w & 1) * VB; };
     char *vl = mine(wave);
-    // (another pair of chunks is an exclusive or, a row 16 on an addition)
+    // Another pair of chunks is an exclusive or (of the bits below 8; the eighth is always 0
+    // here, so that 8 is an addition), a row 16 on an addition.
     const uint32_t v_at = v_place<D>(4 * g + (col >> 2), (col >> 1) & 1) * 16 + (col & 1) * 8;
+    char *v_to[QS];
+#pragma unroll
+    for (int i = 0; i < QS; i++) v_to[i] = vl + v_place<D>(vrow, vq * QS + i) * 16;
 
     f4 o[D / 16];
 #pragma unroll
@@ -140,38 +144,31 @@ __device__ __forceinline__ void thin_item4(const Attn4Args &a, const Item &it, c
             for (int i = 0; i < QS; i++)
                 sc[n] = mfma16(values_of<T>(k[n].w[i], scale_of(ks[n])), q[i], sc[n]);
         }
-        u4 x[2][QS];
-#pragma unroll
-        for (int n = 0; n < 2; n++)
-#pragma unroll
-            for (int i = 0; i < QS; i++)
-                x[n][i] = __builtin_bit_cast(u4, values_of<T>(v[n].w[i], scale_of(vs[n])));
-        if (base + kThinKeys > it.k1)  // slots past the keys hold anything: weight 0 times it
-#pragma unroll
-            for (int n = 0; n < 2; n++)
-                if (base + n * 16 + vrow >= it.k1)
-#pragma unroll
-                    for (int i = 0; i < QS; i++) x[n][i] = u4{0, 0, 0, 0};
         uint32_t marked = 0;  // of the 32 keys
-        if (base + kThinKeys > full && full < it.k1) {
-#pragma unroll
-            for (int n = 0; n < 2; n++)
-#pragma unroll
-                for (int i = 0; i < QS; i++) {
-                    const uint64_t lanes = __ballot(any_not_finite<T>(x[n][i]));
-                    if (lanes) {
-                        x[n][i] = zero_not_finite<T>(x[n][i]);
-                        for (int y = 0; y < 16; y++)
-                            if (lanes >> (y * 4) & 15) marked |= 1u << (n * 16 + y);
-                    }
-                }
-        }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int n = 0; n < 2; n++)
 #pragma unroll
             for (int i = 0; i < QS; i++)
-                *(u4 *)(vl + v_place<D>(n * 16 + vrow, vq * QS + i) * 16) = x[n][i];
+                *(u4 *)(v_to[i] + n * 32 * D) =
+                    __builtin_bit_cast(u4, values_of<T>(v[n].w[i], scale_of(vs[n])));
+        if (base + kThinKeys > full) {  // some of them are changed there (what a lane wrote)
+#pragma unroll 1
+            for (int w = 0; w < 2 * QS; w++) {
+                const int n = w / QS;
+                u4 *at = (u4 *)(vl + v_place<D>(n * 16 + vrow, vq * QS + w % QS) * 16);
+                u4 x = *at;
+                // slots past the keys hold anything: weight 0 times it
+                if (base + n * 16 + vrow >= it.k1) x = u4{0, 0, 0, 0};
+                const uint64_t lanes = __ballot(any_not_finite<T>(x));
+                if (lanes && full < it.k1) {
+                    x = zero_not_finite<T>(x);
+                    for (int y = 0; y < 16; y++)
+                        if (lanes >> (y * 4) & 15) marked |= 1u << (n * 16 + y);
+                }
+                *at = x;
+            }
+        }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (base + stride < it.k1) {
             load(base + stride);
@@ -211,7 +208,8 @@ __device__ __forceinline__ void thin_item4(const Attn4Args &a, const Item &it, c
 #pragma unroll
         for (int i = 0; i < D / 16; i++) {
             // lane c of group g: column d = 16 i + c of the rows 4 g .. 4 g + 3 and 16 on
-            const char *at = vl + (v_at ^ (turned<D>(2 * i) * 16));
+            const int c = turned<D>(2 * i);
+            const char *at = vl + (v_at ^ ((c & 7) * 16)) + (c & 8) * 16;
             const s4 lo = read_tr(at), hi = read_tr(at + 32 * D);
             const s8 t = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
             o[i] = mfma16(__builtin_bit_cast(V, t), p, o[i]);
@@ -526,7 +524,7 @@ __device__ __forceinline__ void wide_item4(const Attn4Args &a, const Item &it, c
 
 // One item a workgroup.
 template <typename T, int D, bool WIDE>
-__global__ __launch_bounds__(256, WIDE ? 2 : 3) void attn4_kernel(Attn4Args a) {
+__global__ __launch_bounds__(256, WIDE ? 2 : 4) void attn4_kernel(Attn4Args a) {
     constexpr int TB = kWideKeys * D * 2;
     // four objects, so that the compiler sees which loads a read has to wait for
     __shared__ __attribute__((aligned(16))) char k0_lds[TB], k1_lds[TB];
