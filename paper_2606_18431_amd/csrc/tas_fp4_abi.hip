@@ -83,7 +83,7 @@ bool valid_tensor(const tas_tensor_fp4 *from, tas_tensor_fp4 *a, int64_t &rows) 
     if (!valid_dtype(a->dtype) || a->reserved) return false;
     if (a->cols < 32 || a->cols % 32) return false;
     rows = 1;
-    int64_t most = (int64_t(1) << 35) / a->cols;
+    int64_t most = kMaxGroups * 256 * 8 / a->cols;  // (a thread has eight elements)
     for (int64_t n : a->n) {
         if (n < 0 || n > most) return false;
         rows *= n;

@@ -164,7 +164,8 @@ def test_refused_tensors():
     assert L.tas_fp4_pack(tensor(), None) == tas.TAS_EINVAL
     assert L.tas_fp4_pack(tensor(n=(2, 0, 5)), None) == 0
     both = [dict(dtype=2), dict(reserved=1), dict(cols=48), dict(cols=0), dict(cols=-32),
-            dict(n=(-1, 3, 5)), dict(n=(1 << 20, 1 << 20, 1)), dict(n=(1 << 62, 1 << 62, 4)),
+            dict(n=(-1, 3, 5)), dict(n=(1 << 20, 1 << 20, 1)), dict(n=(1 << 62, 1 << 62, 4)), dict(n=(1 << 24, 1 << 5, 1)),
+            dict(n=(1, 1 << 29, 1)),
             dict(cols=1 << 36), dict(x=rows(AT + 8, 1920, 640, 128)),
             dict(x=rows(AT, 1920, 640, 136)), dict(x=rows(AT, -1920, 640, 128)),
             dict(x=rows(None, 1920, 640, 128)), dict(codes=rows(AT + 2, 480, 160, 32)),
