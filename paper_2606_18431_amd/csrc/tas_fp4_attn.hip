@@ -37,24 +37,24 @@ __device__ int block_of(int i) {
     return D == 128 ? i : i >> 1;
 }
 
-// Places in LDS (in 16-byte chunks of eight elements) of chunk c of row y. Lanes write
-// quarters of rows, chunks D / 32 apart; eight lanes (two rows) write to different banks
-// because a chunk's low bits are turned by its quarter, and the rows of a pair differ in
-// the lowest bit.
+// Places in LDS (in 16-byte chunks of eight elements) of chunk c of row y. The banks take 16
+// chunks at once: of a write, 16 lanes, which have the quarters of four rows (chunks D / 32
+// apart: their low bits are turned by the quarter); of a transposing read, 32 lanes with two
+// chunks of eight rows (thin items) or four of four; of a read of K, 16 rows' chunk. Each
+// time they lie in different places of 16 (at head size 64 a pair of rows has 16).
 template <int D>
 __device__ constexpr int turned(int c) {
     return D == 128 ? c ^ (c >> 2) : c;
 }
-// V: read by the transposing read, which takes pairs of chunks of four rows: those lie in
-// different quarters of the banks.
 template <int D>
 __device__ int v_place(int y, int c) {
-    return y * (D / 8) + (turned<D>(c) ^ ((y & 3) << 1) ^ (y & 1));
+    if (D == 128) return y * 16 + (turned<D>(c) ^ ((y & 3) << 2 | (y >> 1 & 2)));
+    return y * 8 + (c ^ ((y >> 1 & 1) * 5) ^ (y >> 1 & 2));
 }
-// K: read by columns of chunks.
 template <int D>
 __device__ int k_place(int y, int c) {
-    return y * (D / 8) + (turned<D>(c) ^ (y & (D / 8 - 1)));
+    if (D == 128) return y * 16 + (turned<D>(c) ^ (y & 15));
+    return y * 8 + (c ^ (y >> 1 & 7));
 }
 
 // Up to 16 rows against a run of keys: each of the four waves takes every fourth 32 keys.
@@ -94,8 +94,7 @@ __device__ __forceinline__ void thin_item4(const Attn4Args &a, const Item &it, c
     // a wave's 32 rows of V, and in the end its sums (16 rows of floats, as many bytes)
     auto mine = [&](int w) { return (w < 2 ? lds01 : lds23) + (w & 1) * VB; };
     char *vl = mine(wave);
-    // Another pair of chunks is an exclusive or (of the bits below 8; the eighth is always 0
-    // here, so that 8 is an addition), a row 16 on an addition.
+    // (another pair of chunks is an exclusive or, a row 16 on an addition)
     const uint32_t v_at = v_place<D>(4 * g + (col >> 2), (col >> 1) & 1) * 16 + (col & 1) * 8;
     char *v_to[QS];
 #pragma unroll
@@ -208,8 +207,7 @@ __device__ __forceinline__ void thin_item4(const Attn4Args &a, const Item &it, c
 #pragma unroll
         for (int i = 0; i < D / 16; i++) {
             // lane c of group g: column d = 16 i + c of the rows 4 g .. 4 g + 3 and 16 on
-            const int c = turned<D>(2 * i);
-            const char *at = vl + (v_at ^ ((c & 7) * 16)) + (c & 8) * 16;
+            const char *at = vl + (v_at ^ (turned<D>(2 * i) * 16));
             const s4 lo = read_tr(at), hi = read_tr(at + 32 * D);
             const s8 t = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
             o[i] = mfma16(__builtin_bit_cast(V, t), p, o[i]);
