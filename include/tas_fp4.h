@@ -109,6 +109,18 @@ int tas_fp4_pack(const tas_tensor_fp4 *a, void *stream);
 /* x <- the values that codes and scales stand for. Errors as tas_fp4_pack. */
 int tas_fp4_values(const tas_tensor_fp4 *a, void *stream);
 
+/* The values of a whole cache: k and v, [n_blocks][kv_heads][block_tokens][head_dim] in
+ * a 16-bit type, 16-byte aligned, <- what the cache stands for, in one launch. */
+typedef struct tas_cache_values_fp4 {
+    int32_t dtype;                 /* of k and v                                             */
+    int32_t head_dim;              /* 64 or 128                                              */
+    int64_t n_blocks, kv_heads, block_tokens;
+    tas_cache_fp4 cache;
+    void *k, *v;
+} tas_cache_values_fp4;
+/* Errors as tas_fp4_values. */
+int tas_fp4_cache_values(const tas_cache_values_fp4 *a, void *stream);
+
 /* WEIGHTS: a matrix [rows][cols] in four bits, laid out once for the products, in
  * tas_fp4_weights_bytes bytes of device memory (0: sizes out of range: rows 1 ..
  * 2^24, cols a multiple of 32 up to 2^20). */

@@ -248,20 +248,62 @@ int tas_fp4_pack(const tas_tensor_fp4 *from, void *stream) {
     return done(launch_pack4(tensor_args(a, rows), a->dtype, (hipStream_t)stream));
 }
 
-int tas_fp4_values(const tas_tensor_fp4 *from, void *stream) {
+// What a call that gives values refuses, besides; its kernel's arguments.
+static bool values_args(const tas_tensor_fp4 *from, Tensor4Args &k, int64_t &rows) {
     tas_tensor_fp4 tensor, *const a = &tensor;
-    int64_t rows;
-    if (!valid_tensor(from, a, rows)) return TAS_EINVAL;
-    if (!rows) return TAS_OK;
+    if (!valid_tensor(from, a, rows)) return false;
+    if (!rows) return true;
     const int64_t(&n)[3] = a->n;
     if (!disjoint_slots(a->x.stride[0], a->x.stride[1], a->x.stride[2], n[0], n[1], n[2],
                         a->cols * 2))
-        return TAS_EINVAL;
+        return false;
     const Region x = byte_region(a->x, n, a->cols * 2);
     if (Overlap()(x, byte_region(a->codes, n, a->cols / 2)) ||
         Overlap()(x, byte_region(a->scales, n, a->cols / 32)))
-        return TAS_EINVAL;
-    return done(launch_values4(tensor_args(a, rows), a->dtype, (hipStream_t)stream));
+        return false;
+    k = tensor_args(a, rows);
+    return true;
+}
+
+int tas_fp4_values(const tas_tensor_fp4 *a, void *stream) {
+    Values4Args k{};
+    int64_t rows;
+    if (!values_args(a, k.t[0], rows)) return TAS_EINVAL;
+    if (!rows) return TAS_OK;
+    return done(launch_values4(k, 1, a->dtype, (hipStream_t)stream));
+}
+
+int tas_fp4_cache_values(const tas_cache_values_fp4 *a, void *stream) {
+    if (!a || (a->head_dim != 64 && a->head_dim != 128)) return TAS_EINVAL;
+    tas_tensor_fp4 t[2]{};
+    Values4Args k{};
+    int64_t rows = 0;
+    for (int i = 0; i < 2; i++) {
+        const int64_t row = a->head_dim * 2;
+        t[i].dtype = a->dtype;
+        t[i].n[0] = a->n_blocks;
+        t[i].n[1] = a->kv_heads;
+        t[i].n[2] = a->block_tokens;
+        t[i].cols = a->head_dim;
+        for (int64_t n : t[i].n)
+            if (n < 0 || n > INT32_MAX) return TAS_EINVAL;
+        if (a->kv_heads * a->block_tokens > INT32_MAX) return TAS_EINVAL;
+        t[i].x = {i ? a->v : a->k,
+                  {a->kv_heads * a->block_tokens * row, a->block_tokens * row, row}};
+        t[i].codes = i ? a->cache.v : a->cache.k;
+        t[i].scales = i ? a->cache.v_scale : a->cache.k_scale;
+        if (!values_args(&t[i], k.t[i], rows)) return TAS_EINVAL;
+    }
+    if (!rows) return TAS_OK;
+    for (int i = 0; i < 2; i++) {  // an output over the other tensor's sides
+        const Region x = byte_region(t[i].x, t[i].n, t[i].cols * 2);
+        const tas_tensor_fp4 &y = t[1 - i];
+        if (Overlap()(x, byte_region(y.x, y.n, y.cols * 2)) ||
+            Overlap()(x, byte_region(y.codes, y.n, y.cols / 2)) ||
+            Overlap()(x, byte_region(y.scales, y.n, y.cols / 32)))
+            return TAS_EINVAL;
+    }
+    return done(launch_values4(k, 2, a->dtype, (hipStream_t)stream));
 }
 
 static bool valid_matrix(int64_t rows, int64_t cols) {

@@ -21,6 +21,10 @@ struct Tensor4Args {
     uint32_t units, per_row, n1, n2;  // units in all and of a row; rows i0 n1 n2 + i1 n2 + i2
 };
 
+struct Values4Args {
+    Tensor4Args t[2];  // of as many units
+};
+
 // Weights as the products read them: tiles of 16 rows and 128 columns, the tiles of a run
 // of rows one after another, so that a tile is one load of adjacent 16 bytes a lane. Lane
 // 16 g + r has the words g (elements 8 g .. 8 g + 7) of row r's four blocks: a product's 32
@@ -60,7 +64,8 @@ hipError_t launch_append4(const Append4Args &a, int dtype, int head_dim, hipStre
 hipError_t launch_attention4(const Attn4Args &a, int n_items, int n_merge, int dtype,
                              int head_dim, hipStream_t s);
 hipError_t launch_pack4(const Tensor4Args &a, int dtype, hipStream_t s);
-hipError_t launch_values4(const Tensor4Args &a, int dtype, hipStream_t s);
+// (of one tensor or two)
+hipError_t launch_values4(const Values4Args &a, int n, int dtype, hipStream_t s);
 hipError_t launch_weights4(const Weights4Args &a, hipStream_t s);
 hipError_t launch_linear4(const Linear4Args &a, int dtype, hipStream_t s);
 

@@ -34,7 +34,8 @@ __global__ __launch_bounds__(256) void pack_kernel(Tensor4Args a) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void values_kernel(Tensor4Args a) {
+__global__ __launch_bounds__(256) void values_kernel(Values4Args both) {
+    const Tensor4Args &a = both.t[blockIdx.y];
     const uint32_t u = blockIdx.x * 256 + threadIdx.x;
     if (u >= a.units) return;
     const uint32_t row = u / a.per_row, c = u - row * a.per_row;
@@ -71,10 +72,13 @@ hipError_t launch_pack4(const Tensor4Args &a, int dtype, hipStream_t s) {
     const int64_t n = ((int64_t)a.units + 255) / 256;
     return launch_kernel(dtype == TAS_F16 ? pack_kernel<_Float16> : pack_kernel<__bf16>, n, a, s);
 }
-hipError_t launch_values4(const Tensor4Args &a, int dtype, hipStream_t s) {
-    const int64_t n = ((int64_t)a.units + 255) / 256;
-    return launch_kernel(dtype == TAS_F16 ? values_kernel<_Float16> : values_kernel<__bf16>, n, a,
-                         s);
+hipError_t launch_values4(const Values4Args &a, int n, int dtype, hipStream_t s) {
+    Values4Args copy = a;
+    void *args[] = {&copy};
+    return hipLaunchKernel(dtype == TAS_F16 ? (const void *)values_kernel<_Float16>
+                                            : (const void *)values_kernel<__bf16>,
+                           dim3((uint32_t)(((int64_t)a.t[0].units + 255) / 256), n), dim3(256),
+                           args, 0, s);
 }
 hipError_t launch_weights4(const Weights4Args &a, hipStream_t s) {
     return launch_kernel(weights_kernel, (a.w.tiles_n * a.w.tiles_k + 3) / 4, a, s);

@@ -60,20 +60,27 @@ class tas_tensor_fp4(ctypes.Structure):
                 ("x", tas_rows), ("codes", tas_rows), ("scales", tas_rows)]
 
 
+class tas_cache_values_fp4(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("head_dim", _i32), ("n_blocks", _i64), ("kv_heads", _i64),
+                ("block_tokens", _i64), ("cache", tas_cache_fp4), ("k", _P), ("v", _P)]
+
+
 class tas_linear_fp4(ctypes.Structure):
     _fields_ = [("dtype", _i32), ("reserved", _i32), ("tokens", _i64), ("rows", _i64),
                 ("cols", _i64), ("x", _P), ("x_stride", _i64), ("weights", _P), ("y", _P),
                 ("y_stride", _i64)]
 
 
-# The two of the calls below, packed (a third of the time of a ctypes constructor).
+# Those of the calls below, packed (a third of the time of a ctypes constructor).
 _TENSOR = struct.Struct("iiqqqq" + 3 * "Pqqq")
+_CACHE_VALUES = struct.Struct("iiqqq" + 4 * "Pqqq" + "PP")
 _LINEAR = struct.Struct("iiqqqPqPPq")
 assert _TENSOR.size == ctypes.sizeof(tas_tensor_fp4)
+assert _CACHE_VALUES.size == ctypes.sizeof(tas_cache_values_fp4)
 assert _LINEAR.size == ctypes.sizeof(tas_linear_fp4)
 
 EXPORTS = ["tas_fp4_append", "tas_fp4_attention", "tas_fp4_pack", "tas_fp4_values",
-           "tas_fp4_weights_bytes", "tas_fp4_weights", "tas_fp4_linear"]
+           "tas_fp4_cache_values", "tas_fp4_weights_bytes", "tas_fp4_weights", "tas_fp4_linear"]
 
 
 def _call(index, stream, call, *args):
@@ -203,8 +210,29 @@ class Cache(NamedTuple):
     def values(self, dtype, *, stream=None):
         """The keys and values that the pool stands for, [n_blocks, kv_heads,
         block_tokens, head_dim] in float16 or bfloat16."""
-        return (values(self.k, self.k_scale, dtype, stream=stream),
-                values(self.v, self.v_scale, dtype, stream=stream))
+        code = DTYPES.get(dtype)
+        if code is None:
+            raise ValueError(f"{dtype}: float16 or bfloat16")
+        index = _gpu(self.k, "k")
+        n, half, at = _rows(self.k, 1, "k")
+        for t, row, name in ((self.v, half, "v"), (self.k_scale, half // 16, "k_scale"),
+                             (self.v_scale, half // 16, "v_scale")):
+            rows_n, rows_row, rows_at = _rows(t, 1, name)
+            if rows_n != n or rows_row != row or t.dtype != torch.uint8 \
+                    or t.get_device() != index:
+                raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}, k "
+                                 f"{self.k.dtype} {tuple(self.k.shape)} on {self.k.device}: uint8, "
+                                 "16 bytes of codes to one of scales")
+            at += rows_at
+        if self.k.dtype != torch.uint8 or half not in (32, 64):
+            raise ValueError(f"k is {self.k.dtype}, rows of {half}: uint8, rows of 32 or 64")
+        both = _empty(self.k, (2, *n, 2 * half), dtype, stream)
+        k, v = both.unbind()
+        _call(index, stream, lib().tas_fp4_cache_values,
+              _CACHE_VALUES.pack(code, 2 * half, *n, *at, k.data_ptr(), v.data_ptr()))
+        if stream is not None:
+            _keep(index, stream, *self, both)
+        return k, v
 
 
 class Weights:

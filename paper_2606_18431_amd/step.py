@@ -99,6 +99,7 @@ def lib():
         L.tas_fp4_attention.argtypes = [_P, _P, _P]
         L.tas_fp4_pack.argtypes = [_P, _P]
         L.tas_fp4_values.argtypes = [_P, _P]
+        L.tas_fp4_cache_values.argtypes = [_P, _P]
         L.tas_fp4_weights_bytes.argtypes = [_i64, _i64]
         L.tas_fp4_weights_bytes.restype = ctypes.c_size_t
         L.tas_fp4_weights.argtypes = [_i64, _i64, _P, _i64, _P, _i64, _P, _P]

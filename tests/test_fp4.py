@@ -24,7 +24,7 @@ def test_library_exports_every_declared_symbol():
 
 def test_struct_layouts_match_header(tmp_path):
     structs = [fp4.tas_rows, fp4.tas_cache_fp4, fp4.tas_append_fp4, fp4.tas_attention_fp4,
-               fp4.tas_tensor_fp4, fp4.tas_linear_fp4]
+               fp4.tas_tensor_fp4, fp4.tas_cache_values_fp4, fp4.tas_linear_fp4]
     lines = ['#include <stddef.h>', '#include <stdio.h>', '#include "tas_fp4.h"',
              'int main(void) {']
     for st in structs:
@@ -178,6 +178,28 @@ def test_refused_tensors():
                dict(scales=rows(AT + (1 << 20) + 957, 30, 10, 2))):
         assert L.tas_fp4_pack(tensor(**{**apart, **kw}), None) == tas.TAS_EINVAL, kw
     assert L.tas_fp4_values(tensor(**apart, x=rows(AT, 1920, 0, 128)), None) == tas.TAS_EINVAL
+
+
+def test_refused_cache_values():
+    L = step.lib()
+
+    def call(**kw):
+        a = dict(dtype=1, head_dim=64, n_blocks=4, kv_heads=2, block_tokens=16, cache=cache(),
+                 k=AT + (8 << 20), v=AT + (8 << 20) + 4096)  # v over the end of k
+        a.update(kw)
+        return L.tas_fp4_cache_values(ctypes.byref(fp4.tas_cache_values_fp4(**a)), None)
+
+    assert L.tas_fp4_cache_values(None, None) == tas.TAS_EINVAL
+    assert call() == tas.TAS_EINVAL
+    apart = dict(v=AT + (9 << 20))
+    assert call(**apart, n_blocks=0) == 0
+    for kw in [dict(dtype=2), dict(head_dim=96), dict(n_blocks=-1), dict(kv_heads=1 << 32),
+               dict(n_blocks=1 << 30, kv_heads=1 << 10), dict(kv_heads=1 << 20, block_tokens=1 << 20),
+               dict(k=None), dict(k=AT + 8), dict(v=AT + (9 << 20) + 2), dict(k=AT + (2 << 20)),
+               dict(v=AT + (3 << 20)), dict(v=AT + (1 << 20)), dict(k=AT + (4 << 20) + 128),
+               dict(cache=cache(k=rows(AT + 2, 1024, 512, 32))),
+               dict(cache=cache(v_scale=rows(None, 64, 32, 2)))]:
+        assert call(**{**apart, **kw}) == tas.TAS_EINVAL, kw
 
 
 def test_weights_bytes():

@@ -183,6 +183,25 @@ def cache_of(torch, b, seed, order="head", poison=True):
     return fp4.Cache(*got), vals
 
 
+@pytest.mark.parametrize("size", [64, 128])
+@pytest.mark.parametrize("order", ["head", "token", "beside"])
+def test_cache_values(torch, size, order):
+    """Keys and values at once, as ``values`` gives each; an empty pool."""
+    b = Batch(25, [3, 1], [50, 20], 6, 3, size, block=32)
+    cache, (k, v) = cache_of(torch, b, 4, order)
+    for dt in (torch.bfloat16, torch.float16):
+        got = cache.values(dt)
+        assert got[0].shape == (b.n_blocks, 3, 32, size) and got[0].dtype == dt
+        assert same(got[0].double().cpu(), k) and same(got[1].double().cpu(), v)
+    assert fp4.Cache(*(t[:0] for t in cache)).values(torch.float16)[1].shape == (0, 3, 32, size)
+    for i, t in enumerate(cache):
+        for bad in (t[1:], t.char(), t.cpu(), t[..., ::2]):
+            with pytest.raises(ValueError):
+                fp4.Cache(*(bad if j == i else u for j, u in enumerate(cache))).values(torch.float16)
+    with pytest.raises(ValueError):
+        cache.values(torch.float32)
+
+
 def check_append(torch, b, name, rot, interleaved, norm, order="head"):
     print(f"[gpu] append_fp4 {name} n={b.n.tolist()[:8]} heads={b.heads}/{b.kv_heads}x{b.size} "
           f"block={b.block} rot={rot} interleaved={interleaved} norm={norm}", flush=True)
