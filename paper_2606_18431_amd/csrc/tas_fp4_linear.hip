@@ -129,23 +129,23 @@ constexpr int kWaitLoads = 0x0F70;  // s_waitcnt: no load or store outstanding
 // A barrier behind which the workgroup's LDS reads and all but the wave's last N loads are
 // done. (__syncthreads would wait for all of them. The empty statements keep the compiler from
 // moving memory accesses across, the others from working out scales that have not arrived.)
-template <int N, bool APART>
+template <int N>
 __device__ void barrier_after_loads() {
     static_assert(N < 64, "");
-    if (APART) __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_sched_barrier(0);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (APART) __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_sched_barrier(0);
 }
 
-// More tokens. 16 RT WN rows and 16 TT WT tokens a workgroup, of KS groups of WN by WT waves,
+// More tokens, with too few tiles of 256 by 128. 16 RT WN rows and 16 TT WT tokens a workgroup, of KS groups of WN by WT waves,
 // group n with every KS-th step of 128 columns from n on. A wave has its weights in registers,
 // converted once for all of its tokens; a step of x is in LDS for its group, loaded there
 // directly, S - 1 of the group's steps ahead. Chunk c (of eight elements) of row t lies at
-// c ^ (t mod 16), which spreads the rows of a column over the banks. Bound by the matrix unit
-// and by LDS where there are many tokens, by the loads' latency where there are few.
+// c ^ (t mod 16), which spreads the rows of a column over the banks. Bound by the loads' latency
+// and LDS.
 template <typename T, int WN, int WT, int RT, int TT, int S, int KS>
 __global__ __launch_bounds__(64 * WN * WT * KS, (WN * WT * KS > 8 ? WN * WT * KS / 4 : 2))
 void tile_kernel(Linear4Args a) {
@@ -153,8 +153,9 @@ void tile_kernel(Linear4Args a) {
     constexpr int W = WN * WT, BT = 16 * TT * WT, LB = BT * kTileCols * 2;
     constexpr int NL = LB / 1024 / W;  // loads of a wave for a step
     // objects of their own, so that the compiler sees which loads a read has to wait for
-    __shared__ __attribute__((aligned(16))) char x0[KS * LB], x1[KS * LB],
-        x2[S > 2 ? KS * LB : 16], x3[S > 3 ? KS * LB : 16];
+    static_assert(S == 3 || S == 4, "");
+    __shared__ __attribute__((aligned(16))) char x0[KS * LB], x1[KS * LB], x2[KS * LB],
+        x3[S > 3 ? KS * LB : 16];
     const int lane = threadIdx.x & 63;
     const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wave = all % W, group = all / W;
@@ -233,7 +234,7 @@ void tile_kernel(Linear4Args a) {
     // are counted: a step's weights are asked for before its x.)
     auto middle = [&](auto stage, int n) {
         constexpr int st = decltype(stage)::value;
-        barrier_after_loads<(S - 2) * NL, (S > 2)>();
+        barrier_after_loads<(S - 2) * NL>();
         issue(Const<(st + S - 1) % S>{}, Const<0>{}, n + S - 1);
         products(stage);
     };
@@ -256,11 +257,11 @@ void tile_kernel(Linear4Args a) {
     auto each = [&](auto &step, int n) {
         step(Const<0>{}, n);
         step(Const<1>{}, n + 1);
-        if constexpr (S > 2) step(Const<2>{}, n + 2);
+        step(Const<2>{}, n + 2);
         if constexpr (S > 3) step(Const<3>{}, n + 3);
     };
     issue(Const<0>{}, Const<1>{}, 0);
-    if constexpr (S > 2) issue(Const<1>{}, Const<1>{}, 1);
+    issue(Const<1>{}, Const<1>{}, 1);
     if constexpr (S > 3) issue(Const<2>{}, Const<1>{}, 2);
     int n = 0;
     for (; n + 2 * S - 1 <= whole; n += S) each(middle, n);
@@ -303,6 +304,111 @@ hipError_t launch_tile(const Linear4Args &a, hipStream_t s) {
     return hipLaunchKernel((const void *)tile_kernel<T, WN, WT, RT, TT, S, KS>, grid,
                            dim3(64 * WN * WT * KS), args, 0, s);
 }
+// Many tokens: bound by the matrix unit. 256 rows and 128 tokens a workgroup, all tokens to
+// each of four waves with 64 rows, so that an operand from LDS goes into four products. As
+// above, with a step of x in LDS one step ahead: a step's 128 products a wave last longer than
+// its loads. (8192 tokens, 6144 x 4096: 297 us, 1390 TFLOP/s; 128 by 128 a workgroup, 32 rows to
+// a wave, 340.)
+constexpr int kBigRows = 256, kBigTokens = 128;
+template <typename T>
+__global__ __launch_bounds__(256, 2) void big_kernel(Linear4Args a) {
+    using V = vec8<T>;
+    constexpr int RT = kBigRows / 64, TT = kBigTokens / 16;
+    constexpr int LB = kBigTokens * kTileCols * 2, NL = LB / 4096;
+    __shared__ __attribute__((aligned(16))) char x0[LB], x1[LB];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, g = lane >> 4;
+    const uint32_t groups_n = (a.rows + kBigRows - 1) / kBigRows, at_t = blockIdx.x / groups_n;
+    const int tile0 = (blockIdx.x - at_t * groups_n) * (kBigRows / 16) + wave * RT;
+    const int t0 = at_t * kBigTokens;
+    const char *codes[RT], *scales[RT];
+#pragma unroll
+    for (int i = 0; i < RT; i++) {  // (of tiles that there are not, the last one's)
+        const int64_t tile = min(tile0 + i, a.tiles_n - 1);
+        codes[i] = a.codes + tile * a.tiles_k * 1024;
+        scales[i] = a.scales + tile * a.tiles_k * 64;
+    }
+    // load i of a wave: four rows, 16 lanes each (offsets fit 32 bits: 128 rows of 2^25 bytes)
+    const int lrow = lane >> 4, lch = lane & 15;
+    const char *x_rows = (const char *)((const T *)a.x + t0 * a.x_stride);
+    auto chunk = [&](int i) { return lch ^ (((wave * NL + i) * 4 + lrow) & 15); };
+    uint32_t from[NL];
+#pragma unroll
+    for (int i = 0; i < NL; i++)
+        from[i] = (uint32_t)min((wave * NL + i) * 4 + lrow, a.tokens - 1 - t0) *
+                      (uint32_t)(a.x_stride * 2) + chunk(i) * 16;
+    auto load_x = [&](char *to, int tk) {
+        const bool end = (tk + 1) * 4 > a.blocks;
+        const char *rows = x_rows + tk * 256ll;
+#pragma unroll
+        for (int i = 0; i < NL; i++) {
+            uint32_t at = from[i];
+            // past the end: this step's first chunk, cleared when it is there
+            if (end && tk * 4 + chunk(i) / 4 >= a.blocks) at -= chunk(i) * 16;
+            load_to_lds((Global)rows + at, to + (wave * NL + i) * 1024);
+        }
+    };
+    auto arrive = [&](char *to, int tk) {
+        __builtin_amdgcn_s_waitcnt(kWaitLoads);
+        if ((tk + 1) * 4 > a.blocks)
+#pragma unroll
+            for (int i = 0; i < NL; i++)
+                if (tk * 4 + chunk(i) / 4 >= a.blocks)
+                    *(u4 *)(to + (wave * NL + i) * 1024 + lane * 16) = u4{0, 0, 0, 0};
+        __syncthreads();
+    };
+    u4 c[RT], next_c[RT];
+    uint32_t sc[RT], next_sc[RT];
+    auto load_w = [&](int tk) {
+        tk = min(tk, a.tiles_k - 1);
+#pragma unroll
+        for (int i = 0; i < RT; i++) {
+            next_c[i] = *(const u4 *)(codes[i] + tk * 1024ll + (uint32_t)lane * 16);
+            next_sc[i] = *(const uint32_t *)(scales[i] + tk * 64ll + (uint32_t)col * 4);
+        }
+    };
+    f4 sum[RT][TT];
+#pragma unroll
+    for (int i = 0; i < RT; i++)
+#pragma unroll
+        for (int j = 0; j < TT; j++) sum[i][j] = f4{0, 0, 0, 0};
+    auto step = [&](const char *x, char *next, int tk) {
+#pragma unroll
+        for (int i = 0; i < RT; i++) c[i] = next_c[i], sc[i] = next_sc[i];
+        if (tk + 1 < a.tiles_k) load_x(next, tk + 1);
+        load_w(tk + 1);
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            V b[TT];
+#pragma unroll
+            for (int j = 0; j < TT; j++)
+                b[j] = *(const V *)(x + (j * 16 + col) * 256 + ((k * 4 + g) ^ col) * 16);
+#pragma unroll
+            for (int i = 0; i < RT; i++) {
+                const V w = values_of<T>(c[i][k], scale_of(sc[i] >> (8 * k) & 255));
+#pragma unroll
+                for (int j = 0; j < TT; j++) sum[i][j] = mfma16(w, b[j], sum[i][j]);
+            }
+        }
+        if (tk + 1 < a.tiles_k) arrive(next, tk + 1);
+    };
+    load_x(x0, 0);
+    load_w(0);
+    arrive(x0, 0);
+    for (int tk = 0; tk < a.tiles_k; tk += 2) {
+        step(x0, x1, tk);
+        if (tk + 1 < a.tiles_k) step(x1, x0, tk + 1);
+    }
+#pragma unroll
+    for (int j = 0; j < TT; j++) {
+        const int t = t0 + j * 16 + col;
+        if (t >= a.tokens) break;
+#pragma unroll
+        for (int i = 0; i < RT; i++) store_four<T>(a, t, (tile0 + i) * 16 + g * 4, sum[i][j]);
+    }
+}
+
 template <typename T, int RT>
 hipError_t launch_stream(const Linear4Args &a, hipStream_t s) {
     Linear4Args copy = a;
@@ -328,11 +434,12 @@ struct TileCost {
     int rows, tokens;
     float base, round, least;
 };
-constexpr TileCost kTiles[] = {{32, 32, 2, 7, 9},       // 64 tokens, 4096 rows: 8.9 (the next 11.0)
-                               {64, 32, 4, 7, 11},      // 128 tokens, 4096 rows: 11.2 (14.6, 19.4)
-                               {128, 64, 1, 19, 20},    // 256 tokens, 8192 rows: 22.4 (26.9, 32.4)
-                               {128, 64, 8, 13.4, 31},  // 1024 tokens, 4096 rows: 36.9 (40.5, 48.7)
-                               {128, 128, 3, 28, 48}};  // 1024 tokens, 8192 rows: 59.2 (68.1)
+constexpr TileCost kTiles[] = {
+    {32, 32, 2, 7, 9},                         // 64 tokens, 4096 rows: 8.9 (the next 11.0)
+    {64, 32, 4, 7, 11},                        // 128 tokens, 4096 rows: 11.2 (14.6, 19.4)
+    {128, 64, 1, 19, 20},                      // 256 tokens, 8192 rows: 22.4 (26.9, 32.4)
+    {128, 64, 8, 13.4, 31},                    // 1024 tokens, 4096 rows: 34.8 (40.5, 75.6)
+    {kBigRows, kBigTokens, 0, 49.5, 78}};      // 4096 tokens, 4096 rows: 100 (118)
 int choose_tile(const Linear4Args &a) {
     int best = 0;
     float least = 0;
@@ -354,7 +461,10 @@ hipError_t launch(const Linear4Args &a, hipStream_t s) {
         case 1: return launch_tile<T, 4, 1, 1, 2, 4, 2>(a, s);
         case 2: return launch_tile<T, 4, 1, 2, 4, 4, 2>(a, s);
         case 3: return launch_tile<T, 4, 1, 2, 4, 3, 1>(a, s);
-        default: return launch_tile<T, 4, 1, 2, 8, 2, 1>(a, s);
+        default:
+            return launch_kernel(big_kernel<T>, (int64_t)((a.rows + kBigRows - 1) / kBigRows) *
+                                                    ((a.tokens + kBigTokens - 1) / kBigTokens),
+                                 a, s);
     }
 }
 

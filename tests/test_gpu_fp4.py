@@ -520,6 +520,13 @@ def test_linear_many_rows(torch, tokens, rows):
     check_linear(torch, tokens, rows, 160, "bf16")
 
 
+@pytest.mark.parametrize("name", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens,rows,cols", [(4090, 4100, 160), (4096, 4096, 32), (2100, 8201, 288)])
+def test_linear_many_of_both(torch, name, tokens, rows, cols):
+    """As many tiles as the largest kernel is taken for, some of them beyond the matrix."""
+    check_linear(torch, tokens, rows, cols, name)
+
+
 def test_linear_extremes(torch):
     """Weights at the ends of their exponents."""
     for name, bytes_ in (("bf16", (2, 30, 127, 200)), ("f16", (104, 127, 136))):
