@@ -84,6 +84,8 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(Linear4Args a) {
 #pragma unroll
         for (int n = 0; n < 4; n++) {
             const int tk = u * 4 + n;
+            // (not the last tile again: an infinity in it, times zero, is NaN)
+            if (!decltype(whole)::value && tk >= a.tiles_k) break;
             V b[4];
 #pragma unroll
             for (int k = 0; k < 4; k++)
@@ -140,12 +142,12 @@ __device__ void barrier_after_loads() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// More tokens, with too few tiles of 256 by 128. 16 RT WN rows and 16 TT WT tokens a workgroup, of KS groups of WN by WT waves,
-// group n with every KS-th step of 128 columns from n on. A wave has its weights in registers,
-// converted once for all of its tokens; a step of x is in LDS for its group, loaded there
-// directly, S - 1 of the group's steps ahead. Chunk c (of eight elements) of row t lies at
-// c ^ (t mod 16), which spreads the rows of a column over the banks. Bound by the loads' latency
-// and LDS.
+// More tokens, with too few tiles of 256 by 128. 16 RT WN rows and 16 TT WT tokens a workgroup,
+// of KS groups of WN by WT waves, group n with every KS-th step of 128 columns from n on. A wave
+// has its weights in registers, converted once for all of its tokens; a step of x is in LDS for
+// its group, loaded there directly, S - 1 of the group's steps ahead. Chunk c (of eight
+// elements) of row t lies at c ^ (t mod 16), which spreads the rows of a column over the banks.
+// Bound by the loads' latency and LDS.
 template <typename T, int WN, int WT, int RT, int TT, int S, int KS>
 __global__ __launch_bounds__(64 * WN * WT * KS, (WN * WT * KS > 8 ? WN * WT * KS / 4 : 2))
 void tile_kernel(Linear4Args a) {

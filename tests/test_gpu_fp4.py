@@ -563,6 +563,24 @@ def test_linear_values_that_are_not_finite(torch, tokens):
     assert torch.equal(got, clean)
 
 
+@pytest.mark.parametrize("name", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens", [3, 40, 200])
+@pytest.mark.parametrize("cols", [96, 160, 1120])
+def test_linear_infinite_weights(torch, name, tokens, cols):
+    """A scale that the 16-bit type has not makes a weight infinite, and its products with
+    positive values, in whichever block: infinite, not NaN."""
+    dt = dtype_of(torch, name)
+    codes, scales = fp4.pack(torch.randn((50, cols), device="cuda").to(dt))
+    x = (torch.rand((tokens, cols), device="cuda") + 0.5).to(dt)
+    clean = fp4.linear(x, fp4.Weights(codes, scales))
+    blocks = cols // 32
+    for row, block in ((0, 0), (17, blocks // 2), (49, blocks - 1)):
+        codes[row, block * 16:block * 16 + 16] = 0x77  # all 6
+        scales[row, block] = 254
+        clean[:, row] = math.inf
+    assert torch.equal(fp4.linear(x, fp4.Weights(codes, scales)), clean)
+
+
 def test_linear_strided_tensors(torch):
     x = torch.randn((70, 300), device="cuda", dtype=torch.float16)[:, 8:264]
     x = torch.empty((70, 304), device="cuda", dtype=torch.float16)[:, 8:264].copy_(x)
@@ -669,6 +687,51 @@ def test_other_streams_and_graphs(torch):
         assert all(torch.equal(t, u) for t, u in zip(ke, kg))
         assert all(torch.equal(t, u) for t, u in zip(vals, ke.values(torch.float16)))
         torch.cuda.synchronize()
+
+
+def test_a_step_and_weights_of_two_graphs_and_both_kinds_of_cache(torch):
+    """Calls of both kinds in turn share a step's workspace, and so do two graphs' replays;
+    two threads share weights."""
+    from concurrent.futures import ThreadPoolExecutor
+
+    b = Batch(23, [1, 1, 70], [5000, 17, 900], 8, 2, 128)
+    caches = [cache_of(torch, b, seed, poison=False)[0] for seed in (4, 5)]
+    qs = [torch.randn((b.T, 8, 128), device="cuda").bfloat16() for _ in range(2)]
+    wide = caches[0].values(torch.bfloat16)
+    w = fp4.Weights(*fp4.pack(torch.randn((96, 1024), device="cuda").bfloat16()))
+    torch.cuda.synchronize()
+    want = [b.step().attention_fp4(q, c) for q, c in zip(qs, caches)]
+    want_wide = b.step().attention(qs[1], *wide)
+    want_y = [fp4.linear(o.flatten(1), w) for o in want]
+    s = b.step()
+    for _ in range(3):
+        assert torch.equal(s.attention_fp4(qs[0], caches[0]), want[0])
+        assert torch.equal(s.attention(qs[1], *wide), want_wide)
+        assert torch.equal(s.attention_fp4(qs[1], caches[1]), want[1])
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for q, c in zip(qs, caches):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            o = s.attention_fp4(q, c)
+            outs.append((o, fp4.linear(o.flatten(1), w)))
+        graphs.append(graph)
+    for i in (0, 1, 1, 0, 1, 0, 0):
+        for t in outs[i]:
+            t.zero_()
+        graphs[i].replay()
+        assert torch.equal(s.attention(qs[1], *wide), want_wide)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[i][0], want[i]) and torch.equal(outs[i][1], want_y[i])
+
+    def calls(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            got = [fp4.linear(want[i].flatten(1), w) for _ in range(50)]
+            torch.cuda.current_stream().synchronize()
+        return all(torch.equal(y, want_y[i]) for y in got)
+
+    with ThreadPoolExecutor(2) as pool:
+        assert all(pool.map(calls, (0, 1)))
 
 
 def test_tensors_dropped_while_another_stream_uses_them(torch):
