@@ -349,7 +349,7 @@ int tas_fp4_linear(const tas_linear_fp4 *a, void *stream) {
     if (!bytes || !a->weights || (uintptr_t)a->weights & 255) return TAS_EINVAL;
     if (a->tokens < 0 || a->tokens > (int64_t(1) << 24)) return TAS_EINVAL;
     if (!a->tokens) return TAS_OK;
-    // (the smallest tiles, of 32 by 32, are not taken where there are many)
+    // (smaller tiles are not taken where there are many)
     if (ceil_div(a->rows, 64) * ceil_div(a->tokens, 64) > kMaxGroups / 8) return TAS_EINVAL;
     if (!valid_rows(a->x, a->x_stride, a->cols) || a->x_stride > kMaxTokenStride)
         return TAS_EINVAL;

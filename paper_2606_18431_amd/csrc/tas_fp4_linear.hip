@@ -44,19 +44,51 @@ __device__ void store_four(const Linear4Args &a, int64_t t, int n, f4 x) {
     }
 }
 
-// Up to 16 tokens: bound by the weights' bytes. A workgroup has all of K for 16 RT rows, its
-// eight waves take every eighth unit of 512 columns, and their sums are joined in LDS, in one
-// order: no partial results in memory, no second launch. All of a unit's weights are asked
-// for at once.
-template <typename T, int RT>
-__global__ __launch_bounds__(64 * kWaves) void stream_kernel(Linear4Args a) {
+typedef const __attribute__((address_space(1))) char *Global;
+__device__ void load_to_lds(Global from, char *to) {
+    __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, 0,
+                                     0);
+}
+constexpr int kWaitLoads = 0x0F70;  // s_waitcnt: no load or store outstanding
+constexpr int kWaitLds = 0xC07F;    // no LDS access outstanding
+
+// Waits until all but the wave's last N loads are done. (The empty statements keep the compiler
+// from moving memory accesses across, the others from using earlier what has arrived later.)
+template <int N>
+__device__ void wait_loads() {
+    static_assert(N < 64, "");
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(kWaitLoads | (N & 15) | (N >> 4) << 14);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Few tokens: bound by the weights' bytes. A workgroup has all of K for 16 RT rows and 4 XL tokens
+// (16 TT in the products). Its eight waves take every eighth tile of 128 columns, each by itself:
+// weights in registers, four tiles asked for at once; x, half a tile at a time, through LDS of
+// the wave's own, loaded there directly, whole lines of eight tokens a load, NB halves ahead.
+// (Read as the product wants it, 16 bytes of 16 rows at a time, x takes more time than the
+// weights: 16 tokens, 4096 rows and columns 6.7 us, 4.7 so; loaded to registers and written to
+// LDS 6.0.) The waves' sums are joined in LDS, in one order: no partial results in memory, no
+// second launch, no barrier before the join. Chunk c (of eight elements) of token t lies at
+// c ^ (t / 2 mod 8), which spreads the rows of a column over the banks.
+template <typename T, int RT, int XL, int NB>
+__global__ __launch_bounds__(64 * kWaves, RT == 4 ? 2 : 4)
+void stream_kernel(Linear4Args a) {
     using V = vec8<T>;
-    constexpr int H = kWaves / 2;
-    __shared__ f4 part[H][RT][64];
+    constexpr int H = kWaves / 2, TT = (XL + 3) / 4, PL = XL / 2;  // (loads of half a tile)
+    constexpr int XB = TT * 2048;  // bytes of half a tile of x
+    static_assert(XL % 2 == 0 && (NB == 2 || NB == 4), "");
+    // objects of their own, so that the compiler sees which loads a read has to wait for
+    __shared__ __attribute__((aligned(16))) char x0[kWaves * XB], x1[NB > 1 ? kWaves * XB : 16],
+        x2[NB > 2 ? kWaves * XB : 16], x3[NB > 2 ? kWaves * XB : 16];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
-    const int tile0 = blockIdx.x * RT;
+    const uint32_t groups_n = (a.tiles_n + RT - 1) / RT, at_t = blockIdx.x / groups_n;
+    const int tile0 = (blockIdx.x - at_t * groups_n) * RT;
+    const int t0 = at_t * 4 * XL;
     const char *codes[RT], *scales[RT];
 #pragma unroll
     for (int i = 0; i < RT; i++) {  // (of tiles that there are not, the last one's)
@@ -64,73 +96,117 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(Linear4Args a) {
         codes[i] = a.codes + tile * a.tiles_k * 1024;
         scales[i] = a.scales + tile * a.tiles_k * 64;
     }
-    const T *x = (const T *)a.x + min(col, a.tokens - 1) * a.x_stride + g * 8;
-    f4 sum[RT];
+    // load i: eight rows, 8 lanes each (offsets fit 32 bits: 64 rows of 2^25 bytes)
+    const char *x_rows = (const char *)((const T *)a.x + t0 * a.x_stride);
+    const int lrow = lane >> 3;
+    auto chunk = [&](int i) { return (lane & 7) ^ ((i * 8 + lrow) >> 1 & 7); };
+    uint32_t from[PL];
 #pragma unroll
-    for (int i = 0; i < RT; i++) sum[i] = f4{0, 0, 0, 0};
+    for (int i = 0; i < PL; i++)
+        from[i] = (uint32_t)min(i * 8 + lrow, a.tokens - 1 - t0) * (uint32_t)(a.x_stride * 2) +
+                  chunk(i) * 16;
+    auto buffer = [&](int n) { return (n % NB == 0 ? x0 : n % NB == 1 ? x1 : n % NB == 2 ? x2 : x3) + wave * XB; };
+    f4 sum[RT][TT];
+#pragma unroll
+    for (int i = 0; i < RT; i++)
+#pragma unroll
+        for (int j = 0; j < TT; j++) sum[i][j] = f4{0, 0, 0, 0};
+    // four tiles of each wave, whole ones or those that there are
     auto unit = [&](auto whole, int u) {
+        constexpr bool all = decltype(whole)::value;
         uint32_t sc[4][RT];
         u4 c[4][RT];
+        auto tile = [&](int n) { return (u * 4 + n) * kWaves + wave; };
+        auto load_x = [&](int n) {  // half n % 2 of tile n / 2
+            const int b0 = tile(n / 2) * 4 + n % 2 * 2;
+            if (!all && b0 >= a.blocks) return;
+            const char *rows = x_rows + b0 * 64ll;
+#pragma unroll
+            for (int i = 0; i < PL; i++) {
+                uint32_t at = from[i];
+                // past the end: the first chunk, not used
+                if (!all && b0 + chunk(i) / 4 >= a.blocks) at -= chunk(i) * 16;
+                load_to_lds((Global)rows + at, buffer(n) + i * 1024);
+            }
+        };
 #pragma unroll
         for (int n = 0; n < 4; n++) {
-            const int64_t tk = decltype(whole)::value ? u * 4 + n : min(u * 4 + n, a.tiles_k - 1);
+            const int tk = tile(n);
+            if (!all && tk >= a.tiles_k) break;
 #pragma unroll
             for (int i = 0; i < RT; i++) {
                 c[n][i] = __builtin_nontemporal_load(
-                    (const u4 *)(codes[i] + tk * 1024 + (uint32_t)lane * 16));
-                sc[n][i] = *(const uint32_t *)(scales[i] + tk * 64 + (uint32_t)col * 4);
+                    (const u4 *)(codes[i] + tk * 1024ll + (uint32_t)lane * 16));
+                sc[n][i] = *(const uint32_t *)(scales[i] + tk * 64ll + (uint32_t)col * 4);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int n = 0; n < 4; n++) {
-            const int tk = u * 4 + n;
-            // (not the last tile again: an infinity in it, times zero, is NaN)
-            if (!decltype(whole)::value && tk >= a.tiles_k) break;
-            V b[4];
+        for (int n = 0; n < NB; n++) load_x(n);
+        auto half = [&](auto at) {
+            constexpr int n = decltype(at)::value;
+            const int b0 = tile(n / 2) * 4 + n % 2 * 2;
+            if (!all && b0 >= a.blocks) return;
+            wait_loads<all ? (NB - 1 < 7 - n ? NB - 1 : 7 - n) * PL : 0>();
 #pragma unroll
-            for (int k = 0; k < 4; k++)
-                // blocks beyond the matrix: x is zero there, whatever lies behind it
-                b[k] = decltype(whole)::value || tk * 4 + k < a.blocks
-                           ? *(const V *)(x + tk * kTileCols + k * 32) : V{};
+            for (int k = 0; k < 2; k++) {
+                V b[TT];
 #pragma unroll
-            for (int i = 0; i < RT; i++)
+                for (int j = 0; j < TT; j++) {  // (rows beyond the tokens hold anything)
+                    b[j] = *(const V *)(buffer(n) + (j * 16 + col) * 128 +
+                                        ((k * 4 + g) ^ (col >> 1)) * 16);
+                    // blocks beyond the matrix: zeros, as the weights are
+                    if (!all && b0 + k >= a.blocks) b[j] = V{};
+                }
+                constexpr int q0 = n % 2 * 2;
 #pragma unroll
-                for (int k = 0; k < 4; k++)
-                    sum[i] = mfma16(values_of<T>(c[n][i][k], scale_of(sc[n][i] >> (8 * k) & 255)),
-                                    b[k], sum[i]);
-        }
+                for (int i = 0; i < RT; i++) {
+                    const V w = values_of<T>(c[n / 2][i][q0 + k],
+                                             scale_of(sc[n / 2][i] >> (8 * (q0 + k)) & 255));
+#pragma unroll
+                    for (int j = 0; j < TT; j++) sum[i][j] = mfma16(w, b[j], sum[i][j]);
+                }
+            }
+            __builtin_amdgcn_s_waitcnt(kWaitLds);  // the buffer has been read
+            if (n + NB < 8) load_x(n + NB);
+        };
+        half(Const<0>{});
+        half(Const<1>{});
+        half(Const<2>{});
+        half(Const<3>{});
+        half(Const<4>{});
+        half(Const<5>{});
+        half(Const<6>{});
+        half(Const<7>{});
     };
-    const int whole = a.blocks / 16;
-    int u = wave;
-    for (; u < whole; u += kWaves) unit(Const<1>{}, u);
-    if (u * 4 < a.tiles_k) unit(Const<0>{}, u);
+    const int whole = a.blocks / (16 * kWaves);
+    int u = 0;
+    for (; u < whole; u++) unit(Const<1>{}, u);
+    if (u * 4 * kWaves < a.tiles_k) unit(Const<0>{}, u);
     // the second half's sums are added to the first's, then those to one another
+    static_assert(H * RT * TT * 1024 <= kWaves * XB, "");
+    f4 *part = (f4 *)x0 + lane;
+    auto place = [&](int wave, int i) { return part + (wave * RT * TT + i) * 64; };
+    __syncthreads();
     if (wave >= H)
 #pragma unroll
-        for (int i = 0; i < RT; i++) part[wave - H][i][lane] = sum[i];
+        for (int i = 0; i < RT * TT; i++) *place(wave - H, i) = sum[i / TT][i % TT];
     __syncthreads();
     if (wave < H)
 #pragma unroll
-        for (int i = 0; i < RT; i++) part[wave][i][lane] += sum[i];
+        for (int i = 0; i < RT * TT; i++) *place(wave, i) += sum[i / TT][i % TT];
     __syncthreads();
-    for (int i = wave; i < RT; i += kWaves) {
-        f4 y = part[0][i][lane];
+    for (int i = wave; i < RT * TT; i += kWaves) {
+        f4 y = *place(0, i);
 #pragma unroll
-        for (int w = 1; w < H; w++) y += part[w][i][lane];
-        if (col < a.tokens) store_four<T>(a, col, (tile0 + i) * 16 + g * 4, y);
+        for (int w = 1; w < H; w++) y += *place(w, i);
+        const int t = t0 + i % TT * 16 + col;
+        if (t < min(a.tokens, t0 + 4 * XL)) store_four<T>(a, t, (tile0 + i / TT) * 16 + g * 4, y);
     }
 }
 
-typedef const __attribute__((address_space(1))) char *Global;
-__device__ void load_to_lds(Global from, char *to) {
-    __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, 0,
-                                     0);
-}
-constexpr int kWaitLoads = 0x0F70;  // s_waitcnt: no load or store outstanding
-
-// A barrier behind which the workgroup's LDS reads and all but the wave's last N loads are
-// done. (__syncthreads would wait for all of them. The empty statements keep the compiler from
-// moving memory accesses across, the others from working out scales that have not arrived.)
+// The same with a barrier, behind which the workgroup's LDS reads are done too. (__syncthreads
+// would wait for all loads.)
 template <int N>
 __device__ void barrier_after_loads() {
     static_assert(N < 64, "");
@@ -145,8 +221,7 @@ __device__ void barrier_after_loads() {
 // More tokens, with too few tiles of 256 by 128. 16 RT WN rows and 16 TT WT tokens a workgroup,
 // of KS groups of WN by WT waves, group n with every KS-th step of 128 columns from n on. A wave
 // has its weights in registers, converted once for all of its tokens; a step of x is in LDS for
-// its group, loaded there directly, S - 1 of the group's steps ahead. Chunk c (of eight
-// elements) of row t lies at c ^ (t mod 16), which spreads the rows of a column over the banks.
+// its group, loaded there directly, S - 1 of the group's steps ahead, its chunks placed as above.
 // Bound by the loads' latency and LDS.
 template <typename T, int WN, int WT, int RT, int TT, int S, int KS>
 __global__ __launch_bounds__(64 * WN * WT * KS, (WN * WT * KS > 8 ? WN * WT * KS / 4 : 2))
@@ -262,11 +337,20 @@ void tile_kernel(Linear4Args a) {
         step(Const<2>{}, n + 2);
         if constexpr (S > 3) step(Const<3>{}, n + 3);
     };
-    issue(Const<0>{}, Const<1>{}, 0);
-    issue(Const<1>{}, Const<1>{}, 1);
-    if constexpr (S > 3) issue(Const<2>{}, Const<1>{}, 2);
     int n = 0;
-    for (; n + 2 * S - 1 <= whole; n += S) each(middle, n);
+    if (whole >= 2 * S - 1) {
+        issue(Const<0>{}, Const<0>{}, 0);
+        issue(Const<1>{}, Const<0>{}, 1);
+        if constexpr (S > 3) issue(Const<2>{}, Const<0>{}, 2);
+        do {
+            each(middle, n);
+            n += S;
+        } while (n + 2 * S - 1 <= whole);
+    } else {
+        issue(Const<0>{}, Const<1>{}, 0);
+        issue(Const<1>{}, Const<1>{}, 1);
+        if constexpr (S > 3) issue(Const<2>{}, Const<1>{}, 2);
+    }
     for (; n < steps; n += S) each(last, n);
     if constexpr (KS > 1) {  // the groups' sums are added to the first's, in order
         static_assert((KS - 1) * W * RT * TT * 1024 <= KS * LB, "");
@@ -411,42 +495,50 @@ __global__ __launch_bounds__(256, 2) void big_kernel(Linear4Args a) {
     }
 }
 
-template <typename T, int RT>
+template <typename T, int RT, int XL, int NB>
 hipError_t launch_stream(const Linear4Args &a, hipStream_t s) {
     Linear4Args copy = a;
     void *args[] = {&copy};
-    return hipLaunchKernel((const void *)stream_kernel<T, RT>, dim3((a.tiles_n + RT - 1) / RT),
-                           dim3(64 * kWaves), args, 0, s);
+    const dim3 grid((uint32_t)((a.tiles_n + RT - 1) / RT) * ((a.tokens + 4 * XL - 1) / (4 * XL)));
+    return hipLaunchKernel((const void *)stream_kernel<T, RT, XL, NB>, grid, dim3(64 * kWaves),
+                           args, 0, s);
 }
 
-// Up to 16 tokens. (4096 columns, one token: 4096 rows 4.4 us with RT 1, 5.2 with 2; 16384 rows
-// 10.2, 9.2, and 11.7 with 4. 16 tokens: 4096 rows 6.8, 7.6, 9.7; 8192 rows 10.9, 8.7, 10.2;
-// 32768 rows 34.7, 22.2, 19.2.)
+// Up to 16 tokens. (4096 columns, one token: 4096 rows 4.3 us with RT 1 and XL 2, 5.2 with RT 2,
+// 4.5 with XL 4; 16384 rows 9.0 with RT 2, 9.7 with 4. 16 tokens: 4096 rows 4.7 with RT 1, 5.9
+// with 2; 6144 rows 7.3, 6.3; 16384 rows 10.3 with RT 2, 9.6 with 4; 32768 rows 17.8, 17.2. With
+// NB the other of 2 and 4: 4 to 8 % longer, one where RT and XL are 2 and 1.)
 template <typename T>
 hipError_t launch_few(const Linear4Args &a, hipStream_t s) {
-    if (a.tiles_n <= 256) return launch_stream<T, 1>(a, s);
-    if (a.tiles_n < 1024 || a.tokens <= 8) return launch_stream<T, 2>(a, s);
-    return launch_stream<T, 4>(a, s);
+    const bool eight = a.tokens <= 8;
+    if (a.tiles_n <= 256)
+        return eight ? launch_stream<T, 1, 2, 4>(a, s) : launch_stream<T, 1, 4, 2>(a, s);
+    if (a.tiles_n < (eight ? 2048 : 1024))
+        return eight ? launch_stream<T, 2, 2, 4>(a, s) : launch_stream<T, 2, 4, 4>(a, s);
+    return launch_stream<T, 4, 4, 4>(a, s);
 }
 
-// More: the tile whose rounds of 256 workgroups (one a compute unit) take least, by the times
+// More: the kernel whose rounds of 256 workgroups (one a compute unit) take least, by the times
 // measured with 4096 columns, us: a first part and one for every round, but no less than a
 // compute unit takes for one alone.
-struct TileCost {
+struct Cost {
     int rows, tokens;
     float base, round, least;
 };
-constexpr TileCost kTiles[] = {
-    {32, 32, 2, 7, 9},                         // 64 tokens, 4096 rows: 8.9 (the next 11.0)
-    {64, 32, 4, 7, 11},                        // 128 tokens, 4096 rows: 11.2 (14.6, 19.4)
-    {128, 64, 1, 19, 20},                      // 256 tokens, 8192 rows: 22.4 (26.9, 32.4)
-    {128, 64, 8, 13.4, 31},                    // 1024 tokens, 4096 rows: 34.8 (40.5, 75.6)
+constexpr Cost kCosts[] = {
+    {16, 32, 2.6, 3.7, 6},                     // 32 tokens, 4096 rows: 6.0 (the next 6.8)
+    {32, 32, 3.5, 4.8, 7},                     // 32 tokens, 8192 rows: 8.1 (10.0 and 10.0)
+    {64, 32, 0.5, 10, 9.3},                    // 128 tokens, 4096 rows: 9.2 (11.5, 12.4)
+    {64, 64, 2.2, 13, 12.5},                   // 64 tokens, 16384 rows: 15.3 (20.4, 16.6)
+    {64, 32, 3.5, 7, 10.5},                    // 32 tokens, 32768 rows: 19.3 (21.1, 23.7)
+    {128, 64, 1.5, 18, 19},                    // 256 tokens, 8192 rows: 21.3 (27.1, 32.3)
+    {128, 64, 8.3, 13.4, 31},                  // 1024 tokens, 4096 rows: 35.1 (37.5, 75.6)
     {kBigRows, kBigTokens, 0, 49.5, 78}};      // 4096 tokens, 4096 rows: 100 (118)
-int choose_tile(const Linear4Args &a) {
+int choose(const Linear4Args &a) {
     int best = 0;
     float least = 0;
-    for (int i = 0; i < 5; i++) {
-        const TileCost &t = kTiles[i];
+    for (int i = 0; i < (int)(sizeof(kCosts) / sizeof(Cost)); i++) {
+        const Cost &t = kCosts[i];
         const int64_t groups = (int64_t)((a.rows + t.rows - 1) / t.rows) *
                                ((a.tokens + t.tokens - 1) / t.tokens);
         const float us = fmaxf(t.base + t.round * (float)((groups + 255) / 256), t.least);
@@ -458,11 +550,14 @@ int choose_tile(const Linear4Args &a) {
 template <typename T>
 hipError_t launch(const Linear4Args &a, hipStream_t s) {
     if (a.tokens <= 16) return launch_few<T>(a, s);
-    switch (choose_tile(a)) {
-        case 0: return launch_tile<T, 2, 1, 1, 2, 4, 4>(a, s);
-        case 1: return launch_tile<T, 4, 1, 1, 2, 4, 2>(a, s);
-        case 2: return launch_tile<T, 4, 1, 2, 4, 4, 2>(a, s);
-        case 3: return launch_tile<T, 4, 1, 2, 4, 3, 1>(a, s);
+    switch (choose(a)) {
+        case 0: return launch_stream<T, 1, 8, 2>(a, s);
+        case 1: return launch_stream<T, 2, 8, 2>(a, s);
+        case 2: return launch_stream<T, 4, 8, 4>(a, s);
+        case 3: return launch_stream<T, 4, 16, 2>(a, s);
+        case 4: return launch_tile<T, 4, 1, 1, 2, 4, 2>(a, s);
+        case 5: return launch_tile<T, 4, 1, 2, 4, 4, 2>(a, s);
+        case 6: return launch_tile<T, 4, 1, 2, 4, 3, 1>(a, s);
         default:
             return launch_kernel(big_kernel<T>, (int64_t)((a.rows + kBigRows - 1) / kBigRows) *
                                                     ((a.tokens + kBigTokens - 1) / kBigTokens),
