@@ -214,18 +214,21 @@ class Cache(NamedTuple):
         if code is None:
             raise ValueError(f"{dtype}: float16 or bfloat16")
         index = _gpu(self.k, "k")
-        n, half, at = _rows(self.k, 1, "k")
-        for t, row, name in ((self.v, half, "v"), (self.k_scale, half // 16, "k_scale"),
-                             (self.v_scale, half // 16, "v_scale")):
-            rows_n, rows_row, rows_at = _rows(t, 1, name)
-            if rows_n != n or rows_row != row or t.dtype != torch.uint8 \
+        codes = self.k.shape
+        if len(codes) != 4 or codes[3] not in (32, 64):
+            raise ValueError(f"k is {tuple(codes)}: four dimensions, rows of 32 or 64")
+        *n, half = codes
+        scales, at = (*n, half // 16), []
+        for t, shape, name in ((self.k, codes, "k"), (self.v, codes, "v"),
+                               (self.k_scale, scales, "k_scale"),
+                               (self.v_scale, scales, "v_scale")):
+            stride = t.stride()
+            if t.shape != shape or stride[3] != 1 or t.dtype != torch.uint8 \
                     or t.get_device() != index:
-                raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}, k "
-                                 f"{self.k.dtype} {tuple(self.k.shape)} on {self.k.device}: uint8, "
-                                 "16 bytes of codes to one of scales")
-            at += rows_at
-        if self.k.dtype != torch.uint8 or half not in (32, 64):
-            raise ValueError(f"k is {self.k.dtype}, rows of {half}: uint8, rows of 32 or 64")
+                raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}, strides {stride}, on "
+                                 f"{t.device}, expected adjacent uint8 {tuple(shape)} on "
+                                 f"{self.k.device}")
+            at += t.data_ptr(), *stride[:3]
         both = _empty(self.k, (2, *n, 2 * half), dtype, stream)
         k, v = both.unbind()
         _call(index, stream, lib().tas_fp4_cache_values,

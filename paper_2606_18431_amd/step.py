@@ -313,16 +313,16 @@ class Step:
         return k.data_ptr(), v.data_ptr(), k0, k1, k2, v0, v1, v2
 
     def _cache_fp4(self, cache):
+        codes, scales, index, byte = self.codes_shape, self.scales_shape, self.index, torch.uint8
         got = []
-        for t, shape in ((cache.k, self.codes_shape), (cache.v, self.codes_shape),
-                         (cache.k_scale, self.scales_shape), (cache.v_scale, self.scales_shape)):
-            s0, s1, s2, s3 = t.stride() if t.dim() == 4 else (0, 0, 0, 0)
-            if t.dtype != torch.uint8 or t.get_device() != self.index or t.shape != shape \
-                    or s3 != 1:
+        for t, shape in ((cache.k, codes), (cache.v, codes), (cache.k_scale, scales),
+                         (cache.v_scale, scales)):
+            stride = t.stride()
+            if t.shape != shape or stride[3] != 1 or t.dtype != byte or t.get_device() != index:
                 raise ValueError(f"the cache holds {t.dtype} {tuple(t.shape)}, strides "
-                                 f"{t.stride()}, on {t.device}, expected adjacent uint8 {shape} "
+                                 f"{stride}, on {t.device}, expected adjacent uint8 {shape} "
                                  f"on {self.device}")
-            got += t.data_ptr(), s0, s1, s2
+            got += t.data_ptr(), *stride[:3]
         return got
 
     def _dtype(self, t, what):
