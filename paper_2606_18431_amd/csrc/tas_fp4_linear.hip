@@ -505,43 +505,55 @@ hipError_t launch_stream(const Linear4Args &a, hipStream_t s) {
 }
 
 // Up to 16 tokens. (4096 columns, one token: 4096 rows 4.3 us with RT 1 and XL 2, 5.2 with RT 2,
-// 4.5 with XL 4; 16384 rows 9.0 with RT 2, 9.7 with 4. 16 tokens: 4096 rows 4.7 with RT 1, 5.9
-// with 2; 6144 rows 7.3, 6.3; 16384 rows 10.3 with RT 2, 9.6 with 4; 32768 rows 17.8, 17.2. With
-// NB the other of 2 and 4: 4 to 8 % longer, one where RT and XL are 2 and 1.)
+// 4.5 with XL 4; 16384 rows 9.0 with RT 2, 9.7 with 4; 32768 14.7, 16.9. 16 tokens: 4096 rows 4.7
+// with RT 1, 5.9 with 2; 6144 rows 7.3, 6.3; 16384 rows 10.6 with RT 2, 9.7 with 4; 32768 rows
+// 17.8, 17.2, but of 8192 columns 32.2, 38.6: with RT 4 a compute unit has one workgroup, and a
+// wave's second unit of columns waits. With NB the other of 2 and 4: 4 to 8 % longer, or as long.)
 template <typename T>
 hipError_t launch_few(const Linear4Args &a, hipStream_t s) {
-    const bool eight = a.tokens <= 8;
-    if (a.tiles_n <= 256)
-        return eight ? launch_stream<T, 1, 2, 4>(a, s) : launch_stream<T, 1, 4, 2>(a, s);
-    if (a.tiles_n < (eight ? 2048 : 1024))
-        return eight ? launch_stream<T, 2, 2, 4>(a, s) : launch_stream<T, 2, 4, 4>(a, s);
+    if (a.tokens <= 8)
+        return a.tiles_n <= 256 ? launch_stream<T, 1, 2, 4>(a, s) : launch_stream<T, 2, 2, 4>(a, s);
+    if (a.tiles_n <= 256) return launch_stream<T, 1, 4, 2>(a, s);
+    if (a.tiles_n < 1024 || a.tiles_k > 4 * kWaves) return launch_stream<T, 2, 4, 4>(a, s);
     return launch_stream<T, 4, 4, 4>(a, s);
 }
 
 // More: the kernel whose rounds of 256 workgroups (one a compute unit) take least, by the times
-// measured with 4096 columns, us: a first part and one for every round, but no less than a
-// compute unit takes for one alone.
+// measured with 1024 to 16384 columns, us: a first part, one for every round and one for every
+// round and 1024 columns; but no less than one workgroup takes for its columns, where two on a
+// compute unit hide one another's waits.
 struct Cost {
     int rows, tokens;
-    float base, round, least;
+    float base, round, columns, alone;
 };
 constexpr Cost kCosts[] = {
-    {16, 32, 2.6, 3.7, 6},                     // 32 tokens, 4096 rows: 6.0 (the next 6.8)
-    {32, 32, 3.5, 4.8, 7},                     // 32 tokens, 8192 rows: 8.1 (10.0 and 10.0)
-    {64, 32, 0.5, 10, 9.3},                    // 128 tokens, 4096 rows: 9.2 (11.5, 12.4)
-    {64, 64, 2.2, 13, 12.5},                   // 64 tokens, 16384 rows: 15.3 (20.4, 16.6)
-    {64, 32, 3.5, 7, 10.5},                    // 32 tokens, 32768 rows: 19.3 (21.1, 23.7)
-    {128, 64, 1.5, 18, 19},                    // 256 tokens, 8192 rows: 21.3 (27.1, 32.3)
-    {128, 64, 8.3, 13.4, 31},                  // 1024 tokens, 4096 rows: 35.1 (37.5, 75.6)
-    {kBigRows, kBigTokens, 0, 49.5, 78}};      // 4096 tokens, 4096 rows: 100 (118)
+    // 4096 columns: 32 tokens, 4096 rows 6.0 (the next 6.8)
+    {16, 32, 2.1f, 0.3f, 0.9f, 0},
+    // 32 tokens, 8192 rows 8.1 (10.0 and 10.0); 64 tokens, 4096 rows, 8192 columns 11.5 (15.7)
+    {32, 32, 3.0f, 0, 1.24f, 0},
+    // 128 tokens, 4096 rows 9.2 (11.5, 12.4, 10.5)
+    {64, 32, 0.5f, 2.2f, 1.75f, 0},
+    // 64 tokens, 16384 rows 15.3 (20.7, 16.6)
+    {64, 64, 1.5f, 3, 2.5f, 0},
+    // 32 tokens, 32768 rows 19.3 (21.1, 23.7)
+    {64, 32, 3.2f, 0.2f, 1.75f, 0},
+    // 256 tokens, 8192 rows 21.3 (27.1, 32.3)
+    {128, 64, 1.5f, 4, 3.45f, 0},
+    // 1024 tokens, 4096 rows 35.1 (37.5, 75.6)
+    {128, 64, 8.3f, 0, 3.35f, 7.7f},
+    // 4096 tokens, 4096 rows 100 (118)
+    {kBigRows, kBigTokens, 3, 0, 11.9f, 19.5f}};
 int choose(const Linear4Args &a) {
     int best = 0;
     float least = 0;
+    const float columns = (float)a.blocks / 32;
     for (int i = 0; i < (int)(sizeof(kCosts) / sizeof(Cost)); i++) {
         const Cost &t = kCosts[i];
         const int64_t groups = (int64_t)((a.rows + t.rows - 1) / t.rows) *
                                ((a.tokens + t.tokens - 1) / t.tokens);
-        const float us = fmaxf(t.base + t.round * (float)((groups + 255) / 256), t.least);
+        const float rounds = (float)((groups + 255) / 256);
+        const float us = fmaxf(t.base + rounds * (t.round + t.columns * columns),
+                               t.alone * columns);
         if (!i || us < least) best = i, least = us;
     }
     return best;
