@@ -221,8 +221,8 @@ __device__ void barrier_after_loads() {
 // More tokens, with too few tiles of 256 by 128. 16 RT WN rows and 16 TT WT tokens a workgroup,
 // of KS groups of WN by WT waves, group n with every KS-th step of 128 columns from n on. A wave
 // has its weights in registers, converted once for all of its tokens; a step of x is in LDS for
-// its group, loaded there directly, S - 1 of the group's steps ahead, its chunks placed as above.
-// Bound by the loads' latency and LDS.
+// its group, loaded there directly, S - 1 of the group's steps ahead. Chunk c (of eight
+// elements) of row t lies at c ^ (t mod 16). Bound by the loads' latency and LDS.
 template <typename T, int WN, int WT, int RT, int TT, int S, int KS>
 __global__ __launch_bounds__(64 * WN * WT * KS, (WN * WT * KS > 8 ? WN * WT * KS / 4 : 2))
 void tile_kernel(Linear4Args a) {
@@ -539,9 +539,11 @@ constexpr Cost kCosts[] = {
     {64, 32, 3.2f, 0.2f, 1.75f, 0},
     // 256 tokens, 8192 rows 21.3 (27.1, 32.3)
     {128, 64, 1.5f, 4, 3.45f, 0},
-    // 1024 tokens, 4096 rows 35.1 (37.5, 75.6)
-    {128, 64, 8.3f, 0, 3.35f, 7.7f},
-    // 4096 tokens, 4096 rows 100 (118)
+    // 1024 tokens, 4096 rows 34.4 (39.2, 40.5); three stages in LDS instead of four 36.0
+    {128, 64, 3.5f, 0, 3.85f, 4.9f},
+    // 2048 tokens, 4096 rows 57.5 (65.3, 81.5)
+    {256, 64, 4.5f, 0, 6.6f, 10.3f},
+    // 1024 tokens, 16384 rows 97.8 (109.8)
     {kBigRows, kBigTokens, 3, 0, 11.9f, 19.5f}};
 int choose(const Linear4Args &a) {
     int best = 0;
@@ -569,7 +571,8 @@ hipError_t launch(const Linear4Args &a, hipStream_t s) {
         case 3: return launch_stream<T, 4, 16, 2>(a, s);
         case 4: return launch_tile<T, 4, 1, 1, 2, 4, 2>(a, s);
         case 5: return launch_tile<T, 4, 1, 2, 4, 4, 2>(a, s);
-        case 6: return launch_tile<T, 4, 1, 2, 4, 3, 1>(a, s);
+        case 6: return launch_tile<T, 4, 1, 2, 4, 4, 1>(a, s);
+        case 7: return launch_tile<T, 8, 1, 2, 4, 3, 1>(a, s);
         default:
             return launch_kernel(big_kernel<T>, (int64_t)((a.rows + kBigRows - 1) / kBigRows) *
                                                     ((a.tokens + kBigTokens - 1) / kBigTokens),
