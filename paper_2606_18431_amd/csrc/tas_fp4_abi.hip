@@ -374,6 +374,7 @@ int tas_fp4_linear(const tas_linear_fp4 *a, void *stream) {
     k.tiles_n = (int32_t)w.tiles_n;
     k.tiles_k = (int32_t)w.tiles_k;
     k.y_fours = a->rows % 4 == 0 && a->y_stride % 4 == 0 && (uintptr_t)a->y % 8 == 0;
+    k.x_much = a->tokens / 4 > a->rows;  // (an element of x has four times the bits)
     return done(launch_linear4(k, a->dtype, (hipStream_t)stream));
 }
 

@@ -57,6 +57,7 @@ struct Linear4Args {
     int32_t tokens, rows, blocks;  // blocks of a row
     int32_t tiles_n, tiles_k;
     int32_t y_fours;  // y can be written four elements at once
+    int32_t x_much;   // x has more than 16 times the weights' bytes
 };
 
 // Return hipSuccess or the launch's error.

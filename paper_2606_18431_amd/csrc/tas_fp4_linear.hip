@@ -44,6 +44,23 @@ __device__ void store_four(const Linear4Args &a, int64_t t, int n, f4 x) {
     }
 }
 
+// A workgroup's part of the product. The eight dies take consecutive workgroups in turn, and each
+// has an L2 of its own. Where x is much the larger side a die gets adjacent parts, so that x is
+// fetched by one die, not by all that have some of its rows of W. (4096 columns, 8192 tokens, 100
+// rows 34.5 us without, 16.0 so; 2000 tokens, 300 rows 18.4, 13.6; 8000 tokens, 1000 rows 61.3,
+// 57.0. With sides of like size up to 7 % longer: 1024 tokens, 16384 rows 98.1, 105.2.)
+struct Place {
+    int n, t;  // of groups_n by some number
+};
+__device__ Place place_of(const Linear4Args &a, uint32_t groups_n) {
+    uint32_t at = blockIdx.x;
+    if (a.x_much) {
+        const uint32_t die = at & 7, each = gridDim.x >> 3, more = gridDim.x & 7;
+        at = die * each + min(die, more) + (at >> 3);
+    }
+    return {(int)(at % groups_n), (int)(at / groups_n)};
+}
+
 typedef const __attribute__((address_space(1))) char *Global;
 __device__ void load_to_lds(Global from, char *to) {
     __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, 0,
@@ -86,9 +103,8 @@ void stream_kernel(Linear4Args a) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
-    const uint32_t groups_n = (a.tiles_n + RT - 1) / RT, at_t = blockIdx.x / groups_n;
-    const int tile0 = (blockIdx.x - at_t * groups_n) * RT;
-    const int t0 = at_t * 4 * XL;
+    const Place at = place_of(a, (a.tiles_n + RT - 1) / RT);
+    const int tile0 = at.n * RT, t0 = at.t * 4 * XL;
     const char *codes[RT], *scales[RT];
 #pragma unroll
     for (int i = 0; i < RT; i++) {  // (of tiles that there are not, the last one's)
@@ -238,10 +254,8 @@ void tile_kernel(Linear4Args a) {
     const int wave = all % W, group = all / W;
     const int wn = wave % WN, wt = wave / WN;
     const int col = lane & 15, g = lane >> 4;
-    const uint32_t groups_n = (a.tiles_n + RT * WN - 1) / (RT * WN);
-    const uint32_t at_t = blockIdx.x / groups_n;
-    const int tile0 = ((blockIdx.x - at_t * groups_n) * WN + wn) * RT;
-    const int t0 = at_t * BT;
+    const Place at = place_of(a, (a.tiles_n + RT * WN - 1) / (RT * WN));
+    const int tile0 = (at.n * WN + wn) * RT, t0 = at.t * BT;
     const char *codes[RT], *scales[RT];
 #pragma unroll
     for (int i = 0; i < RT; i++) {  // (of tiles that there are not, the last one's)
@@ -405,9 +419,8 @@ __global__ __launch_bounds__(256, 2) void big_kernel(Linear4Args a) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
-    const uint32_t groups_n = (a.rows + kBigRows - 1) / kBigRows, at_t = blockIdx.x / groups_n;
-    const int tile0 = (blockIdx.x - at_t * groups_n) * (kBigRows / 16) + wave * RT;
-    const int t0 = at_t * kBigTokens;
+    const Place at = place_of(a, (a.rows + kBigRows - 1) / kBigRows);
+    const int tile0 = at.n * (kBigRows / 16) + wave * RT, t0 = at.t * kBigTokens;
     const char *codes[RT], *scales[RT];
 #pragma unroll
     for (int i = 0; i < RT; i++) {  // (of tiles that there are not, the last one's)

@@ -532,7 +532,7 @@ def test_linear_many_of_both(torch, name, tokens, rows, cols):
     (8, 4100, 4384), (16, 4100, 4384), (9, 100, 8224), (7, 100, 16512), (12, 16400, 4384),
     (3, 32800, 160), (32, 1000, 8224), (20, 4100, 4384), (40, 4200, 4384), (64, 8200, 4384),
     (63, 8200, 96), (100, 16400, 1120), (200, 8100, 1120), (200, 8100, 4384), (250, 8200, 4384),
-    (2040, 4090, 1120)])
+    (2040, 4090, 1120), (8190, 100, 4384), (1870, 300, 1120), (1700, 3, 64)])
 def test_linear_every_kernel(torch, name, tokens, rows, cols):
     """Rows enough for each number of them to a workgroup, columns that leave units of a wave
     whole, in part and empty."""
