@@ -68,7 +68,8 @@ __device__ int k_place(int y, int c) {
 // Up to 16 rows against a run of keys: each of the four waves takes every fourth 32 keys.
 // K goes straight into registers as the left operand: lane 16 g + r has the quarter g of key
 // r, so that the k-slots of step i stand for elements g D / 4 + 8 i + 0..7, for the queries
-// too. V goes through the wave's own LDS. Memory bound.
+// too. V goes through the wave's own LDS. Memory
+// bound: 256 decodes 99 us, 6.0 TB/s.
 template <typename T, int D>
 __device__ __forceinline__ void thin_item4(const Attn4Args &a, const Item &it, char *lds01,
                                            char *lds23, float (*stat)[kThinRows][2]) {
@@ -240,7 +241,8 @@ __device__ __forceinline__ void mix4() {
 // 128 rows against a run of keys, as the 16-bit kernel's wide item: 64 keys a step, 32 rows
 // to a wave, K and V of a step in LDS as 16-bit rows for all four waves, double buffered.
 // A wave fetches a run of 16 keys of K and of V a whole step before it converts them and
-// writes them to LDS.
+// writes them to LDS. Bound by matrix and vector work in turn: 11777 tokens of 16 chunks 803 us,
+// 1080 TFLOP/s, the matrix unit busy half of the time.
 template <typename T, int D>
 __device__ __forceinline__ void wide_item4(const Attn4Args &a, const Item &it, char *k0_lds,
                                            char *k1_lds, char *v0_lds, char *v1_lds,
