@@ -151,8 +151,10 @@ void stream_kernel(Linear4Args a) {
             if (!all && tk >= a.tiles_k) break;
 #pragma unroll
             for (int i = 0; i < RT; i++) {
-                c[n][i] = __builtin_nontemporal_load(
-                    (const u4 *)(codes[i] + tk * 1024ll + (uint32_t)lane * 16));
+                const u4 *at = (const u4 *)(codes[i] + tk * 1024ll + (uint32_t)lane * 16);
+                // (other tokens' workgroups read them too. 2000 tokens, 300 rows: 13.5 us with
+                // lines that are not kept, 10.6 so; 256 tokens, 16384 columns 41.7, 39.3)
+                c[n][i] = XL > 4 ? *at : __builtin_nontemporal_load(at);
                 sc[n][i] = *(const uint32_t *)(scales[i] + tk * 64ll + (uint32_t)col * 4);
             }
         }
