@@ -83,8 +83,8 @@ typedef struct tas_attention_fp4 {
 /* Norm, rotate and append as tas_step_append: queries go to q_out, in 32 bits and
  * rounded once; keys and values are rounded to four bits, keys to the codes that
  * the formula has in 64 bits (so that the order of their norm's sum does not
- * decide between two), and go to the token's slots. TAS_EINVAL: as there, or the cos, sin or weights overlap
- * an output. */
+ * decide between two), and go to the token's slots. TAS_EINVAL: as there, or the
+ * cos, sin or weights overlap an output. */
 int tas_fp4_append(tas_step *step, const tas_append_fp4 *a, void *stream);
 
 /* Attention as tas_step_attention over the values that the cache stands for. (A

@@ -68,8 +68,7 @@ __device__ int k_place(int y, int c) {
 // Up to 16 rows against a run of keys: each of the four waves takes every fourth 32 keys.
 // K goes straight into registers as the left operand: lane 16 g + r has the quarter g of key
 // r, so that the k-slots of step i stand for elements g D / 4 + 8 i + 0..7, for the queries
-// too. V goes through the wave's own LDS. Memory
-// bound: 256 decodes 99 us, 6.0 TB/s.
+// too. V goes through the wave's own LDS. Memory bound: 256 decodes 99 us, 6.0 TB/s.
 template <typename T, int D>
 __device__ __forceinline__ void thin_item4(const Attn4Args &a, const Item &it, char *lds01,
                                            char *lds23, float (*stat)[kThinRows][2]) {

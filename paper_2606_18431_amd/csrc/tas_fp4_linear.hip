@@ -121,7 +121,10 @@ void stream_kernel(Linear4Args a) {
     for (int i = 0; i < PL; i++)
         from[i] = (uint32_t)min(i * 8 + lrow, a.tokens - 1 - t0) * (uint32_t)(a.x_stride * 2) +
                   chunk(i) * 16;
-    auto buffer = [&](int n) { return (n % NB == 0 ? x0 : n % NB == 1 ? x1 : n % NB == 2 ? x2 : x3) + wave * XB; };
+    auto buffer = [&](int n) {
+        n %= NB;
+        return (n == 0 ? x0 : n == 1 ? x1 : n == 2 ? x2 : x3) + wave * XB;
+    };
     f4 sum[RT][TT];
 #pragma unroll
     for (int i = 0; i < RT; i++)
