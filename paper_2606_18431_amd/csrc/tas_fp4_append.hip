@@ -25,6 +25,7 @@
 
 #include "tas_fp4_convert.h"
 #include "tas_fp4_internal.h"
+#include "tas_step_norm.h"
 
 namespace tas_step_impl {
 namespace {
@@ -46,7 +47,11 @@ __device__ __forceinline__ float norm_and_turn(const AppendArgs &a, const void *
                                                const Part &p, const vec8<T> &x0,
                                                const vec8<T> &x1, float (&y0)[8], float (&y1)[8]) {
     using V = vec8<T>;
-    bool in_range = true;  // where roundings are relative ones
+    // Where nothing overflows, roundings are relative ones, but for what is lost below the
+    // smallest normal number: 2^-150 of an element before its weight (and of that, times an
+    // element), and of each product of the rotation.
+    bool in_range = true;
+    float lost = 0;
 #pragma unroll
     for (int e = 0; e < 8; e++) y0[e] = (float)x0[e], y1[e] = (float)x1[e];
     if (weight) {
@@ -58,15 +63,23 @@ __device__ __forceinline__ float norm_and_turn(const AppendArgs &a, const void *
         in_range = mean > 0x1p-100f && mean < 0x1p120f;
         const V w0 = *(const V *)((const T *)weight + p.c0 * 8);
         const V w1 = *(const V *)((const T *)weight + p.c1 * 8);
+        weighted<T>(y0, y1, f, w0, w1);
+        float most_w = 0;
 #pragma unroll
-        for (int e = 0; e < 8; e++) y0[e] *= f * (float)w0[e], y1[e] *= f * (float)w1[e];
+        for (int e = 0; e < 8; e++)
+            most_w = fmaxf(most_w, fmaxf(fabsf((float)w0[e]), fabsf((float)w1[e])));
+        in_range &= most_w < 0x1p120f;
+        lost = most_w * 0x1p-148f + 0x1p-143f;
     }
-    float most = 0;
+    float most = 0, most_turn = 1;
     if (p.turned) {
         const int64_t at = (int64_t)p.pos * (a.rot / 2) + p.i * 8;
         float c[8], s[8];
         *(f4 *)c = *(const f4 *)(a.cos + at), *(f4 *)(c + 4) = *(const f4 *)(a.cos + at + 4);
         *(f4 *)s = *(const f4 *)(a.sin + at), *(f4 *)(s + 4) = *(const f4 *)(a.sin + at + 4);
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            most_turn = fmaxf(most_turn, fmaxf(fabsf(c[e]), fabsf(s[e])));
         auto turn = [&](float &x, float &y, float c, float s) {
             const float u = x, v = y;
             most = fmaxf(most, fmaxf(fabsf(u * c) + fabsf(v * s), fabsf(v * c) + fabsf(u * s)));
@@ -87,8 +100,9 @@ __device__ __forceinline__ float norm_and_turn(const AppendArgs &a, const void *
 #pragma unroll
         for (int e = 0; e < 8; e++) most = fmaxf(most, fmaxf(fabsf(y0[e]), fabsf(y1[e])));
     }
-    in_range &= most == 0 || (most > 0x1p-100f && most < 0x1p120f);
-    return in_range ? most * 0x1p-19f : INFINITY;
+    if (!weight && !p.turned) return 0;
+    const float off = most * 0x1p-19f + (lost * most_turn + 0x1p-148f);
+    return in_range && most < 0x1p120f && off < 0x1p120f ? off : INFINITY;
 }
 
 // The same in 64 bits, to floats on the same side of every border; `to`: 16 floats of the

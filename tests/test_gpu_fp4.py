@@ -317,6 +317,78 @@ def test_append_keys_at_borders(torch, name, scale):
     assert bool((close < 2.0 ** -22).any())
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rot", [0, 64, 128])
+@pytest.mark.parametrize("size,weight", [(40, -98), (55, -99), (58, -60), (-10, 118), (-10, 121),
+                                         (-40, 90), (0, -126), (0, 121)])
+def test_append_weights_at_the_ends(torch, size, weight, rot, interleaved):
+    """Heads and norm weights of opposite sizes, whose quotient leaves the range of 32 bits
+    though the result does not; zeros among the elements. Keys have the codes of the formula
+    in 64 bits, queries its value within the roundings of 32."""
+    T = 150
+    b = Batch(24, [T], [T], 4, 2, 128)
+    cache = fp4.Cache.zeros(b.n_blocks, 2, 16, 128)
+    g = torch.Generator().manual_seed(14)
+    qkv = (2.0 ** size * torch.randn((T, 8, 128), generator=g)).bfloat16()
+    qkv[:, :, ::5] = 0
+    qkv[::2, :, 3::4] = 0  # whole rotated pairs, of both kinds, among them
+    qkv[::2, :, 2::4] = 0
+    w = torch.randint(1, 9, (2, 128), generator=g) / 4
+    w[:, 32:64] *= 2.0 ** weight
+    w[:, 96:] *= 2.0 ** weight
+    qw, kw = w.bfloat16()
+    cos = sin = None
+    if rot:
+        a = torch.rand((T, rot // 2), generator=g) * 6.3
+        a[::2] = torch.randint(0, 9, (T // 2, rot // 2), generator=g) * (math.pi / 4)
+        cos, sin = a.cos().cuda(), a.sin().cuda()
+    want, tol = append_reference(torch, b, qkv, cos, sin, qw, kw, 0.0, interleaved)
+    assert torch.isfinite(want).all()
+    q = b.step().append_fp4(qkv.cuda(), cache, cos, sin, q_weight=qw.cuda(), k_weight=kw.cuda(),
+                            eps=0.0, interleaved=interleaved)
+    k, _ = cache.values(torch.bfloat16)
+    page = torch.from_numpy(b.blocks[0]).long()[torch.arange(T) // 16]
+    got = k.double().cpu()[page, :, torch.arange(T) % 16]
+    keys, close = rounded(torch, want[:, 4:6], "bf16")
+    # 64 bits: some 150 roundings of 2^-53, on terms a few times the result
+    assert bool(((got == keys) | (close < 2.0 ** -40)).all())
+    # a bfloat16 is a multiple of 2^-133, and 32 bits of 2^-149
+    near(q, want[:, :4], tol[:, :4] + ROUND["bf16"] * want[:, :4].abs() * 1.01 + 2.0 ** -133,
+         "queries")
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("small,weight,turn", [(-133, 110, 0), (-125, 40, 60), (-100, 0, 100),
+                                               (-133, 127, 20), (-120, 60, 0)])
+def test_append_keys_lost_in_32_bits(torch, small, weight, turn, interleaved):
+    """Keys of which 32 bits keep a part or nothing at a stage, brought back by weights or
+    angles: the codes of the formula in 64 bits."""
+    T = 150
+    b = Batch(24, [T], [T], 2, 2, 128)
+    cache = fp4.Cache.zeros(b.n_blocks, 2, 16, 128)
+    g = torch.Generator().manual_seed(15)
+    qkv = torch.randn((T, 6, 128), generator=g, dtype=torch.float64)
+    w = (torch.randint(1, 9, (128,), generator=g) / 4).double()
+    for at in (slice(32, 64), slice(96, 128)):  # rotated with one another, or by themselves
+        qkv[:, :, at] *= 2.0 ** small
+        w[at] *= 2.0 ** min(weight, 126)
+    qkv[:, :, :32] *= 2.0 ** 55
+    qkv, w = qkv.bfloat16(), w.bfloat16()
+    a = torch.rand((T, 64), generator=g) * 6.3
+    cos, sin = 2.0 ** turn * a.cos(), 2.0 ** turn * a.sin()
+    want, _ = append_reference(torch, b, qkv, cos, sin, w, w, 0.0, interleaved)
+    assert torch.isfinite(want.float()).all()
+    b.step().append_fp4(qkv.cuda(), cache, cos.cuda(), sin.cuda(), q_weight=w.cuda(),
+                        k_weight=w.cuda(), eps=0.0, interleaved=interleaved)
+    k, _ = cache.values(torch.bfloat16)
+    page = torch.from_numpy(b.blocks[0]).long()[torch.arange(T) // 16]
+    got = k.double().cpu()[page, :, torch.arange(T) % 16]
+    keys, close = rounded(torch, want[:, 2:4], "bf16")
+    # 64 bits: some 150 roundings of 2^-53, on terms a few times the result
+    assert bool(((got == keys) | (close < 2.0 ** -40)).all())
+    assert (got[..., 32:64] != 0).any()  # (not all below the smallest scale's codes)
+
+
 # ------------------------------------------------------------------ attention
 
 
