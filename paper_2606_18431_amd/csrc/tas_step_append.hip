@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include "tas_step_internal.h"
+#include "tas_step_norm.h"
 
 namespace tas_step_impl {
 namespace {
@@ -58,7 +59,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
             const float f = 1.0f / sqrtf(sum / D + a.eps);
             const T *w = (const T *)(is_q ? a.q_weight : a.k_weight);
             const V w0 = *(const V *)(w + c0 * 8), w1 = *(const V *)(w + c1 * 8);
-            for (int e = 0; e < 8; e++) y0[e] *= f * (float)w0[e], y1[e] *= f * (float)w1[e];
+            weighted<T>(y0, y1, f, w0, w1);
         }
         if (turned) {
             const int64_t p = (int64_t)(r.prefix_len + own) * (a.rot / 2) + i * 8;

@@ -461,6 +461,36 @@ def test_append(torch, name, size, rot, interleaved):
                  name, rot, interleaved, norm=rot == 32, order="token")
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rot", [0, 64, 128])
+@pytest.mark.parametrize("size,weight", [(40, -98), (55, -99), (-10, 118), (-40, 90), (0, 121)])
+def test_append_weights_at_the_ends(torch, size, weight, rot, interleaved):
+    """Heads and norm weights of opposite sizes, whose quotient leaves the range of 32 bits
+    though the result does not; zeros among the elements."""
+    T = 150
+    b = Batch(24, [T], [T], 4, 2, 128)
+    g = torch.Generator().manual_seed(14)
+    qkv = (2.0 ** size * torch.randn((T, 8, 128), generator=g)).bfloat16()
+    qkv[:, :, ::5] = 0
+    w = torch.randint(1, 9, (2, 128), generator=g) / 4
+    w[:, 32:64] *= 2.0 ** weight
+    w[:, 96:] *= 2.0 ** weight
+    qw, kw = w.bfloat16()
+    cos = sin = None
+    if rot:
+        a = torch.rand((T, rot // 2), generator=g) * 6.3
+        cos, sin = a.cos().cuda(), a.sin().cuda()
+    want, tol = append_reference(torch, b, qkv, cos, sin, qw, kw, 0.0, interleaved)
+    # a bfloat16 is a multiple of 2^-133, and 32 bits of 2^-149
+    tol = tol + ROUND["bf16"] * want.abs() * 1.01 + 2.0 ** -133
+    k, v = caches(torch, b, torch.bfloat16, 8, poison=False)
+    q = b.step().append(qkv.cuda(), k, v, cos, sin, q_weight=qw.cuda(), k_weight=kw.cuda(),
+                        eps=0.0, interleaved=interleaved)
+    page = torch.from_numpy(b.blocks[0]).long()[torch.arange(T) // 16]
+    near(q, want[:, :4], tol[:, :4], "queries")
+    near(k.cpu()[page, :, torch.arange(T) % 16], want[:, 4:6], tol[:, 4:6], "keys")
+
+
 @pytest.mark.parametrize("heads,kv_heads", [(1, 1), (8, 1), (33, 3)])
 def test_append_heads(torch, heads, kv_heads):
     check_append(torch, Batch(22, [1, 3], [1, 60], heads, kv_heads, 128), "bf16", 128, False, True)
