@@ -18,7 +18,7 @@ Every operator runs in the HIP kernels of ``libtas_step.so``: no fallback. Calls
 enqueued on ``stream`` (a torch stream; default: the current one of the tensors' device),
 outputs are allocated there, and the tensors of a call may be dropped while it is under way.
 There is no backward pass: one through an output of inputs that require a gradient raises
-NotImplementedError.
+NotImplementedError, and so does a call with a dual tensor of forward-mode differentiation.
 """
 from __future__ import annotations
 
@@ -28,7 +28,7 @@ from typing import NamedTuple
 
 import torch
 
-from .step import DTYPES, _NoBackward, lib
+from .step import DTYPES, _NoBackward, _no_tangent, lib
 from .tas import TAS_OK, TasError
 
 _P, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
@@ -146,6 +146,7 @@ def _adjacent(t, n, row):
 def pack(x, *, stream=None):
     """(codes [..., n / 2], scales [..., n / 32]), uint8, of a float16 or bfloat16 tensor
     [..., n] of one to four dimensions, rows adjacent."""
+    _no_tangent(x)
     dtype = DTYPES.get(x.dtype)
     if dtype is None:
         raise ValueError(f"x is {x.dtype}: float16 or bfloat16")
@@ -299,6 +300,7 @@ def linear(x, weights, *, out=None, stream=None):
     """x W^T of float16 or bfloat16 tokens [tokens, cols] (adjacent rows, any stride that is
     a multiple of 8) and ``Weights`` of [rows, cols]: [tokens, rows] of x's type. The
     products are summed in 32 bits, in an order that depends on the sizes alone."""
+    _no_tangent(x, out)
     dtype, index, rows, cols = DTYPES.get(x.dtype), weights.index, weights.rows, weights.cols
     shape, stride = x.shape, x.stride()
     if dtype is None or len(shape) != 2 or x.get_device() != index or shape[1] != cols \

@@ -21,6 +21,7 @@ import struct
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 from .tas import TAS_OK, TasError, _stream
 
@@ -211,6 +212,15 @@ def tas_step_destroy(ctx):
         lib().tas_step_destroy(ctx)
 
 
+def _no_tangent(*tensors):
+    """Refuses dual tensors of forward-mode differentiation: a result without a tangent
+    would say that its derivative is zero."""
+    if forward_ad._current_level >= 0:
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise NotImplementedError("the serving step has no forward-mode derivative")
+
+
 class _NoBackward(torch.autograd.Function):
     """Outputs of inputs that require a gradient say so, and refuse to compute it."""
 
@@ -237,7 +247,8 @@ class Step:
     its calls reads its workspace: keep the step as long as the graph.
 
     There is no backward pass: where an input requires a gradient (and grad mode is on),
-    the output does too, and a backward pass through it raises NotImplementedError."""
+    the output does too, and a backward pass through it raises NotImplementedError. So does
+    a call with a dual tensor of forward-mode differentiation."""
 
     def __init__(self, n_new, kv_len, blocks, *, heads, kv_heads, head_dim, block_tokens,
                  n_blocks, prefix_first=None, prefix_len=None, prefix_blocks=None, causal=True,
@@ -433,6 +444,7 @@ class Step:
         ``cos``, ``sin``: float32 [positions, rot_dim / 2], rot_dim a multiple of
         16; None: no rotation. ``q_weight``, ``k_weight``: [head_dim], or both
         None. Keys and values go to the caches; returns the queries."""
+        _no_tangent(qkv, k_cache, v_cache, cos, sin, q_weight, k_weight, out)
         dtype = self._dtype(qkv, "qkv")
         qkv_p, qkv_s = self._rows(qkv, self.qkv_shape, qkv.dtype, "qkv")
         cache = self._cache(k_cache, v_cache, qkv.dtype)
@@ -450,6 +462,7 @@ class Step:
         prefix and context. ``scale``: default 1 / sqrt(head_dim). ``lse``: a
         float32 [tokens, heads] to receive the log of the sum of the exponentials.
         ``out`` may be ``q``. Returns [tokens, heads, head_dim]."""
+        _no_tangent(q, k_cache, v_cache, out, lse)
         dtype = self._dtype(q, "q")
         q_p, q_s = self._rows(q, self.q_shape, q.dtype, "q")
         cache = self._cache(k_cache, v_cache, q.dtype)
@@ -467,6 +480,7 @@ class Step:
                    eps=1e-6, interleaved=False, out=None, stream=None):
         """``append`` to a cache in four bits (``fp4.Cache``): keys and values are
         rounded to it. Returns the queries."""
+        _no_tangent(qkv, cos, sin, q_weight, k_weight, out)
         dtype = self._dtype(qkv, "qkv")
         qkv_p, qkv_s = self._rows(qkv, self.qkv_shape, qkv.dtype, "qkv")
         tensors = self._cache_fp4(cache)
@@ -481,6 +495,7 @@ class Step:
 
     def attention_fp4(self, q, cache, *, scale=None, out=None, lse=None, stream=None):
         """``attention`` over a cache in four bits (``fp4.Cache``)."""
+        _no_tangent(q, out, lse)
         dtype = self._dtype(q, "q")
         q_p, q_s = self._rows(q, self.q_shape, q.dtype, "q")
         tensors = self._cache_fp4(cache)

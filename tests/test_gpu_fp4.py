@@ -1045,6 +1045,53 @@ def test_a_backward_pass_is_refused(torch):
         fp4.pack(grad(x))
 
 
+def test_forward_mode_is_refused(torch):
+    """A dual tensor, whose tangent the result would not have, in every place of every call;
+    nothing is written then. Within a level, tensors without a tangent go on as ever."""
+    import torch.autograd.forward_ad as fwd
+
+    b = Batch(38, [1, 20], [30, 40], 4, 2, 64)
+    cache, _ = cache_of(torch, b, 9, poison=False)
+    wide = cache.values(torch.bfloat16)
+    s = b.step()
+    qkv = torch.randn((21, 8, 64), device="cuda", dtype=torch.bfloat16)
+    q, out = qkv[:, :4].contiguous(), torch.zeros((21, 4, 64), device="cuda", dtype=torch.bfloat16)
+    cos, sin = torch.rand((2, 60, 32), device="cuda")
+    w = torch.ones(64, device="cuda", dtype=torch.bfloat16)
+    lse = torch.zeros((21, 4), device="cuda")
+    m = fp4.Weights(*fp4.pack(torch.randn((6, 64), device="cuda", dtype=torch.bfloat16)))
+    y = torch.zeros((21, 6), device="cuda", dtype=torch.bfloat16)
+    norm = lambda c, n, qw, kw, o: dict(cos=c, sin=n, q_weight=qw, k_weight=kw, out=o)
+    calls = [(lambda t, *a: s.append_fp4(t, cache, **norm(*a)), [qkv, cos, sin, w, w, out]),
+             (lambda t, k, v, *a: s.append(t, k, v, **norm(*a)), [qkv, *wide, cos, sin, w, w, out]),
+             (lambda t, o, l: s.attention_fp4(t, cache, out=o, lse=l), [q, out, lse]),
+             (lambda t, k, v, o, l: s.attention(t, k, v, out=o, lse=l), [q, *wide, out, lse]),
+             (lambda t, o: fp4.linear(t, m, out=o), [q[:, 0], y]), (fp4.pack, [qkv])]
+    written = [*cache, *wide, out, lse, y]
+    before = [t.clone() for t in written]
+    for call, args in calls:
+        with fwd.dual_level():
+            for i, t in enumerate(args):
+                dual = fwd.make_dual(t, torch.ones_like(t))
+                with pytest.raises(NotImplementedError):
+                    call(*args[:i], dual, *args[i + 1:])
+                with torch.no_grad(), pytest.raises(NotImplementedError):
+                    call(*args[:i], dual, *args[i + 1:])
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, u) for t, u in zip(written, before))
+    for call, args in calls:
+        def run():
+            got = call(*args)
+            return [t.clone() for t in (got if isinstance(got, tuple) else (got,))]
+
+        want = run()
+        with fwd.dual_level():
+            got = run()
+        assert all(torch.equal(t, u) for t, u in zip(got, want))
+    with pytest.raises((NotImplementedError, RuntimeError)):
+        torch.func.jvp(lambda t: fp4.linear(t, m), (q[:, 0],), (q[:, 0],))
+
+
 # ------------------------------------------------------------------ the command
 
 
