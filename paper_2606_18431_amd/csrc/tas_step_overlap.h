@@ -6,9 +6,9 @@
 
 namespace tas_step_impl {
 
-// Rows of `row` adjacent chunks of 16 bytes, at base + i0 stride[0] + i1 stride[1] +
-// i2 stride[2] (chunks) for all 0 <= i < n. (In chunks, whose number stays below 2^60, sums
-// and differences of places cannot overflow.)
+// Rows of `row` adjacent units, at base + i0 stride[0] + i1 stride[1] + i2 stride[2] (units)
+// for all 0 <= i < n, none of them negative but base, an address of any 64 bits. The unit is the
+// caller's, the same on both sides: 16 bytes, two or one.
 struct Region {
     int64_t base, row;
     int64_t stride[3], n[3];
@@ -18,9 +18,11 @@ struct Region {
 // b - a is a sum of multiples: of every s from 0 to n - 1, of every t from 1 - n to 0, and
 // of 1 between the rows' lengths. Tried from the longest stride on; what the shorter ones
 // reach leaves a multiple or two of each where tensors are nested as usual. Past kTries
-// (strides that no usual tensors have) they count as overlapping.
+// (strides that no usual tensors have) they count as overlapping, and so do regions of kLongest
+// units, more than there are addresses: below it no sum or difference of places overflows.
 class Overlap {
     static constexpr int kTries = 1 << 14;
+    static constexpr int64_t kLongest = int64_t(1) << 60;
     struct Axis {
         int64_t stride, lo, hi;  // lo to hi times the stride
     };
@@ -38,6 +40,18 @@ class Overlap {
             }
         axes[n++] = {stride, lo, hi};
     }
+    // From the first unit of a region to behind the last.
+    static int64_t span(const Region &r) {
+        int64_t sum = r.row;
+        for (int i = 0; i < 3; i++) {
+            int64_t x;
+            if (sum >= kLongest || __builtin_mul_overflow(r.stride[i], r.n[i] - 1, &x) ||
+                x >= kLongest)
+                return kLongest;
+            sum += x;
+        }
+        return sum;
+    }
     static int64_t floor_div(int64_t x, int64_t y) { return x / y - (x % y < 0); }
     bool reached(int i, int64_t d) {
         if (d < least[i] || d > most[i]) return false;
@@ -53,13 +67,12 @@ class Overlap {
   public:
     bool operator()(const Region &a, const Region &b) {
         n = tries = 0;
-        int64_t end_a = a.base + a.row, end_b = b.base + b.row;
-        for (int i = 0; i < 3; i++) {
+        for (int i = 0; i < 3; i++)
             if (!a.n[i] || !b.n[i]) return false;
-            end_a += a.stride[i] * (a.n[i] - 1);
-            end_b += b.stride[i] * (b.n[i] - 1);
-        }
-        if (end_a <= b.base || end_b <= a.base) return false;
+        const int64_t span_a = span(a), span_b = span(b);
+        if (span_a >= kLongest || span_b >= kLongest) return true;
+        const uint64_t from_a = (uint64_t)b.base - (uint64_t)a.base, from_b = 0 - from_a;
+        if (from_a >= (uint64_t)span_a && from_b >= (uint64_t)span_b) return false;
         for (int i = 0; i < 3; i++) {
             add(a.stride[i], 0, a.n[i] - 1);
             add(b.stride[i], 1 - b.n[i], 0);
@@ -71,7 +84,7 @@ class Overlap {
             least[i] = least[i + 1] + axes[i].lo * axes[i].stride;
             most[i] = most[i + 1] + axes[i].hi * axes[i].stride;
         }
-        return reached(0, b.base - a.base);
+        return reached(0, (int64_t)from_a);
     }
 };
 

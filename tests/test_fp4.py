@@ -134,6 +134,32 @@ def test_refused_append(bound):
         assert refused(L.tas_fp4_append, bound, args(**apart, cache=cache(**c))), c
 
 
+def test_refused_strides_beyond_memory():
+    """Token strides whose places pass 64 bits, where two rows would be one (nothing runs: the
+    stride is refused before any launch); over 16-bit caches too."""
+    L = step.lib()
+    b, keep = step.make_batch([5], [20], [[0, 1]], heads=4, kv_heads=2, head_dim=64,
+                              block_tokens=16, n_blocks=4)
+    ctx = step.tas_step_create(b)
+    step.tas_step_attach(ctx, AT, step.tas_step_bytes(ctx))
+    wide = step.tas_cache(AT + (1 << 20), AT + (2 << 20), 2048, 1024, 64, 2048, 1024, 64)
+    rows_ = dict(q=AT + (8 << 20), q_stride=256, out=AT + (9 << 20), out_stride=256)
+    turn = dict(eps=1e-6, qkv=AT + (8 << 20), qkv_stride=512, q_out=AT + (9 << 20),
+                q_out_stride=256)
+    for stride in (1 << 62, (1 << 61) + 8, (1 << 63) - 8):
+        for kw in (dict(q_stride=stride), dict(out_stride=stride),
+                   dict(q_stride=stride, out_stride=stride, out=rows_["q"])):
+            a = dict(dtype=1, scale=0.125, **{**rows_, **kw})
+            assert refused(L.tas_fp4_attention, ctx, fp4.tas_attention_fp4(cache=cache(), **a)), kw
+            assert refused(L.tas_step_attention, ctx, step.tas_attention(cache=wide, **a)), kw
+        for kw in (dict(qkv_stride=stride), dict(q_out_stride=stride),
+                   dict(qkv_stride=stride, q_out_stride=stride, q_out=turn["qkv"])):
+            a = dict(dtype=1, **{**turn, **kw})
+            assert refused(L.tas_fp4_append, ctx, fp4.tas_append_fp4(cache=cache(), **a)), kw
+            assert refused(L.tas_step_append, ctx, step.tas_append(cache=wide, **a)), kw
+    step.tas_step_destroy(ctx)
+
+
 def test_unbound_steps_and_batches_that_cannot_be_appended():
     L = step.lib()
     b, keep = step.make_batch([1], [1], [[0]], heads=1, kv_heads=1, head_dim=64, block_tokens=16,

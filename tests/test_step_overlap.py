@@ -128,3 +128,23 @@ def test_caches(overlap):
     for p, w, (x, y, us) in zip(pairs, want, overlap(pairs)):
         assert x == y and (w is None or x == w), (p, w)
         assert us < 20000, (p, us)
+
+
+def test_places_beyond_64_bits(overlap):
+    """Strides and bases at the ends of 64 bits: nothing overflows (the sanitizer would end the
+    program), and regions longer than memory count as overlapping."""
+    top, row = 1 << 63, (1 << 40, 8, [8, 0, 0], [4, 1, 1])
+    pairs = [((0, 8, [1 << 62, 0, 0], [3, 1, 1]), row, 1),
+             ((0, 8, [top - 8, 0, 0], [3, 1, 1]), row, 1),
+             ((0, 8, [1 << 40, 0, 0], [1 << 24, 1, 1]), row, 1),
+             ((0, 8, [1 << 59, 1 << 59, 1 << 59], [2, 2, 2]), row, 1),
+             ((0, top - 1, [0, 0, 0], [1, 1, 1]), row, 1),
+             ((0, 8, [top - 1, 1 - top, -top], [1, 1, 1]), row, 0),  # (the strides of one)
+             ((1 << 40, 8, [top - 1, 1 - top, -top], [1, 1, 1]), row, 1),
+             ((top - 16, 8, [8, 0, 0], [2, 1, 1]), (-top, 8, [8, 0, 0], [4, 1, 1]), 0),
+             ((top - 16, 9, [8, 0, 0], [2, 1, 1]), (-top, 8, [8, 0, 0], [4, 1, 1]), 1),
+             ((top - 16, 8, [16, 0, 0], [2, 1, 1]), (-top, 8, [8, 0, 0], [4, 1, 1]), 1),
+             ((-8, 8, [8, 0, 0], [1, 1, 1]), (top - 8, 8, [8, 0, 0], [1, 1, 1]), 0),
+             ((0, 8, [8, 0, 0], [0, 1, 1]), (0, top - 1, [top - 1, 0, 0], [9, 1, 1]), 0)]
+    for (a, b, w), (x, y, _) in zip(pairs, overlap([p[:2] for p in pairs])):
+        assert x == y == w, (a, b)
