@@ -30,8 +30,6 @@
 namespace tas_step_impl {
 namespace {
 
-typedef float f4 __attribute__((ext_vector_type(4)));
-
 // A lane's part of a head.
 struct Part {
     int c0, c1;   // its chunks

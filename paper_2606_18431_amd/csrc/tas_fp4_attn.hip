@@ -21,7 +21,6 @@ struct Quarter {
     uint32_t w[W];
 };
 
-typedef const __attribute__((address_space(1))) char *Global;
 // ONCE: its line is not read again soon. (256 decodes 102 us, 113 with lines kept; 16 chunks, whose
 // items share K and V, 812, 850 with lines not kept.)
 template <int D, bool ONCE>

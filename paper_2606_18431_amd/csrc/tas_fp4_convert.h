@@ -3,14 +3,10 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "tas_step_matrix.h"
+
 namespace tas_step_impl {
 namespace {
-
-template <typename T>
-using vec8 = T __attribute__((ext_vector_type(8)));
-template <typename T>
-using vec2 = T __attribute__((ext_vector_type(2)));
-typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 // A scale's byte as the float 2^e that the conversions take (of its exponent bits: 255
 // makes every element NaN, 0 is 2^-127; checked over all 256 bytes).

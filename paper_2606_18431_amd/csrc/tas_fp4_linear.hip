@@ -13,21 +13,7 @@
 namespace tas_step_impl {
 namespace {
 
-typedef float f4 __attribute__((ext_vector_type(4)));
-
-__device__ f4 mfma16(vec8<__bf16> a, vec8<__bf16> b, f4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-__device__ f4 mfma16(vec8<_Float16> a, vec8<_Float16> b, f4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
-
 constexpr int kWaves = 8;
-
-template <int N>
-struct Const {
-    static constexpr int value = N;
-};
 
 // Four adjacent n of token t.
 template <typename T>
@@ -61,13 +47,7 @@ __device__ Place place_of(const Linear4Args &a, uint32_t groups_n) {
     return {(int)(at % groups_n), (int)(at / groups_n)};
 }
 
-typedef const __attribute__((address_space(1))) char *Global;
-__device__ void load_to_lds(Global from, char *to) {
-    __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, 0,
-                                     0);
-}
-constexpr int kWaitLoads = 0x0F70;  // s_waitcnt: no load or store outstanding
-constexpr int kWaitLds = 0xC07F;    // no LDS access outstanding
+constexpr int kWaitLds = 0xC07F;  // s_waitcnt: no LDS access outstanding
 
 // Waits until all but the wave's last N loads are done. (The empty statements keep the compiler
 // from moving memory accesses across, the others from using earlier what has arrived later.)
@@ -98,7 +78,7 @@ void stream_kernel(Linear4Args a) {
     constexpr int XB = TT * 2048;  // bytes of half a tile of x
     static_assert(XL % 2 == 0 && (NB == 2 || NB == 4), "");
     // objects of their own, so that the compiler sees which loads a read has to wait for
-    __shared__ __attribute__((aligned(16))) char x0[kWaves * XB], x1[NB > 1 ? kWaves * XB : 16],
+    __shared__ __attribute__((aligned(16))) char x0[kWaves * XB], x1[kWaves * XB],
         x2[NB > 2 ? kWaves * XB : 16], x3[NB > 2 ? kWaves * XB : 16];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -239,28 +219,27 @@ __device__ void barrier_after_loads() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// More tokens, with too few tiles of 256 by 128. 16 RT WN rows and 16 TT WT tokens a workgroup,
-// of KS groups of WN by WT waves, group n with every KS-th step of 128 columns from n on. A wave
+// More tokens, with too few tiles of 256 by 128. 16 RT WN rows and 16 TT tokens a workgroup,
+// of KS groups of WN waves, group n with every KS-th step of 128 columns from n on. A wave
 // has its weights in registers, converted once for all of its tokens; a step of x is in LDS for
 // its group, loaded there directly, S - 1 of the group's steps ahead. Chunk c (of eight
 // elements) of row t lies at c ^ (t mod 16). Bound by the loads' latency and LDS.
-template <typename T, int WN, int WT, int RT, int TT, int S, int KS>
-__global__ __launch_bounds__(64 * WN * WT * KS, (WN * WT * KS > 8 ? WN * WT * KS / 4 : 2))
+template <typename T, int WN, int RT, int TT, int S, int KS>
+__global__ __launch_bounds__(64 * WN * KS, 2)
 void tile_kernel(Linear4Args a) {
     using V = vec8<T>;
-    constexpr int W = WN * WT, BT = 16 * TT * WT, LB = BT * kTileCols * 2;
-    constexpr int NL = LB / 1024 / W;  // loads of a wave for a step
+    constexpr int BT = 16 * TT, LB = BT * kTileCols * 2;
+    constexpr int NL = LB / 1024 / WN;  // loads of a wave for a step
     // objects of their own, so that the compiler sees which loads a read has to wait for
     static_assert(S == 3 || S == 4, "");
     __shared__ __attribute__((aligned(16))) char x0[KS * LB], x1[KS * LB], x2[KS * LB],
         x3[S > 3 ? KS * LB : 16];
     const int lane = threadIdx.x & 63;
     const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wave = all % W, group = all / W;
-    const int wn = wave % WN, wt = wave / WN;
+    const int wave = all % WN, group = all / WN;
     const int col = lane & 15, g = lane >> 4;
     const Place at = place_of(a, (a.tiles_n + RT * WN - 1) / (RT * WN));
-    const int tile0 = (at.n * WN + wn) * RT, t0 = at.t * BT;
+    const int tile0 = (at.n * WN + wave) * RT, t0 = at.t * BT;
     const char *codes[RT], *scales[RT];
 #pragma unroll
     for (int i = 0; i < RT; i++) {  // (of tiles that there are not, the last one's)
@@ -311,7 +290,7 @@ void tile_kernel(Linear4Args a) {
         for (int j = 0; j < TT; j++) sum[i][j] = f4{0, 0, 0, 0};
     auto products = [&](auto stage) {
         constexpr int st = decltype(stage)::value;
-        const char *x = buffer(st) + wt * TT * 16 * 256;
+        const char *x = buffer(st);
 #pragma unroll
         for (int k = 0; k < 4; k++) {
             V w[RT];
@@ -372,9 +351,9 @@ void tile_kernel(Linear4Args a) {
     }
     for (; n < steps; n += S) each(last, n);
     if constexpr (KS > 1) {  // the groups' sums are added to the first's, in order
-        static_assert((KS - 1) * W * RT * TT * 1024 <= KS * LB, "");
+        static_assert((KS - 1) * WN * RT * TT * 1024 <= KS * LB, "");
         auto place = [&](int group) {
-            return (f4 *)(x0 + ((group - 1) * W + wave) * RT * TT * 1024) + lane;
+            return (f4 *)(x0 + ((group - 1) * WN + wave) * RT * TT * 1024) + lane;
         };
         __syncthreads();
         if (group)
@@ -393,21 +372,21 @@ void tile_kernel(Linear4Args a) {
     }
 #pragma unroll
     for (int j = 0; j < TT; j++) {
-        const int t = t0 + (wt * TT + j) * 16 + col;
+        const int t = t0 + j * 16 + col;
         if (t >= a.tokens) break;
 #pragma unroll
         for (int i = 0; i < RT; i++) store_four<T>(a, t, (tile0 + i) * 16 + g * 4, sum[i][j]);
     }
 }
 
-template <typename T, int WN, int WT, int RT, int TT, int S, int KS>
+template <typename T, int WN, int RT, int TT, int S, int KS>
 hipError_t launch_tile(const Linear4Args &a, hipStream_t s) {
     Linear4Args copy = a;
     void *args[] = {&copy};
-    constexpr int BN = RT * WN, BT = 16 * TT * WT;
+    constexpr int BN = RT * WN, BT = 16 * TT;
     const dim3 grid((uint32_t)((a.tiles_n + BN - 1) / BN) * ((a.tokens + BT - 1) / BT));
-    return hipLaunchKernel((const void *)tile_kernel<T, WN, WT, RT, TT, S, KS>, grid,
-                           dim3(64 * WN * WT * KS), args, 0, s);
+    return hipLaunchKernel((const void *)tile_kernel<T, WN, RT, TT, S, KS>, grid,
+                           dim3(64 * WN * KS), args, 0, s);
 }
 // Many tokens: bound by the matrix unit. 256 rows and 128 tokens a workgroup, all tokens to
 // each of four waves with 64 rows, so that an operand from LDS goes into four products. As
@@ -587,10 +566,10 @@ hipError_t launch(const Linear4Args &a, hipStream_t s) {
         case 1: return launch_stream<T, 2, 8, 2>(a, s);
         case 2: return launch_stream<T, 4, 8, 4>(a, s);
         case 3: return launch_stream<T, 4, 16, 2>(a, s);
-        case 4: return launch_tile<T, 4, 1, 1, 2, 4, 2>(a, s);
-        case 5: return launch_tile<T, 4, 1, 2, 4, 4, 2>(a, s);
-        case 6: return launch_tile<T, 4, 1, 2, 4, 4, 1>(a, s);
-        case 7: return launch_tile<T, 8, 1, 2, 4, 3, 1>(a, s);
+        case 4: return launch_tile<T, 4, 1, 2, 4, 2>(a, s);
+        case 5: return launch_tile<T, 4, 2, 4, 4, 2>(a, s);
+        case 6: return launch_tile<T, 4, 2, 4, 4, 1>(a, s);
+        case 7: return launch_tile<T, 8, 2, 4, 3, 1>(a, s);
         default:
             return launch_kernel(big_kernel<T>, (int64_t)((a.rows + kBigRows - 1) / kBigRows) *
                                                     ((a.tokens + kBigTokens - 1) / kBigTokens),

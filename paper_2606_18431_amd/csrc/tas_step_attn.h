@@ -4,31 +4,19 @@
 #include <hip/hip_runtime.h>
 
 #include "tas_step_internal.h"
+#include "tas_step_matrix.h"
 
 namespace tas_step_impl {
 namespace {
 
-typedef float f4 __attribute__((ext_vector_type(4)));
 typedef float f16x __attribute__((ext_vector_type(16)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef short s8 __attribute__((ext_vector_type(8)));
-typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-
-template <typename T>
-using vec8 = T __attribute__((ext_vector_type(8)));
-template <typename T>
-using vec2 = T __attribute__((ext_vector_type(2)));
 typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
 
 // Block numbers: constant while a kernel runs, read by scalar loads.
 typedef const __attribute__((address_space(4))) int *Table;
 
-__device__ f4 mfma16(vec8<__bf16> a, vec8<__bf16> b, f4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-__device__ f4 mfma16(vec8<_Float16> a, vec8<_Float16> b, f4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
 __device__ f16x mfma32(vec8<__bf16> a, vec8<__bf16> b, f16x c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
@@ -172,12 +160,7 @@ __device__ uint32_t first_bits(int n) { return n >= 32 ? ~0u : n > 0 ? (1u << n)
 // 448k tokens of 8 heads of 128: 282 us, with ordinary loads 311).
 __device__ u4 stream(const char *p) { return __builtin_nontemporal_load((const u4 *)p); }
 
-template <int N>
-struct Const {
-    static constexpr int value = N;
-};
 constexpr int kMarks = 8;  // words of 32 keys
-constexpr int kWaitLoads = 0x0F70;  // s_waitcnt: no load or store outstanding
 
 // The end of a thin item: the four waves' results are joined (each wave's sums through its
 // own LDS) and go to the output or to the partial results.

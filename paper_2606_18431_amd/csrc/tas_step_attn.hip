@@ -179,11 +179,6 @@ __device__ __forceinline__ void thin_item(const AttnArgs &a, const Item &it, cha
     thin_end<T, D>(a, it, l, m, o, lds01, lds23, stat);
 }
 
-typedef const __attribute__((address_space(1))) char *Global;
-__device__ void load_to_lds(Global from, char *to) {
-    __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, 0,
-                                     0);
-}
 // The order of a stretch: N times a matrix product, a load to LDS at every other of
 // them, vector work that does not wait for it, and LDS reads for the next stretch.
 template <int N, int VECTOR, int READS, bool LOADS = false>
