@@ -147,6 +147,10 @@ typedef struct tas_linear_fp4 {
  * an argument out of range or unaligned, y over x or the weights, more than 2^33 elements
  * of y (about: 2^21 tiles of 64 by 64). */
 int tas_fp4_linear(const tas_linear_fp4 *a, void *stream);
+/* Which of its kernels tas_fp4_linear takes for these sizes (0 on; tokens at least 1): for
+ * tests and timings that have to reach each. Host only. TAS_EINVAL: sizes out of range. */
+int tas_fp4_linear_kernel(int64_t tokens, int64_t rows, int64_t cols);
+enum { TAS_FP4_LINEAR_KERNELS = 14 };
 
 #ifdef __cplusplus
 }

@@ -343,14 +343,35 @@ int tas_fp4_weights(int64_t rows, int64_t cols, const void *codes, int64_t codes
     return done(launch_weights4(k, (hipStream_t)stream));
 }
 
+// The sizes of a product, of a matrix that there can be.
+static bool valid_product(int64_t tokens, int64_t rows) {
+    if (tokens < 0 || tokens > (int64_t(1) << 24)) return false;
+    // (smaller tiles are not taken where there are many)
+    return ceil_div(rows, 64) * ceil_div(tokens, 64) <= kMaxGroups / 8;
+}
+static Linear4Args linear_sizes(int64_t tokens, int64_t rows, int64_t cols) {
+    const WeightsShape w = weights_shape(rows, cols);
+    Linear4Args k{};
+    k.tokens = (int32_t)tokens;
+    k.rows = (int32_t)rows;
+    k.blocks = (int32_t)(cols / 32);
+    k.tiles_n = (int32_t)w.tiles_n;
+    k.tiles_k = (int32_t)w.tiles_k;
+    return k;
+}
+
+int tas_fp4_linear_kernel(int64_t tokens, int64_t rows, int64_t cols) {
+    if (!tas_fp4_weights_bytes(rows, cols) || tokens < 1 || !valid_product(tokens, rows))
+        return TAS_EINVAL;
+    return linear4_kernel(linear_sizes(tokens, rows, cols));
+}
+
 int tas_fp4_linear(const tas_linear_fp4 *a, void *stream) {
     if (!a || !valid_dtype(a->dtype) || a->reserved) return TAS_EINVAL;
     const size_t bytes = tas_fp4_weights_bytes(a->rows, a->cols);
     if (!bytes || !a->weights || (uintptr_t)a->weights & 255) return TAS_EINVAL;
-    if (a->tokens < 0 || a->tokens > (int64_t(1) << 24)) return TAS_EINVAL;
+    if (!valid_product(a->tokens, a->rows)) return TAS_EINVAL;
     if (!a->tokens) return TAS_OK;
-    // (smaller tiles are not taken where there are many)
-    if (ceil_div(a->rows, 64) * ceil_div(a->tokens, 64) > kMaxGroups / 8) return TAS_EINVAL;
     if (!valid_rows(a->x, a->x_stride, a->cols) || a->x_stride > kMaxTokenStride)
         return TAS_EINVAL;
     if (!a->y || (uintptr_t)a->y % 2 || a->y_stride < a->rows ||
@@ -360,19 +381,13 @@ int tas_fp4_linear(const tas_linear_fp4 *a, void *stream) {
     if (Overlap()(y, tokens_of(a->x, a->x_stride, a->cols, a->tokens)) ||
         Overlap()(y, bytes_of(a->weights, (int64_t)bytes)))
         return TAS_EINVAL;
-    const WeightsShape w = weights_shape(a->rows, a->cols);
-    Linear4Args k{};
+    Linear4Args k = linear_sizes(a->tokens, a->rows, a->cols);
     k.x = a->x;
     k.codes = (const char *)a->weights;
-    k.scales = (const char *)a->weights + w.scales_at;
+    k.scales = (const char *)a->weights + weights_shape(a->rows, a->cols).scales_at;
     k.y = a->y;
     k.x_stride = a->x_stride;
     k.y_stride = a->y_stride;
-    k.tokens = (int32_t)a->tokens;
-    k.rows = (int32_t)a->rows;
-    k.blocks = (int32_t)(a->cols / 32);
-    k.tiles_n = (int32_t)w.tiles_n;
-    k.tiles_k = (int32_t)w.tiles_k;
     k.y_fours = a->rows % 4 == 0 && a->y_stride % 4 == 0 && (uintptr_t)a->y % 8 == 0;
     k.x_much = a->tokens / 4 > a->rows;  // (an element of x has four times the bits)
     return done(launch_linear4(k, a->dtype, (hipStream_t)stream));

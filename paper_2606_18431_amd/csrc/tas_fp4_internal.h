@@ -69,5 +69,7 @@ hipError_t launch_pack4(const Tensor4Args &a, int dtype, hipStream_t s);
 hipError_t launch_values4(const Values4Args &a, int n, int dtype, hipStream_t s);
 hipError_t launch_weights4(const Weights4Args &a, hipStream_t s);
 hipError_t launch_linear4(const Linear4Args &a, int dtype, hipStream_t s);
+// The number of the kernel that it takes, by the sizes alone.
+int linear4_kernel(const Linear4Args &a);
 
 }  // namespace tas_step_impl

@@ -7,6 +7,8 @@
 // block each.
 #include <hip/hip_runtime.h>
 
+#include <utility>
+
 #include "tas_fp4_convert.h"
 #include "tas_fp4_internal.h"
 
@@ -501,86 +503,98 @@ hipError_t launch_stream(const Linear4Args &a, hipStream_t s) {
                            args, 0, s);
 }
 
-// Up to 16 tokens. (4096 columns, one token: 4096 rows 4.3 us with RT 1 and XL 2, 5.2 with RT 2,
-// 4.5 with XL 4; 16384 rows 9.0 with RT 2, 9.7 with 4; 32768 14.7, 16.9. 16 tokens: 4096 rows 4.7
-// with RT 1, 5.9 with 2; 6144 rows 7.3, 6.3; 16384 rows 10.6 with RT 2, 9.7 with 4; 32768 rows
-// 17.8, 17.2, but of 8192 columns 32.2, 38.6: with RT 4 a compute unit has one workgroup, and a
-// wave's second unit of columns waits. With NB the other of 2 and 4: 4 to 8 % longer, or as long.)
-template <typename T>
-hipError_t launch_few(const Linear4Args &a, hipStream_t s) {
-    if (a.tokens <= 8)
-        return a.tiles_n <= 256 ? launch_stream<T, 1, 2, 4>(a, s) : launch_stream<T, 2, 2, 4>(a, s);
-    if (a.tiles_n <= 256) return launch_stream<T, 1, 4, 2>(a, s);
-    if (a.tiles_n < 1024 || a.tiles_k > 4 * kWaves) return launch_stream<T, 2, 4, 4>(a, s);
-    return launch_stream<T, 4, 4, 4>(a, s);
-}
-
-// More: the kernel whose rounds of 256 workgroups (one a compute unit) take least, by the times
-// measured with 1024 to 16384 columns, us: a first part, one for every round and one for every
-// round and 1024 columns; but no less than one workgroup takes for its columns, where two on a
-// compute unit hide one another's waits.
-struct Cost {
-    int rows, tokens;
+// The kernels, by number: rows and tokens of a workgroup; tiles: the waves of a group, the steps
+// in LDS and the groups; stream: the halves of a tile in LDS; and for more than 16 tokens the
+// times measured with 1024 to 16384 columns, us: a first part, one for every round of 256
+// workgroups (one a compute unit) and one for every round and 1024 columns; but no less than one
+// workgroup takes for its columns, where two on a compute unit hide one another's waits.
+enum Kind { kStream, kTile, kBig };
+struct Kernel {
+    Kind kind;
+    int rows, tokens, waves, ahead, groups;
     float base, round, columns, alone;
 };
-constexpr Cost kCosts[] = {
+constexpr int kFew = 5;  // for up to 16 tokens
+constexpr Kernel kKernels[] = {
+    {kStream, 16, 8, 0, 4, 0, 0, 0, 0, 0},
+    {kStream, 32, 8, 0, 4, 0, 0, 0, 0, 0},
+    {kStream, 16, 16, 0, 2, 0, 0, 0, 0, 0},
+    {kStream, 32, 16, 0, 4, 0, 0, 0, 0, 0},
+    {kStream, 64, 16, 0, 4, 0, 0, 0, 0, 0},
     // 4096 columns: 32 tokens, 4096 rows 6.0 (the next 6.8)
-    {16, 32, 2.1f, 0.3f, 0.9f, 0},
+    {kStream, 16, 32, 0, 2, 0, 2.1f, 0.3f, 0.9f, 0},
     // 32 tokens, 8192 rows 8.1 (10.0 and 10.0); 64 tokens, 4096 rows, 8192 columns 11.5 (15.7)
-    {32, 32, 3.0f, 0, 1.24f, 0},
+    {kStream, 32, 32, 0, 2, 0, 3.0f, 0, 1.24f, 0},
     // 128 tokens, 4096 rows 9.2 (11.5, 12.4, 10.5)
-    {64, 32, 0.5f, 2.2f, 1.75f, 0},
+    {kStream, 64, 32, 0, 4, 0, 0.5f, 2.2f, 1.75f, 0},
     // 64 tokens, 16384 rows 15.3 (20.7, 16.6)
-    {64, 64, 1.5f, 3, 2.5f, 0},
+    {kStream, 64, 64, 0, 2, 0, 1.5f, 3, 2.5f, 0},
     // 32 tokens, 32768 rows 19.3 (21.1, 23.7)
-    {64, 32, 3.2f, 0.2f, 1.75f, 0},
+    {kTile, 64, 32, 4, 4, 2, 3.2f, 0.2f, 1.75f, 0},
     // 256 tokens, 8192 rows 21.3 (27.1, 32.3)
-    {128, 64, 1.5f, 4, 3.45f, 0},
+    {kTile, 128, 64, 4, 4, 2, 1.5f, 4, 3.45f, 0},
     // 1024 tokens, 4096 rows 34.4 (39.2, 40.5); three stages in LDS instead of four 36.0
-    {128, 64, 3.5f, 0, 3.85f, 4.9f},
+    {kTile, 128, 64, 4, 4, 1, 3.5f, 0, 3.85f, 4.9f},
     // 2048 tokens, 4096 rows 57.5 (65.3, 81.5)
-    {256, 64, 4.5f, 0, 6.6f, 10.3f},
+    {kTile, 256, 64, 8, 3, 1, 4.5f, 0, 6.6f, 10.3f},
     // 1024 tokens, 16384 rows 97.8 (109.8)
-    {kBigRows, kBigTokens, 3, 0, 11.9f, 19.5f}};
+    {kBig, kBigRows, kBigTokens, 0, 0, 0, 3, 0, 11.9f, 19.5f}};
+constexpr int kNumber = sizeof(kKernels) / sizeof(Kernel);
+static_assert(kNumber == TAS_FP4_LINEAR_KERNELS, "");
+
+// Up to 16 tokens. (4096 columns, one token: 4096 rows 4.3 us with 16 rows and 8 tokens, 5.2 with
+// 32 rows, 4.5 with 16 tokens; 16384 rows 9.0 with 32 rows, 9.7 with 64; 32768 14.7, 16.9. 16
+// tokens: 4096 rows 4.7 with 16 rows, 5.9 with 32; 6144 rows 7.3, 6.3; 16384 rows 10.6 with 32
+// rows, 9.7 with 64; 32768 rows 17.8, 17.2, but of 8192 columns 32.2, 38.6: with 64 rows a compute
+// unit has one workgroup, and a wave's second unit of columns waits. With the other of two and
+// four halves in LDS: 4 to 8 % longer, or as long.)
+int choose_few(const Linear4Args &a) {
+    if (a.tokens <= 8) return a.tiles_n <= 256 ? 0 : 1;
+    if (a.tiles_n <= 256) return 2;
+    return a.tiles_n < 1024 || a.tiles_k > 4 * kWaves ? 3 : 4;
+}
+// More: the kernel that takes least.
 int choose(const Linear4Args &a) {
+    if (a.tokens <= 16) return choose_few(a);
     int best = 0;
     float least = 0;
     const float columns = (float)a.blocks / 32;
-    for (int i = 0; i < (int)(sizeof(kCosts) / sizeof(Cost)); i++) {
-        const Cost &t = kCosts[i];
+    for (int i = kFew; i < kNumber; i++) {
+        const Kernel &t = kKernels[i];
         const int64_t groups = (int64_t)((a.rows + t.rows - 1) / t.rows) *
                                ((a.tokens + t.tokens - 1) / t.tokens);
         const float rounds = (float)((groups + 255) / 256);
         const float us = fmaxf(t.base + rounds * (t.round + t.columns * columns),
                                t.alone * columns);
-        if (!i || us < least) best = i, least = us;
+        if (i == kFew || us < least) best = i, least = us;
     }
     return best;
 }
 
-template <typename T>
-hipError_t launch(const Linear4Args &a, hipStream_t s) {
-    if (a.tokens <= 16) return launch_few<T>(a, s);
-    switch (choose(a)) {
-        case 0: return launch_stream<T, 1, 8, 2>(a, s);
-        case 1: return launch_stream<T, 2, 8, 2>(a, s);
-        case 2: return launch_stream<T, 4, 8, 4>(a, s);
-        case 3: return launch_stream<T, 4, 16, 2>(a, s);
-        case 4: return launch_tile<T, 4, 1, 2, 4, 2>(a, s);
-        case 5: return launch_tile<T, 4, 2, 4, 4, 2>(a, s);
-        case 6: return launch_tile<T, 4, 2, 4, 4, 1>(a, s);
-        case 7: return launch_tile<T, 8, 2, 4, 3, 1>(a, s);
-        default:
-            return launch_kernel(big_kernel<T>, (int64_t)((a.rows + kBigRows - 1) / kBigRows) *
-                                                    ((a.tokens + kBigTokens - 1) / kBigTokens),
-                                 a, s);
-    }
+template <typename T, int N>
+hipError_t launch_number(const Linear4Args &a, hipStream_t s) {
+    constexpr Kernel k = kKernels[N];
+    if constexpr (k.kind == kStream)
+        return launch_stream<T, k.rows / 16, k.tokens / 4, k.ahead>(a, s);
+    else if constexpr (k.kind == kTile)
+        return launch_tile<T, k.waves, k.rows / 16 / k.waves, k.tokens / 16, k.ahead, k.groups>(a, s);
+    else
+        return launch_kernel(big_kernel<T>, (int64_t)((a.rows + kBigRows - 1) / kBigRows) *
+                                                ((a.tokens + kBigTokens - 1) / kBigTokens),
+                             a, s);
+}
+template <typename T, int... N>
+hipError_t launch(const Linear4Args &a, hipStream_t s, std::integer_sequence<int, N...>) {
+    constexpr hipError_t (*launchers[])(const Linear4Args &, hipStream_t) = {launch_number<T, N>...};
+    return launchers[choose(a)](a, s);
 }
 
 }  // namespace
 
 hipError_t launch_linear4(const Linear4Args &a, int dtype, hipStream_t s) {
-    return dtype == TAS_F16 ? launch<_Float16>(a, s) : launch<__bf16>(a, s);
+    constexpr std::make_integer_sequence<int, kNumber> all;
+    return dtype == TAS_F16 ? launch<_Float16>(a, s, all) : launch<__bf16>(a, s, all);
 }
+int linear4_kernel(const Linear4Args &a) { return choose(a); }
 
 }  // namespace tas_step_impl

@@ -80,7 +80,9 @@ assert _CACHE_VALUES.size == ctypes.sizeof(tas_cache_values_fp4)
 assert _LINEAR.size == ctypes.sizeof(tas_linear_fp4)
 
 EXPORTS = ["tas_fp4_append", "tas_fp4_attention", "tas_fp4_pack", "tas_fp4_values",
-           "tas_fp4_cache_values", "tas_fp4_weights_bytes", "tas_fp4_weights", "tas_fp4_linear"]
+           "tas_fp4_cache_values", "tas_fp4_weights_bytes", "tas_fp4_weights", "tas_fp4_linear",
+           "tas_fp4_linear_kernel"]
+LINEAR_KERNELS = 14
 
 
 def _call(index, stream, call, *args):

@@ -105,6 +105,7 @@ def lib():
         L.tas_fp4_weights_bytes.restype = ctypes.c_size_t
         L.tas_fp4_weights.argtypes = [_i64, _i64, _P, _i64, _P, _i64, _P, _P]
         L.tas_fp4_linear.argtypes = [_P, _P]
+        L.tas_fp4_linear_kernel.argtypes = [_i64, _i64, _i64]
         _lib = L
     return _lib
 

@@ -238,6 +238,47 @@ def test_weights_bytes():
         assert L.tas_fp4_weights_bytes(*bad) == 0, bad
 
 
+# Sizes (tokens, rows, columns) for each of the product's kernels, by its number: columns that end
+# inside a tile and that do not, that leave steps and groups of waves whole, in part or empty.
+KERNEL_SHAPES = {
+    0: [(1, 130, 1120), (8, 4090, 4192), (5, 100, 96)],
+    1: [(8, 4100, 1184), (3, 8200, 96)],
+    2: [(16, 100, 1120), (9, 4090, 4192)],
+    3: [(16, 4100, 2144), (12, 16400, 4384)],
+    4: [(16, 16400, 1120), (9, 16390, 4064), (12, 33000, 96), (16, 16390, 128), (13, 16390, 2080)],
+    5: [(17, 5, 96), (32, 1000, 8224), (200, 100, 1120)],
+    6: [(17, 4100, 1120), (31, 4100, 4192), (20, 16390, 544)],
+    7: [(33, 4100, 1184), (17, 4100, 288), (127, 4090, 2144)],
+    8: [(130, 5000, 1120), (33, 10000, 2144), (64, 10000, 4384)],
+    9: [(17, 26000, 544), (25, 26000, 1184), (20, 16390, 4384), (32, 33000, 2080), (17, 26000, 2176)],
+    10: [(33, 16390, 4128), (64, 16390, 4384), (200, 8100, 4384), (50, 16390, 8288)],
+    11: [(33, 16390, 1120), (180, 10000, 96), (33, 26000, 160), (1030, 4090, 1184),
+         (33, 33000, 4128)],
+    12: [(33, 33000, 1120), (130, 33000, 544), (2040, 4090, 1120), (400, 33000, 288),
+         (2000, 4000, 2080)],
+    13: [(70, 26000, 96), (200, 26000, 544), (600, 20000, 1120), (2100, 8201, 288),
+         (4090, 4100, 160)]}
+
+
+def test_every_kernel_of_the_product_has_sizes():
+    """Whatever the rule that chooses: the tests on a GPU reach each of its kernels."""
+    header = open(os.path.join(ROOT, "include", "tas_fp4.h")).read()
+    assert f"TAS_FP4_LINEAR_KERNELS = {fp4.LINEAR_KERNELS} " in header
+    assert sorted(KERNEL_SHAPES) == list(range(fp4.LINEAR_KERNELS))
+    number = step.lib().tas_fp4_linear_kernel
+    for kernel, shapes in KERNEL_SHAPES.items():
+        assert any(cols % 128 for _, _, cols in shapes)
+        for shape in shapes:
+            assert number(*shape) == kernel, shape
+
+
+def test_kernel_of_refused_products():
+    number = step.lib().tas_fp4_linear_kernel
+    for bad in ((0, 40, 64), (-1, 40, 64), ((1 << 24) + 1, 40, 64), (3, 0, 64), (3, 40, 48),
+                (3, (1 << 24) + 1, 64), (1 << 24, 1 << 24, 64)):
+        assert number(*bad) == tas.TAS_EINVAL, bad
+
+
 def test_refused_weights_and_products():
     L = step.lib()
     ok = [40, 64, AT, 32, AT + (1 << 20), 2, AT + (1 << 20)]  # (onto the scales)
