@@ -333,3 +333,54 @@ def test_every_layer_has_a_cache_of_its_own():
     assert [c[0] for c in s.calls] == ["append", "attention"] * 5
     assert all(s.calls[i][1:] == s.calls[i + 1][1:] for i in range(0, 10, 2))
     assert len({p for c in s.calls for p in c[1:]}) == 20
+
+
+def test_a_layer_gives_each_product_the_result_before(monkeypatch):
+    """Of a layer's run with its weights: the state through the heads' matrix to the append, the
+    queries to the attention, its result back from the heads, up and down; each layer with its
+    own matrices and cache."""
+    torch = pytest.importorskip("torch")
+    from paper_2606_18431_amd import iteration_cost as C
+    from paper_2606_18431_amd import workloads as W
+
+    calls = []
+
+    class Weights:
+        def __init__(self, codes, scales):
+            assert scales.shape == (codes.shape[0], codes.shape[1] // 16)
+            self.shape = codes.shape[0], 2 * codes.shape[1]
+
+    def linear(x, w):
+        assert x.shape == (3, w.shape[1])
+        y = torch.empty((3, w.shape[0]), dtype=x.dtype)
+        calls.append(("linear", x, w, y))
+        return y
+
+    class Step:
+        tokens = 3
+
+        def append_fp4(self, qkv, cache, *args, **kw):
+            assert qkv.shape == (3, 8, 64)
+            calls.append(("append", qkv, cache, torch.empty((3, 4, 64))))
+            return calls[-1][-1]
+
+        def attention_fp4(self, q, cache):
+            calls.append(("attention", q, cache, torch.empty((3, 4, 64))))
+            return calls[-1][-1]
+
+    monkeypatch.setattr(fp4, "Weights", Weights)
+    monkeypatch.setattr(fp4, "linear", linear)
+    m = C.Layers(W.Engine(kv_blocks=4, max_tokens=64), 2, heads=4, kv_heads=2, head_dim=64,
+                 dtype=torch.float16, device="cpu", positions=10, cache_bits=4, hidden=128, ffn=160)
+    m.run(Step())
+    assert [c[0] for c in calls] == \
+        ["linear", "append", "attention", "linear", "linear", "linear"] * 2
+    for layer in range(2):
+        part = calls[6 * layer:6 * layer + 6]
+        assert part[0][1].data_ptr() == m.x.data_ptr()
+        for before, after in zip(part, part[1:]):
+            assert after[1].data_ptr() == before[-1].data_ptr()
+        products = [c[2] for c in part if c[0] == "linear"]
+        assert [w.shape for w in products] == [(512, 128), (128, 256), (160, 128), (128, 160)]
+        assert all(x is y for x, y in zip(products, m.weights[layer]))
+        assert part[1][2] is part[2][2] is m.caches[layer]
