@@ -283,7 +283,7 @@ class Weights:
     def _admit(self, raw, stream):
         """Orders a call's stream behind the layout, and the end of the memory behind the
         stream."""
-        on = torch.cuda.ExternalStream(raw, self.device) if stream is None else stream
+        on = torch.cuda.current_stream(self.device) if stream is None else stream
         self._there = self._there or self._laid.query()
         if not self._there:
             with torch.cuda.stream(on):

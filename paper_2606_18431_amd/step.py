@@ -421,7 +421,7 @@ class Step:
     def _admit(self, raw, stream):
         """Orders a call's stream behind the plan's copy, and the end of the workspace behind
         the stream."""
-        on = torch.cuda.ExternalStream(raw, self.device) if stream is None else stream
+        on = torch.cuda.current_stream(self.device) if stream is None else stream
         self._there = self._there or self._copied.query()
         if not self._there:
             with torch.cuda.stream(on):

@@ -908,6 +908,40 @@ def test_weights_under_way(torch):
         assert torch.equal(out, want)
 
 
+def test_weights_of_another_stream_on_the_default_one(torch):
+    """Products on the default stream wait for a layout under way on another, and its memory is
+    not given away there before they are done."""
+    x = torch.randn((5, 512), device="cuda", dtype=torch.bfloat16)
+    codes, scales = fp4.pack(torch.randn((640, 512), device="cuda", dtype=torch.bfloat16))
+    want = fp4.linear(x, fp4.Weights(codes, scales))
+    a = torch.randn((8192, 8192), device="cuda", dtype=torch.bfloat16)
+    side = torch.cuda.Stream()
+    for s in (side, torch.cuda.current_stream()):
+        with torch.cuda.stream(s):
+            a @ a
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(250):
+            torch.mm(a, a)
+    w = fp4.Weights(codes, scales, stream=side)
+    y, z = fp4.linear(x, w), fp4.linear(x, w, stream=torch.cuda.default_stream())
+    assert not w._laid.query()
+    torch.cuda.synchronize()
+    assert torch.equal(y, want) and torch.equal(z, want)
+    w = fp4.Weights(codes, scales, stream=side)
+    torch.cuda.synchronize()
+    for _ in range(250):
+        torch.mm(a, a)
+    y = fp4.linear(x, w)
+    at, n = w._data.data_ptr(), w._data.numel()
+    del w
+    with torch.cuda.stream(side):
+        again = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    assert again.data_ptr() != at
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
+
+
 # ------------------------------------------------------------------ refusals
 
 

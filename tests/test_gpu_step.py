@@ -921,3 +921,40 @@ def test_plan_under_way(torch):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+def test_a_step_of_another_stream_on_the_default_one(torch):
+    """Calls on the default stream wait for a plan under way on another, and the workspace is
+    not given away there before they are done."""
+    b = Batch(42, [1, 20], [30, 40], 4, 2, 64)
+    k, v = caches(torch, b, torch.bfloat16, 9, poison=False)
+    q = torch.randn((21, 4, 64), device="cuda", dtype=torch.bfloat16)
+    want = b.step().attention(q, k, v)
+    a = torch.randn((8192, 8192), device="cuda", dtype=torch.bfloat16)
+    side = torch.cuda.Stream()
+    for s in (side, torch.cuda.current_stream()):
+        with torch.cuda.stream(s):
+            a @ a
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(250):
+            torch.mm(a, a)
+        s = b.step()
+    x, y = s.attention(q, k, v), s.attention(q, k, v, stream=torch.cuda.default_stream())
+    assert not s._copied.query()
+    torch.cuda.synchronize()
+    assert torch.equal(x, want) and torch.equal(y, want)
+    with torch.cuda.stream(side):
+        s = b.step()
+    torch.cuda.synchronize()
+    for _ in range(250):
+        torch.mm(a, a)
+    x = s.attention(q, k, v)
+    at, n = s.ws.data_ptr(), s.ws.numel()
+    s.close()
+    del s
+    with torch.cuda.stream(side):
+        again = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    assert again.data_ptr() != at
+    torch.cuda.synchronize()
+    assert torch.equal(x, want)
