@@ -99,6 +99,10 @@ class Layers:
                  cache_bits=16, hidden=0, ffn=0):
         import torch
 
+        if cache_bits not in (4, 16):
+            raise ValueError(f"caches of {cache_bits} bits: 4 or 16")
+        if hidden < 0 or hidden % 32 or ffn < 0 or ffn % 32 or (ffn and not hidden):
+            raise ValueError(f"hidden {hidden}, ffn {ffn}: multiples of 32, ffn with hidden")
         self.torch, self.cache_bits = torch, cache_bits
         shape = (e.kv_blocks, kv_heads, e.block_tokens, head_dim)
         g = torch.Generator(device=device)

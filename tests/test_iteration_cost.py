@@ -130,3 +130,13 @@ def test_whole_terms_fit_the_engine():
                 assert b < 0 or off(base, tok, div) <= off(b, t, d)
     base, tok, div = C.whole_terms(tokens, context, 5.0 * tokens)  # no price of context
     assert (base, tok) == (0, 5) and div == 2 ** 31 - 1
+
+
+def test_layers_refuse_what_they_would_not_run():
+    """Other bits of a cache, and a second half of a layer without its first."""
+    torch = pytest.importorskip("torch")
+    for kw in (dict(cache_bits=8), dict(cache_bits=0), dict(ffn=64), dict(hidden=48),
+               dict(hidden=-32), dict(hidden=64, ffn=100), dict(hidden=64, ffn=-64)):
+        with pytest.raises(ValueError):
+            C.Layers(W.Engine(kv_blocks=4, max_tokens=64), 1, heads=2, kv_heads=1, head_dim=64,
+                     dtype=torch.float16, device="cpu", positions=10, **kw)
