@@ -95,7 +95,7 @@ int tas_fp4_attention(tas_step *step, const tas_attention_fp4 *a, void *stream);
 /* A tensor of n[0] * n[1] * n[2] rows of `cols` elements, cols a multiple of 32:
  * `x` in a 16-bit type (16-byte aligned, strides multiples of 16), `codes` and
  * `scales` (codes 4-byte aligned, strides multiples of 4); the stride of a dimension of one
- * says nothing. Fewer than 2^35 - 2^11 elements. */
+ * says nothing. At most 2^35 - 2^11 elements. */
 typedef struct tas_tensor_fp4 {
     int32_t dtype;                 /* of x: TAS_F16 or TAS_BF16                              */
     int32_t reserved;              /* 0                                                      */

@@ -147,7 +147,7 @@ def _adjacent(t, n, row):
 
 def pack(x, *, stream=None):
     """(codes [..., n / 2], scales [..., n / 32]), uint8, of a float16 or bfloat16 tensor
-    [..., n] of one to four dimensions, rows adjacent."""
+    [..., n] of one to four dimensions, elements of a row adjacent, rows 16-byte aligned."""
     _no_tangent(x)
     dtype = DTYPES.get(x.dtype)
     if dtype is None:
@@ -170,8 +170,8 @@ def pack(x, *, stream=None):
 
 
 def values(codes, scales, dtype, *, stream=None):
-    """What codes [..., n / 2] and scales [..., n / 32] (uint8) stand for, [..., n] in
-    float16 or bfloat16."""
+    """What codes [..., n / 2] and scales [..., n / 32] (uint8, bytes of a row adjacent, rows
+    of codes 4-byte aligned) stand for, [..., n] in float16 or bfloat16."""
     code = DTYPES.get(dtype)
     if code is None:
         raise ValueError(f"{dtype}: float16 or bfloat16")
@@ -195,7 +195,8 @@ def values(codes, scales, dtype, *, stream=None):
 class Cache(NamedTuple):
     """One layer's paged cache in four bits: ``k`` and ``v`` are the codes, uint8
     [n_blocks, kv_heads, block_tokens, head_dim / 2], ``k_scale`` and ``v_scale`` uint8
-    [n_blocks, kv_heads, block_tokens, head_dim / 32]; any strides whose last is 1."""
+    [n_blocks, kv_heads, block_tokens, head_dim / 32]; any strides whose last is 1, rows of
+    codes 16-byte aligned, of scales to their length."""
 
     k: torch.Tensor
     v: torch.Tensor
@@ -243,8 +244,8 @@ class Cache(NamedTuple):
 
 class Weights:
     """A matrix [rows, cols] in four bits, laid out for the products: made once from its
-    codes [rows, cols / 2] and scales [rows, cols / 32] (as ``pack`` gives them), on the
-    current stream or ``stream``. Other streams' products wait for that. A graph that
+    codes [rows, cols / 2] and scales [rows, cols / 32] (as ``pack`` gives them; bytes of a
+    row adjacent, rows of codes 16-byte aligned), on the current stream or ``stream``. Other streams' products wait for that. A graph that
     captured its products reads it: keep it as long as the graph."""
 
     def __init__(self, codes, scales, *, stream=None):
@@ -299,8 +300,8 @@ class Weights:
 
 
 def linear(x, weights, *, out=None, stream=None):
-    """x W^T of float16 or bfloat16 tokens [tokens, cols] (adjacent rows, any stride that is
-    a multiple of 8) and ``Weights`` of [rows, cols]: [tokens, rows] of x's type. The
+    """x W^T of float16 or bfloat16 tokens [tokens, cols] (16-byte aligned, any stride that is
+    a multiple of 8 up to 2^24) and ``Weights`` of [rows, cols]: [tokens, rows] of x's type. The
     products are summed in 32 bits, in an order that depends on the sizes alone."""
     _no_tangent(x, out)
     dtype, index, rows, cols = DTYPES.get(x.dtype), weights.index, weights.rows, weights.cols
