@@ -389,6 +389,22 @@ def test_append_keys_lost_in_32_bits(torch, small, weight, turn, interleaved):
     assert (got[..., 32:64] != 0).any()  # (not all below the smallest scale's codes)
 
 
+
+@pytest.mark.parametrize("size", [64, 128])
+def test_append_in_place(torch, size):
+    """The queries over their own rows of queries, keys and values, the others as they were."""
+    b = Batch(26, [1, 7, 0, 40], [33, 9, 5, 90], 8, 2, size)
+    qkv = torch.randn((48, 12, size), device="cuda", dtype=torch.bfloat16)
+    cos, sin = torch.rand((2, 100, size // 2), device="cuda")
+    w = torch.rand(size, device="cuda").bfloat16()
+    one, two = (fp4.Cache.zeros(b.n_blocks, 2, 16, size) for _ in range(2))
+    s, x = b.step(), qkv.clone()
+    want = s.append_fp4(qkv, one, cos, sin, q_weight=w, k_weight=w)
+    got = s.append_fp4(x, two, cos, sin, q_weight=w, k_weight=w, out=x[:, :8])
+    assert got.data_ptr() == x.data_ptr() and torch.equal(got, want)
+    assert torch.equal(x[:, 8:], qkv[:, 8:])
+    assert all(torch.equal(t, u) for t, u in zip(one, two))
+
 # ------------------------------------------------------------------ attention
 
 

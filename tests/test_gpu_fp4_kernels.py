@@ -109,3 +109,25 @@ def test_values_that_are_not_finite(torch, kernel, tokens, rows, cols, name):
         assert bool(((got[token] == want) | (got[token].isnan() & want.isnan())).all())
         got[token] = clean[token]
         assert torch.equal(got, clean)
+
+
+def test_rows_as_far_apart_as_they_may_be(torch):
+    """Strides of 2^24 elements, with which the last of a workgroup's rows lie beyond 4 GB, and
+    results 2^31 - 1 and 2^31 - 4 elements apart."""
+    big = torch.full((200, 1 << 24), math.nan, device="cuda", dtype=torch.bfloat16)
+    for kernel, shapes in KERNEL_SHAPES.items():
+        tokens, rows, cols = max(s for s in shapes if s[0] <= 200)
+        selects(kernel, tokens, rows, cols)
+        x, codes, scales = operands(torch, "bf16", tokens, rows, cols)
+        w = fp4.Weights(codes, scales)
+        far = big[:tokens, 8:8 + cols].copy_(x)
+        assert torch.equal(fp4.linear(far, w), fp4.linear(x, w))
+        far.fill_(math.nan)
+    del big, far
+    x, codes, scales = operands(torch, "bf16", 3, 100, 96)
+    w = fp4.Weights(codes, scales)
+    for stride in ((1 << 31) - 1, (1 << 31) - 4):
+        out = torch.empty_strided((3, 100), (stride, 1), device="cuda", dtype=torch.bfloat16)
+        fp4.linear(x, w, out=out)
+        assert torch.equal(out, fp4.linear(x, w))
+        del out
